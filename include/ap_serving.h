@@ -169,13 +169,39 @@ typedef struct ap_batch_desc {
 int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *batch, void *stream);
 int ap_plan_destroy(ap_plan *plan);
 
+/*
+ * The same for a layer with a sliding window: the new token at position p sees
+ * key j if j <= p and (j > p - window or j < sinks), i.e. its last `window`
+ * keys, itself among them, and the first `sinks` keys of its context (attention
+ * sinks).  A window that covers the context gives what ap_plan_create gives.
+ * The plan is used like any other: ap_kv_append, ap_attention_iteration, ...
+ * A model that alternates windowed and full layers makes one plan of each kind
+ * per iteration (the append is the same for both).
+ * Table entries of pages that hold no key visible to any of the sequence's new
+ * tokens are neither validated nor read: a page that has slid out of the window
+ * for good can be freed (pages between ceil(sinks/16) and
+ * (ctx - q_len - window + 1)/16 are never read again).  ap_plan_info.kv_tokens
+ * and ap_plan_predict count visible keys only.
+ * A masked key has weight 0 whatever its K holds; the V of a key that no new
+ * token of the sequence sees (in a prefill chunk: of the same block of 128 query
+ * rows) does not reach the result either, but a non-finite V that one row of a
+ * block sees reaches every row of that block, as it does past the causal bound.
+ * window >= 1, sinks >= 0 (else INVALID_ARG).
+ */
+typedef struct ap_window_desc {
+    int32_t window;
+    int32_t sinks;
+} ap_window_desc;
+int ap_plan_create_windowed(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *batch, const ap_window_desc *window,
+                            void *stream);
+
 /* Bytes of caller-provided device workspace (split-K partials) that
  * ap_attention_iteration needs for this plan; may be 0. */
 size_t ap_plan_workspace_bytes(const ap_plan *plan);
 
 typedef struct ap_plan_info {
     int64_t n_new;           /* rows of q / k_new / v_new / out */
-    int64_t kv_tokens;       /* sum of ctx_len over sequences with q_len > 0 */
+    int64_t kv_tokens;       /* sum of ctx_len over sequences with q_len > 0 (with a window: of the keys a new token sees) */
     int64_t decode_rows;     /* sequences with q_len == 1 */
     int64_t prefill_seqs;    /* sequences with q_len > 1 */
     int64_t prefill_pairs;   /* unmasked (query row, key) pairs of the prefill chunks, one head */
@@ -219,7 +245,8 @@ int ap_plan_predict(const ap_plan *plan, double hbm_gbs, double tensor_tflops, a
  * blob is an int32 array; the layout gives the offset (in int32 units) of each
  * section:
  *   append_dst    [n_new]             page*16 + slot of every new token row
- *   bt_flat       [n_bt]              used block-table entries, sequences with q_len > 0 concatenated
+ *   bt_flat       [n_bt]              used block-table entries, sequences with q_len > 0 concatenated (with a window:
+ *                                     decode rows, then each block of 128 prefill rows, without the pages it does not see)
  *   decode_items  [decode_items][8]   q_row, first kv_head of the item's block, bt_offset, page_begin, page_count, kv_len, part_slot, merge_index
  *   cta_begin     [n_cta_begin]       item range of decode CTA c is [cta_begin[c], cta_begin[c+1])
  *   merge_entries [merge_entries][4]  q_row, first kv_head of the block, part_begin, part_count

@@ -40,6 +40,7 @@ EXPORTED_SYMBOLS = (
     "ap_profile_enable", "ap_profile_collect",
     "ap_static_workspace_bytes", "ap_attention_iteration_static",
     "ap_kv_pool_set_wait_limit", "ap_selftest_wait_timeout", "ap_kv_pool_set_single_launch",
+    "ap_plan_create_windowed",
 )
 
 
@@ -60,6 +61,10 @@ class BatchDesc(ctypes.Structure):
                 ("q_lens", ctypes.c_void_p), ("ctx_lens", ctypes.c_void_p),
                 ("block_tables", ctypes.c_void_p), ("table_stride", ctypes.c_int32),
                 ("softmax_scale", ctypes.c_float)]
+
+
+class WindowDesc(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
 
 
 class PlanInfo(ctypes.Structure):
@@ -122,6 +127,8 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "ap_kv_pool_num_free": (i32, [vp]),
         "ap_kv_pool_set_side_by_side": (ctypes.c_int, [vp, i32]),
         "ap_plan_create": (ctypes.c_int, [ctypes.POINTER(vp), vp, ctypes.POINTER(BatchDesc), vp]),
+        "ap_plan_create_windowed": (ctypes.c_int, [ctypes.POINTER(vp), vp, ctypes.POINTER(BatchDesc),
+                                                   ctypes.POINTER(WindowDesc), vp]),
         "ap_plan_destroy": (ctypes.c_int, [vp]),
         "ap_plan_workspace_bytes": (sz, [vp]),
         "ap_plan_predict": (ctypes.c_int, [vp, ctypes.c_double, ctypes.c_double, ctypes.POINTER(PlanPrediction)]),
@@ -285,6 +292,19 @@ def plan_create(pool: KVPool, q_lens, ctx_lens, block_tables, num_q_heads: int,
     h = ctypes.c_void_p()
     _check(load().ap_plan_create(ctypes.byref(h), pool.handle, ctypes.byref(desc), _stream(stream)),
            "ap_plan_create")
+    del keep
+    return Plan(h.value, pool)
+
+
+def plan_create_windowed(pool: KVPool, q_lens, ctx_lens, block_tables, num_q_heads: int, window: int, sinks: int = 0,
+                         softmax_scale: float = 0.0, stream=None) -> Plan:
+    """Plan of a sliding-window layer: a new token sees its last ``window`` keys (itself among them) and the
+    first ``sinks`` keys of its context.  Used like a plan of :func:`plan_create`."""
+    desc, keep = _batch_desc(q_lens, ctx_lens, block_tables, num_q_heads, softmax_scale)
+    win = WindowDesc(int(window), int(sinks))
+    h = ctypes.c_void_p()
+    _check(load().ap_plan_create_windowed(ctypes.byref(h), pool.handle, ctypes.byref(desc), ctypes.byref(win),
+                                          _stream(stream)), "ap_plan_create_windowed")
     del keep
     return Plan(h.value, pool)
 

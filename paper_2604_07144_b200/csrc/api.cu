@@ -104,6 +104,27 @@ constexpr double kDecodeFixedUs = 8.0;       // first-data latency and finishing
 constexpr double kAppendGBs = 4000.0;        // scatter of 256-byte rows
 constexpr double kAppendFixedUs = 3.0;
 
+// Which pages of a context the rows at positions p0 .. end - 1 see: all up to the last row's, or, with a
+// window of W keys and S sinks, those that hold a key j with j < S or j > p0 - W.  The two runs of pages
+// [0, sink_pages) and [first, end) are kept; what lies between is cut out, so that a key at position j of
+// the second run has position j - shift() in the compacted context (shift() is a multiple of the page).
+struct PageSpan {
+    int32_t sink_pages, first, end;
+    int32_t count() const { return sink_pages + end - first; }
+    int32_t shift() const { return (first - sink_pages) * kPageSize; }
+};
+struct WindowView {
+    int32_t window, sinks;                                // window 0: none
+    // first key of the window of the row at position p (everything from here up to p is seen)
+    int32_t low(int32_t p) const { return window > 0 && p >= window ? p - window + 1 : 0; }
+    // keys that the row at position p sees
+    int32_t keys(int32_t p) const { return p + 1 - std::max(0, low(p) - sinks); }
+    PageSpan pages(int32_t p0, int32_t end) const {
+        const int32_t first = low(p0) / kPageSize;
+        return {std::min(first, sinks / kPageSize + (sinks % kPageSize != 0)), first, end / kPageSize + (end % kPageSize != 0)};
+    }
+};
+
 // GB/s of KV one SM's decode pipeline sustains, by the size of its TMA requests (the tiles of one page
 // that an item takes in one request): the TMA unit handles ~14 M requests per second.
 inline double decode_sm_gbs(int request_bytes) {
@@ -117,7 +138,8 @@ inline double side_by_side_us(double decode_bytes, double w_p, int k, double sm_
     return std::max(t_dec, (t_dec * k + w_p) / sms);
 }
 
-int side_by_side_decode_ctas(const ap_kv_pool *pool, const ap_batch_desc *b, int d, int Hkv, int G, int max_ctas) {
+int side_by_side_decode_ctas(const ap_kv_pool *pool, const ap_batch_desc *b, const WindowView &win, int d, int Hkv, int G,
+                             int max_ctas) {
     const int mode = pool->side_by_side_mode;
     if (mode == 0) return 0;
     double decode_bytes = 0.0, w_p = 0.0;
@@ -127,11 +149,12 @@ int side_by_side_decode_ctas(const ap_kv_pool *pool, const ap_batch_desc *b, int
         const int32_t ql = b->q_lens[s], cl = b->ctx_lens[s];
         if (ql == 1) {
             ++decode_rows;
-            decode_bytes += (double)((cl + kPageSize - 1) / kPageSize) * kPageSize * Hkv * d * 4.0;
+            decode_bytes += (double)win.pages(cl - 1, cl).count() * kPageSize * Hkv * d * 4.0;
         } else if (ql > 1) {
             ++prefill_seqs;
             for (int32_t t0 = 0; t0 < ql; t0 += 128) {
-                const int steps = (cl - ql + t0 + std::min(128, ql - t0) + 127) / 128;
+                const int32_t p0 = cl - ql + t0, end = p0 + std::min(128, ql - t0);
+                const int steps = (end - win.pages(p0, end).shift() + 127) / 128;
                 const int pairs = G / 2, singles = G % 2;
                 w_p += (double)Hkv * (pairs * (steps * kPrefillStepUs * d_scale + kPrefillUnitUs) +
                                       singles * (steps * kPrefillStepSingleUs * d_scale + kPrefillUnitUs));
@@ -419,7 +442,7 @@ int32_t ap_kv_pool_num_free(const ap_kv_pool *pool) {
 
 // ---------------------------------------------------------------- planner --
 
-int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void *stream) {
+static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, const WindowView win, void *stream) {
     if (!out) return AP_ERR_INVALID_ARG;
     *out = nullptr;
     if (!pool || !b || b->batch < 0 || b->num_q_heads <= 0) return AP_ERR_INVALID_ARG;
@@ -443,31 +466,58 @@ int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void
         const int64_t need = ((int64_t)cl + kPageSize - 1) / kPageSize;
         if (need > b->table_stride) return AP_ERR_INVALID_ARG;
         const int32_t *row = b->block_tables + (size_t)s * (size_t)b->table_stride;
-        for (int64_t i = 0; i < need; ++i)
+        const PageSpan span = win.pages(cl - ql, cl);     // the pages that any new token of the sequence sees
+        for (int32_t i = 0; i < span.sink_pages; ++i)
             if (row[i] < 0 || row[i] >= num_pages) return AP_ERR_BAD_BLOCK_TABLE;
+        for (int32_t i = span.first; i < span.end; ++i)
+            if (row[i] < 0 || row[i] >= num_pages) return AP_ERR_BAD_BLOCK_TABLE;
+        const int64_t seen = cl - std::max(0, win.low(cl - ql) - win.sinks);      // keys that any new token sees
         n_new += ql;
-        kv_tokens += cl;
-        bt_total += need;
+        kv_tokens += seen;
         if (ql == 1) ++decode_rows; else ++prefill_seqs;
-        if (ql > 1) pairs += (int64_t)ql * (cl - ql) + (int64_t)ql * (ql + 1) / 2;
-        if (ql == 1) { decode_kv += cl; decode_bt += need; } else { prefill_kv += cl; prefill_rows += ql; }
+        if (ql == 1) {
+            bt_total += span.count();
+            decode_kv += seen;
+            decode_bt += span.count();
+        } else {
+            if (win.window == 0) {
+                bt_total += need;
+                pairs += (int64_t)ql * (cl - ql) + (int64_t)ql * (ql + 1) / 2;
+            } else {                                      // every block of query rows has entries of its own
+                for (int32_t t0 = 0; t0 < ql; t0 += 128)
+                    bt_total += win.pages(cl - ql + t0, cl - ql + std::min(ql, t0 + 128)).count();
+                for (int32_t t = 0; t < ql; ++t) pairs += win.keys(cl - ql + t);
+            }
+            prefill_kv += seen;
+            prefill_rows += ql;
+        }
     }
-    if (n_new > (int64_t)1 << 30) return AP_ERR_UNSUPPORTED;
+    if (n_new > (int64_t)1 << 30 || bt_total > (int64_t)1 << 30) return AP_ERR_UNSUPPORTED;
 
-    std::vector<int32_t> append_dst((size_t)n_new);
-    std::vector<int32_t> bt_off((size_t)B, 0);
+    std::vector<int32_t> append_dst((size_t)n_new), positions((size_t)n_new);
+    std::vector<int32_t> bt_flat;
+    bt_flat.reserve((size_t)bt_total);
+    // appends the kept pages' table entries of sequence s; returns the offset of the first
+    auto push_table = [&](int s, const PageSpan &span) {
+        const int32_t at = (int32_t)bt_flat.size();
+        const int32_t *row = b->block_tables + (size_t)s * (size_t)b->table_stride;
+        bt_flat.insert(bt_flat.end(), row, row + span.sink_pages);
+        bt_flat.insert(bt_flat.end(), row + span.first, row + span.end);
+        return at;
+    };
+    std::vector<int32_t> bt_off((size_t)B, 0);       // a sequence's entries (with a window: a decode row's)
     std::vector<int32_t> row0((size_t)B + 1, 0);
     {
-        int64_t r = 0, off = 0;
+        int64_t r = 0;
         for (int s = 0; s < B; ++s) {
             row0[(size_t)s] = (int32_t)r;
             const int32_t ql = b->q_lens[s], cl = b->ctx_lens[s];
             if (ql == 0) continue;
-            bt_off[(size_t)s] = (int32_t)off;
-            off += ((int64_t)cl + kPageSize - 1) / kPageSize;
+            if (ql == 1 || win.window == 0) bt_off[(size_t)s] = push_table(s, win.pages(cl - ql, cl));
             const int32_t *row = b->block_tables + (size_t)s * (size_t)b->table_stride;
             for (int32_t t = 0; t < ql; ++t) {
                 const int32_t p = cl - ql + t;
+                positions[(size_t)r] = p;
                 append_dst[(size_t)r++] = row[p / kPageSize] * kPageSize + p % kPageSize;
             }
         }
@@ -499,7 +549,7 @@ int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void
 
     // ---- decode: cut the (row, kv head block) page streams into per-CTA item lists
     int max_ctas = std::max(1, pool->sm_count * decode_ctas_per_sm(d));
-    const int side_ctas = side_by_side_decode_ctas(pool, b, (int)d, (int)Hkv, G, max_ctas);
+    const int side_ctas = side_by_side_decode_ctas(pool, b, win, (int)d, (int)Hkv, G, max_ctas);
     if (side_ctas > 0) max_ctas = side_ctas;
     // Costs are counted in (page, kv head) tiles.  An item covers HB kv heads, so a page of it is HB
     // tiles; a ring stage of the kernel holds kStageTiles tiles = PS pages of an item, and streams are
@@ -525,7 +575,7 @@ int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void
         int64_t left = 0;
         for (int s = 0; s < B; ++s)
             if (b->q_lens[s] == 1)
-                left += (int64_t)NB * ((((int64_t)b->ctx_lens[s] + kPageSize - 1) / kPageSize) * HB + kItemCost);
+                left += (int64_t)NB * ((int64_t)win.pages(b->ctx_lens[s] - 1, b->ctx_lens[s]).count() * HB + kItemCost);
         const int64_t min_share = 2 * kStageTiles + kItemCost;
         items.reserve((size_t)decode_rows * NB + 2 * (size_t)max_ctas);
         cta_begin.reserve((size_t)max_ctas + 1);
@@ -540,8 +590,8 @@ int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void
         };
         for (int s = 0; s < B; ++s) {
             if (b->q_lens[s] != 1) continue;
-            const int32_t cl = b->ctx_lens[s];
-            const int32_t pages = (cl + kPageSize - 1) / kPageSize;
+            const PageSpan span = win.pages(b->ctx_lens[s] - 1, b->ctx_lens[s]);
+            const int32_t kv_len = b->ctx_lens[s] - span.shift(), pages = span.count();
             for (int hb = 0; hb < NB; ++hb) {
                 int32_t rem = pages, pb = 0;
                 const size_t first = items.size();
@@ -556,7 +606,7 @@ int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void
                     it.bt_offset = bt_off[(size_t)s];
                     it.page_begin = pb;
                     it.page_count = take;
-                    it.kv_len = cl;
+                    it.kv_len = kv_len;
                     it.part_slot = -1;
                     it.merge_index = -1;
                     items.push_back(it);
@@ -594,17 +644,26 @@ int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void
         const int32_t ql = b->q_lens[s], cl = b->ctx_lens[s];
         if (ql <= 1) continue;
         for (int32_t t0 = 0; t0 < ql; t0 += 128) {
+            const int32_t rows = std::min(128, ql - t0);
+            int32_t bt = bt_off[(size_t)s], pos0 = cl - ql + t0, ctx = cl;
+            if (win.window > 0) {
+                // the unit's own compacted context, which ends with its last row (no row sees further)
+                const PageSpan span = win.pages(pos0, pos0 + rows);
+                bt = push_table(s, span);
+                ctx = pos0 + rows - span.shift();
+                pos0 -= span.shift();
+            }
             // two q heads of one kv head share a work unit (and its K/V stream); an odd head is alone
             for (int h = 0; h < b->num_q_heads; h += ((h % G) + 1 < G ? 2 : 1)) {
                 PrefillTile t{};
                 t.q_row0 = row0[(size_t)s] + t0;
-                t.rows = std::min(128, ql - t0);
+                t.rows = rows;
                 t.q_head = h;
                 t.q_head_b = (h % G) + 1 < G ? h + 1 : -1;
                 t.kv_head = h / G;
-                t.bt_offset = bt_off[(size_t)s];
-                t.pos0 = cl - ql + t0;
-                t.ctx_len = cl;
+                t.bt_offset = bt;
+                t.pos0 = pos0;
+                t.ctx_len = ctx;
                 tiles.push_back(t);
             }
         }
@@ -621,7 +680,8 @@ int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void
     };
     size_t cursor = 0;
     const size_t o_append = sec(cursor, (size_t)n_new);
-    const size_t o_bt = sec(cursor, (size_t)bt_total);
+    const size_t o_pos = sec(cursor, (size_t)n_new);
+    const size_t o_bt = sec(cursor, bt_flat.size());
     const size_t o_items = sec(cursor, items.size() * 8);
     const size_t o_cta = sec(cursor, cta_begin.size());
     const size_t o_merge = sec(cursor, merges.size() * 4);
@@ -633,11 +693,8 @@ int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void
     plan->blob.assign(total_ints, 0);
     int32_t *h = plan->blob.data();
     if (n_new) std::memcpy(h + o_append, append_dst.data(), (size_t)n_new * 4);
-    for (int s = 0; s < B; ++s) {
-        if (b->q_lens[s] == 0) continue;
-        const size_t need = ((size_t)b->ctx_lens[s] + kPageSize - 1) / kPageSize;
-        std::memcpy(h + o_bt + bt_off[(size_t)s], b->block_tables + (size_t)s * (size_t)b->table_stride, need * 4);
-    }
+    if (n_new) std::memcpy(h + o_pos, positions.data(), (size_t)n_new * 4);
+    if (!bt_flat.empty()) std::memcpy(h + o_bt, bt_flat.data(), bt_flat.size() * 4);
     if (!items.empty()) std::memcpy(h + o_items, items.data(), items.size() * sizeof(DecodeItem));
     if (!cta_begin.empty()) std::memcpy(h + o_cta, cta_begin.data(), cta_begin.size() * 4);
     if (!merges.empty()) std::memcpy(h + o_merge, merges.data(), merges.size() * sizeof(MergeEntry));
@@ -649,7 +706,7 @@ int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void
     plan->layout.cta_begin = (int64_t)o_cta;
     plan->layout.merge_entries = (int64_t)o_merge;
     plan->layout.prefill_tiles = (int64_t)o_tiles;
-    plan->layout.n_bt = bt_total;
+    plan->layout.n_bt = (int64_t)bt_flat.size();
     plan->layout.n_cta_begin = (int64_t)cta_begin.size();
 
     if (pool->desc.device >= 0) {
@@ -674,7 +731,10 @@ int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void
     plan->scale = b->softmax_scale > 0.f ? b->softmax_scale : 1.0f / std::sqrt((float)d);
     plan->n_part_slots = n_slots;
     plan->head_block = HB;
+    plan->window = win.window;
+    plan->sinks = win.sinks;
     plan->d_append_dst = plan->buf.dev + o_append;
+    plan->d_positions = plan->buf.dev + o_pos;
     plan->d_bt_flat = plan->buf.dev + o_bt;
     plan->d_items = (const DecodeItem *)(plan->buf.dev + o_items);
     plan->d_cta_begin = plan->buf.dev + o_cta;
@@ -719,6 +779,34 @@ int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void
     info.decode_head_block = HB;
     *out = plan;
     return AP_OK;
+}
+
+int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, void *stream) {
+    try {
+        return plan_create(out, pool, b, WindowView{0, 0}, stream);
+    } catch (const std::bad_alloc &) {
+        return AP_ERR_CUDA;
+    }
+}
+
+int ap_plan_create_windowed(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, const ap_window_desc *window,
+                            void *stream) {
+    if (!out) return AP_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!window || window->window < 1 || window->sinks < 0) return AP_ERR_INVALID_ARG;
+    // A window or a number of sinks beyond the longest context means the same as that context's length; cut
+    // down to it, sums and differences of positions, window and sinks stay within 32 bits everywhere.
+    WindowView win{window->window, window->sinks};
+    if (b && b->batch > 0 && b->ctx_lens) {
+        const int32_t longest = std::max(1, *std::max_element(b->ctx_lens, b->ctx_lens + b->batch));
+        win.window = std::min(win.window, longest);
+        win.sinks = std::min(win.sinks, longest);
+    }
+    try {
+        return plan_create(out, pool, b, win, stream);
+    } catch (const std::bad_alloc &) {
+        return AP_ERR_CUDA;
+    }
 }
 
 int ap_plan_predict(const ap_plan *plan, double hbm_gbs, double tensor_tflops, ap_plan_prediction *out) {

@@ -227,14 +227,17 @@ __device__ __forceinline__ void combine_item(const DecodeItem item, const float 
 
 // The work of one decode CTA: list number `cta` of the plan.  Called by kDecodeThreads threads of a CTA
 // (any further threads of the block must not call it).
-template <int D>
+// kWin: sliding window.  The planner has cut the pages without a visible key out of the row's table, so of
+// the kv_len keys that are left only [sinks, kv_len - window) are hidden: the rest of the last sink page and
+// the head of the window's first page, fewer than two pages.
+template <int D, bool kWin>
 __device__ __forceinline__ void decode_cta(const CUtensorMap &k_map, const CUtensorMap &v_map, const __nv_bfloat16 *__restrict__ q,
                                            const DecodeItem *__restrict__ items, const int32_t *__restrict__ cta_begin,
                                            const int32_t *__restrict__ bt_flat, const MergeEntry *__restrict__ merges,
                                            float *o_part, float *lse_part, __nv_bfloat16 *__restrict__ out,
                                            float *__restrict__ lse_out, int Hq, int Hkv, int G, int HB, int n_stages, int n_bufs,
                                            int num_pages, float scale_log2, int *status, int *merge_counters,
-                                           uint64_t wait_limit_ns, int cta) {
+                                           uint64_t wait_limit_ns, int cta, int window, int sinks) {
     using Cfg = DecodeCfg<D>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -545,6 +548,21 @@ __device__ __forceinline__ void decode_cta(const CUtensorMap &k_map, const CUten
                     fence_proxy_async_smem();
                     __syncwarp();
                 }
+                int h0 = 0, h1 = 0;                      // tokens [h0, h1) of this page are hidden by the window
+                if constexpr (kWin) {
+                    const int base = (item.page_begin + my_page) * kPageSize;
+                    h0 = max(sinks - base, 0);
+                    h1 = min(item.kv_len - window - base, kPageSize);
+                    if (h0 < h1) {
+                        // like the slots past the context: whatever V holds there, 0 * V must be 0
+                        for (int idx = lane; idx < (h1 - h0) * (D / 8); idx += 32) {
+                            const int tok = h0 + idx / (D / 8), ch = idx % (D / 8);
+                            *(uint4 *)(v_ptr + tile_off<D>(tok, ch)) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                }
                 // ---- S^T = K Q^T : tokens (g, g+8) x heads (2t, 2t+1)
                 float s[4] = {0.f, 0.f, 0.f, 0.f};
                 {
@@ -559,6 +577,10 @@ __device__ __forceinline__ void decode_cta(const CUtensorMap &k_map, const CUten
                 }
                 if (g >= tv) s[0] = s[1] = -INFINITY;
                 if (g + 8 >= tv) s[2] = s[3] = -INFINITY;
+                if constexpr (kWin) {                    // (a kept page has a visible key: the maximum below is finite)
+                    if (g >= h0 && g < h1) s[0] = s[1] = -INFINITY;
+                    if (g + 8 >= h0 && g + 8 < h1) s[2] = s[3] = -INFINITY;
+                }
                 float mx0 = fmaxf(s[0], s[2]), mx1 = fmaxf(s[1], s[3]);
 #pragma unroll
                 for (int sh = 4; sh <= 16; sh <<= 1) {

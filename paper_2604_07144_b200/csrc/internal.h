@@ -129,12 +129,17 @@ struct ap_plan {
     ap_plan_layout layout{};
     std::vector<int32_t> blob;   // host copy of the uploaded work lists
     int n_part_slots = 0;
+    // Sliding window (0: none).  The plan's lists then count keys in compacted contexts: the pages no new
+    // token of a decode row (of a prefill unit) sees are left out of its block-table entries, and bt_offset,
+    // kv_len, pos0 and ctx_len refer to what is left.
+    int window = 0, sinks = 0;
     ap::PlanWork work{};
     bool side_by_side = false;   // decode confined to part of the GPU, prefill on the rest at the same time
     bool single_launch = false;  // ... and both in one launch (else: two kernels on two streams)
     ap::WorkspaceLayout ws{};
     // device pointers into buf.dev
     const int32_t *d_append_dst = nullptr;
+    const int32_t *d_positions = nullptr;    // position in its sequence of every new token row
     const int32_t *d_bt_flat = nullptr;
     const ap::DecodeItem *d_items = nullptr;
     const int32_t *d_cta_begin = nullptr;

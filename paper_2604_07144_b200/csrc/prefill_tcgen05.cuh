@@ -132,11 +132,15 @@ __device__ __noinline__ void rescale_o(uint32_t taddr, float alpha) {
 }
 
 // One work unit: entry `unit` of the plan's list.  Called by all kPrefillThreads threads of a CTA.
-template <int D>
+// kWin: sliding window.  The row at position p sees key v if v <= p and (v > p - window or v < sinks), in
+// positions of the unit's compacted context (the planner leaves out the pages that no row of the unit sees,
+// which lie between the sinks and the first row's window, so both tests hold for compacted positions too).
+template <int D, bool kWin>
 __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUtensorMap &k_map, const CUtensorMap &v_map,
                                              const PrefillTile *__restrict__ tiles, const int32_t *__restrict__ bt_flat,
                                              __nv_bfloat16 *__restrict__ out, float *__restrict__ lse_out, int Hq, int Hkv,
-                                             int num_pages, float scale_log2, int *status, uint64_t wait_limit_ns, int unit) {
+                                             int num_pages, float scale_log2, int *status, uint64_t wait_limit_ns, int unit,
+                                             int window, int sinks) {
     using Cfg = PrefillCfg<D>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -305,7 +309,8 @@ __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUt
                         !wait_or_abort(&p_full[x], (uint32_t)j & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
                     // In the last step tile A's softmax group clears the V rows past the context before it
                     // hands P_A over; tile B's product reads the same V tile and has to see that too.
-                    if (x == 1 && j == n_steps - 1 && tile.ctx_len < n_steps * kTileN &&
+                    // (With a window both groups clear the rows themselves: see below.)
+                    if (!kWin && x == 1 && j == n_steps - 1 && tile.ctx_len < n_steps * kTileN &&
                         !wait_or_abort(&p_full[0], (uint32_t)j & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
                     tcgen05_fence_after();
                     issue_pv(nv % kKvSlots, j == 0);
@@ -342,7 +347,21 @@ __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUt
                 if (lane == 0) mbar_arrive(&s_out[x]);
                 const int tok0 = j * kTileN;
                 float mx = -INFINITY;
-                if (tok0 + kTileN - 1 > tile.pos0) {
+                if (kWin && (tok0 + kTileN - 1 > tile.pos0 ||
+                             (tok0 <= tile.pos0 + kTileM - 1 - window && tok0 + kTileN > sinks))) {
+                    // some row's window begins or ends in this step
+                    const int lo = my_pos - window;                     // keys up to lo are hidden unless sinks
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const int key = tok0 + c * 32 + i;
+                            float v = __uint_as_float(sreg[c][i]);
+                            if (key > my_pos || (key <= lo && key >= sinks)) v = -INFINITY;
+                            sreg[c][i] = __float_as_uint(v);
+                            mx = fmaxf(mx, v);
+                        }
+                } else if (!kWin && tok0 + kTileN - 1 > tile.pos0) {
                     // diagonal or last step: keys past the row's position (or past the context) are masked
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
@@ -373,10 +392,12 @@ __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUt
                 float alpha = 1.f;
                 if (rescale) {
                     alpha = exp2_approx((m_used - m_new) * scale_log2);   // 0 on the first step
+                    if (kWin && m_new == -INFINITY) alpha = 1.f;         // no key seen yet: l and O hold nothing
                     m_used = m_new;
                     if (j > 0) rescale_o<D>(lane_addr + col_o, alpha);
                 }
-                const float ms = m_used * scale_log2;
+                // (with a window a row may see no key of the unit's first steps: its scores stay -inf, the weights 0)
+                const float ms = kWin && m_used == -INFINITY ? 0.f : m_used * scale_log2;
                 const float2 sc2 = make_float2(scale_log2, scale_log2), nms2 = make_float2(-ms, -ms);
                 float2 sum2 = make_float2(0.f, 0.f), sum2b = make_float2(0.f, 0.f);
 #pragma unroll
@@ -403,7 +424,32 @@ __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUt
                 const float sum = (sum2.x + sum2b.x) + (sum2.y + sum2b.y);
                 l = l * alpha + sum;
                 tmem_st_wait();
-                if (x == 0 && j == n_steps - 1 && tile.ctx_len < n_steps * kTileN) {
+                if constexpr (kWin) {
+                    // Keys no row of the unit sees, in pages that are kept: [sinks, first row's window) and the
+                    // slots past the last row.  Whatever V holds there, 0 * V must be 0.  Each group clears them
+                    // before it hands its own P over (the same zeros to the same rows, so it does not matter
+                    // which comes first): the clearing may fall into any step, and a tile's issuer following
+                    // the other tile's hand-over through all steps could fall more than one phase behind.
+                    const int hole0 = max(sinks, tok0) - tok0;
+                    const int hole1 = min(max(tile.pos0 - window + 1, 0), tok0 + kTileN) - tok0;
+                    const int tail = max(tile.ctx_len - tok0, 0);
+                    if (hole0 < hole1 || tail < kTileN) {
+                        const int nv = kv_seq_v(j, n_steps), s = nv % kKvSlots;
+                        if (!wait_or_abort(&kv_full[s], (uint32_t)(nv / kKvSlots) & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
+                        uint8_t *v_tile = smem + Cfg::kOffK + s * Cfg::kKvTileBytes;
+                        auto clear_rows = [&](int first, int end) {
+                            for (int idx = r; idx < (end - first) * (D / 8); idx += 128) {
+                                const int key = first + idx / (D / 8), ch = idx % (D / 8);
+                                *(uint4 *)(v_tile + (key >> 3) * (1024 * Cfg::kHalves) + (ch >> 3) * 1024 + (key & 7) * 128 +
+                                           ((ch & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                            }
+                        };
+                        if (hole0 < hole1) clear_rows(hole0, hole1);
+                        clear_rows(tail, kTileN);
+                        fence_proxy_async_smem();
+                    }
+                }
+                if (!kWin && x == 0 && j == n_steps - 1 && tile.ctx_len < n_steps * kTileN) {
                     // keys past the context hold no token: clear their V rows so 0 * garbage cannot
                     // poison O (tile A's group does it; tile B's issuer waits for tile A's hand-over too)
                     const int nv = kv_seq_v(j, n_steps), s = nv % kKvSlots;
