@@ -100,6 +100,30 @@ size_t ap_kv_pool_bytes(const ap_pool_desc *desc);
  * (head_dim/page_size), CUDA (no device, allocation failure). */
 int ap_kv_pool_create(ap_kv_pool **out, const ap_pool_desc *desc);
 
+/*
+ * The same for a pool that holds K and V in 4 bits.  Planes:
+ *     K, V : [num_pages][num_kv_heads] tiles of 16 * (head_dim / 2 + head_dim / 16) bytes
+ * A tile is 16 token rows of head_dim / 2 bytes of codes, then 16 x head_dim / 32
+ * bf16 steps.  32 consecutive elements of a row share a step s, and code c (0..15)
+ * stands for (c - 8) s.  The head_dim / 8 words of a row (8 codes each, lowest
+ * nibble first) are stored at index t * (head_dim / 32) + g for elements
+ * 32 g + 8 t .. + 7.
+ * ap_kv_append quantises: s = max|x| / 7 rounded up to five significant bits,
+ * c = rint(x / s) + 8 (1..15).  So |x - (c - 8) s| <= s / 2, and (c - 8) s is
+ * exactly a bf16 number: attention over the pool is attention over those numbers,
+ * whatever kernel does it.  A group of 32 with an element that is not finite, or
+ * not below 2^120 in magnitude, stands for NaN.
+ * Everything that takes a pool takes such a pool: plans (with a window too),
+ * ap_kv_append, ap_kv_append_rope, ap_kv_read_new, ap_attention_iteration,
+ * ap_kv_copy_pages (between 4-bit pools), ap_serving_iteration_host.  Decode and
+ * prefill of a mixed iteration run one after the other (ap_kv_pool_set_side_by_side
+ * has no effect).  A plan with prefill chunks needs workspace for the pages they
+ * read, widened to bf16: 2 * 16 * head_dim * 2 bytes per page and kv head.
+ * ap_kv_pool_bytes_4bit: bytes of one plane; 0 if the description is invalid.
+ */
+size_t ap_kv_pool_bytes_4bit(const ap_pool_desc *desc);
+int ap_kv_pool_create_4bit(ap_kv_pool **out, const ap_pool_desc *desc);
+
 /* Frees the handle and only what the library allocated.  Synchronises the device. */
 int ap_kv_pool_destroy(ap_kv_pool *pool);
 
@@ -266,7 +290,7 @@ int ap_plan_export(const ap_plan *plan, int32_t *blob, size_t capacity_ints, ap_
  * from one serving plan to the next migrates KV caches; the page is the unit
  * that moves).  For i in [0, n): page src_ids[i] of src_pool -- every kv head,
  * every slot, K and V -- is copied bit for bit to page dst_ids[i] of dst_pool.
- * The pools must have the same kv heads, head_dim and page size (else
+ * The pools must have the same kv heads, head_dim, page size and format (else
  * INVALID_ARG) and live on the same device (else UNSUPPORTED: a move between
  * GPUs is the caller's peer copy); they may be the same pool (copy-on-write of
  * a shared prefix page).  dst_ids, src_ids: host, n entries each; they are read
@@ -290,6 +314,45 @@ int ap_kv_copy_pages(ap_kv_pool *dst_pool, const ap_kv_pool *src_pool, int32_t n
  */
 int ap_kv_append(ap_kv_pool *pool, const ap_plan *plan, const void *k_new, const void *v_new,
                  void *stream);
+
+/*
+ * KV append with the rotary position embedding applied on the way.  Pair i of a
+ * head's first rotary_dim elements turns by the angle p * f_i, p the token's
+ * position in its sequence (ctx_len - q_len + t):
+ *     (a, b) -> amplitude * (a cos - b sin, b cos + a sin)
+ * (a, b) = elements (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if interleaved.
+ * f_i = base^(-2 i / rotary_dim), or inv_freq[i] where inv_freq is given (scaled
+ * frequencies of any kind).  The rest of the head is copied.  K is rotated and
+ * appended, V is appended as it is, q is rotated into q_rot.  Angles are formed
+ * in 64 bits, the rotation in fp32, and the result is rounded once to bf16 (and
+ * for a 4-bit pool quantised from there).
+ * inv_freq: host, rotary_dim / 2 entries, or NULL; read before the call returns.
+ * rotary_dim: a multiple of 16 up to head_dim (other even numbers UNSUPPORTED).
+ * amplitude: factor on cosine and sine, 0 selects 1.
+ * q, k_new, v_new: device, 16-byte aligned rows [N_new][heads][head_dim] bf16;
+ * *_row_stride: elements from one token's row to the next, a multiple of 8 (0:
+ * contiguous), so that they may be cut out of one projection's output.
+ * q_rot: device, [N_new][num_q_heads][head_dim] contiguous, 16-byte aligned; it may
+ * be q itself if q is contiguous, and may not overlap an input otherwise
+ * (INVALID_ARG).  q and q_rot may both be NULL: K and V only.
+ */
+typedef struct ap_rope_desc {
+    int32_t rotary_dim;
+    int32_t interleaved;    /* 0 or 1 */
+    double base;            /* > 0; not used when inv_freq is given */
+    const double *inv_freq; /* host or NULL */
+    float amplitude;
+    int64_t q_row_stride, k_row_stride, v_row_stride;
+} ap_rope_desc;
+int ap_kv_append_rope(ap_kv_pool *pool, const ap_plan *plan, const ap_rope_desc *rope, const void *q, const void *k_new,
+                      const void *v_new, void *q_rot, void *stream);
+
+/*
+ * Reads the rows of the plan's new tokens back from the pool, as the bf16 numbers
+ * it holds or, in 4 bits, stands for.  k, v: device, [N_new][num_kv_heads][head_dim]
+ * bf16, 16-byte aligned.
+ */
+int ap_kv_read_new(ap_kv_pool *pool, const ap_plan *plan, void *k, void *v, void *stream);
 
 /*
  * Attention for every new token of the batch (decode rows: split-K
@@ -329,7 +392,9 @@ int ap_attention_iteration(ap_kv_pool *pool, const ap_plan *plan, const void *q,
  *    is rejected with AP_ERR_WORKSPACE_TOO_SMALL before anything is launched
  *    (A plan needs at most 2 partials per decode CTA, each head_dim + 1 floats for
  *    every query head of a block of up to 4 kv heads: 4.9 MB on 148 SMs at
- *    head_dim 128 with 8 query heads per kv head, whatever the context lengths.)
+ *    head_dim 128 with 8 query heads per kv head, whatever the context lengths.
+ *    On a 4-bit pool the decode kernel has twice as many CTAs, and prefill chunks
+ *    need their pages in bf16 on top: such plans can be over the limit.)
  *  - The array's device address is looked up once per device when a pool is
  *    created on it (ap_kv_pool_create, which allocates anyway and must not run
  *    inside a stream capture); that is also when the runtime brings the array

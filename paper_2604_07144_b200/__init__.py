@@ -12,5 +12,5 @@ from .binding import (  # noqa: F401
     kv_pool_seed_free_list, kv_pool_v_base, last_device_status, plan_create, plan_destroy,
     plan_predict, plan_export, plan_get_info, plan_workspace_bytes, profile_collect, profile_enable,
     serving_iteration_host, status_string, kv_pool_set_wait_limit, selftest_wait_timeout, kv_pool_set_single_launch,
-    plan_create_windowed,
+    plan_create_windowed, kv_pool_bytes_4bit, kv_pool_create_4bit, kv_append_rope, kv_read_new,
 )

@@ -40,7 +40,7 @@ EXPORTED_SYMBOLS = (
     "ap_profile_enable", "ap_profile_collect",
     "ap_static_workspace_bytes", "ap_attention_iteration_static",
     "ap_kv_pool_set_wait_limit", "ap_selftest_wait_timeout", "ap_kv_pool_set_single_launch",
-    "ap_plan_create_windowed",
+    "ap_plan_create_windowed", "ap_kv_pool_bytes_4bit", "ap_kv_pool_create_4bit", "ap_kv_append_rope", "ap_kv_read_new",
 )
 
 
@@ -65,6 +65,12 @@ class BatchDesc(ctypes.Structure):
 
 class WindowDesc(ctypes.Structure):
     _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("base", ctypes.c_double),
+                ("inv_freq", ctypes.c_void_p), ("amplitude", ctypes.c_float), ("q_row_stride", ctypes.c_int64),
+                ("k_row_stride", ctypes.c_int64), ("v_row_stride", ctypes.c_int64)]
 
 
 class PlanInfo(ctypes.Structure):
@@ -127,6 +133,10 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "ap_kv_pool_num_free": (i32, [vp]),
         "ap_kv_pool_set_side_by_side": (ctypes.c_int, [vp, i32]),
         "ap_plan_create": (ctypes.c_int, [ctypes.POINTER(vp), vp, ctypes.POINTER(BatchDesc), vp]),
+        "ap_kv_pool_bytes_4bit": (sz, [ctypes.POINTER(PoolDesc)]),
+        "ap_kv_pool_create_4bit": (ctypes.c_int, [ctypes.POINTER(vp), ctypes.POINTER(PoolDesc)]),
+        "ap_kv_append_rope": (ctypes.c_int, [vp, vp, ctypes.POINTER(RopeDesc), vp, vp, vp, vp, vp]),
+        "ap_kv_read_new": (ctypes.c_int, [vp, vp, vp, vp, vp]),
         "ap_plan_create_windowed": (ctypes.c_int, [ctypes.POINTER(vp), vp, ctypes.POINTER(BatchDesc),
                                                    ctypes.POINTER(WindowDesc), vp]),
         "ap_plan_destroy": (ctypes.c_int, [vp]),
@@ -218,6 +228,20 @@ def kv_pool_create(num_pages: int, num_kv_heads: int, head_dim: int, k_base=None
     d = PoolDesc(num_pages, page_size, num_kv_heads, head_dim, _ptr(k_base), _ptr(v_base), device)
     h = ctypes.c_void_p()
     _check(load().ap_kv_pool_create(ctypes.byref(h), ctypes.byref(d)), "ap_kv_pool_create")
+    return KVPool(h.value, d, (k_base, v_base))
+
+
+def kv_pool_bytes_4bit(num_pages: int, num_kv_heads: int, head_dim: int, page_size: int = 16) -> int:
+    d = PoolDesc(num_pages, page_size, num_kv_heads, head_dim, None, None, 0)
+    return int(load().ap_kv_pool_bytes_4bit(ctypes.byref(d)))
+
+
+def kv_pool_create_4bit(num_pages: int, num_kv_heads: int, head_dim: int, k_base=None, v_base=None,
+                        device: int = 0, page_size: int = 16) -> KVPool:
+    """Pool that holds K and V in 4 bits (see ap_kv_pool_create_4bit for the planes' layout)."""
+    d = PoolDesc(num_pages, page_size, num_kv_heads, head_dim, _ptr(k_base), _ptr(v_base), device)
+    h = ctypes.c_void_p()
+    _check(load().ap_kv_pool_create_4bit(ctypes.byref(h), ctypes.byref(d)), "ap_kv_pool_create_4bit")
     return KVPool(h.value, d, (k_base, v_base))
 
 
@@ -360,6 +384,38 @@ def plan_export(plan: Plan) -> dict:
 def kv_append(pool: KVPool, plan: Plan, k_new, v_new, stream=None) -> None:
     _check(load().ap_kv_append(pool.handle, plan.handle, _ptr(k_new), _ptr(v_new), _stream(stream)),
            "ap_kv_append")
+
+
+def _row_stride(x) -> int:
+    """Elements from one row of a [rows, heads, head_dim] tensor to the next (0: contiguous, or not a tensor)."""
+    if x is None or not hasattr(x, "stride") or x.dim() != 3 or x.shape[0] < 2:
+        return 0
+    rows, heads, dim = x.stride()
+    if dim != 1 or (x.shape[1] > 1 and heads != x.shape[2]):
+        raise ValueError("a token's heads must be contiguous")
+    return int(rows)
+
+
+def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, rotary_dim: Optional[int] = None,
+                   base: float = 10000.0, interleaved: bool = False, inv_freq=None, amplitude: float = 1.0,
+                   stream=None) -> None:
+    """Append with the rotary embedding: K rotated by its position, V as it is, ``q`` rotated into ``q_rot``.
+    Tensors [rows, heads, head_dim] may be strided by row (slices of one projection)."""
+    freq = None if inv_freq is None else np.ascontiguousarray(inv_freq, dtype=np.float64)
+    rotary = pool.head_dim if rotary_dim is None else int(rotary_dim)
+    if freq is not None and freq.shape != (rotary // 2,):
+        raise ValueError("inv_freq must have rotary_dim / 2 entries")
+    if q_rot is not None and hasattr(q_rot, "is_contiguous") and not q_rot.is_contiguous():
+        raise ValueError("q_rot must be contiguous")
+    desc = RopeDesc(rotary, int(bool(interleaved)), float(base), _ptr(freq), float(amplitude), _row_stride(q),
+                    _row_stride(k_new), _row_stride(v_new))
+    _check(load().ap_kv_append_rope(pool.handle, plan.handle, ctypes.byref(desc), _ptr(q), _ptr(k_new), _ptr(v_new),
+                                    _ptr(q_rot), _stream(stream)), "ap_kv_append_rope")
+
+
+def kv_read_new(pool: KVPool, plan: Plan, k, v, stream=None) -> None:
+    """The rows of the plan's new tokens, read back as the bf16 numbers the pool holds (or, in 4 bits, stands for)."""
+    _check(load().ap_kv_read_new(pool.handle, plan.handle, _ptr(k), _ptr(v), _stream(stream)), "ap_kv_read_new")
 
 
 def kv_copy_pages(dst_pool: KVPool, src_pool: KVPool, dst_ids: Sequence[int], src_ids: Sequence[int], stream=None) -> None:

@@ -28,6 +28,11 @@ struct DeviceGuard {
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// bytes of one (page, kv head) tile of a plane: 16 rows of d bf16 numbers, or of d 4-bit codes and d / 32 steps
+inline int pool_tile_bytes(int head_dim, bool four_bit) {
+    return four_bit ? kPageSize * (head_dim / 2 + head_dim / 16) : kPageSize * head_dim * 2;
+}
+
 bool desc_valid(const ap_pool_desc *d) {
     return d && d->num_pages > 0 && d->num_kv_heads > 0 && d->head_dim > 0 && d->page_size > 0;
 }
@@ -141,7 +146,7 @@ inline double side_by_side_us(double decode_bytes, double w_p, int k, double sm_
 int side_by_side_decode_ctas(const ap_kv_pool *pool, const ap_batch_desc *b, const WindowView &win, int d, int Hkv, int G,
                              int max_ctas) {
     const int mode = pool->side_by_side_mode;
-    if (mode == 0) return 0;
+    if (mode == 0 || pool->four_bit) return 0;           // (a 4-bit pool's decode and prefill kernels run one after the other)
     double decode_bytes = 0.0, w_p = 0.0;
     int64_t decode_rows = 0, prefill_seqs = 0;
     const double d_scale = (double)d / 128.0;
@@ -202,8 +207,30 @@ namespace ap {
 // The attention kernels of a plan, in the plan's dispatch mode.  Shared by every entry point that
 // runs attention; allocates nothing (the second stream and the events belong to the pool).
 cudaError_t launch_attention_kernels(ap_kv_pool *pool, const ap_plan *plan, const void *q, void *out, float *lse,
-                                     float *o_part, float *lse_part, cudaStream_t st) {
+                                     char *ws, cudaStream_t st) {
+    float *o_part = plan->ws.bytes ? (float *)(ws + plan->ws.o_part_off) : nullptr;
+    float *lse_part = plan->ws.bytes ? (float *)(ws + plan->ws.lse_part_off) : nullptr;
     cudaError_t e = cudaSuccess;
+    if (pool->four_bit) {
+        if (plan->info.decode_items > 0) {
+            TimedScope timed(pool, AP_KERNEL_DECODE, st);
+            e = launch_kv4_decode(pool, plan, q, out, lse, o_part, lse_part, st);
+        }
+        if (e == cudaSuccess && plan->info.prefill_tiles > 0) {
+            // prefill is bound by the tensor cores and reads a page's K/V once per unit: the pages are widened to
+            // bf16 once, into the workspace, and the units read them from there
+            TimedScope timed(pool, AP_KERNEL_PREFILL, st);
+            void *k = ws + plan->ws.wide_k_off, *v = ws + plan->ws.wide_v_off;
+            const ap_pool_desc &d = pool->desc;
+            CUtensorMap k_map, v_map;
+            if (encode_pool_tensor_map(&k_map, k, plan->n_wide_pages, d.num_kv_heads, d.head_dim, 1) != AP_OK ||
+                encode_pool_tensor_map(&v_map, v, plan->n_wide_pages, d.num_kv_heads, d.head_dim, 1) != AP_OK)
+                return cudaErrorInvalidValue;
+            e = launch_kv4_widen(pool, plan, k, v, st);
+            if (e == cudaSuccess) e = launch_prefill(pool, plan, q, out, lse, k_map, v_map, plan->n_wide_pages, st);
+        }
+        return e;
+    }
     if (plan->single_launch) {
         // One grid: the decode CTAs have the lowest block indices, so they are resident first and the
         // prefill units fill the remaining SMs and, as decode CTAs retire, those too.
@@ -221,7 +248,7 @@ cudaError_t launch_attention_kernels(ap_kv_pool *pool, const ap_plan *plan, cons
         if (e == cudaSuccess) e = cudaStreamWaitEvent(pool->side_stream, pool->fork_event, 0);
         if (e == cudaSuccess) {
             TimedScope timed(pool, AP_KERNEL_PREFILL, pool->side_stream);
-            e = launch_prefill(pool, plan, q, out, lse, pool->side_stream);
+            e = launch_prefill(pool, plan, q, out, lse, pool->k_map, pool->v_map, pool->desc.num_pages, pool->side_stream);
         }
         if (e == cudaSuccess) e = cudaEventRecord(pool->join_event, pool->side_stream);
         if (e == cudaSuccess) e = cudaStreamWaitEvent(st, pool->join_event, 0);
@@ -232,7 +259,7 @@ cudaError_t launch_attention_kernels(ap_kv_pool *pool, const ap_plan *plan, cons
         }
         if (e == cudaSuccess && plan->info.prefill_tiles > 0) {
             TimedScope timed(pool, AP_KERNEL_PREFILL, st);
-            e = launch_prefill(pool, plan, q, out, lse, st);
+            e = launch_prefill(pool, plan, q, out, lse, pool->k_map, pool->v_map, pool->desc.num_pages, st);
         }
     }
     return e;
@@ -262,7 +289,12 @@ size_t ap_kv_pool_bytes(const ap_pool_desc *d) {
            (size_t)d->head_dim * 2u;
 }
 
-int ap_kv_pool_create(ap_kv_pool **out, const ap_pool_desc *desc) {
+size_t ap_kv_pool_bytes_4bit(const ap_pool_desc *d) {
+    if (!desc_valid(d) || d->page_size != kPageSize || (d->head_dim != 64 && d->head_dim != 128)) return 0;
+    return (size_t)d->num_pages * (size_t)d->num_kv_heads * (size_t)pool_tile_bytes(d->head_dim, true);
+}
+
+static int pool_create(ap_kv_pool **out, const ap_pool_desc *desc, bool four_bit) {
     if (!out) return AP_ERR_INVALID_ARG;
     *out = nullptr;
     if (!desc_valid(desc)) return AP_ERR_INVALID_ARG;
@@ -281,6 +313,8 @@ int ap_kv_pool_create(ap_kv_pool **out, const ap_pool_desc *desc) {
         ap_kv_pool *hp = new (std::nothrow) ap_kv_pool();
         if (!hp) return AP_ERR_CUDA;
         hp->desc = *desc;
+        hp->four_bit = four_bit;
+        hp->tile_bytes = pool_tile_bytes(desc->head_dim, four_bit);
         hp->head_block = decode_head_block(desc->num_kv_heads);
         hp->sm_count = 148;
         hp->free_list.resize((size_t)desc->num_pages);
@@ -296,6 +330,8 @@ int ap_kv_pool_create(ap_kv_pool **out, const ap_pool_desc *desc) {
     ap_kv_pool *p = new (std::nothrow) ap_kv_pool();
     if (!p) return AP_ERR_CUDA;
     p->desc = *desc;
+    p->four_bit = four_bit;
+    p->tile_bytes = pool_tile_bytes(desc->head_dim, four_bit);
     p->head_block = decode_head_block(desc->num_kv_heads);
     int rc = AP_OK;
     do {
@@ -303,7 +339,7 @@ int ap_kv_pool_create(ap_kv_pool **out, const ap_pool_desc *desc) {
             rc = AP_ERR_CUDA;
             break;
         }
-        const size_t bytes = ap_kv_pool_bytes(desc);
+        const size_t bytes = four_bit ? ap_kv_pool_bytes_4bit(desc) : ap_kv_pool_bytes(desc);
         if (!desc->k_base) {
             p->owns_planes = true;
             if (cudaMalloc(&p->desc.k_base, bytes) != cudaSuccess ||
@@ -334,16 +370,18 @@ int ap_kv_pool_create(ap_kv_pool **out, const ap_pool_desc *desc) {
         }
         rc = prepare_static_workspace(desc->device);
         if (rc != AP_OK) break;
-        rc = encode_pool_tensor_map(&p->k_map, p->desc.k_base, desc->num_pages, desc->num_kv_heads, desc->head_dim, 1);
-        if (rc != AP_OK) break;
-        rc = encode_pool_tensor_map(&p->v_map, p->desc.v_base, desc->num_pages, desc->num_kv_heads, desc->head_dim, 1);
-        if (rc != AP_OK) break;
-        rc = encode_pool_tensor_map(&p->k_map_blk, p->desc.k_base, desc->num_pages, desc->num_kv_heads, desc->head_dim,
-                                    p->head_block);
-        if (rc != AP_OK) break;
-        rc = encode_pool_tensor_map(&p->v_map_blk, p->desc.v_base, desc->num_pages, desc->num_kv_heads, desc->head_dim,
-                                    p->head_block);
-        if (rc != AP_OK) break;
+        if (!four_bit) {
+            rc = encode_pool_tensor_map(&p->k_map, p->desc.k_base, desc->num_pages, desc->num_kv_heads, desc->head_dim, 1);
+            if (rc != AP_OK) break;
+            rc = encode_pool_tensor_map(&p->v_map, p->desc.v_base, desc->num_pages, desc->num_kv_heads, desc->head_dim, 1);
+            if (rc != AP_OK) break;
+            rc = encode_pool_tensor_map(&p->k_map_blk, p->desc.k_base, desc->num_pages, desc->num_kv_heads, desc->head_dim,
+                                        p->head_block);
+            if (rc != AP_OK) break;
+            rc = encode_pool_tensor_map(&p->v_map_blk, p->desc.v_base, desc->num_pages, desc->num_kv_heads, desc->head_dim,
+                                        p->head_block);
+            if (rc != AP_OK) break;
+        }
         p->free_list.resize((size_t)desc->num_pages);
         for (int32_t i = 0; i < desc->num_pages; ++i) p->free_list[(size_t)i] = desc->num_pages - 1 - i;
         p->allocated.assign((size_t)desc->num_pages, 0);
@@ -356,6 +394,9 @@ int ap_kv_pool_create(ap_kv_pool **out, const ap_pool_desc *desc) {
     *out = p;
     return AP_OK;
 }
+
+int ap_kv_pool_create(ap_kv_pool **out, const ap_pool_desc *desc) { return pool_create(out, desc, false); }
+int ap_kv_pool_create_4bit(ap_kv_pool **out, const ap_pool_desc *desc) { return pool_create(out, desc, true); }
 
 int ap_kv_pool_destroy(ap_kv_pool *pool) {
     if (!pool) return AP_ERR_INVALID_ARG;
@@ -458,6 +499,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     // ---- validation + row bookkeeping
     int64_t n_new = 0, kv_tokens = 0, bt_total = 0, pairs = 0;
     int64_t decode_rows = 0, prefill_seqs = 0;
+    int64_t prefill_bt = 0;                          // pages that prefill sequences see
     int64_t decode_kv = 0, decode_bt = 0, prefill_kv = 0, prefill_rows = 0;   // for the work figures of ap_plan_predict
     for (int s = 0; s < B; ++s) {
         const int32_t ql = b->q_lens[s], cl = b->ctx_lens[s];
@@ -489,9 +531,12 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
                 for (int32_t t = 0; t < ql; ++t) pairs += win.keys(cl - ql + t);
             }
             prefill_kv += seen;
+            prefill_bt += span.count();
             prefill_rows += ql;
         }
     }
+    // (widened pages are addressed like a pool's: 8-row groups with a 32-bit extent)
+    if (pool->four_bit && prefill_bt * Hkv * 2 >= (int64_t)1 << 31) return AP_ERR_UNSUPPORTED;
     if (n_new > (int64_t)1 << 30 || bt_total > (int64_t)1 << 30) return AP_ERR_UNSUPPORTED;
 
     std::vector<int32_t> append_dst((size_t)n_new), positions((size_t)n_new);
@@ -506,6 +551,16 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
         return at;
     };
     std::vector<int32_t> bt_off((size_t)B, 0);       // a sequence's entries (with a window: a decode row's)
+    // 4-bit pool: the pages that prefill units read are widened into the workspace; their units' table entries
+    // number those copies.  Sequence s's are wide_first[s], ...: the pages of its span over all its new tokens.
+    std::vector<int32_t> wide_pages, wide_first((size_t)B, 0);
+    auto push_wide = [&](int s, const PageSpan &all, const PageSpan &span) {
+        const int32_t at = (int32_t)bt_flat.size(), w0 = wide_first[(size_t)s];
+        auto copy_of = [&](int32_t page) { return w0 + (page < all.sink_pages ? page : page - all.first + all.sink_pages); };
+        for (int32_t i = 0; i < span.sink_pages; ++i) bt_flat.push_back(copy_of(i));
+        for (int32_t i = span.first; i < span.end; ++i) bt_flat.push_back(copy_of(i));
+        return at;
+    };
     std::vector<int32_t> row0((size_t)B + 1, 0);
     {
         int64_t r = 0;
@@ -513,7 +568,15 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
             row0[(size_t)s] = (int32_t)r;
             const int32_t ql = b->q_lens[s], cl = b->ctx_lens[s];
             if (ql == 0) continue;
-            if (ql == 1 || win.window == 0) bt_off[(size_t)s] = push_table(s, win.pages(cl - ql, cl));
+            const PageSpan all = win.pages(cl - ql, cl);
+            if (ql > 1 && pool->four_bit) {
+                wide_first[(size_t)s] = (int32_t)wide_pages.size();
+                const int32_t *row = b->block_tables + (size_t)s * (size_t)b->table_stride;
+                wide_pages.insert(wide_pages.end(), row, row + all.sink_pages);
+                wide_pages.insert(wide_pages.end(), row + all.first, row + all.end);
+            }
+            if (ql == 1 || win.window == 0)
+                bt_off[(size_t)s] = ql > 1 && pool->four_bit ? push_wide(s, all, all) : push_table(s, all);
             const int32_t *row = b->block_tables + (size_t)s * (size_t)b->table_stride;
             for (int32_t t = 0; t < ql; ++t) {
                 const int32_t p = cl - ql + t;
@@ -548,7 +611,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     }
 
     // ---- decode: cut the (row, kv head block) page streams into per-CTA item lists
-    int max_ctas = std::max(1, pool->sm_count * decode_ctas_per_sm(d));
+    int max_ctas = std::max(1, pool->sm_count * (pool->four_bit ? kKv4CtasPerSm : decode_ctas_per_sm(d)));
     const int side_ctas = side_by_side_decode_ctas(pool, b, win, (int)d, (int)Hkv, G, max_ctas);
     if (side_ctas > 0) max_ctas = side_ctas;
     // Costs are counted in (page, kv head) tiles.  An item covers HB kv heads, so a page of it is HB
@@ -559,8 +622,10 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     // ~58 to ~90 GB/s.  With the whole GPU decode is HBM-bound at ~41 GB/s per SM either way, and
     // one kv head per item keeps the partials (and their merge in the kernel's tail) small -- except at
     // head_dim 64, where a tile is 2 KB and single-tile requests cannot even feed 148 SMs.
-    const int HB = (side_ctas > 0 || d < 128) ? pool->head_block : 1, NB = Hkv / HB;
-    constexpr int kStageTiles = kDecodeTilesPerStage;
+    // (The 4-bit kernel always takes blocks: the HB small tiles of a page that lie together, and eight warps
+    // that share a row's pages among fewer of them.)
+    const int HB = (side_ctas > 0 || d < 128 || pool->four_bit) ? pool->head_block : 1, NB = Hkv / HB;
+    const int kStageTiles = pool->four_bit ? kKv4TilesPerRound : kDecodeTilesPerStage;
     const int PS = kStageTiles / HB;      // pages of an item per stage
     constexpr int kItemCost = 3;          // fixed per-item cost (its query load, the hand-over of its result)
     std::vector<DecodeItem> items;
@@ -649,7 +714,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
             if (win.window > 0) {
                 // the unit's own compacted context, which ends with its last row (no row sees further)
                 const PageSpan span = win.pages(pos0, pos0 + rows);
-                bt = push_table(s, span);
+                bt = pool->four_bit ? push_wide(s, win.pages(cl - ql, cl), span) : push_table(s, span);
                 ctx = pos0 + rows - span.shift();
                 pos0 -= span.shift();
             }
@@ -686,6 +751,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     const size_t o_cta = sec(cursor, cta_begin.size());
     const size_t o_merge = sec(cursor, merges.size() * 4);
     const size_t o_tiles = sec(cursor, tiles.size() * 8);
+    const size_t o_wide = sec(cursor, wide_pages.size());
     const size_t total_ints = std::max<size_t>(cursor, 8);
 
     ap_plan *plan = new (std::nothrow) ap_plan();
@@ -698,6 +764,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     if (!items.empty()) std::memcpy(h + o_items, items.data(), items.size() * sizeof(DecodeItem));
     if (!cta_begin.empty()) std::memcpy(h + o_cta, cta_begin.data(), cta_begin.size() * 4);
     if (!merges.empty()) std::memcpy(h + o_merge, merges.data(), merges.size() * sizeof(MergeEntry));
+    if (!wide_pages.empty()) std::memcpy(h + o_wide, wide_pages.data(), wide_pages.size() * 4);
     if (!tiles.empty()) std::memcpy(h + o_tiles, tiles.data(), tiles.size() * sizeof(PrefillTile));
     plan->layout.total_ints = (int64_t)total_ints;
     plan->layout.append_dst = (int64_t)o_append;
@@ -743,6 +810,14 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     plan->ws.o_part_off = 0;
     plan->ws.lse_part_off = align_up((size_t)n_slots * HB * G * d * sizeof(float), 256);
     plan->ws.bytes = n_slots ? plan->ws.lse_part_off + align_up((size_t)n_slots * HB * G * sizeof(float), 256) : 0;
+    plan->n_wide_pages = (int)wide_pages.size();
+    plan->d_wide_pages = plan->buf.dev + o_wide;
+    if (!wide_pages.empty()) {
+        const size_t plane = align_up(wide_pages.size() * (size_t)Hkv * (size_t)pool_tile_bytes(d, false), 256);
+        plan->ws.wide_k_off = plan->ws.bytes;
+        plan->ws.wide_v_off = plan->ws.bytes + plane;
+        plan->ws.bytes += 2 * plane;
+    }
 
     ap_plan_info &info = plan->info;
     info.n_new = n_new;
@@ -758,11 +833,11 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     {
         // algorithmic work of one layer: every attended KV token's K and V once per kv head, q read,
         // out + lse written, used block-table entries once; 4 d flop per (q head, query row, unmasked key)
-        const double per_kv_token = 2.0 * (double)Hkv * (double)d * 2.0;
+        const double per_kv_token = 2.0 * (double)Hkv * (double)pool->tile_bytes / kPageSize;
         const double per_row = 2.0 * (double)b->num_q_heads * (double)d * 2.0 + (double)b->num_q_heads * 4.0;
         plan->work.decode_bytes = (double)decode_kv * per_kv_token + (double)decode_rows * per_row + (double)decode_bt * 4.0;
         plan->work.prefill_bytes = (double)prefill_kv * per_kv_token + (double)prefill_rows * per_row;
-        plan->work.append_bytes = 2.0 * (double)n_new * per_kv_token;
+        plan->work.append_bytes = (double)n_new * (2.0 * (double)Hkv * (double)d * 2.0 + per_kv_token);
         plan->work.decode_flops = 4.0 * (double)b->num_q_heads * (double)d * (double)decode_kv;
         plan->work.prefill_flops = 4.0 * (double)b->num_q_heads * (double)d * (double)pairs;
         double w_p = 0.0;
@@ -774,7 +849,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     }
     plan->side_by_side = side_ctas > 0 && !items.empty() && !tiles.empty();
     plan->single_launch = plan->side_by_side && pool->single_launch;
-    info.launches_attention = plan->single_launch ? 1 : (items.empty() ? 0 : 1) + (tiles.empty() ? 0 : 1);
+    info.launches_attention = plan->single_launch ? 1 : (items.empty() ? 0 : 1) + (tiles.empty() ? 0 : pool->four_bit ? 2 : 1);
     info.side_by_side = plan->side_by_side ? 1 : 0;
     info.decode_head_block = HB;
     *out = plan;
@@ -882,7 +957,70 @@ int ap_kv_append(ap_kv_pool *pool, const ap_plan *plan, const void *k_new, const
     DeviceGuard guard(pool->desc.device);
     if (!guard.ok) return AP_ERR_CUDA;
     TimedScope timed(pool, AP_KERNEL_APPEND, (cudaStream_t)stream);
-    if (launch_kv_append(pool, plan, k_new, v_new, (cudaStream_t)stream) != cudaSuccess) {
+    const cudaError_t e = pool->four_bit ? launch_kv4_append(pool, plan, k_new, v_new, (cudaStream_t)stream)
+                                         : launch_kv_append(pool, plan, k_new, v_new, (cudaStream_t)stream);
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();
+        return AP_ERR_CUDA;
+    }
+    return AP_OK;
+}
+
+int ap_kv_append_rope(ap_kv_pool *pool, const ap_plan *plan, const ap_rope_desc *rope, const void *q, const void *k_new,
+                      const void *v_new, void *q_rot, void *stream) {
+    if (!pool || !plan || plan->pool != pool || !rope) return AP_ERR_INVALID_ARG;
+    const int d = pool->desc.head_dim, Hkv = pool->desc.num_kv_heads, Hq = plan->num_q_heads;
+    if (rope->rotary_dim < 2 || rope->rotary_dim > d || rope->rotary_dim % 2) return AP_ERR_INVALID_ARG;
+    if (rope->rotary_dim % 16) return AP_ERR_UNSUPPORTED;
+    if (!rope->inv_freq && !(rope->base > 0.0 && std::isfinite(rope->base))) return AP_ERR_INVALID_ARG;
+    if (!std::isfinite(rope->amplitude) || (rope->interleaved != 0 && rope->interleaved != 1)) return AP_ERR_INVALID_ARG;
+    RopeParams params{};
+    params.units = rope->rotary_dim / 16;
+    params.interleaved = rope->interleaved;
+    params.amplitude = rope->amplitude == 0.f ? 1.f : rope->amplitude;
+    for (int i = 0; i < rope->rotary_dim / 2; ++i) {
+        const double f = rope->inv_freq ? rope->inv_freq[i] : std::pow(rope->base, -2.0 * i / rope->rotary_dim);
+        if (!std::isfinite(f)) return AP_ERR_INVALID_ARG;
+        params.turn[i] = f / 6.283185307179586476925286766559;
+    }
+    auto stride_of = [](int64_t given, int heads, int dim) { return given ? given : (int64_t)heads * dim; };
+    const int64_t qs = stride_of(rope->q_row_stride, Hq, d), ks = stride_of(rope->k_row_stride, Hkv, d),
+                  vs = stride_of(rope->v_row_stride, Hkv, d);
+    if (qs < (int64_t)Hq * d || ks < (int64_t)Hkv * d || vs < (int64_t)Hkv * d || (qs | ks | vs) % 8) return AP_ERR_INVALID_ARG;
+    if ((q == nullptr) != (q_rot == nullptr)) return AP_ERR_INVALID_ARG;
+    if (pool->desc.device < 0) return AP_ERR_CUDA;
+    const int64_t n = plan->info.n_new;
+    if (n == 0) return AP_OK;
+    if (!k_new || !v_new || (((uintptr_t)q | (uintptr_t)q_rot | (uintptr_t)k_new | (uintptr_t)v_new) & 15u))
+        return AP_ERR_INVALID_ARG;
+    if (q) {
+        // q_rot is q itself (same rows at the same places) or overlaps none of the inputs
+        const uintptr_t o0 = (uintptr_t)q_rot, o1 = o0 + (uintptr_t)(n * Hq * d * 2);
+        auto overlaps = [&](const void *p, int64_t stride, int heads) {
+            const uintptr_t a = (uintptr_t)p, e = a + (uintptr_t)(((n - 1) * stride + (int64_t)heads * d) * 2);
+            return a < o1 && o0 < e;
+        };
+        const bool in_place = q == q_rot && (qs == (int64_t)Hq * d || n == 1);
+        if ((!in_place && overlaps(q, qs, Hq)) || overlaps(k_new, ks, Hkv) || overlaps(v_new, vs, Hkv)) return AP_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(pool->desc.device);
+    if (!guard.ok) return AP_ERR_CUDA;
+    TimedScope timed(pool, AP_KERNEL_APPEND, (cudaStream_t)stream);
+    if (launch_kv_append_rope(pool, plan, params, q, k_new, v_new, q_rot, qs, ks, vs, (cudaStream_t)stream) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return AP_ERR_CUDA;
+    }
+    return AP_OK;
+}
+
+int ap_kv_read_new(ap_kv_pool *pool, const ap_plan *plan, void *k, void *v, void *stream) {
+    if (!pool || !plan || plan->pool != pool) return AP_ERR_INVALID_ARG;
+    if (pool->desc.device < 0) return AP_ERR_CUDA;
+    if (plan->info.n_new == 0) return AP_OK;
+    if (!k || !v || (((uintptr_t)k | (uintptr_t)v) & 15u)) return AP_ERR_INVALID_ARG;
+    DeviceGuard guard(pool->desc.device);
+    if (!guard.ok) return AP_ERR_CUDA;
+    if (launch_kv_read_new(pool, plan, k, v, (cudaStream_t)stream) != cudaSuccess) {
         (void)cudaGetLastError();
         return AP_ERR_CUDA;
     }
@@ -893,7 +1031,8 @@ int ap_kv_copy_pages(ap_kv_pool *dst_pool, const ap_kv_pool *src_pool, int32_t n
                      const int32_t *src_ids, void *stream) {
     if (!dst_pool || !src_pool || n < 0 || (n > 0 && (!dst_ids || !src_ids))) return AP_ERR_INVALID_ARG;
     const ap_pool_desc &dd = dst_pool->desc, &sd = src_pool->desc;
-    if (dd.num_kv_heads != sd.num_kv_heads || dd.head_dim != sd.head_dim || dd.page_size != sd.page_size)
+    if (dd.num_kv_heads != sd.num_kv_heads || dd.head_dim != sd.head_dim || dd.page_size != sd.page_size ||
+        dst_pool->four_bit != src_pool->four_bit)
         return AP_ERR_INVALID_ARG;
     if ((dd.device < 0) != (sd.device < 0) || (dd.device >= 0 && dd.device != sd.device)) return AP_ERR_UNSUPPORTED;
     // Validation on the host, before anything is queued.  The copies run in parallel, so a
@@ -949,9 +1088,7 @@ int ap_attention_iteration(ap_kv_pool *pool, const ap_plan *plan, const void *q,
     DeviceGuard guard(pool->desc.device);
     if (!guard.ok) return AP_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)stream;
-    float *o_part = plan->ws.bytes ? (float *)((char *)workspace + plan->ws.o_part_off) : nullptr;
-    float *lse_part = plan->ws.bytes ? (float *)((char *)workspace + plan->ws.lse_part_off) : nullptr;
-    const cudaError_t e = ap::launch_attention_kernels(pool, plan, q, out, lse, o_part, lse_part, st);
+    const cudaError_t e = ap::launch_attention_kernels(pool, plan, q, out, lse, (char *)workspace, st);
     if (e != cudaSuccess) {
         (void)cudaGetLastError();
         return e == cudaErrorNotSupported ? AP_ERR_UNSUPPORTED : AP_ERR_CUDA;
@@ -1060,10 +1197,18 @@ int ap_serving_iteration_host(ap_kv_pool *pool, const ap_batch_desc *batch, cons
     const size_t q_bytes = align_up(n * Hq * d * 2, 256), kv_bytes = align_up(n * Hkv * d * 2, 256);
     const size_t lse_bytes = align_up(n * Hq * 4, 256);
     // every decode CTA leaves at most two partials, which bounds the workspace before planning
-    const size_t max_slots = 2 * (size_t)std::max(1, pool->sm_count * decode_ctas_per_sm((int)d));
+    const size_t max_slots =
+        2 * (size_t)std::max(1, pool->sm_count * (pool->four_bit ? kKv4CtasPerSm : decode_ctas_per_sm((int)d)));
     const size_t part_heads = (size_t)pool->head_block * (Hq / Hkv);      // query heads of one decode item
+    size_t wide_bytes = 0;                                  // a 4-bit pool's pages that prefill chunks read, in bf16
+    if (pool->four_bit && batch->ctx_lens) {
+        size_t pages = 0;
+        for (int s = 0; s < batch->batch; ++s)
+            if (batch->q_lens[s] > 1) pages += ((size_t)std::max(0, batch->ctx_lens[s]) + kPageSize - 1) / kPageSize;
+        wide_bytes = 2 * align_up(pages * Hkv * (size_t)pool_tile_bytes((int)d, false), 256);
+    }
     const size_t ws_bytes = align_up(max_slots * part_heads * d * sizeof(float), 256) +
-                            align_up(max_slots * part_heads * sizeof(float), 256);
+                            align_up(max_slots * part_heads * sizeof(float), 256) + wide_bytes;
     const size_t total = 2 * q_bytes + 2 * kv_bytes + lse_bytes + ws_bytes;
     if (total > pool->stage_bytes) {
         if (pool->stage_dev) {

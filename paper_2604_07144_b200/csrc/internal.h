@@ -60,10 +60,21 @@ static_assert(sizeof(PrefillTile) == 32, "PrefillTile layout");
 
 // Partial buffers inside the caller's workspace: o_part [slots][HB * G][d] fp32
 // followed by lse_part [slots][HB * G] fp32.
+// For prefill on a 4-bit pool the pages its units read follow, widened to bf16: one plane of K, one of V.
 struct WorkspaceLayout {
     size_t o_part_off = 0;
     size_t lse_part_off = 0;
+    size_t wide_k_off = 0;
+    size_t wide_v_off = 0;
     size_t bytes = 0;
+};
+
+// Rotation of ap_kv_append_rope, passed to the kernel by value.
+struct RopeParams {
+    double turn[64];     // frequency of pair i in turns per position: inv_freq[i] / (2 pi)
+    int32_t units;       // rotary_dim / 16
+    int32_t interleaved;
+    float amplitude;     // factor on cosine and sine
 };
 
 // ---- host objects ----------------------------------------------------------
@@ -89,6 +100,8 @@ struct TimedLaunch {
 
 struct ap_kv_pool {
     ap_pool_desc desc{};
+    bool four_bit = false;            // planes in the 4-bit format of kv4.cuh (no tensor maps)
+    int tile_bytes = 0;               // bytes of one (page, kv head) tile of a plane
     bool owns_planes = false;
     int sm_count = 0;
     int *h_status = nullptr;          // the status word: pinned host memory mapped into the device's address space
@@ -133,6 +146,8 @@ struct ap_plan {
     // token of a decode row (of a prefill unit) sees are left out of its block-table entries, and bt_offset,
     // kv_len, pos0 and ctx_len refer to what is left.
     int window = 0, sinks = 0;
+    int n_wide_pages = 0;        // 4-bit pool: pages that prefill units read, widened to bf16 in the workspace; the
+                                 // units' block-table entries number them in this order
     ap::PlanWork work{};
     bool side_by_side = false;   // decode confined to part of the GPU, prefill on the rest at the same time
     bool single_launch = false;  // ... and both in one launch (else: two kernels on two streams)
@@ -145,6 +160,7 @@ struct ap_plan {
     const int32_t *d_cta_begin = nullptr;
     const ap::MergeEntry *d_merge = nullptr;
     const ap::PrefillTile *d_tiles = nullptr;
+    const int32_t *d_wide_pages = nullptr;
 };
 
 namespace ap {
@@ -154,16 +170,28 @@ cudaError_t launch_kv_append(const ap_kv_pool *pool, const ap_plan *plan, const 
                              const void *v_new, cudaStream_t stream);
 cudaError_t launch_decode_splitk(const ap_kv_pool *pool, const ap_plan *plan, const void *q, void *out,
                                  float *lse, float *o_part, float *lse_part, cudaStream_t stream);
+// (k_map, v_map: bf16 planes of num_pages pages)
 cudaError_t launch_prefill(const ap_kv_pool *pool, const ap_plan *plan, const void *q, void *out,
-                           float *lse, cudaStream_t stream);
+                           float *lse, const CUtensorMap &k_map, const CUtensorMap &v_map, int num_pages, cudaStream_t stream);
 // Both parts of a mixed plan in one launch: the plan's decode CTAs first, then one block per prefill unit.
 cudaError_t launch_mixed_iteration(const ap_kv_pool *pool, const ap_plan *plan, const void *q, void *out, float *lse,
                                    float *o_part, float *lse_part, cudaStream_t stream);
 // Decode and prefill kernels of a plan: one after the other on `stream`, or, for a side-by-side plan,
 // both in one launch (or, if the pool asks for it, decode on `stream` and prefill on the pool's second
 // stream, joined back into `stream`).
+// `ws`: workspace of at least plan->ws.bytes (not used when that is 0).
 cudaError_t launch_attention_kernels(ap_kv_pool *pool, const ap_plan *plan, const void *q, void *out, float *lse,
-                                     float *o_part, float *lse_part, cudaStream_t stream);
+                                     char *ws, cudaStream_t stream);
+cudaError_t launch_kv_append_rope(const ap_kv_pool *pool, const ap_plan *plan, const RopeParams &rope, const void *q,
+                                  const void *k_new, const void *v_new, void *q_rot, int64_t q_stride, int64_t k_stride,
+                                  int64_t v_stride, cudaStream_t stream);
+// 4-bit pools
+cudaError_t launch_kv4_append(const ap_kv_pool *pool, const ap_plan *plan, const void *k_new, const void *v_new,
+                              cudaStream_t stream);
+cudaError_t launch_kv_read_new(const ap_kv_pool *pool, const ap_plan *plan, void *k, void *v, cudaStream_t stream);
+cudaError_t launch_kv4_widen(const ap_kv_pool *pool, const ap_plan *plan, void *k, void *v, cudaStream_t stream);
+cudaError_t launch_kv4_decode(const ap_kv_pool *pool, const ap_plan *plan, const void *q, void *out, float *lse, float *o_part,
+                              float *lse_part, cudaStream_t stream);
 // One warp waits on an mbarrier that nothing arrives on, with the given limit (see ap_selftest_wait_timeout).
 cudaError_t launch_selftest_wait(const ap_kv_pool *pool, uint64_t limit_ns, int leave_counter, cudaStream_t stream);
 // d_pairs: device [n_pairs][2] = (destination page, source page)
@@ -194,6 +222,8 @@ int prepare_static_workspace(int device);
 
 // Decode kernel launch geometry (used by the planner to size the item lists).
 int decode_ctas_per_sm(int head_dim);
+constexpr int kKv4CtasPerSm = 2;           // of the 4-bit decode kernel
+constexpr int kKv4TilesPerRound = 8;       // its eight warps take one tile each
 constexpr int kDecodeTilesPerStage = 4;    // (page, kv head) tiles of one plane in a ring stage: one per warp of a consumer group
 // kv heads per decode item: the largest of 4, 2, 1 that divides the number of kv heads.  A stage then holds
 // kDecodeTilesPerStage / HB pages of HB heads each.

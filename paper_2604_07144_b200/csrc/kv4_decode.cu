@@ -1,0 +1,430 @@
+// Decode attention over a 4-bit paged cache: split-K flash-decoding like the bf16 kernel's, on the same
+// kind of item lists, but built around warps that stream for themselves.
+//
+// At 4.5 bits a value a (page, kv head) tile is 1152 bytes (d = 128): too small for one TMA request each (an
+// SM's TMA unit handles ~14 M requests/s, 16 GB/s at that size; HBM gives an SM 43), and what an SM has to do
+// per byte is 3.6 times the bf16 kernel's.  So every warp copies its own tiles with 16-byte cp.async into a
+// private ring of kDepth tiles (K and V of one page) and no warp waits for another one inside an item: there
+// is no barrier in the stream.  Warp w of an item works on kv head w mod HB of the item's block and on pages
+// w / HB, w / HB + 8 / HB, ...; the HB tiles of a page lie together in HBM.
+//
+// Per tile, with M = 16 tokens and N = 8 query heads (mma.sync m16n8k16):
+//   S^T_g = (16 + c_K) Q_g^T   per group g of 32 elements; the codes go into the MMA as the bf16 numbers
+//                              16 + c (one shift and one LOP3 per two codes), the accumulator starts at
+//                              -24 sum_g q, so what comes out is sum (c - 8) q, and the step of (token,
+//                              group) multiplies it afterwards: S = sum_g s_g S_g;
+//   softmax                    running maximum and sum in fp32, shuffles across the token lanes;
+//   O^T += V^T P^T             V is widened to bf16 in registers: the same two operations per pair and one
+//                              HFMA2, (16 + c) s - 24 s = (c - 8) s, exact.
+// The order of d inside a product is free, so lanes take the words of a row as they are stored: K fragments
+// read 16 bytes of a row per lane, V fragments 8 bytes of four rows per lane, pairs of rows interleaved with
+// PRMT.
+//
+// At the end of an item the warps drop (m, l, O) into shared memory, the block folds them per head and
+// writes the bf16 output or, for a stream cut across blocks, an fp32 partial; the block that counts the last
+// partial in merges the stream.  Two blocks share an SM, so one streams while the other folds.
+#include "decode_splitk.cuh"
+#include "kv4.cuh"
+
+namespace ap {
+
+namespace {
+
+using namespace ptx;
+using namespace kv4;
+
+constexpr int kWarps = 8;
+constexpr int kThreads = kWarps * 32;
+constexpr int kDepth = 4;                // tiles of a warp's ring (a page's K and V each)
+constexpr int kListItems = 32;           // item descriptors of a block kept in shared memory
+
+template <int D>
+struct Kv4Cfg {
+    static constexpr int kSlotBytes = 2 * Tile<D>::kBytes;
+    static constexpr int kRingBytes = kWarps * kDepth * kSlotBytes;
+    static constexpr int kORow = D + 4;
+    static constexpr int kFoldFloats = 8 * kORow + 16;            // O[8][D + 4], m[8], l[8] of a warp
+    static constexpr int kOffFold = kRingBytes;
+    static constexpr int kOffItems = kOffFold + kWarps * kFoldFloats * 4;
+    static constexpr int kSmemBytes = kOffItems + kListItems * 32;
+    static_assert(2 * (kSmemBytes + 1024) <= 228 * 1024, "two blocks per SM");
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t a) {
+    uint16_t v;
+    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+    uint2 v;
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+    return v;
+}
+
+// Where 16-byte chunk `c` of a tile's codes (row * chunks per row + chunk) lies in a ring slot: chunks are
+// permuted within their 128-byte line so that the rows 2t that a V fragment reads at once, which lie 256 (128)
+// bytes apart, fall into different banks.
+template <int D>
+__device__ __forceinline__ int ring_chunk(int c) {
+    const int line = c >> 3;
+    return D == 128 ? c ^ (2 * (line & 3)) : c ^ (2 * (line & 1));
+}
+
+template <int D, bool kWin>
+__global__ void __launch_bounds__(kThreads, 2)
+kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict__ v_pool, const __nv_bfloat16 *__restrict__ q,
+                  const DecodeItem *__restrict__ items, const int32_t *__restrict__ cta_begin, const int32_t *__restrict__ bt_flat,
+                  const MergeEntry *__restrict__ merges, float *o_part, float *lse_part, __nv_bfloat16 *__restrict__ out,
+                  float *__restrict__ lse_out, int Hq, int Hkv, int G, int HB, int num_pages, float scale_log2, int *status,
+                  int *merge_counters, int window, int sinks) {
+    using Cfg = Kv4Cfg<D>;
+    using T = Tile<D>;
+    constexpr int NG = T::kGroups;          // groups of a row: 4 (2)
+    constexpr int NW = D / 64;              // V words of a token per lane: 2 (1)
+    constexpr int kCodeChunks = T::kCodeBytes / 16, kStepChunks = (T::kBytes - T::kCodeBytes) / 16;
+    constexpr int kRowChunks = T::kRowBytes / 16;
+    extern __shared__ __align__(128) uint8_t smem[];
+    float *fold = reinterpret_cast<float *>(smem + Cfg::kOffFold);
+    DecodeItem *s_items = reinterpret_cast<DecodeItem *>(smem + Cfg::kOffItems);
+    __shared__ int s_last;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int g = lane >> 2, t = lane & 3;
+    const int cta = blockIdx.x;
+    const int item_begin = cta_begin[cta], n_items = cta_begin[cta + 1] - item_begin;
+    const int my_head = warp % HB, my_page0 = warp / HB, page_step = kWarps / HB;
+    {
+        const int n_ints = min(n_items, kListItems) * (int)(sizeof(DecodeItem) / 4);
+        const int32_t *src = reinterpret_cast<const int32_t *>(items + item_begin);
+        for (int i = threadIdx.x; i < n_ints; i += kThreads) reinterpret_cast<int32_t *>(s_items)[i] = __ldg(src + i);
+    }
+    __syncthreads();
+    auto get_item = [&](int n) { return n < kListItems ? s_items[n] : items[item_begin + n]; };
+
+    // ---- the warp's stream of tiles: a cursor that runs ahead of the consumer, across items; block-table
+    // entries are loaded two tiles before they are needed
+    int cur_item = -1, cur_page = 0, cur_end = 0, cur_bt = 0, cur_head = 0;
+    struct Fetch { int32_t page; int head; };                 // head < 0: past the last tile
+    auto next_fetch = [&]() {
+        Fetch f{0, -1};
+        while (cur_page >= cur_end) {
+            if (++cur_item >= n_items) { cur_item = n_items; return f; }
+            const DecodeItem it = get_item(cur_item);
+            cur_page = it.page_begin + my_page0;
+            cur_end = it.page_begin + it.page_count;
+            cur_bt = it.bt_offset;
+            cur_head = it.kv_head + my_head;
+        }
+        f.page = __ldg(bt_flat + cur_bt + cur_page);
+        f.head = cur_head;
+        cur_page += page_step;
+        return f;
+    };
+    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * kDepth * Cfg::kSlotBytes);
+    Fetch f0 = next_fetch(), f1 = next_fetch();
+    griddep_launch_dependents();
+    griddep_wait();              // all of the above reads the plan only
+    auto issue = [&](int slot) {
+        if (f0.head >= 0) {
+            int32_t page = f0.page;
+            if (page < 0 || page >= num_pages) {
+                record_status(status, AP_ERR_BAD_BLOCK_TABLE);
+                page = 0;
+            }
+            const int64_t tile = ((int64_t)page * Hkv + f0.head) * T::kBytes;
+            const uint8_t *k = k_pool + tile, *v = v_pool + tile;
+            const uint32_t dk = ring + (uint32_t)(slot * Cfg::kSlotBytes), dv = dk + T::kBytes;
+#pragma unroll
+            for (int i = 0; i < kCodeChunks / 32; ++i) {
+                const int c = lane + 32 * i;
+                cp_async16(dk + 16 * ring_chunk<D>(c), k + 16 * c);
+                cp_async16(dv + 16 * ring_chunk<D>(c), v + 16 * c);
+            }
+            if (lane < 2 * kStepChunks) {
+                const int c = kCodeChunks + lane % kStepChunks;
+                cp_async16((lane < kStepChunks ? dk : dv) + 16 * c, (lane < kStepChunks ? k : v) + 16 * c);
+            }
+        }
+        cp_async_commit();       // (an empty group past the last tile keeps the count of groups in step)
+        f0 = f1;
+        f1 = next_fetch();
+    };
+#pragma unroll 1
+    for (int s = 0; s < kDepth; ++s) issue(s);
+
+    int slot = 0;
+    for (int n = 0; n < n_items; ++n) {
+        const DecodeItem item = get_item(n);
+        const int kv_head = item.kv_head + my_head;
+        // ---- Q^T as the B operand, in the order in which a lane's word of K holds the elements, and the
+        // accumulators' start -24 sum_g q
+        uint32_t qf[NG][4];
+        float init[NG][2];
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (g < G)
+                x = __ldg(reinterpret_cast<const uint4 *>(q + ((size_t)item.q_row * Hq + (size_t)kv_head * G + g) * D + 32 * gr + 8 * t));
+            qf[gr][0] = prmt(x.x, x.z, 0x5410);       // (e0, e4)
+            qf[gr][1] = prmt(x.x, x.z, 0x7632);       // (e1, e5)
+            qf[gr][2] = prmt(x.y, x.w, 0x5410);
+            qf[gr][3] = prmt(x.y, x.w, 0x7632);
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += __uint_as_float(qf[gr][i] << 16) + __uint_as_float(qf[gr][i] & 0xFFFF0000u);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            init[gr][0] = -24.f * __shfl_sync(0xffffffffu, sum, 8 * t);
+            init[gr][1] = -24.f * __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+        }
+        float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+        float o[4 * NW][4];
+#pragma unroll
+        for (int i = 0; i < 4 * NW; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+
+        for (int p = item.page_begin + my_page0; p < item.page_begin + item.page_count; p += page_step) {
+            cp_async_wait<kDepth - 1>();
+            __syncwarp();
+            const uint32_t tk = ring + (uint32_t)(slot * Cfg::kSlotBytes), tv = tk + T::kBytes;
+            // ---- S^T
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+            {
+                uint32_t w[2][NG];
+                uint32_t st[2][NG / 2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const int row = g + 8 * r;
+                    if constexpr (D == 128) {
+                        const uint4 x = lds128(tk + 16 * ring_chunk<D>(row * kRowChunks + t));
+                        w[r][0] = x.x; w[r][1] = x.y; w[r][2] = x.z; w[r][3] = x.w;
+                        const uint2 y = lds64(tk + T::kCodeBytes + row * 8);
+                        st[r][0] = y.x; st[r][1] = y.y;
+                    } else {
+                        const uint2 x = lds64(tk + 16 * ring_chunk<D>(row * kRowChunks + (t >> 1)) + 8 * (t & 1));
+                        w[r][0] = x.x; w[r][1] = x.y;
+                        st[r][0] = lds32(tk + T::kCodeBytes + row * 4);
+                    }
+                }
+#pragma unroll
+                for (int gr = 0; gr < NG; ++gr) {
+                    uint32_t a[4], b[4];
+                    codes_to_bf16(w[0][gr], a);
+                    codes_to_bf16(w[1][gr], b);
+                    float acc[4] = {init[gr][0], init[gr][1], init[gr][0], init[gr][1]};
+                    mma_bf16_16816(acc, a[0], b[0], a[1], b[1], qf[gr][0], qf[gr][1]);
+                    mma_bf16_16816(acc, a[2], b[2], a[3], b[3], qf[gr][2], qf[gr][3]);
+                    const uint32_t u0 = st[0][gr / 2], u1 = st[1][gr / 2];
+                    const float s0 = __uint_as_float(gr & 1 ? u0 & 0xFFFF0000u : u0 << 16);
+                    const float s1 = __uint_as_float(gr & 1 ? u1 & 0xFFFF0000u : u1 << 16);
+                    s[0] = fmaf(acc[0], s0, s[0]); s[1] = fmaf(acc[1], s0, s[1]);
+                    s[2] = fmaf(acc[2], s1, s[2]); s[3] = fmaf(acc[3], s1, s[3]);
+                }
+            }
+            // ---- V's words and steps: tokens 2t, 2t + 1, 2t + 8, 2t + 9
+            uint32_t vw[4][NW], vs[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = 2 * t + (r & 1) + 8 * (r >> 1);
+                if constexpr (D == 128) {
+                    const uint2 x = lds64(tv + 16 * ring_chunk<D>(row * kRowChunks + (g >> 1)) + 8 * (g & 1));
+                    vw[r][0] = x.x; vw[r][1] = x.y;
+                    vs[r] = lds32(tv + T::kCodeBytes + row * 8 + 4 * (g & 1));
+                } else {
+                    vw[r][0] = lds32(tv + 16 * ring_chunk<D>(row * kRowChunks + (g >> 2)) + 4 * (g & 3));
+                    vs[r] = lds16(tv + T::kCodeBytes + row * 4 + 2 * (g & 1));
+                }
+            }
+            // ---- hidden tokens: past the context, or before the window; whatever they hold, they weigh nothing
+            const int left = item.kv_len - p * kPageSize;               // tokens of the context in this page
+            int h0 = 0, h1 = 0;
+            if constexpr (kWin) {
+                h0 = max(sinks - p * kPageSize, 0);
+                h1 = min(left - window, kPageSize);
+            }
+            if (left < kPageSize || (kWin && h0 < h1)) {
+                auto hidden = [&](int tok) { return tok >= left || (kWin && tok >= h0 && tok < h1); };
+                if (hidden(g)) s[0] = s[1] = -INFINITY;
+                if (hidden(g + 8)) s[2] = s[3] = -INFINITY;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (hidden(2 * t + (r & 1) + 8 * (r >> 1))) vs[r] = 0;
+            }
+            // ---- online softmax over the page's tokens (every page has a visible one)
+            float mx0 = fmaxf(s[0], s[2]), mx1 = fmaxf(s[1], s[3]);
+#pragma unroll
+            for (int sh = 4; sh <= 16; sh <<= 1) {
+                mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, sh));
+                mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, sh));
+            }
+            const float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);
+            const float al0 = exp2_approx((m0 - mn0) * scale_log2), al1 = exp2_approx((m1 - mn1) * scale_log2);
+            const float ms0 = mn0 * scale_log2, ms1 = mn1 * scale_log2;
+            const float p0 = exp2_approx(s[0] * scale_log2 - ms0), p1 = exp2_approx(s[1] * scale_log2 - ms1);
+            const float p2 = exp2_approx(s[2] * scale_log2 - ms0), p3 = exp2_approx(s[3] * scale_log2 - ms1);
+            l0 = l0 * al0 + p0 + p2;
+            l1 = l1 * al1 + p1 + p3;
+            m0 = mn0;
+            m1 = mn1;
+#pragma unroll
+            for (int i = 0; i < 4 * NW; ++i) {
+                o[i][0] *= al0; o[i][1] *= al1; o[i][2] *= al0; o[i][3] *= al1;
+            }
+            const uint32_t b0 = decode::movmatrix_trans(pack_bf16x2(p0, p1)), b1 = decode::movmatrix_trans(pack_bf16x2(p2, p3));
+            // ---- O^T += V^T P^T
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const uint32_t sel = w == 0 ? 0x5410u : 0x7632u;
+                const uint32_t sa = prmt(vs[0], vs[1], sel), sb = prmt(vs[2], vs[3], sel);
+                const uint32_t na = minus24(sa), nb = minus24(sb);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t hs = half == 0 ? 0x5410u : 0x7632u;
+                    uint32_t a[4], b[4];
+                    codes_to_bf16(prmt(vw[0][w], vw[1][w], hs), a);
+                    codes_to_bf16(prmt(vw[2][w], vw[3][w], hs), b);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        a[i] = scale_pair(a[i], sa, na);
+                        b[i] = scale_pair(b[i], sb, nb);
+                    }
+                    mma_bf16_16816(o[4 * w + 2 * half], a[0], a[1], b[0], b[1], b0, b1);
+                    mma_bf16_16816(o[4 * w + 2 * half + 1], a[2], a[3], b[2], b[3], b0, b1);
+                }
+            }
+            __syncwarp();
+            issue(slot);
+            slot = slot + 1 == kDepth ? 0 : slot + 1;
+        }
+
+        // ---- the item's end: every warp's (m, l, O) to shared memory, folded by the block per head
+#pragma unroll
+        for (int sh = 4; sh <= 16; sh <<= 1) {
+            l0 += __shfl_xor_sync(0xffffffffu, l0, sh);
+            l1 += __shfl_xor_sync(0xffffffffu, l1, sh);
+        }
+        float *mine = fold + warp * Cfg::kFoldFloats;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const int d0 = D == 128 ? 32 * (2 * (g & 1) + w) + 8 * (g >> 1) : 32 * (g & 1) + 8 * (g >> 1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                *reinterpret_cast<float2 *>(mine + (2 * t) * Cfg::kORow + d0 + 2 * i) = make_float2(o[4 * w + i][0], o[4 * w + i][2]);
+                *reinterpret_cast<float2 *>(mine + (2 * t + 1) * Cfg::kORow + d0 + 2 * i) = make_float2(o[4 * w + i][1], o[4 * w + i][3]);
+            }
+        }
+        if (g == 0) {
+            mine[8 * Cfg::kORow + 2 * t] = m0;
+            mine[8 * Cfg::kORow + 2 * t + 1] = m1;
+            mine[8 * Cfg::kORow + 8 + 2 * t] = l0;
+            mine[8 * Cfg::kORow + 8 + 2 * t + 1] = l1;
+        }
+        __syncthreads();
+        const int PH = HB * G;
+        const bool col_ok = lane * 4 < D;
+        for (int ph = warp; ph < PH; ph += kWarps) {
+            const int hh = ph / G, h = ph % G;
+            float mstar = -INFINITY;
+            for (int w = hh; w < kWarps; w += HB) mstar = fmaxf(mstar, fold[w * Cfg::kFoldFloats + 8 * Cfg::kORow + h]);
+            float L = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int w = hh; w < kWarps; w += HB) {
+                const float *wb = fold + w * Cfg::kFoldFloats;
+                const float wt = exp2_approx((wb[8 * Cfg::kORow + h] - mstar) * scale_log2);
+                L += wt * wb[8 * Cfg::kORow + 8 + h];
+                if (col_ok) {
+                    const float4 x = *reinterpret_cast<const float4 *>(wb + h * Cfg::kORow + lane * 4);
+                    acc.x += wt * x.x; acc.y += wt * x.y; acc.z += wt * x.z; acc.w += wt * x.w;
+                }
+            }
+            const float inv = 1.f / L;
+            const float lse = (mstar * scale_log2 + log2f(L)) * 0.6931471805599453f;
+            acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
+            if (item.part_slot < 0) {
+                const size_t row = (size_t)item.q_row * Hq + (size_t)(item.kv_head + hh) * G + h;
+                if (col_ok)
+                    *reinterpret_cast<uint2 *>(out + row * D + lane * 4) =
+                        make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+                if (lane == 0 && lse_out) lse_out[row] = lse;
+            } else {
+                const size_t row = (size_t)item.part_slot * PH + ph;
+                if (col_ok) *reinterpret_cast<float4 *>(o_part + row * D + lane * 4) = acc;
+                if (lane == 0) lse_part[row] = lse;
+            }
+        }
+        if (item.part_slot >= 0) {
+            // count the partial in; whoever completes the stream merges it, a head per warp
+            __threadfence();
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                int old;
+                asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;"
+                             : "=r"(old) : "l"(merge_counters + item.merge_index) : "memory");
+                s_last = old == __ldg(&merges[item.merge_index].part_count) - 1;
+                if (s_last) merge_counters[item.merge_index] = 0;      // ready for the next launch
+            }
+            __syncthreads();
+            if (s_last) {
+                __threadfence();
+                const MergeEntry me = merges[item.merge_index];
+                for (int ph = warp; ph < PH; ph += kWarps)
+                    decode::merge_stream<D, 1>(me, o_part, lse_part, out, lse_out, Hq, lane, PH, ph, me.kv_head * G);
+            }
+        }
+        __syncthreads();         // the buffer (and s_last) may be used again
+    }
+    cp_async_wait<0>();
+}
+
+template <int D, bool kWin>
+cudaError_t launch_t(const ap_kv_pool *pool, const ap_plan *plan, const void *q, void *out, float *lse, float *o_part,
+                     float *lse_part, cudaStream_t stream) {
+    using Cfg = Kv4Cfg<D>;
+    static bool configured[64] = {};
+    const int dev = pool->desc.device & 63;
+    if (!configured[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(kv4_decode_kernel<D, kWin>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   Cfg::kSmemBytes);
+        if (e != cudaSuccess) return e;
+        configured[dev] = true;
+    }
+    const float scale_log2 = plan->scale * 1.4426950408889634f;
+    return launch_overlapped(kv4_decode_kernel<D, kWin>, (unsigned)plan->info.decode_ctas, (unsigned)kThreads,
+                             (size_t)Cfg::kSmemBytes, stream, (const uint8_t *)pool->desc.k_base,
+                             (const uint8_t *)pool->desc.v_base, (const __nv_bfloat16 *)q, plan->d_items, plan->d_cta_begin,
+                             plan->d_bt_flat, plan->d_merge, o_part, lse_part, (__nv_bfloat16 *)out, lse, plan->num_q_heads,
+                             pool->desc.num_kv_heads, plan->group, plan->head_block, pool->desc.num_pages, scale_log2,
+                             pool->status_dev, pool->d_counters, plan->window, plan->sinks);
+}
+
+}  // namespace
+
+cudaError_t launch_kv4_decode(const ap_kv_pool *pool, const ap_plan *plan, const void *q, void *out, float *lse, float *o_part,
+                              float *lse_part, cudaStream_t stream) {
+    cudaError_t e;
+    if (plan->window > 0)
+        e = pool->desc.head_dim == 128 ? launch_t<128, true>(pool, plan, q, out, lse, o_part, lse_part, stream)
+                                       : launch_t<64, true>(pool, plan, q, out, lse, o_part, lse_part, stream);
+    else
+        e = pool->desc.head_dim == 128 ? launch_t<128, false>(pool, plan, q, out, lse, o_part, lse_part, stream)
+                                       : launch_t<64, false>(pool, plan, q, out, lse, o_part, lse_part, stream);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace ap

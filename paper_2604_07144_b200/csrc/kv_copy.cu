@@ -52,7 +52,7 @@ kv_copy_pages_kernel(uint4 *__restrict__ k_dst, uint4 *__restrict__ v_dst, const
 
 cudaError_t launch_kv_copy_pages(const ap_kv_pool *dst_pool, const ap_kv_pool *src_pool, const int32_t *d_pairs,
                                  int n_pairs, cudaStream_t stream) {
-    const int page_vecs = dst_pool->desc.num_kv_heads * kPageSize * dst_pool->desc.head_dim * 2 / 16;
+    const int page_vecs = dst_pool->desc.num_kv_heads * (dst_pool->tile_bytes / 16);
     const unsigned chunks = (unsigned)((page_vecs + kVecPerBlock - 1) / kVecPerBlock);
     cudaError_t e = cudaSuccess;
     // gridDim.y is limited to 65535: larger requests go out in slices

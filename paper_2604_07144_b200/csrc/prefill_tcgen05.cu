@@ -21,7 +21,7 @@ prefill_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
 
 template <int D, bool kWin>
 cudaError_t launch_prefill_t(const ap_kv_pool *pool, const ap_plan *plan, const void *q, void *out, float *lse,
-                             cudaStream_t stream) {
+                             const CUtensorMap &k_map, const CUtensorMap &v_map, int num_pages, cudaStream_t stream) {
     using Cfg = PrefillCfg<D>;
     static bool configured[64] = {};
     const int dev = pool->desc.device & 63;
@@ -36,8 +36,8 @@ cudaError_t launch_prefill_t(const ap_kv_pool *pool, const ap_plan *plan, const 
     const float scale_log2 = plan->scale * 1.4426950408889634f;
     cudaError_t e = launch_overlapped(
         prefill_tcgen05_kernel<D, kWin>, (unsigned)plan->info.prefill_tiles, (unsigned)kPrefillThreads,
-        (size_t)Cfg::kSmemBytes, stream, q_map, pool->k_map, pool->v_map, plan->d_tiles, plan->d_bt_flat,
-        (__nv_bfloat16 *)out, lse, plan->num_q_heads, pool->desc.num_kv_heads, pool->desc.num_pages, scale_log2,
+        (size_t)Cfg::kSmemBytes, stream, q_map, k_map, v_map, plan->d_tiles, plan->d_bt_flat,
+        (__nv_bfloat16 *)out, lse, plan->num_q_heads, pool->desc.num_kv_heads, num_pages, scale_log2,
         pool->status_dev, pool->wait_limit_ns, plan->window, plan->sinks);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -45,13 +45,13 @@ cudaError_t launch_prefill_t(const ap_kv_pool *pool, const ap_plan *plan, const 
 }  // namespace
 
 cudaError_t launch_prefill(const ap_kv_pool *pool, const ap_plan *plan, const void *q, void *out, float *lse,
-                           cudaStream_t stream) {
+                           const CUtensorMap &k_map, const CUtensorMap &v_map, int num_pages, cudaStream_t stream) {
     if (plan->window > 0) {
-        if (pool->desc.head_dim == 128) return launch_prefill_t<128, true>(pool, plan, q, out, lse, stream);
-        return launch_prefill_t<64, true>(pool, plan, q, out, lse, stream);
+        if (pool->desc.head_dim == 128) return launch_prefill_t<128, true>(pool, plan, q, out, lse, k_map, v_map, num_pages, stream);
+        return launch_prefill_t<64, true>(pool, plan, q, out, lse, k_map, v_map, num_pages, stream);
     }
-    if (pool->desc.head_dim == 128) return launch_prefill_t<128, false>(pool, plan, q, out, lse, stream);
-    return launch_prefill_t<64, false>(pool, plan, q, out, lse, stream);
+    if (pool->desc.head_dim == 128) return launch_prefill_t<128, false>(pool, plan, q, out, lse, k_map, v_map, num_pages, stream);
+    return launch_prefill_t<64, false>(pool, plan, q, out, lse, k_map, v_map, num_pages, stream);
 }
 
 }  // namespace ap

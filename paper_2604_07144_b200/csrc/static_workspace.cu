@@ -70,9 +70,7 @@ int ap_attention_iteration_static(ap_kv_pool *pool, const ap_plan *plan, const v
         // Every partial slot is written in full by its decode item before the
         // last-arriving item of the stream merges them, so nothing left over
         // from an earlier call is ever read and nothing needs clearing.
-        float *o_part = plan->ws.bytes ? (float *)((char *)ws + plan->ws.o_part_off) : nullptr;
-        float *lse_part = plan->ws.bytes ? (float *)((char *)ws + plan->ws.lse_part_off) : nullptr;
-        const cudaError_t e = ap::launch_attention_kernels(pool, plan, q, out, lse, o_part, lse_part, st);
+        const cudaError_t e = ap::launch_attention_kernels(pool, plan, q, out, lse, (char *)ws, st);
         if (e != cudaSuccess) {
             (void)cudaGetLastError();
             rc = e == cudaErrorNotSupported ? AP_ERR_UNSUPPORTED : AP_ERR_CUDA;
