@@ -4,18 +4,25 @@
 // At 4.5 bits a value a (page, kv head) tile is 1152 bytes (d = 128): too small for one TMA request each (an
 // SM's TMA unit handles ~14 M requests/s, 16 GB/s at that size; HBM gives an SM 43), and what an SM has to do
 // per byte is 3.6 times the bf16 kernel's.  So every warp copies its own tiles with 16-byte cp.async into a
-// private ring of kDepth tiles (K and V of one page) and no warp waits for another one inside an item: there
+// private ring of kDepth pairs of pages and no warp waits for another one inside an item: there
 // is no barrier in the stream.  Warp w of an item works on kv head w mod HB of the item's block and on pages
 // w / HB, w / HB + 8 / HB, ...; the HB tiles of a page lie together in HBM.
 //
-// Per tile, with M = 16 tokens and N = 8 query heads (mma.sync m16n8k16):
-//   S^T_g = (16 + c_K) Q_g^T   per group g of 32 elements; the codes go into the MMA as the bf16 numbers
-//                              16 + c (one shift and one LOP3 per two codes), the accumulator starts at
-//                              -24 sum_g q, so what comes out is sum (c - 8) q, and the step of (token,
-//                              group) multiplies it afterwards: S = sum_g s_g S_g;
-//   softmax                    running maximum and sum in fp32, shuffles across the token lanes;
-//   O^T += V^T P^T             V is widened to bf16 in registers: the same two operations per pair and one
-//                              HFMA2, (16 + c) s - 24 s = (c - 8) s, exact.
+// What bounds the kernel is the ALU pipe (LOP3, PRMT, shifts: one warp instruction in two clocks) on the
+// way from nibbles to MMA operands, so that way is short.  The bits of a byte b, put into a bf16 pattern with
+// nothing above them, ARE the number b 2^-133 (bits 0 .. 6 are a subnormal's mantissa, and from bit 7, the
+// exponent's last, the scale goes on linearly).  One AND therefore turns two nibbles of a word into two bf16
+// numbers, c 2^-133 where they lie at bits 0 .. 3 of their halves and c 2^-129 at bits 4 .. 7; a shift by
+// eight brings the other four.  Tensor cores and HFMA2 take subnormal operands exactly.
+//   S^T_g = c_K (2^a Q_g)^T    per group g of 32 elements, M = 16 tokens, N = 8 query heads (mma.sync
+//                              m16n8k16).  Q is scaled by a power of two per head (its largest element to
+//                              2^120; elements facing nibbles at bits 4 .. 7 by 2^-4 less), which is exact;
+//                              the accumulator starts at -8 sum_g q, so sum (c - 8) q comes out, and the step
+//                              of (token, group) multiplies it: S = sum_g s_g S_g;
+//   softmax                    running maximum and sum in fp32, shuffles across the token lanes, once per two
+//                              pages; O is rescaled only when some lane's maximum has moved;
+//   O^T += V^T P^T             V is widened to bf16 in registers, exactly: c 2^-133 times 2^127 (c 2^-129 times
+//                              2^123) is c / 64, and fma(c / 64, 64 s, -8 s) is (c - 8) s.
 // The order of d inside a product is free, so lanes take the words of a row as they are stored: K fragments
 // read 16 bytes of a row per lane, V fragments 8 bytes of four rows per lane, pairs of rows interleaved with
 // PRMT.
@@ -35,12 +42,13 @@ using namespace kv4;
 
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
-constexpr int kDepth = 4;                // tiles of a warp's ring (a page's K and V each)
+constexpr int kDepth = 2;                // pairs of pages in a warp's ring (K and V tile of each)
 constexpr int kListItems = 32;           // item descriptors of a block kept in shared memory
 
 template <int D>
 struct Kv4Cfg {
-    static constexpr int kSlotBytes = 2 * Tile<D>::kBytes;
+    static constexpr int kPageBytes = 2 * Tile<D>::kBytes;        // K tile, V tile
+    static constexpr int kSlotBytes = 2 * kPageBytes;
     static constexpr int kRingBytes = kWarps * kDepth * kSlotBytes;
     static constexpr int kORow = D + 4;
     static constexpr int kFoldFloats = 8 * kORow + 16;            // O[8][D + 4], m[8], l[8] of a warp
@@ -76,6 +84,19 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
     uint4 v;
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
     return v;
+}
+
+constexpr uint32_t kLow = 0x000F000Fu, kHigh = 0x00F000F0u;     // two nibbles of a word, one in each half
+
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
 }
 
 // Where 16-byte chunk `c` of a tile's codes (row * chunks per row + chunk) lies in a ring slot: chunks are
@@ -118,12 +139,14 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
     __syncthreads();
     auto get_item = [&](int n) { return n < kListItems ? s_items[n] : items[item_begin + n]; };
 
-    // ---- the warp's stream of tiles: a cursor that runs ahead of the consumer, across items; block-table
-    // entries are loaded two tiles before they are needed
+    // ---- the warp's stream of page pairs: a cursor that runs ahead of the consumer, across items; block-table
+    // entries are loaded a pair before they are needed
     int cur_item = -1, cur_page = 0, cur_end = 0, cur_bt = 0, cur_head = 0;
-    struct Fetch { int32_t page; int head; };                 // head < 0: past the last tile
+    struct Fetch { int32_t page[2]; int head, n; };           // n pages (0: past the last)
     auto next_fetch = [&]() {
-        Fetch f{0, -1};
+        Fetch f;
+        f.n = 0;
+        f.page[0] = f.page[1] = f.head = 0;
         while (cur_page >= cur_end) {
             if (++cur_item >= n_items) { cur_item = n_items; return f; }
             const DecodeItem it = get_item(cur_item);
@@ -132,180 +155,254 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
             cur_bt = it.bt_offset;
             cur_head = it.kv_head + my_head;
         }
-        f.page = __ldg(bt_flat + cur_bt + cur_page);
+        f.n = cur_page + page_step < cur_end ? 2 : 1;
+        f.page[0] = __ldg(bt_flat + cur_bt + cur_page);
+        if (f.n == 2) f.page[1] = __ldg(bt_flat + cur_bt + cur_page + page_step);
         f.head = cur_head;
-        cur_page += page_step;
+        cur_page += 2 * page_step;
         return f;
     };
     const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * kDepth * Cfg::kSlotBytes);
-    Fetch f0 = next_fetch(), f1 = next_fetch();
+    // a lane's share of a tile's copy: code chunks lane (and lane + 32, four lines on), and, for the first
+    // lanes, a chunk of K's or V's steps
+    const uint32_t c_dst = 16 * ring_chunk<D>(lane);
+    const uint8_t *const k_src = k_pool + 16 * lane, *const v_src = v_pool + 16 * lane;
+    const bool step_lane = lane < 2 * kStepChunks, k_steps = lane < kStepChunks;
+    const uint32_t s_dst = (k_steps ? 0 : T::kBytes) + 16 * (kCodeChunks + lane % kStepChunks);
+    const uint8_t *const s_src = (k_steps ? k_pool : v_pool) + 16 * (kCodeChunks + lane % kStepChunks);
+    Fetch f0 = next_fetch();
     griddep_launch_dependents();
     griddep_wait();              // all of the above reads the plan only
     auto issue = [&](int slot) {
-        if (f0.head >= 0) {
-            int32_t page = f0.page;
-            if (page < 0 || page >= num_pages) {
-                record_status(status, AP_ERR_BAD_BLOCK_TABLE);
-                page = 0;
-            }
-            const int64_t tile = ((int64_t)page * Hkv + f0.head) * T::kBytes;
-            const uint8_t *k = k_pool + tile, *v = v_pool + tile;
-            const uint32_t dk = ring + (uint32_t)(slot * Cfg::kSlotBytes), dv = dk + T::kBytes;
+        const uint32_t dst = ring + (uint32_t)(slot * Cfg::kSlotBytes);
 #pragma unroll
-            for (int i = 0; i < kCodeChunks / 32; ++i) {
-                const int c = lane + 32 * i;
-                cp_async16(dk + 16 * ring_chunk<D>(c), k + 16 * c);
-                cp_async16(dv + 16 * ring_chunk<D>(c), v + 16 * c);
-            }
-            if (lane < 2 * kStepChunks) {
-                const int c = kCodeChunks + lane % kStepChunks;
-                cp_async16((lane < kStepChunks ? dk : dv) + 16 * c, (lane < kStepChunks ? k : v) + 16 * c);
+        for (int u = 0; u < 2; ++u) {
+            if (u < f0.n) {
+                int32_t page = f0.page[u];
+                if ((uint32_t)page >= (uint32_t)num_pages) {
+                    record_status(status, AP_ERR_BAD_BLOCK_TABLE);
+                    page = 0;
+                }
+                const int64_t tile = (int64_t)((uint32_t)page * (uint32_t)Hkv + (uint32_t)f0.head) * T::kBytes;
+                const uint32_t d = dst + u * Cfg::kPageBytes;
+                const uint8_t *k = k_src + tile, *v = v_src + tile;
+                cp_async16(d + c_dst, k);
+                cp_async16(d + c_dst + T::kBytes, v);
+                if constexpr (kCodeChunks > 32) {
+                    cp_async16(d + c_dst + 512, k + 512);
+                    cp_async16(d + c_dst + T::kBytes + 512, v + 512);
+                }
+                if (step_lane) cp_async16(d + s_dst, s_src + tile);
             }
         }
-        cp_async_commit();       // (an empty group past the last tile keeps the count of groups in step)
-        f0 = f1;
-        f1 = next_fetch();
+        cp_async_commit();       // (an empty group past the last pair keeps the count of groups in step)
+        f0 = next_fetch();
     };
 #pragma unroll 1
     for (int s = 0; s < kDepth; ++s) issue(s);
+
+    // a lane's places in a tile: K words of rows g and g + 8 (four or two lines on), K steps; V words of rows
+    // 2t and 2t + 1 (and 2t + 8, 2t + 9), V steps
+    const uint32_t k_off = D == 128 ? 16 * ring_chunk<D>(g * kRowChunks + t)
+                                    : 16 * ring_chunk<D>(g * kRowChunks + (t >> 1)) + 8 * (t & 1);
+    const uint32_t v_chunk = D == 128 ? g >> 1 : g >> 2, v_byte = D == 128 ? 8 * (g & 1) : 4 * (g & 3);
+    const uint32_t v_off0 = T::kBytes + 16 * ring_chunk<D>(2 * t * kRowChunks + v_chunk) + v_byte;
+    const uint32_t v_off1 = T::kBytes + 16 * ring_chunk<D>((2 * t + 1) * kRowChunks + v_chunk) + v_byte;
+    constexpr uint32_t kRow8 = 8 * T::kRowBytes;           // rows r and r + 8 are permuted alike
+    const uint32_t ks_off = T::kCodeBytes + 2 * NG * g;
+    const uint32_t vs_off = T::kBytes + T::kCodeBytes + 2 * NG * 2 * t + (D == 128 ? 4 : 2) * (g & 1);
 
     int slot = 0;
     for (int n = 0; n < n_items; ++n) {
         const DecodeItem item = get_item(n);
         const int kv_head = item.kv_head + my_head;
-        // ---- Q^T as the B operand, in the order in which a lane's word of K holds the elements, and the
-        // accumulators' start -24 sum_g q
+        // ---- Q^T as the B operand, in the order in which a lane's word of K holds the elements, scaled; the
+        // accumulators' start; and what turns a score into a power of two's exponent, per column (head)
         uint32_t qf[NG][4];
-        float init[NG][2];
+        float init[NG][2], f_col[2];
+        {
+            uint4 x[NG];
+            uint32_t amax = 0;
 #pragma unroll
-        for (int gr = 0; gr < NG; ++gr) {
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (g < G)
-                x = __ldg(reinterpret_cast<const uint4 *>(q + ((size_t)item.q_row * Hq + (size_t)kv_head * G + g) * D + 32 * gr + 8 * t));
-            qf[gr][0] = prmt(x.x, x.z, 0x5410);       // (e0, e4)
-            qf[gr][1] = prmt(x.x, x.z, 0x7632);       // (e1, e5)
-            qf[gr][2] = prmt(x.y, x.w, 0x5410);
-            qf[gr][3] = prmt(x.y, x.w, 0x7632);
-            float sum = 0.f;
+            for (int gr = 0; gr < NG; ++gr) {
+                x[gr] = make_uint4(0, 0, 0, 0);
+                if (g < G)
+                    x[gr] = __ldg(reinterpret_cast<const uint4 *>(q + ((size_t)item.q_row * Hq + (size_t)kv_head * G + g) * D + 32 * gr + 8 * t));
+                const uint32_t w[4] = {x[gr].x, x[gr].y, x[gr].z, x[gr].w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum += __uint_as_float(qf[gr][i] << 16) + __uint_as_float(qf[gr][i] & 0xFFFF0000u);
-            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-            init[gr][0] = -24.f * __shfl_sync(0xffffffffu, sum, 8 * t);
-            init[gr][1] = -24.f * __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+                for (int i = 0; i < 4; ++i) amax = max(amax, max((w[i] << 16) & 0x7FFFFFFFu, w[i] & 0x7FFF0000u));
+            }
+            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+            const int a = min(max(120 + 127 - (int)(amax >> 23), 7), 126);
+            const float up = __int_as_float((a + 127) << 23);                          // 2^a
+            const float f = scale_log2 * __int_as_float((133 - a + 127) << 23);        // scale log2(e) 2^(133 - a)
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                const uint32_t w[4] = {x[gr].x, x[gr].y, x[gr].z, x[gr].w};
+                float e[8], sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    e[2 * i] = __uint_as_float(w[i] << 16) * up;
+                    e[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u) * up;
+                    sum += e[2 * i] + e[2 * i + 1];
+                }
+                qf[gr][0] = pack_bf16x2(e[0], e[4]);
+                qf[gr][1] = pack_bf16x2(e[1] * 0.0625f, e[5] * 0.0625f);
+                qf[gr][2] = pack_bf16x2(e[2], e[6]);
+                qf[gr][3] = pack_bf16x2(e[3] * 0.0625f, e[7] * 0.0625f);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                const float start = sum * -7.3468396926392969e-40f;                     // -8 2^-133 = -2^-130
+                init[gr][0] = __shfl_sync(0xffffffffu, start, 8 * t);
+                init[gr][1] = __shfl_sync(0xffffffffu, start, 8 * t + 4);
+            }
+            f_col[0] = __shfl_sync(0xffffffffu, f, 8 * t);
+            f_col[1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
         }
+        // running maximum (of scores times f_col: exponents of 2), sum and O
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         float o[4 * NW][4];
 #pragma unroll
         for (int i = 0; i < 4 * NW; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
 
-        for (int p = item.page_begin + my_page0; p < item.page_begin + item.page_count; p += page_step) {
+        const int page_end = item.page_begin + item.page_count;
+#pragma unroll 1
+        for (int p = item.page_begin + my_page0; p < page_end; p += 2 * page_step) {
             cp_async_wait<kDepth - 1>();
             __syncwarp();
-            const uint32_t tk = ring + (uint32_t)(slot * Cfg::kSlotBytes), tv = tk + T::kBytes;
-            // ---- S^T
-            float s[4] = {0.f, 0.f, 0.f, 0.f};
-            {
-                uint32_t w[2][NG];
-                uint32_t st[2][NG / 2];
+            const uint32_t base = ring + (uint32_t)(slot * Cfg::kSlotBytes);
+            // ---- S^T of both pages
+            float s[2][4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t tile = base + u * Cfg::kPageBytes;
+                uint32_t w[2][NG], st[2][NG / 2];
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const int row = g + 8 * r;
                     if constexpr (D == 128) {
-                        const uint4 x = lds128(tk + 16 * ring_chunk<D>(row * kRowChunks + t));
+                        const uint4 x = lds128(tile + k_off + r * kRow8);
                         w[r][0] = x.x; w[r][1] = x.y; w[r][2] = x.z; w[r][3] = x.w;
-                        const uint2 y = lds64(tk + T::kCodeBytes + row * 8);
+                        const uint2 y = lds64(tile + ks_off + r * 16 * NG);
                         st[r][0] = y.x; st[r][1] = y.y;
                     } else {
-                        const uint2 x = lds64(tk + 16 * ring_chunk<D>(row * kRowChunks + (t >> 1)) + 8 * (t & 1));
+                        const uint2 x = lds64(tile + k_off + r * kRow8);
                         w[r][0] = x.x; w[r][1] = x.y;
-                        st[r][0] = lds32(tk + T::kCodeBytes + row * 4);
+                        st[r][0] = lds32(tile + ks_off + r * 16 * NG);
                     }
                 }
+                s[u][0] = s[u][1] = s[u][2] = s[u][3] = 0.f;
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr) {
-                    uint32_t a[4], b[4];
-                    codes_to_bf16(w[0][gr], a);
-                    codes_to_bf16(w[1][gr], b);
+                    const uint32_t x = w[0][gr], y = w[1][gr], x8 = x >> 8, y8 = y >> 8;
                     float acc[4] = {init[gr][0], init[gr][1], init[gr][0], init[gr][1]};
-                    mma_bf16_16816(acc, a[0], b[0], a[1], b[1], qf[gr][0], qf[gr][1]);
-                    mma_bf16_16816(acc, a[2], b[2], a[3], b[3], qf[gr][2], qf[gr][3]);
+                    mma_bf16_16816(acc, x & kLow, y & kLow, x & kHigh, y & kHigh, qf[gr][0], qf[gr][1]);
+                    mma_bf16_16816(acc, x8 & kLow, y8 & kLow, x8 & kHigh, y8 & kHigh, qf[gr][2], qf[gr][3]);
                     const uint32_t u0 = st[0][gr / 2], u1 = st[1][gr / 2];
                     const float s0 = __uint_as_float(gr & 1 ? u0 & 0xFFFF0000u : u0 << 16);
                     const float s1 = __uint_as_float(gr & 1 ? u1 & 0xFFFF0000u : u1 << 16);
-                    s[0] = fmaf(acc[0], s0, s[0]); s[1] = fmaf(acc[1], s0, s[1]);
-                    s[2] = fmaf(acc[2], s1, s[2]); s[3] = fmaf(acc[3], s1, s[3]);
+                    s[u][0] = fmaf(acc[0], s0, s[u][0]); s[u][1] = fmaf(acc[1], s0, s[u][1]);
+                    s[u][2] = fmaf(acc[2], s1, s[u][2]); s[u][3] = fmaf(acc[3], s1, s[u][3]);
+                }
+                s[u][0] *= f_col[0]; s[u][1] *= f_col[1]; s[u][2] *= f_col[0]; s[u][3] *= f_col[1];
+            }
+            // ---- hidden tokens: past the context, before the window, or of a second page that is not there;
+            // whatever they hold, they weigh nothing
+            int left[2], h0[2] = {0, 0}, h1[2] = {0, 0};
+            bool some_hidden = false;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int page = p + u * page_step;
+                left[u] = page < page_end ? item.kv_len - page * kPageSize : 0;     // tokens of the context in this page
+                if constexpr (kWin) {
+                    h0[u] = max(sinks - page * kPageSize, 0);
+                    h1[u] = page < page_end ? min(left[u] - window, kPageSize) : 0;
+                }
+                some_hidden |= left[u] < kPageSize || (kWin && h0[u] < h1[u]);
+            }
+            auto hidden = [&](int u, int tok) { return tok >= left[u] || (kWin && tok >= h0[u] && tok < h1[u]); };
+            if (some_hidden) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    if (hidden(u, g)) s[u][0] = s[u][1] = -INFINITY;
+                    if (hidden(u, g + 8)) s[u][2] = s[u][3] = -INFINITY;
                 }
             }
-            // ---- V's words and steps: tokens 2t, 2t + 1, 2t + 8, 2t + 9
-            uint32_t vw[4][NW], vs[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 2 * t + (r & 1) + 8 * (r >> 1);
-                if constexpr (D == 128) {
-                    const uint2 x = lds64(tv + 16 * ring_chunk<D>(row * kRowChunks + (g >> 1)) + 8 * (g & 1));
-                    vw[r][0] = x.x; vw[r][1] = x.y;
-                    vs[r] = lds32(tv + T::kCodeBytes + row * 8 + 4 * (g & 1));
-                } else {
-                    vw[r][0] = lds32(tv + 16 * ring_chunk<D>(row * kRowChunks + (g >> 2)) + 4 * (g & 3));
-                    vs[r] = lds16(tv + T::kCodeBytes + row * 4 + 2 * (g & 1));
-                }
-            }
-            // ---- hidden tokens: past the context, or before the window; whatever they hold, they weigh nothing
-            const int left = item.kv_len - p * kPageSize;               // tokens of the context in this page
-            int h0 = 0, h1 = 0;
-            if constexpr (kWin) {
-                h0 = max(sinks - p * kPageSize, 0);
-                h1 = min(left - window, kPageSize);
-            }
-            if (left < kPageSize || (kWin && h0 < h1)) {
-                auto hidden = [&](int tok) { return tok >= left || (kWin && tok >= h0 && tok < h1); };
-                if (hidden(g)) s[0] = s[1] = -INFINITY;
-                if (hidden(g + 8)) s[2] = s[3] = -INFINITY;
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (hidden(2 * t + (r & 1) + 8 * (r >> 1))) vs[r] = 0;
-            }
-            // ---- online softmax over the page's tokens (every page has a visible one)
-            float mx0 = fmaxf(s[0], s[2]), mx1 = fmaxf(s[1], s[3]);
+            // ---- online softmax over the pages' tokens (the first page has a visible one)
+            float mx0 = fmaxf(fmaxf(s[0][0], s[0][2]), fmaxf(s[1][0], s[1][2]));
+            float mx1 = fmaxf(fmaxf(s[0][1], s[0][3]), fmaxf(s[1][1], s[1][3]));
 #pragma unroll
             for (int sh = 4; sh <= 16; sh <<= 1) {
                 mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, sh));
                 mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, sh));
             }
-            const float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);
-            const float al0 = exp2_approx((m0 - mn0) * scale_log2), al1 = exp2_approx((m1 - mn1) * scale_log2);
-            const float ms0 = mn0 * scale_log2, ms1 = mn1 * scale_log2;
-            const float p0 = exp2_approx(s[0] * scale_log2 - ms0), p1 = exp2_approx(s[1] * scale_log2 - ms1);
-            const float p2 = exp2_approx(s[2] * scale_log2 - ms0), p3 = exp2_approx(s[3] * scale_log2 - ms1);
-            l0 = l0 * al0 + p0 + p2;
-            l1 = l1 * al1 + p1 + p3;
-            m0 = mn0;
-            m1 = mn1;
+            if (__any_sync(0xffffffffu, mx0 > m0 || mx1 > m1)) {
+                const float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);
+                const float al0 = exp2_approx(m0 - mn0), al1 = exp2_approx(m1 - mn1);
+                l0 *= al0;
+                l1 *= al1;
+                m0 = mn0;
+                m1 = mn1;
 #pragma unroll
-            for (int i = 0; i < 4 * NW; ++i) {
-                o[i][0] *= al0; o[i][1] *= al1; o[i][2] *= al0; o[i][3] *= al1;
+                for (int i = 0; i < 4 * NW; ++i) {
+                    o[i][0] *= al0; o[i][1] *= al1; o[i][2] *= al0; o[i][3] *= al1;
+                }
             }
-            const uint32_t b0 = decode::movmatrix_trans(pack_bf16x2(p0, p1)), b1 = decode::movmatrix_trans(pack_bf16x2(p2, p3));
+            uint32_t b0[2], b1[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const float p0 = exp2_approx(s[u][0] - m0), p1 = exp2_approx(s[u][1] - m1);
+                const float p2 = exp2_approx(s[u][2] - m0), p3 = exp2_approx(s[u][3] - m1);
+                l0 += p0 + p2;
+                l1 += p1 + p3;
+                b0[u] = decode::movmatrix_trans(pack_bf16x2(p0, p1));
+                b1[u] = decode::movmatrix_trans(pack_bf16x2(p2, p3));
+            }
             // ---- O^T += V^T P^T
 #pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                const uint32_t sel = w == 0 ? 0x5410u : 0x7632u;
-                const uint32_t sa = prmt(vs[0], vs[1], sel), sb = prmt(vs[2], vs[3], sel);
-                const uint32_t na = minus24(sa), nb = minus24(sb);
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t tile = base + u * Cfg::kPageBytes;
+                uint32_t vw[4][NW], vs[4];            // tokens 2t, 2t + 1, 2t + 8, 2t + 9
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint32_t hs = half == 0 ? 0x5410u : 0x7632u;
-                    uint32_t a[4], b[4];
-                    codes_to_bf16(prmt(vw[0][w], vw[1][w], hs), a);
-                    codes_to_bf16(prmt(vw[2][w], vw[3][w], hs), b);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        a[i] = scale_pair(a[i], sa, na);
-                        b[i] = scale_pair(b[i], sb, nb);
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t at = tile + (r & 1 ? v_off1 : v_off0) + (r >> 1) * kRow8;
+                    const uint32_t st = tile + vs_off + ((r & 1) + 8 * (r >> 1)) * 2 * NG;
+                    if constexpr (D == 128) {
+                        const uint2 x = lds64(at);
+                        vw[r][0] = x.x; vw[r][1] = x.y;
+                        vs[r] = lds32(st);
+                    } else {
+                        vw[r][0] = lds32(at);
+                        vs[r] = lds16(st);
                     }
-                    mma_bf16_16816(o[4 * w + 2 * half], a[0], a[1], b[0], b[1], b0, b1);
-                    mma_bf16_16816(o[4 * w + 2 * half + 1], a[2], a[3], b[2], b[3], b0, b1);
+                }
+                if (some_hidden) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (hidden(u, 2 * t + (r & 1) + 8 * (r >> 1))) vs[r] = 0;
+                }
+#pragma unroll
+                for (int w = 0; w < NW; ++w) {
+                    const uint32_t sel = w == 0 ? 0x5410u : 0x7632u;
+                    const uint32_t sa = prmt(vs[0], vs[1], sel), sb = prmt(vs[2], vs[3], sel);
+                    const uint32_t sa64 = mul_bf16x2(sa, 0x42804280u), sb64 = mul_bf16x2(sb, 0x42804280u);   // 64 s
+                    const uint32_t na = mul_bf16x2(sa, 0xC100C100u), nb = mul_bf16x2(sb, 0xC100C100u);       // -8 s
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t hs = half == 0 ? 0x5410u : 0x7632u;
+                        const uint32_t x = prmt(vw[0][w], vw[1][w], hs), y = prmt(vw[2][w], vw[3][w], hs);
+                        const uint32_t x8 = x >> 8, y8 = y >> 8;
+                        auto even = [&](uint32_t v, uint32_t s64, uint32_t n) {       // nibbles at bits 0 .. 3: times 2^127
+                            return fma_bf16x2(mul_bf16x2(v & kLow, 0x7F007F00u), s64, n);
+                        };
+                        auto odd = [&](uint32_t v, uint32_t s64, uint32_t n) {        // at bits 4 .. 7: times 2^123
+                            return fma_bf16x2(mul_bf16x2(v & kHigh, 0x7D007D00u), s64, n);
+                        };
+                        mma_bf16_16816(o[4 * w + 2 * half], even(x, sa64, na), odd(x, sa64, na), even(y, sb64, nb), odd(y, sb64, nb),
+                                       b0[u], b1[u]);
+                        mma_bf16_16816(o[4 * w + 2 * half + 1], even(x8, sa64, na), odd(x8, sa64, na), even(y8, sb64, nb),
+                                       odd(y8, sb64, nb), b0[u], b1[u]);
+                    }
                 }
             }
             __syncwarp();
@@ -346,7 +443,7 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int w = hh; w < kWarps; w += HB) {
                 const float *wb = fold + w * Cfg::kFoldFloats;
-                const float wt = exp2_approx((wb[8 * Cfg::kORow + h] - mstar) * scale_log2);
+                const float wt = exp2_approx(wb[8 * Cfg::kORow + h] - mstar);
                 L += wt * wb[8 * Cfg::kORow + 8 + h];
                 if (col_ok) {
                     const float4 x = *reinterpret_cast<const float4 *>(wb + h * Cfg::kORow + lane * 4);
@@ -354,7 +451,7 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
                 }
             }
             const float inv = 1.f / L;
-            const float lse = (mstar * scale_log2 + log2f(L)) * 0.6931471805599453f;
+            const float lse = (mstar + log2f(L)) * 0.6931471805599453f;
             acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
             if (item.part_slot < 0) {
                 const size_t row = (size_t)item.q_row * Hq + (size_t)(item.kv_head + hh) * G + h;
