@@ -230,14 +230,14 @@ typedef struct ap_plan_info {
     int64_t prefill_seqs;    /* sequences with q_len > 1 */
     int64_t prefill_pairs;   /* unmasked (query row, key) pairs of the prefill chunks, one head */
     int64_t decode_items;    /* split-K work items */
-    int64_t decode_ctas;     /* persistent CTAs of the decode kernel */
+    int64_t decode_ctas;     /* persistent CTAs of the decode kernel (4-bit pool: lists of items, each of decode_head_block warps) */
     int64_t merge_entries;   /* (row, kv head) results assembled from > 1 partial */
     int64_t prefill_tiles;   /* work units of the prefill kernel */
     int64_t launches_append; /* kernels ap_kv_append launches for this plan */
     int64_t launches_attention; /* kernels ap_attention_iteration launches for this plan */
     int64_t side_by_side;    /* 1 if the decode and prefill kernels of this plan run concurrently */
     int64_t decode_head_block; /* kv heads one decode item covers: 1, or 4 / 2 (the largest that divides the
-                                  pool's kv heads) when decode is confined to part of the GPU */
+                                  pool's kv heads) when decode is confined to part of the GPU; 4-bit pool: 8 / 4 / 2 / 1 */
 } ap_plan_info;
 int ap_plan_get_info(const ap_plan *plan, ap_plan_info *info);
 
@@ -393,8 +393,8 @@ int ap_attention_iteration(ap_kv_pool *pool, const ap_plan *plan, const void *q,
  *    (A plan needs at most 2 partials per decode CTA, each head_dim + 1 floats for
  *    every query head of a block of up to 4 kv heads: 4.9 MB on 148 SMs at
  *    head_dim 128 with 8 query heads per kv head, whatever the context lengths.
- *    On a 4-bit pool the decode kernel has twice as many CTAs, and prefill chunks
- *    need their pages in bf16 on top: such plans can be over the limit.)
+ *    On a 4-bit pool decode has up to 16 lists per SM and kv head, and prefill
+ *    chunks need their pages in bf16 on top: such plans can be over the limit.)
  *  - The array's device address is looked up once per device when a pool is
  *    created on it (ap_kv_pool_create, which allocates anyway and must not run
  *    inside a stream capture); that is also when the runtime brings the array

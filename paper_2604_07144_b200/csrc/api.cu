@@ -143,6 +143,12 @@ inline double side_by_side_us(double decode_bytes, double w_p, int k, double sm_
     return std::max(t_dec, (t_dec * k + w_p) / sms);
 }
 
+// Lists of decode items a plan may have: one per persistent CTA, or per HB warps of the 4-bit kernel.
+int max_decode_lists(const ap_kv_pool *pool) {
+    return std::max(1, pool->four_bit ? pool->sm_count * kKv4WarpsPerSm / pool->head_block
+                                      : pool->sm_count * decode_ctas_per_sm(pool->desc.head_dim));
+}
+
 int side_by_side_decode_ctas(const ap_kv_pool *pool, const ap_batch_desc *b, const WindowView &win, int d, int Hkv, int G,
                              int max_ctas) {
     const int mode = pool->side_by_side_mode;
@@ -315,7 +321,7 @@ static int pool_create(ap_kv_pool **out, const ap_pool_desc *desc, bool four_bit
         hp->desc = *desc;
         hp->four_bit = four_bit;
         hp->tile_bytes = pool_tile_bytes(desc->head_dim, four_bit);
-        hp->head_block = decode_head_block(desc->num_kv_heads);
+        hp->head_block = four_bit ? kv4_head_block(desc->num_kv_heads) : decode_head_block(desc->num_kv_heads);
         hp->sm_count = 148;
         hp->free_list.resize((size_t)desc->num_pages);
         for (int32_t i = 0; i < desc->num_pages; ++i) hp->free_list[(size_t)i] = desc->num_pages - 1 - i;
@@ -332,7 +338,7 @@ static int pool_create(ap_kv_pool **out, const ap_pool_desc *desc, bool four_bit
     p->desc = *desc;
     p->four_bit = four_bit;
     p->tile_bytes = pool_tile_bytes(desc->head_dim, four_bit);
-    p->head_block = decode_head_block(desc->num_kv_heads);
+    p->head_block = four_bit ? kv4_head_block(desc->num_kv_heads) : decode_head_block(desc->num_kv_heads);
     int rc = AP_OK;
     do {
         if (cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, desc->device) != cudaSuccess) {
@@ -611,7 +617,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     }
 
     // ---- decode: cut the (row, kv head block) page streams into per-CTA item lists
-    int max_ctas = std::max(1, pool->sm_count * (pool->four_bit ? kKv4CtasPerSm : decode_ctas_per_sm(d)));
+    int max_ctas = max_decode_lists(pool);
     const int side_ctas = side_by_side_decode_ctas(pool, b, win, (int)d, (int)Hkv, G, max_ctas);
     if (side_ctas > 0) max_ctas = side_ctas;
     // Costs are counted in (page, kv head) tiles.  An item covers HB kv heads, so a page of it is HB
@@ -622,12 +628,13 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     // ~58 to ~90 GB/s.  With the whole GPU decode is HBM-bound at ~41 GB/s per SM either way, and
     // one kv head per item keeps the partials (and their merge in the kernel's tail) small -- except at
     // head_dim 64, where a tile is 2 KB and single-tile requests cannot even feed 148 SMs.
-    // (The 4-bit kernel always takes blocks: the HB small tiles of a page that lie together, and eight warps
-    // that share a row's pages among fewer of them.)
+    // (The 4-bit kernel always takes blocks: one warp per kv head, side by side on the small tiles of a page.)
     const int HB = (side_ctas > 0 || d < 128 || pool->four_bit) ? pool->head_block : 1, NB = Hkv / HB;
-    const int kStageTiles = pool->four_bit ? kKv4TilesPerRound : kDecodeTilesPerStage;
+    const int kStageTiles = pool->four_bit ? 2 * HB : kDecodeTilesPerStage;      // (the 4-bit kernel takes pages in pairs)
     const int PS = kStageTiles / HB;      // pages of an item per stage
-    constexpr int kItemCost = 3;          // fixed per-item cost (its query load, the hand-over of its result)
+    // fixed per-item cost (its query load, the hand-over of its result), in tiles; in the 4-bit kernel every head's
+    // warp pays it
+    const int kItemCost = pool->four_bit ? 3 * HB : 3;
     std::vector<DecodeItem> items;
     std::vector<int32_t> cta_begin;
     std::vector<MergeEntry> merges;
@@ -849,7 +856,9 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     }
     plan->side_by_side = side_ctas > 0 && !items.empty() && !tiles.empty();
     plan->single_launch = plan->side_by_side && pool->single_launch;
-    info.launches_attention = plan->single_launch ? 1 : (items.empty() ? 0 : 1) + (tiles.empty() ? 0 : pool->four_bit ? 2 : 1);
+    info.launches_attention = plan->single_launch ? 1 : (items.empty() ? 0 : 1) + (tiles.empty() ? 0 : 1);
+    if (pool->four_bit)      // decode, merge, widen, prefill
+        info.launches_attention += (merges.empty() ? 0 : 1) + (tiles.empty() ? 0 : 1);
     info.side_by_side = plan->side_by_side ? 1 : 0;
     info.decode_head_block = HB;
     *out = plan;
@@ -1197,8 +1206,7 @@ int ap_serving_iteration_host(ap_kv_pool *pool, const ap_batch_desc *batch, cons
     const size_t q_bytes = align_up(n * Hq * d * 2, 256), kv_bytes = align_up(n * Hkv * d * 2, 256);
     const size_t lse_bytes = align_up(n * Hq * 4, 256);
     // every decode CTA leaves at most two partials, which bounds the workspace before planning
-    const size_t max_slots =
-        2 * (size_t)std::max(1, pool->sm_count * (pool->four_bit ? kKv4CtasPerSm : decode_ctas_per_sm((int)d)));
+    const size_t max_slots = 2 * (size_t)max_decode_lists(pool);
     const size_t part_heads = (size_t)pool->head_block * (Hq / Hkv);      // query heads of one decode item
     size_t wide_bytes = 0;                                  // a 4-bit pool's pages that prefill chunks read, in bf16
     if (pool->four_bit && batch->ctx_lens) {

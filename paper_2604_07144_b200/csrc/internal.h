@@ -222,8 +222,12 @@ int prepare_static_workspace(int device);
 
 // Decode kernel launch geometry (used by the planner to size the item lists).
 int decode_ctas_per_sm(int head_dim);
-constexpr int kKv4CtasPerSm = 2;           // of the 4-bit decode kernel
-constexpr int kKv4TilesPerRound = 8;       // its eight warps take one tile each
+// The 4-bit decode kernel: 16 warps on an SM, each on its own kv head of an item; a list of items belongs to HB
+// warps, HB the largest of 8, 4, 2, 1 that divides the number of kv heads.
+constexpr int kKv4WarpsPerSm = 16;
+inline int kv4_head_block(int num_kv_heads) {
+    return num_kv_heads % 8 == 0 ? 8 : num_kv_heads % 4 == 0 ? 4 : num_kv_heads % 2 == 0 ? 2 : 1;
+}
 constexpr int kDecodeTilesPerStage = 4;    // (page, kv head) tiles of one plane in a ring stage: one per warp of a consumer group
 // kv heads per decode item: the largest of 4, 2, 1 that divides the number of kv heads.  A stage then holds
 // kDecodeTilesPerStage / HB pages of HB heads each.

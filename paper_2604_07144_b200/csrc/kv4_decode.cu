@@ -1,12 +1,14 @@
 // Decode attention over a 4-bit paged cache: split-K flash-decoding like the bf16 kernel's, on the same
-// kind of item lists, but built around warps that stream for themselves.
+// kind of item lists, but built of warps that work for themselves.
 //
 // At 4.5 bits a value a (page, kv head) tile is 1152 bytes (d = 128): too small for one TMA request each (an
 // SM's TMA unit handles ~14 M requests/s, 16 GB/s at that size; HBM gives an SM 43), and what an SM has to do
 // per byte is 3.6 times the bf16 kernel's.  So every warp copies its own tiles with 16-byte cp.async into a
-// private ring of kDepth pairs of pages and no warp waits for another one inside an item: there
-// is no barrier in the stream.  Warp w of an item works on kv head w mod HB of the item's block and on pages
-// w / HB, w / HB + 8 / HB, ...; the HB tiles of a page lie together in HBM.
+// private ring of kDepth pairs of pages, and no warp ever waits for another one: there is no barrier in the
+// kernel.  An item is a range of a row's pages for a block of HB kv heads (8, 4, 2 or 1, the largest that
+// divides the pool's); each of the plan's lists belongs to HB warps of a block, one per kv head, which read
+// the HB tiles that lie together in HBM.  (With blocks of warps that share a head and fold their results at
+// an item's end, barriers and uneven shares cost 20 of 49 us on 64 rows of 128 .. 8192 tokens.)
 //
 // What bounds the kernel is the ALU pipe (LOP3, PRMT, shifts: one warp instruction in two clocks) on the
 // way from nibbles to MMA operands, so that way is short.  The bits of a byte b, put into a bf16 pattern with
@@ -17,8 +19,9 @@
 //   S^T_g = c_K (2^a Q_g)^T    per group g of 32 elements, M = 16 tokens, N = 8 query heads (mma.sync
 //                              m16n8k16).  Q is scaled by a power of two per head (its largest element to
 //                              2^120; elements facing nibbles at bits 4 .. 7 by 2^-4 less), which is exact;
-//                              the accumulator starts at -8 sum_g q, so sum (c - 8) q comes out, and the step
-//                              of (token, group) multiplies it: S = sum_g s_g S_g;
+//                              the step of (token, group) multiplies what comes out, and the codes' offset,
+//                              -8 sum_g s_g sum q, is a further small MMA over the steps themselves (sum q in
+//                              three bf16 parts): S = sum_g s_g (sum c q - 8 sum q);
 //   softmax                    running maximum and sum in fp32, shuffles across the token lanes, once per two
 //                              pages; O is rescaled only when some lane's maximum has moved;
 //   O^T += V^T P^T             V is widened to bf16 in registers, exactly: c 2^-133 times 2^127 (c 2^-129 times
@@ -27,9 +30,8 @@
 // read 16 bytes of a row per lane, V fragments 8 bytes of four rows per lane, pairs of rows interleaved with
 // PRMT.
 //
-// At the end of an item the warps drop (m, l, O) into shared memory, the block folds them per head and
-// writes the bf16 output or, for a stream cut across blocks, an fp32 partial; the block that counts the last
-// partial in merges the stream.  Two blocks share an SM, so one streams while the other folds.
+// At the end of an item a warp has its head's complete (m, l, O) in registers and writes the bf16 output or, for
+// a stream cut across lists, an fp32 partial for the merge kernel.
 #include "decode_splitk.cuh"
 #include "kv4.cuh"
 
@@ -42,19 +44,13 @@ using namespace kv4;
 
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
-constexpr int kDepth = 2;                // pairs of pages in a warp's ring (K and V tile of each)
-constexpr int kListItems = 32;           // item descriptors of a block kept in shared memory
+constexpr int kDepth = 3;                // pairs of pages in a warp's ring (K and V tile of each)
 
 template <int D>
 struct Kv4Cfg {
     static constexpr int kPageBytes = 2 * Tile<D>::kBytes;        // K tile, V tile
     static constexpr int kSlotBytes = 2 * kPageBytes;
-    static constexpr int kRingBytes = kWarps * kDepth * kSlotBytes;
-    static constexpr int kORow = D + 4;
-    static constexpr int kFoldFloats = 8 * kORow + 16;            // O[8][D + 4], m[8], l[8] of a warp
-    static constexpr int kOffFold = kRingBytes;
-    static constexpr int kOffItems = kOffFold + kWarps * kFoldFloats * 4;
-    static constexpr int kSmemBytes = kOffItems + kListItems * 32;
+    static constexpr int kSmemBytes = kWarps * kDepth * kSlotBytes;
     static_assert(2 * (kSmemBytes + 1024) <= 228 * 1024, "two blocks per SM");
 };
 
@@ -88,6 +84,18 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
 
 constexpr uint32_t kLow = 0x000F000Fu, kHigh = 0x00F000F0u;     // two nibbles of a word, one in each half
 
+// D(16x8, f32) = A(16x16, bf16) B(16x8, bf16), or D += A B.  Not volatile: the compiler may interleave them.
+__device__ __forceinline__ void mma_zero(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void mma_add(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
@@ -112,9 +120,8 @@ template <int D, bool kWin>
 __global__ void __launch_bounds__(kThreads, 2)
 kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict__ v_pool, const __nv_bfloat16 *__restrict__ q,
                   const DecodeItem *__restrict__ items, const int32_t *__restrict__ cta_begin, const int32_t *__restrict__ bt_flat,
-                  const MergeEntry *__restrict__ merges, float *o_part, float *lse_part, __nv_bfloat16 *__restrict__ out,
-                  float *__restrict__ lse_out, int Hq, int Hkv, int G, int HB, int num_pages, float scale_log2, int *status,
-                  int *merge_counters, int window, int sinks) {
+                  float *o_part, float *lse_part, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse_out, int Hq, int Hkv,
+                  int G, int HB, int n_lists, int num_pages, float scale_log2, int *status, int window, int sinks) {
     using Cfg = Kv4Cfg<D>;
     using T = Tile<D>;
     constexpr int NG = T::kGroups;          // groups of a row: 4 (2)
@@ -122,45 +129,49 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
     constexpr int kCodeChunks = T::kCodeBytes / 16, kStepChunks = (T::kBytes - T::kCodeBytes) / 16;
     constexpr int kRowChunks = T::kRowBytes / 16;
     extern __shared__ __align__(128) uint8_t smem[];
-    float *fold = reinterpret_cast<float *>(smem + Cfg::kOffFold);
-    DecodeItem *s_items = reinterpret_cast<DecodeItem *>(smem + Cfg::kOffItems);
-    __shared__ int s_last;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
-    const int cta = blockIdx.x;
-    const int item_begin = cta_begin[cta], n_items = cta_begin[cta + 1] - item_begin;
-    const int my_head = warp % HB, my_page0 = warp / HB, page_step = kWarps / HB;
-    {
-        const int n_ints = min(n_items, kListItems) * (int)(sizeof(DecodeItem) / 4);
-        const int32_t *src = reinterpret_cast<const int32_t *>(items + item_begin);
-        for (int i = threadIdx.x; i < n_ints; i += kThreads) reinterpret_cast<int32_t *>(s_items)[i] = __ldg(src + i);
+    const int list = blockIdx.x * (kWarps / HB) + warp / HB, my_head = warp % HB;
+    if (list >= n_lists) {
+        griddep_launch_dependents();
+        griddep_wait();
+        return;
     }
-    __syncthreads();
-    auto get_item = [&](int n) { return n < kListItems ? s_items[n] : items[item_begin + n]; };
+    const int item_begin = __ldg(cta_begin + list), n_items = __ldg(cta_begin + list + 1) - item_begin;
+    auto get_item = [&](int n) {
+        const int4 *src = reinterpret_cast<const int4 *>(items + item_begin + n);
+        const int4 x = __ldg(src), y = __ldg(src + 1);
+        return DecodeItem{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    };
 
     // ---- the warp's stream of page pairs: a cursor that runs ahead of the consumer, across items; block-table
     // entries are loaded a pair before they are needed
-    int cur_item = -1, cur_page = 0, cur_end = 0, cur_bt = 0, cur_head = 0;
-    struct Fetch { int32_t page[2]; int head, n; };           // n pages (0: past the last)
-    auto next_fetch = [&]() {
-        Fetch f;
-        f.n = 0;
-        f.page[0] = f.page[1] = f.head = 0;
-        while (cur_page >= cur_end) {
-            if (++cur_item >= n_items) { cur_item = n_items; return f; }
+    int cur_item = -1, cur_left = 0, cur_head = 0;            // cur_left: pages of the item still ahead
+    const int32_t *cur_bt = bt_flat;
+    int32_t next_page0 = 0, next_page1 = 0;
+    int next_head = 0, next_n = 0;                            // n pages of the next pair (0: past the last)
+    auto fetch = [&]() {
+        while (cur_left <= 0) {
+            if (++cur_item >= n_items) {
+                cur_item = n_items;
+                next_n = 0;
+                return;
+            }
             const DecodeItem it = get_item(cur_item);
-            cur_page = it.page_begin + my_page0;
-            cur_end = it.page_begin + it.page_count;
-            cur_bt = it.bt_offset;
+            cur_left = it.page_count;
+            cur_bt = bt_flat + it.bt_offset + it.page_begin;
             cur_head = it.kv_head + my_head;
         }
-        f.n = cur_page + page_step < cur_end ? 2 : 1;
-        f.page[0] = __ldg(bt_flat + cur_bt + cur_page);
-        if (f.n == 2) f.page[1] = __ldg(bt_flat + cur_bt + cur_page + page_step);
-        f.head = cur_head;
-        cur_page += 2 * page_step;
-        return f;
+        next_head = cur_head;
+        next_page0 = __ldg(cur_bt);
+        next_n = 1;
+        if (cur_left > 1) {
+            next_page1 = __ldg(cur_bt + 1);
+            next_n = 2;
+        }
+        cur_bt += 2;
+        cur_left -= 2;
     };
     const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * kDepth * Cfg::kSlotBytes);
     // a lane's share of a tile's copy: code chunks lane (and lane + 32, four lines on), and, for the first
@@ -170,33 +181,32 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
     const bool step_lane = lane < 2 * kStepChunks, k_steps = lane < kStepChunks;
     const uint32_t s_dst = (k_steps ? 0 : T::kBytes) + 16 * (kCodeChunks + lane % kStepChunks);
     const uint8_t *const s_src = (k_steps ? k_pool : v_pool) + 16 * (kCodeChunks + lane % kStepChunks);
-    Fetch f0 = next_fetch();
+    fetch();
     griddep_launch_dependents();
     griddep_wait();              // all of the above reads the plan only
+    auto issue_page = [&](uint32_t d, int32_t page) {
+        if ((uint32_t)page >= (uint32_t)num_pages) {
+            record_status(status, AP_ERR_BAD_BLOCK_TABLE);
+            page = 0;
+        }
+        const int64_t tile = (int64_t)((uint64_t)((uint32_t)page * (uint32_t)Hkv + (uint32_t)next_head) * (uint32_t)T::kBytes);
+        const uint8_t *k = k_src + tile, *v = v_src + tile;
+        cp_async16(d + c_dst, k);
+        cp_async16(d + c_dst + T::kBytes, v);
+        if constexpr (kCodeChunks > 32) {
+            cp_async16(d + c_dst + 512, k + 512);
+            cp_async16(d + c_dst + T::kBytes + 512, v + 512);
+        }
+        if (step_lane) cp_async16(d + s_dst, s_src + tile);
+    };
     auto issue = [&](int slot) {
         const uint32_t dst = ring + (uint32_t)(slot * Cfg::kSlotBytes);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if (u < f0.n) {
-                int32_t page = f0.page[u];
-                if ((uint32_t)page >= (uint32_t)num_pages) {
-                    record_status(status, AP_ERR_BAD_BLOCK_TABLE);
-                    page = 0;
-                }
-                const int64_t tile = (int64_t)((uint32_t)page * (uint32_t)Hkv + (uint32_t)f0.head) * T::kBytes;
-                const uint32_t d = dst + u * Cfg::kPageBytes;
-                const uint8_t *k = k_src + tile, *v = v_src + tile;
-                cp_async16(d + c_dst, k);
-                cp_async16(d + c_dst + T::kBytes, v);
-                if constexpr (kCodeChunks > 32) {
-                    cp_async16(d + c_dst + 512, k + 512);
-                    cp_async16(d + c_dst + T::kBytes + 512, v + 512);
-                }
-                if (step_lane) cp_async16(d + s_dst, s_src + tile);
-            }
+        if (next_n > 0) {
+            issue_page(dst, next_page0);
+            if (next_n > 1) issue_page(dst + Cfg::kPageBytes, next_page1);
+            fetch();
         }
         cp_async_commit();       // (an empty group past the last pair keeps the count of groups in step)
-        f0 = next_fetch();
     };
 #pragma unroll 1
     for (int s = 0; s < kDepth; ++s) issue(s);
@@ -218,8 +228,8 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
         const int kv_head = item.kv_head + my_head;
         // ---- Q^T as the B operand, in the order in which a lane's word of K holds the elements, scaled; the
         // accumulators' start; and what turns a score into a power of two's exponent, per column (head)
-        uint32_t qf[NG][4];
-        float init[NG][2], f_col[2];
+        uint32_t qf[NG][4], off0 = 0, off1 = 0;
+        float f_col[2];
         {
             uint4 x[NG];
             uint32_t amax = 0;
@@ -253,9 +263,18 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
                 qf[gr][3] = pack_bf16x2(e[3] * 0.0625f, e[7] * 0.0625f);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                const float start = sum * -7.3468396926392969e-40f;                     // -8 2^-133 = -2^-130
-                init[gr][0] = __shfl_sync(0xffffffffu, start, 8 * t);
-                init[gr][1] = __shfl_sync(0xffffffffu, start, 8 * t + 4);
+                // -8 sum q of this group in three bf16 parts (24 bits), in the units of the accumulators; element
+                // gr & 1 of the B registers whose k indices the part's steps have in the offset product
+                const float part0 = sum * -7.3468396926392969e-40f;                     // -8 2^-133 = -2^-130
+                const float hi = __uint_as_float(__float_as_uint(part0) & 0xFFFF0000u), rest = part0 - hi;
+                const float mid = __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u), lo = rest - mid;
+                auto put = [&](uint32_t &reg, float v) { reg |= (pack_bf16x2(v, 0.f) & 0xFFFFu) << (16 * (gr & 1)); };
+                if constexpr (D == 128) {      // k = 0 .. 3: high parts of groups 0 .. 3, 4 .. 7: middle, 8 .. 11: low
+                    if (t == gr / 2) { put(off0, hi); put(off1, lo); }
+                    if (t == 2 + gr / 2) put(off0, mid);
+                } else {                       // k = 0, 1: high, 2, 3: middle, 4, 5: low
+                    put(off0, t == 0 ? hi : t == 1 ? mid : t == 2 ? lo : 0.f);
+                }
             }
             f_col[0] = __shfl_sync(0xffffffffu, f, 8 * t);
             f_col[1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
@@ -268,59 +287,78 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
 
         const int page_end = item.page_begin + item.page_count;
 #pragma unroll 1
-        for (int p = item.page_begin + my_page0; p < page_end; p += 2 * page_step) {
+        for (int p = item.page_begin; p < page_end; p += 2) {
             cp_async_wait<kDepth - 1>();
             __syncwarp();
             const uint32_t base = ring + (uint32_t)(slot * Cfg::kSlotBytes);
-            // ---- S^T of both pages
+            // ---- S^T of both pages (all loads ahead of the products)
             float s[2][4];
+            {
+                uint32_t w[2][2][NG], st[2][2][NG / 2], so[2][2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const uint32_t tile = base + u * Cfg::kPageBytes;
+                        if constexpr (D == 128) {
+                            const uint4 x = lds128(tile + k_off + r * kRow8);
+                            w[u][r][0] = x.x; w[u][r][1] = x.y; w[u][r][2] = x.z; w[u][r][3] = x.w;
+                            const uint2 y = lds64(tile + ks_off + r * 16 * NG);
+                            st[u][r][0] = y.x; st[u][r][1] = y.y;
+                            so[u][r] = lds32(tile + ks_off + r * 16 * NG + 4 * (t & 1));
+                        } else {
+                            const uint2 x = lds64(tile + k_off + r * kRow8);
+                            w[u][r][0] = x.x; w[u][r][1] = x.y;
+                            so[u][r] = st[u][r][0] = lds32(tile + ks_off + r * 16 * NG);
+                        }
+                    }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    // sum_g s_g (-8 sum_g q): steps are bf16 numbers, a small product of its own
+                    mma_zero(s[u], so[u][0], so[u][1], so[u][0], so[u][1], off0, off1);
+#pragma unroll
+                    for (int gr = 0; gr < NG; ++gr) {
+                        const uint32_t x = w[u][0][gr], y = w[u][1][gr], x8 = x >> 8, y8 = y >> 8;
+                        float acc[4];
+                        mma_zero(acc, x & kLow, y & kLow, x & kHigh, y & kHigh, qf[gr][0], qf[gr][1]);
+                        mma_add(acc, x8 & kLow, y8 & kLow, x8 & kHigh, y8 & kHigh, qf[gr][2], qf[gr][3]);
+                        const uint32_t u0 = st[u][0][gr / 2], u1 = st[u][1][gr / 2];
+                        const float s0 = __uint_as_float(gr & 1 ? u0 & 0xFFFF0000u : u0 << 16);
+                        const float s1 = __uint_as_float(gr & 1 ? u1 & 0xFFFF0000u : u1 << 16);
+                        s[u][0] = fmaf(acc[0], s0, s[u][0]); s[u][1] = fmaf(acc[1], s0, s[u][1]);
+                        s[u][2] = fmaf(acc[2], s1, s[u][2]); s[u][3] = fmaf(acc[3], s1, s[u][3]);
+                    }
+                    s[u][0] *= f_col[0]; s[u][1] *= f_col[1]; s[u][2] *= f_col[0]; s[u][3] *= f_col[1];
+                }
+            }
+            // ---- V words and steps, tokens 2t, 2t + 1, 2t + 8, 2t + 9; the first page's ahead of the softmax
+            uint32_t vw[2][4][NW], vs[2][4];
+            auto load_v = [&](int u) {
                 const uint32_t tile = base + u * Cfg::kPageBytes;
-                uint32_t w[2][NG], st[2][NG / 2];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t at = tile + (r & 1 ? v_off1 : v_off0) + (r >> 1) * kRow8;
+                    const uint32_t st = tile + vs_off + ((r & 1) + 8 * (r >> 1)) * 2 * NG;
                     if constexpr (D == 128) {
-                        const uint4 x = lds128(tile + k_off + r * kRow8);
-                        w[r][0] = x.x; w[r][1] = x.y; w[r][2] = x.z; w[r][3] = x.w;
-                        const uint2 y = lds64(tile + ks_off + r * 16 * NG);
-                        st[r][0] = y.x; st[r][1] = y.y;
+                        const uint2 x = lds64(at);
+                        vw[u][r][0] = x.x; vw[u][r][1] = x.y;
+                        vs[u][r] = lds32(st);
                     } else {
-                        const uint2 x = lds64(tile + k_off + r * kRow8);
-                        w[r][0] = x.x; w[r][1] = x.y;
-                        st[r][0] = lds32(tile + ks_off + r * 16 * NG);
+                        vw[u][r][0] = lds32(at);
+                        vs[u][r] = lds16(st);
                     }
                 }
-                s[u][0] = s[u][1] = s[u][2] = s[u][3] = 0.f;
-#pragma unroll
-                for (int gr = 0; gr < NG; ++gr) {
-                    const uint32_t x = w[0][gr], y = w[1][gr], x8 = x >> 8, y8 = y >> 8;
-                    float acc[4] = {init[gr][0], init[gr][1], init[gr][0], init[gr][1]};
-                    mma_bf16_16816(acc, x & kLow, y & kLow, x & kHigh, y & kHigh, qf[gr][0], qf[gr][1]);
-                    mma_bf16_16816(acc, x8 & kLow, y8 & kLow, x8 & kHigh, y8 & kHigh, qf[gr][2], qf[gr][3]);
-                    const uint32_t u0 = st[0][gr / 2], u1 = st[1][gr / 2];
-                    const float s0 = __uint_as_float(gr & 1 ? u0 & 0xFFFF0000u : u0 << 16);
-                    const float s1 = __uint_as_float(gr & 1 ? u1 & 0xFFFF0000u : u1 << 16);
-                    s[u][0] = fmaf(acc[0], s0, s[u][0]); s[u][1] = fmaf(acc[1], s0, s[u][1]);
-                    s[u][2] = fmaf(acc[2], s1, s[u][2]); s[u][3] = fmaf(acc[3], s1, s[u][3]);
-                }
-                s[u][0] *= f_col[0]; s[u][1] *= f_col[1]; s[u][2] *= f_col[0]; s[u][3] *= f_col[1];
-            }
+            };
+            load_v(0);
             // ---- hidden tokens: past the context, before the window, or of a second page that is not there;
             // whatever they hold, they weigh nothing
-            int left[2], h0[2] = {0, 0}, h1[2] = {0, 0};
-            bool some_hidden = false;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int page = p + u * page_step;
-                left[u] = page < page_end ? item.kv_len - page * kPageSize : 0;     // tokens of the context in this page
-                if constexpr (kWin) {
-                    h0[u] = max(sinks - page * kPageSize, 0);
-                    h1[u] = page < page_end ? min(left[u] - window, kPageSize) : 0;
-                }
-                some_hidden |= left[u] < kPageSize || (kWin && h0[u] < h1[u]);
-            }
-            auto hidden = [&](int u, int tok) { return tok >= left[u] || (kWin && tok >= h0[u] && tok < h1[u]); };
+            const int page1 = p + 1;
+            const bool some_hidden = page1 >= page_end || (page1 + 1) * kPageSize > item.kv_len ||
+                                     (kWin && p * kPageSize < item.kv_len - window && (page1 + 1) * kPageSize > sinks);
+            auto hidden = [&](int u, int tok) {
+                const int page = p + u, key = page * kPageSize + tok;
+                return page >= page_end || key >= item.kv_len || (kWin && key >= sinks && key < item.kv_len - window);
+            };
             if (some_hidden) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
@@ -359,38 +397,24 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
                 b1[u] = decode::movmatrix_trans(pack_bf16x2(p2, p3));
             }
             // ---- O^T += V^T P^T
+            load_v(1);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const uint32_t tile = base + u * Cfg::kPageBytes;
-                uint32_t vw[4][NW], vs[4];            // tokens 2t, 2t + 1, 2t + 8, 2t + 9
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t at = tile + (r & 1 ? v_off1 : v_off0) + (r >> 1) * kRow8;
-                    const uint32_t st = tile + vs_off + ((r & 1) + 8 * (r >> 1)) * 2 * NG;
-                    if constexpr (D == 128) {
-                        const uint2 x = lds64(at);
-                        vw[r][0] = x.x; vw[r][1] = x.y;
-                        vs[r] = lds32(st);
-                    } else {
-                        vw[r][0] = lds32(at);
-                        vs[r] = lds16(st);
-                    }
-                }
                 if (some_hidden) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (hidden(u, 2 * t + (r & 1) + 8 * (r >> 1))) vs[r] = 0;
+                        if (hidden(u, 2 * t + (r & 1) + 8 * (r >> 1))) vs[u][r] = 0;
                 }
 #pragma unroll
                 for (int w = 0; w < NW; ++w) {
                     const uint32_t sel = w == 0 ? 0x5410u : 0x7632u;
-                    const uint32_t sa = prmt(vs[0], vs[1], sel), sb = prmt(vs[2], vs[3], sel);
+                    const uint32_t sa = prmt(vs[u][0], vs[u][1], sel), sb = prmt(vs[u][2], vs[u][3], sel);
                     const uint32_t sa64 = mul_bf16x2(sa, 0x42804280u), sb64 = mul_bf16x2(sb, 0x42804280u);   // 64 s
                     const uint32_t na = mul_bf16x2(sa, 0xC100C100u), nb = mul_bf16x2(sb, 0xC100C100u);       // -8 s
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const uint32_t hs = half == 0 ? 0x5410u : 0x7632u;
-                        const uint32_t x = prmt(vw[0][w], vw[1][w], hs), y = prmt(vw[2][w], vw[3][w], hs);
+                        const uint32_t x = prmt(vw[u][0][w], vw[u][1][w], hs), y = prmt(vw[u][2][w], vw[u][3][w], hs);
                         const uint32_t x8 = x >> 8, y8 = y >> 8;
                         auto even = [&](uint32_t v, uint32_t s64, uint32_t n) {       // nibbles at bits 0 .. 3: times 2^127
                             return fma_bf16x2(mul_bf16x2(v & kLow, 0x7F007F00u), s64, n);
@@ -398,9 +422,9 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
                         auto odd = [&](uint32_t v, uint32_t s64, uint32_t n) {        // at bits 4 .. 7: times 2^123
                             return fma_bf16x2(mul_bf16x2(v & kHigh, 0x7D007D00u), s64, n);
                         };
-                        mma_bf16_16816(o[4 * w + 2 * half], even(x, sa64, na), odd(x, sa64, na), even(y, sb64, nb), odd(y, sb64, nb),
+                        mma_add(o[4 * w + 2 * half], even(x, sa64, na), odd(x, sa64, na), even(y, sb64, nb), odd(y, sb64, nb),
                                        b0[u], b1[u]);
-                        mma_bf16_16816(o[4 * w + 2 * half + 1], even(x8, sa64, na), odd(x8, sa64, na), even(y8, sb64, nb),
+                        mma_add(o[4 * w + 2 * half + 1], even(x8, sa64, na), odd(x8, sa64, na), even(y8, sb64, nb),
                                        odd(y8, sb64, nb), b0[u], b1[u]);
                     }
                 }
@@ -410,83 +434,102 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
             slot = slot + 1 == kDepth ? 0 : slot + 1;
         }
 
-        // ---- the item's end: every warp's (m, l, O) to shared memory, folded by the block per head
+        // ---- the item's end: this lane has columns d0 .. d0 + 7 (per V word) of heads 2t and 2t + 1
 #pragma unroll
         for (int sh = 4; sh <= 16; sh <<= 1) {
             l0 += __shfl_xor_sync(0xffffffffu, l0, sh);
             l1 += __shfl_xor_sync(0xffffffffu, l1, sh);
         }
-        float *mine = fold + warp * Cfg::kFoldFloats;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const int d0 = D == 128 ? 32 * (2 * (g & 1) + w) + 8 * (g >> 1) : 32 * (g & 1) + 8 * (g >> 1);
+        for (int c = 0; c < 2; ++c) {
+            const int h = 2 * t + c;
+            if (h >= G) continue;
+            const float l = c ? l1 : l0, inv = 1.f / l;
+            const float lse = ((c ? m1 : m0) + log2f(l)) * 0.6931471805599453f;
+            const size_t row = item.part_slot < 0 ? (size_t)item.q_row * Hq + (size_t)kv_head * G + h
+                                                  : (size_t)item.part_slot * (HB * G) + my_head * G + h;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                *reinterpret_cast<float2 *>(mine + (2 * t) * Cfg::kORow + d0 + 2 * i) = make_float2(o[4 * w + i][0], o[4 * w + i][2]);
-                *reinterpret_cast<float2 *>(mine + (2 * t + 1) * Cfg::kORow + d0 + 2 * i) = make_float2(o[4 * w + i][1], o[4 * w + i][3]);
-            }
-        }
-        if (g == 0) {
-            mine[8 * Cfg::kORow + 2 * t] = m0;
-            mine[8 * Cfg::kORow + 2 * t + 1] = m1;
-            mine[8 * Cfg::kORow + 8 + 2 * t] = l0;
-            mine[8 * Cfg::kORow + 8 + 2 * t + 1] = l1;
-        }
-        __syncthreads();
-        const int PH = HB * G;
-        const bool col_ok = lane * 4 < D;
-        for (int ph = warp; ph < PH; ph += kWarps) {
-            const int hh = ph / G, h = ph % G;
-            float mstar = -INFINITY;
-            for (int w = hh; w < kWarps; w += HB) mstar = fmaxf(mstar, fold[w * Cfg::kFoldFloats + 8 * Cfg::kORow + h]);
-            float L = 0.f;
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int w = hh; w < kWarps; w += HB) {
-                const float *wb = fold + w * Cfg::kFoldFloats;
-                const float wt = exp2_approx(wb[8 * Cfg::kORow + h] - mstar);
-                L += wt * wb[8 * Cfg::kORow + 8 + h];
-                if (col_ok) {
-                    const float4 x = *reinterpret_cast<const float4 *>(wb + h * Cfg::kORow + lane * 4);
-                    acc.x += wt * x.x; acc.y += wt * x.y; acc.z += wt * x.z; acc.w += wt * x.w;
+            for (int w = 0; w < NW; ++w) {
+                const int d0 = D == 128 ? 32 * (2 * (g & 1) + w) + 8 * (g >> 1) : 32 * (g & 1) + 8 * (g >> 1);
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[2 * i] = o[4 * w + i][c] * inv;
+                    v[2 * i + 1] = o[4 * w + i][2 + c] * inv;
+                }
+                if (item.part_slot < 0) {
+                    *reinterpret_cast<uint4 *>(out + row * D + d0) = make_uint4(
+                        pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+                } else {
+                    *reinterpret_cast<float4 *>(o_part + row * D + d0) = make_float4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<float4 *>(o_part + row * D + d0 + 4) = make_float4(v[4], v[5], v[6], v[7]);
                 }
             }
-            const float inv = 1.f / L;
-            const float lse = (mstar + log2f(L)) * 0.6931471805599453f;
-            acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
-            if (item.part_slot < 0) {
-                const size_t row = (size_t)item.q_row * Hq + (size_t)(item.kv_head + hh) * G + h;
-                if (col_ok)
-                    *reinterpret_cast<uint2 *>(out + row * D + lane * 4) =
-                        make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
-                if (lane == 0 && lse_out) lse_out[row] = lse;
-            } else {
-                const size_t row = (size_t)item.part_slot * PH + ph;
-                if (col_ok) *reinterpret_cast<float4 *>(o_part + row * D + lane * 4) = acc;
-                if (lane == 0) lse_part[row] = lse;
+            if (g == 0) {
+                if (item.part_slot >= 0) lse_part[row] = lse;
+                else if (lse_out) lse_out[row] = lse;
             }
         }
-        if (item.part_slot >= 0) {
-            // count the partial in; whoever completes the stream merges it, a head per warp
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                int old;
-                asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;"
-                             : "=r"(old) : "l"(merge_counters + item.merge_index) : "memory");
-                s_last = old == __ldg(&merges[item.merge_index].part_count) - 1;
-                if (s_last) merge_counters[item.merge_index] = 0;      // ready for the next launch
-            }
-            __syncthreads();
-            if (s_last) {
-                __threadfence();
-                const MergeEntry me = merges[item.merge_index];
-                for (int ph = warp; ph < PH; ph += kWarps)
-                    decode::merge_stream<D, 1>(me, o_part, lse_part, out, lse_out, Hq, lane, PH, ph, me.kv_head * G);
-            }
-        }
-        __syncthreads();         // the buffer (and s_last) may be used again
     }
     cp_async_wait<0>();
+}
+
+// Merges the partials of a cut stream, one query head per block:
+//   lse = m* + ln sum_k exp(lse_k - m*),  o = sum_k exp(lse_k - lse) o_k,  m* = max_k lse_k.
+// A kernel of its own, overlapped with the decode kernel's end: with 64 query heads and ~20 partials each, the
+// warp that finishes a stream would still be merging for 30 us when all others are through (204 -> 221 us on 16
+// rows of 32 - 64 k tokens); here every head has four warps, eight partial rows in flight each.
+constexpr int kMergeThreads = 128;
+
+template <int D>
+__global__ void __launch_bounds__(kMergeThreads)
+kv4_merge_kernel(const MergeEntry *__restrict__ merges, const float *__restrict__ o_part, const float *__restrict__ lse_part,
+                 __nv_bfloat16 *__restrict__ out, float *__restrict__ lse_out, int Hq, int PH, int G) {
+    constexpr int kW = kMergeThreads / 32, kBatch = 8;
+    __shared__ float4 sums[kW][32];
+    const MergeEntry me = merges[blockIdx.x / PH];
+    const int ph = blockIdx.x % PH, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    griddep_launch_dependents();
+    griddep_wait();
+    const float *lse = lse_part + (size_t)me.part_begin * PH + ph;
+    const int n = me.part_count;
+    float mx = -INFINITY, sum = 0.f;
+    for (int k = lane; k < n; k += 32) mx = fmaxf(mx, __ldcg(lse + (size_t)k * PH));
+#pragma unroll
+    for (int sh = 16; sh >= 1; sh >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, sh));
+    for (int k = lane; k < n; k += 32) sum += __expf(__ldcg(lse + (size_t)k * PH) - mx);
+#pragma unroll
+    for (int sh = 16; sh >= 1; sh >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, sh);
+    const float total = mx + __logf(sum);
+    const bool col_ok = lane * 4 < D;
+    const float4 *o = reinterpret_cast<const float4 *>(o_part + ((size_t)me.part_begin * PH + ph) * D) + lane;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = warp; k0 < n; k0 += kW * kBatch) {
+        float4 x[kBatch];
+        float w[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int k = k0 + i * kW;
+            x[i] = k < n && col_ok ? __ldcg(o + (size_t)k * PH * (D / 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            w[i] = k < n ? __expf(__ldcg(lse + (size_t)k * PH) - total) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            acc.x += w[i] * x[i].x; acc.y += w[i] * x[i].y; acc.z += w[i] * x[i].z; acc.w += w[i] * x[i].w;
+        }
+    }
+    sums[warp][lane] = acc;
+    __syncthreads();
+    if (warp == 0 && col_ok) {
+#pragma unroll
+        for (int i = 1; i < kW; ++i) {
+            const float4 x = sums[i][lane];
+            acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+        }
+        const size_t row = (size_t)me.q_row * Hq + (size_t)me.kv_head * G + ph;
+        *reinterpret_cast<uint2 *>(out + row * D + lane * 4) = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+        if (lane == 0 && lse_out) lse_out[row] = total;
+    }
 }
 
 template <int D, bool kWin>
@@ -502,12 +545,19 @@ cudaError_t launch_t(const ap_kv_pool *pool, const ap_plan *plan, const void *q,
         configured[dev] = true;
     }
     const float scale_log2 = plan->scale * 1.4426950408889634f;
-    return launch_overlapped(kv4_decode_kernel<D, kWin>, (unsigned)plan->info.decode_ctas, (unsigned)kThreads,
-                             (size_t)Cfg::kSmemBytes, stream, (const uint8_t *)pool->desc.k_base,
-                             (const uint8_t *)pool->desc.v_base, (const __nv_bfloat16 *)q, plan->d_items, plan->d_cta_begin,
-                             plan->d_bt_flat, plan->d_merge, o_part, lse_part, (__nv_bfloat16 *)out, lse, plan->num_q_heads,
-                             pool->desc.num_kv_heads, plan->group, plan->head_block, pool->desc.num_pages, scale_log2,
-                             pool->status_dev, pool->d_counters, plan->window, plan->sinks);
+    const int lists = (int)plan->info.decode_ctas, per_block = kWarps / plan->head_block;
+    cudaError_t e = launch_overlapped(
+        kv4_decode_kernel<D, kWin>, (unsigned)((lists + per_block - 1) / per_block), (unsigned)kThreads, (size_t)Cfg::kSmemBytes,
+        stream, (const uint8_t *)pool->desc.k_base, (const uint8_t *)pool->desc.v_base, (const __nv_bfloat16 *)q, plan->d_items,
+        plan->d_cta_begin, plan->d_bt_flat, o_part, lse_part, (__nv_bfloat16 *)out, lse, plan->num_q_heads,
+        pool->desc.num_kv_heads, plan->group, plan->head_block, lists, pool->desc.num_pages, scale_log2, pool->status_dev,
+        plan->window, plan->sinks);
+    const int part_heads = plan->head_block * plan->group;
+    if (e == cudaSuccess && plan->info.merge_entries > 0)
+        e = launch_overlapped(kv4_merge_kernel<D>, (unsigned)(plan->info.merge_entries * part_heads), (unsigned)kMergeThreads, 0,
+                              stream, plan->d_merge, (const float *)o_part, (const float *)lse_part, (__nv_bfloat16 *)out, lse,
+                              plan->num_q_heads, part_heads, plan->group);
+    return e;
 }
 
 }  // namespace
