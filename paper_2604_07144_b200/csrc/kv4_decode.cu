@@ -130,7 +130,10 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
     constexpr int kRowChunks = T::kRowBytes / 16;
     extern __shared__ __align__(128) uint8_t smem[];
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // what is the same in all lanes passes through a broadcast, so that the compiler can keep it on the uniform
+    // datapath (addresses, loop counters, branches) instead of the ALU
+    auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
     const int list = blockIdx.x * (kWarps / HB) + warp / HB, my_head = warp % HB;
     if (list >= n_lists) {
@@ -138,11 +141,11 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
         griddep_wait();
         return;
     }
-    const int item_begin = __ldg(cta_begin + list), n_items = __ldg(cta_begin + list + 1) - item_begin;
+    const int item_begin = uniform(__ldg(cta_begin + list)), n_items = uniform(__ldg(cta_begin + list + 1)) - item_begin;
     auto get_item = [&](int n) {
         const int4 *src = reinterpret_cast<const int4 *>(items + item_begin + n);
         const int4 x = __ldg(src), y = __ldg(src + 1);
-        return DecodeItem{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        return DecodeItem{uniform(x.x), uniform(x.y), uniform(x.z), uniform(x.w), uniform(y.x), uniform(y.y), uniform(y.z), uniform(y.w)};
     };
 
     // ---- the warp's stream of page pairs: a cursor that runs ahead of the consumer, across items; block-table
@@ -177,7 +180,7 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
     // a lane's share of a tile's copy: code chunks lane (and lane + 32, four lines on), and, for the first
     // lanes, a chunk of K's or V's steps
     const uint32_t c_dst = 16 * ring_chunk<D>(lane);
-    const uint8_t *const k_src = k_pool + 16 * lane, *const v_src = v_pool + 16 * lane;
+    const uint32_t c_src = 16 * lane;
     const bool step_lane = lane < 2 * kStepChunks, k_steps = lane < kStepChunks;
     const uint32_t s_dst = (k_steps ? 0 : T::kBytes) + 16 * (kCodeChunks + lane % kStepChunks);
     const uint8_t *const s_src = (k_steps ? k_pool : v_pool) + 16 * (kCodeChunks + lane % kStepChunks);
@@ -190,7 +193,7 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
             page = 0;
         }
         const int64_t tile = (int64_t)((uint64_t)((uint32_t)page * (uint32_t)Hkv + (uint32_t)next_head) * (uint32_t)T::kBytes);
-        const uint8_t *k = k_src + tile, *v = v_src + tile;
+        const uint8_t *k = k_pool + tile + c_src, *v = v_pool + tile + c_src;
         cp_async16(d + c_dst, k);
         cp_async16(d + c_dst + T::kBytes, v);
         if constexpr (kCodeChunks > 32) {
@@ -202,8 +205,8 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
     auto issue = [&](int slot) {
         const uint32_t dst = ring + (uint32_t)(slot * Cfg::kSlotBytes);
         if (next_n > 0) {
-            issue_page(dst, next_page0);
-            if (next_n > 1) issue_page(dst + Cfg::kPageBytes, next_page1);
+            issue_page(dst, uniform(next_page0));
+            if (next_n > 1) issue_page(dst + Cfg::kPageBytes, uniform(next_page1));
             fetch();
         }
         cp_async_commit();       // (an empty group past the last pair keeps the count of groups in step)
@@ -279,7 +282,7 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
             f_col[0] = __shfl_sync(0xffffffffu, f, 8 * t);
             f_col[1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
         }
-        // running maximum (of scores times f_col: exponents of 2), sum and O
+        // running maximum of the scores (f_col makes exponents of 2 of them), sum and O
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         float o[4 * NW][4];
 #pragma unroll
@@ -328,7 +331,6 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
                         s[u][0] = fmaf(acc[0], s0, s[u][0]); s[u][1] = fmaf(acc[1], s0, s[u][1]);
                         s[u][2] = fmaf(acc[2], s1, s[u][2]); s[u][3] = fmaf(acc[3], s1, s[u][3]);
                     }
-                    s[u][0] *= f_col[0]; s[u][1] *= f_col[1]; s[u][2] *= f_col[0]; s[u][3] *= f_col[1];
                 }
             }
             // ---- V words and steps, tokens 2t, 2t + 1, 2t + 8, 2t + 9; the first page's ahead of the softmax
@@ -376,7 +378,7 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
             }
             if (__any_sync(0xffffffffu, mx0 > m0 || mx1 > m1)) {
                 const float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);
-                const float al0 = exp2_approx(m0 - mn0), al1 = exp2_approx(m1 - mn1);
+                const float al0 = exp2_approx((m0 - mn0) * f_col[0]), al1 = exp2_approx((m1 - mn1) * f_col[1]);
                 l0 *= al0;
                 l1 *= al1;
                 m0 = mn0;
@@ -386,11 +388,12 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
                     o[i][0] *= al0; o[i][1] *= al1; o[i][2] *= al0; o[i][3] *= al1;
                 }
             }
+            const float mf0 = m0 * f_col[0], mf1 = m1 * f_col[1];
             uint32_t b0[2], b1[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const float p0 = exp2_approx(s[u][0] - m0), p1 = exp2_approx(s[u][1] - m1);
-                const float p2 = exp2_approx(s[u][2] - m0), p3 = exp2_approx(s[u][3] - m1);
+                const float p0 = exp2_approx(s[u][0] * f_col[0] - mf0), p1 = exp2_approx(s[u][1] * f_col[1] - mf1);
+                const float p2 = exp2_approx(s[u][2] * f_col[0] - mf0), p3 = exp2_approx(s[u][3] * f_col[1] - mf1);
                 l0 += p0 + p2;
                 l1 += p1 + p3;
                 b0[u] = decode::movmatrix_trans(pack_bf16x2(p0, p1));
@@ -445,7 +448,7 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
             const int h = 2 * t + c;
             if (h >= G) continue;
             const float l = c ? l1 : l0, inv = 1.f / l;
-            const float lse = ((c ? m1 : m0) + log2f(l)) * 0.6931471805599453f;
+            const float lse = ((c ? m1 * f_col[1] : m0 * f_col[0]) + log2f(l)) * 0.6931471805599453f;
             const size_t row = item.part_slot < 0 ? (size_t)item.q_row * Hq + (size_t)kv_head * G + h
                                                   : (size_t)item.part_slot * (HB * G) + my_head * G + h;
 #pragma unroll
