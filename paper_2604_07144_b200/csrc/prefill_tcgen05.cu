@@ -38,7 +38,7 @@ cudaError_t launch_prefill_t(const ap_kv_pool *pool, const ap_plan *plan, const 
         prefill_tcgen05_kernel<D, kWin>, (unsigned)plan->info.prefill_tiles, (unsigned)kPrefillThreads,
         (size_t)Cfg::kSmemBytes, stream, q_map, k_map, v_map, plan->d_tiles, plan->d_bt_flat,
         (__nv_bfloat16 *)out, lse, plan->num_q_heads, pool->desc.num_kv_heads, num_pages, scale_log2,
-        pool->status_dev, pool->wait_limit_ns, plan->window, plan->sinks);
+        pool->status_dev, pool->wait_limit_ns, plan->window > 0 ? plan->window : 1 << 30, plan->sinks);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -46,7 +46,9 @@ cudaError_t launch_prefill_t(const ap_kv_pool *pool, const ap_plan *plan, const 
 
 cudaError_t launch_prefill(const ap_kv_pool *pool, const ap_plan *plan, const void *q, void *out, float *lse,
                            const CUtensorMap &k_map, const CUtensorMap &v_map, int num_pages, cudaStream_t stream) {
-    if (plan->window > 0) {
+    // A plan without a window keeps a kernel without the window's tests.  (On a 4-bit pool it takes the windowed one, with
+    // a window that no context fills, for its finer exponential.)
+    if (plan->window > 0 || pool->four_bit) {
         if (pool->desc.head_dim == 128) return launch_prefill_t<128, true>(pool, plan, q, out, lse, k_map, v_map, num_pages, stream);
         return launch_prefill_t<64, true>(pool, plan, q, out, lse, k_map, v_map, num_pages, stream);
     }

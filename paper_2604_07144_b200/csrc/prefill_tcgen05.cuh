@@ -80,10 +80,18 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
+// the lowest n bits (none for n <= 0, all for n >= 32)
+__device__ __forceinline__ uint32_t low_bits(int n) {
+    return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
+}
+
 // 2^x for two values on the FMA pipe (relieves the special-function unit, which would otherwise
 // bound the softmax): x = n + f with n = round(x), f in [-0.5, 0.5]; 2^f by a cubic fitted for
 // relative error (7.7e-5, well inside the bf16 rounding P gets anyway); 2^n by adding n to the
 // exponent field.  x is clamped at -125 so the exponent cannot wrap (2^-125 is zero for our purposes).
+// kFine: a quartic instead (2.7e-6), one more packed FMA; short windows average the cubic's error over few keys, and
+// it would show in lse.
+template <bool kFine>
 __device__ __forceinline__ float2 exp2_poly2(float2 x) {
     const float kMagic = 12582912.f;                       // 1.5 * 2^23: x + kMagic holds round(x) in its low bits
     x.x = fmaxf(x.x, -125.f);
@@ -91,9 +99,17 @@ __device__ __forceinline__ float2 exp2_poly2(float2 x) {
     const float2 t = __fadd2_rn(x, make_float2(kMagic, kMagic));
     const float2 n = __fadd2_rn(t, make_float2(-kMagic, -kMagic));
     const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
-    float2 p = __ffma2_rn(f, make_float2(0.05508868f, 0.05508868f), make_float2(0.24260405f, 0.24260405f));
-    p = __ffma2_rn(p, f, make_float2(0.69327624f, 0.69327624f));
-    p = __ffma2_rn(p, f, make_float2(0.99992894f, 0.99992894f));
+    float2 p;
+    if constexpr (kFine) {
+        p = __ffma2_rn(f, make_float2(0.00957011f, 0.00957011f), make_float2(0.0559179f, 0.0559179f));
+        p = __ffma2_rn(p, f, make_float2(0.24024744f, 0.24024744f));
+        p = __ffma2_rn(p, f, make_float2(0.6931218f, 0.6931218f));
+        p = __ffma2_rn(p, f, make_float2(0.9999993f, 0.9999993f));
+    } else {
+        p = __ffma2_rn(f, make_float2(0.05508868f, 0.05508868f), make_float2(0.24260405f, 0.24260405f));
+        p = __ffma2_rn(p, f, make_float2(0.69327624f, 0.69327624f));
+        p = __ffma2_rn(p, f, make_float2(0.99992894f, 0.99992894f));
+    }
     p.x = __int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23));
     p.y = __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23));
     return p;
@@ -350,17 +366,18 @@ __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUt
                 if (kWin && (tok0 + kTileN - 1 > tile.pos0 ||
                              (tok0 <= tile.pos0 + kTileM - 1 - window && tok0 + kTileN > sinks))) {
                     // some row's window begins or ends in this step
-                    const int lo = my_pos - window;                     // keys up to lo are hidden unless sinks
+                    // (one bit per key; the tests by bit cost two instructions a score, comparisons of positions five)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < 4; ++c) {
+                        const int k0 = tok0 + c * 32;
+                        const uint32_t seen = low_bits(my_pos + 1 - k0) & (~low_bits(my_pos - window + 1 - k0) | low_bits(sinks - k0));
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const int key = tok0 + c * 32 + i;
-                            float v = __uint_as_float(sreg[c][i]);
-                            if (key > my_pos || (key <= lo && key >= sinks)) v = -INFINITY;
-                            sreg[c][i] = __float_as_uint(v);
-                            mx = fmaxf(mx, v);
-                        }
+                        for (int i = 0; i < 32; ++i)
+                            if (!(seen >> i & 1u)) sreg[c][i] = 0xFF800000u;            // -inf
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2)
+                            mx = max3(mx, __uint_as_float(sreg[c][i]), __uint_as_float(sreg[c][i + 1]));
+                    }
                 } else if (!kWin && tok0 + kTileN - 1 > tile.pos0) {
                     // diagonal or last step: keys past the row's position (or past the context) are masked
 #pragma unroll
@@ -411,7 +428,7 @@ __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUt
                                                sc2, nms2);
                         // one pair in eight goes to the FMA pipe instead of the special-function unit
                         if ((i & 7) == 7) {
-                            xy = exp2_poly2(xy);
+                            xy = exp2_poly2<kWin>(xy);
                         } else {
                             xy.x = exp2_approx(xy.x);
                             xy.y = exp2_approx(xy.y);

@@ -173,7 +173,9 @@ def test_windowed_mixed_iterations(shape, mode, single):
 
 @pytest.mark.gpu
 def test_a_window_that_covers_the_context_gives_the_plain_result():
-    """Same pages, same order of summation: bit for bit what the plan without a window gives."""
+    """Decode rows: same pages, same arithmetic, same order of summation, so bit for bit what the plan without a window
+    gives.  Prefill rows use a finer polynomial for one weight in eight (2.7e-6 of it instead of 7.7e-5), so their bits
+    may differ; both are held against the 64-bit result."""
     b = _batch((32, 8, 128), 14, [1, 1, 1, 70], [40, 3000, 129, 500])
     got = []
     for make in (None, lambda pool: ap.plan_create_windowed(pool, b.q_lens, b.ctx_lens, b.block_tables, 32, BIG, 7)):
@@ -181,5 +183,9 @@ def test_a_window_that_covers_the_context_gives_the_plain_result():
         ap.kv_append(dev.pool, dev.plan, dev.k_new, dev.v_new)
         dev.attend()
         got.append(dev.results())
+        k, v = (W.bf16_bits_to_f64(R.to_bits(p)) for p in (dev.k_pool, dev.v_pool))
         dev.close()
-    assert np.array_equal(got[0][0], got[1][0]) and np.array_equal(got[0][1], got[1][1])
+    ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b)
+    for out, lse in got:
+        R.check(out, lse, ref)
+    assert np.array_equal(got[0][0][:3], got[1][0][:3]) and np.array_equal(got[0][1][:3], got[1][1][:3])
