@@ -177,16 +177,26 @@ def _ptr(x) -> Optional[int]:
     raise TypeError(f"cannot take the address of {type(x)}")
 
 
-def _stream(stream) -> Optional[int]:
-    """CUDA stream handle: a torch stream, an integer, or None for torch's current stream."""
+_torch = None
+
+
+def _stream(stream, device: Optional[int] = None) -> Optional[int]:
+    """CUDA stream handle: a torch stream, an integer, or None for torch's current stream on ``device`` (a pool's
+    device; the current device where it is not given)."""
+    global _torch
     if stream is None:
-        try:
-            import torch
-            if torch.cuda.is_available():
-                return int(torch.cuda.current_stream().cuda_stream) or None
-        except ImportError:
-            pass
-        return None
+        if _torch is None:
+            try:
+                import torch
+                _torch = torch
+            except ImportError:
+                return None
+        if not _torch.cuda.is_initialized():
+            return None                      # nobody can have chosen a stream yet
+        if device is None or device < 0:
+            device = _torch.cuda.current_device()
+        # torch.cuda.current_stream(device).cuda_stream takes 3 us, as long as a launch
+        return int(_torch._C._cuda_getCurrentRawStream(device)) or None
     if hasattr(stream, "cuda_stream"):
         return int(stream.cuda_stream) or None
     return int(stream) or None
@@ -314,7 +324,7 @@ def plan_create(pool: KVPool, q_lens, ctx_lens, block_tables, num_q_heads: int,
                 softmax_scale: float = 0.0, stream=None) -> Plan:
     desc, keep = _batch_desc(q_lens, ctx_lens, block_tables, num_q_heads, softmax_scale)
     h = ctypes.c_void_p()
-    _check(load().ap_plan_create(ctypes.byref(h), pool.handle, ctypes.byref(desc), _stream(stream)),
+    _check(load().ap_plan_create(ctypes.byref(h), pool.handle, ctypes.byref(desc), _stream(stream, pool.device)),
            "ap_plan_create")
     del keep
     return Plan(h.value, pool)
@@ -328,7 +338,7 @@ def plan_create_windowed(pool: KVPool, q_lens, ctx_lens, block_tables, num_q_hea
     win = WindowDesc(int(window), int(sinks))
     h = ctypes.c_void_p()
     _check(load().ap_plan_create_windowed(ctypes.byref(h), pool.handle, ctypes.byref(desc), ctypes.byref(win),
-                                          _stream(stream)), "ap_plan_create_windowed")
+                                          _stream(stream, pool.device)), "ap_plan_create_windowed")
     del keep
     return Plan(h.value, pool)
 
@@ -382,18 +392,18 @@ def plan_export(plan: Plan) -> dict:
 # ---------------------------------------------------------------- kernels --
 
 def kv_append(pool: KVPool, plan: Plan, k_new, v_new, stream=None) -> None:
-    _check(load().ap_kv_append(pool.handle, plan.handle, _ptr(k_new), _ptr(v_new), _stream(stream)),
+    _check(load().ap_kv_append(pool.handle, plan.handle, _ptr(k_new), _ptr(v_new), _stream(stream, pool.device)),
            "ap_kv_append")
 
 
 def _row_stride(x) -> int:
     """Elements from one row of a [rows, heads, head_dim] tensor to the next (0: contiguous, or not a tensor)."""
-    if x is None or not hasattr(x, "stride") or x.dim() != 3 or x.shape[0] < 2:
+    if x is None or not hasattr(x, "stride") or x.is_contiguous():
         return 0
-    rows, heads, dim = x.stride()
-    if dim != 1 or (x.shape[1] > 1 and heads != x.shape[2]):
-        raise ValueError("a token's heads must be contiguous")
-    return int(rows)
+    stride, shape = x.stride(), x.shape
+    if len(shape) != 3 or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2]):
+        raise ValueError("expected [rows, heads, head_dim] with a token's heads contiguous")
+    return int(stride[0]) if shape[0] > 1 else 0
 
 
 def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, rotary_dim: Optional[int] = None,
@@ -410,12 +420,12 @@ def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, r
     desc = RopeDesc(rotary, int(bool(interleaved)), float(base), _ptr(freq), float(amplitude), _row_stride(q),
                     _row_stride(k_new), _row_stride(v_new))
     _check(load().ap_kv_append_rope(pool.handle, plan.handle, ctypes.byref(desc), _ptr(q), _ptr(k_new), _ptr(v_new),
-                                    _ptr(q_rot), _stream(stream)), "ap_kv_append_rope")
+                                    _ptr(q_rot), _stream(stream, pool.device)), "ap_kv_append_rope")
 
 
 def kv_read_new(pool: KVPool, plan: Plan, k, v, stream=None) -> None:
     """The rows of the plan's new tokens, read back as the bf16 numbers the pool holds (or, in 4 bits, stands for)."""
-    _check(load().ap_kv_read_new(pool.handle, plan.handle, _ptr(k), _ptr(v), _stream(stream)), "ap_kv_read_new")
+    _check(load().ap_kv_read_new(pool.handle, plan.handle, _ptr(k), _ptr(v), _stream(stream, pool.device)), "ap_kv_read_new")
 
 
 def kv_copy_pages(dst_pool: KVPool, src_pool: KVPool, dst_ids: Sequence[int], src_ids: Sequence[int], stream=None) -> None:
@@ -425,7 +435,7 @@ def kv_copy_pages(dst_pool: KVPool, src_pool: KVPool, dst_ids: Sequence[int], sr
     if dst.shape != src.shape or dst.ndim != 1:
         raise ValueError("dst_ids and src_ids must be 1-D and of the same length")
     _check(load().ap_kv_copy_pages(dst_pool.handle, src_pool.handle, int(dst.size), dst.ctypes.data, src.ctypes.data,
-                                   _stream(stream) if dst_pool.desc.device >= 0 else None), "ap_kv_copy_pages")
+                                   _stream(stream, dst_pool.device) if dst_pool.desc.device >= 0 else None), "ap_kv_copy_pages")
 
 
 def attention_iteration(pool: KVPool, plan: Plan, q, out, lse=None, workspace=None,
@@ -435,7 +445,7 @@ def attention_iteration(pool: KVPool, plan: Plan, q, out, lse=None, workspace=No
         if workspace is not None and hasattr(workspace, "numel"):
             workspace_bytes = int(workspace.numel() * workspace.element_size())
     _check(load().ap_attention_iteration(pool.handle, plan.handle, _ptr(q), _ptr(out), _ptr(lse),
-                                         _ptr(workspace), workspace_bytes, _stream(stream)),
+                                         _ptr(workspace), workspace_bytes, _stream(stream, pool.device)),
            "ap_attention_iteration")
 
 
@@ -452,7 +462,7 @@ def attention_iteration_static(pool: KVPool, plan: Plan, q, out, lse=None, strea
     more raise ``ApError`` (``AP_ERR_WORKSPACE_TOO_SMALL``).  Calls share that
     array, so two of them must not overlap on the GPU."""
     _check(load().ap_attention_iteration_static(pool.handle, plan.handle, _ptr(q), _ptr(out), _ptr(lse),
-                                                _stream(stream)), "ap_attention_iteration_static")
+                                                _stream(stream, pool.device)), "ap_attention_iteration_static")
 
 
 def serving_iteration_host(pool: KVPool, q_lens, ctx_lens, block_tables, num_q_heads: int, q_host,
@@ -461,12 +471,12 @@ def serving_iteration_host(pool: KVPool, q_lens, ctx_lens, block_tables, num_q_h
     desc, keep = _batch_desc(q_lens, ctx_lens, block_tables, num_q_heads, softmax_scale)
     _check(load().ap_serving_iteration_host(pool.handle, ctypes.byref(desc), _ptr(q_host), _ptr(k_new_host),
                                             _ptr(v_new_host), _ptr(out_host), _ptr(lse_host),
-                                            _stream(stream)), "ap_serving_iteration_host")
+                                            _stream(stream, pool.device)), "ap_serving_iteration_host")
     del keep
 
 
 def last_device_status(pool: KVPool, stream=None) -> int:
-    return int(load().ap_last_device_status(pool.handle, _stream(stream)))
+    return int(load().ap_last_device_status(pool.handle, _stream(stream, pool.device)))
 
 
 def kv_pool_set_wait_limit(pool: KVPool, limit_ns: int) -> None:
@@ -476,7 +486,7 @@ def kv_pool_set_wait_limit(pool: KVPool, limit_ns: int) -> None:
 
 def selftest_wait_timeout(pool: KVPool, limit_ns: int, leave_counter: bool = False, stream=None) -> None:
     """Queues the one-warp kernel whose bounded wait always runs out (see ap_selftest_wait_timeout)."""
-    _check(load().ap_selftest_wait_timeout(pool.handle, int(limit_ns), int(bool(leave_counter)), _stream(stream)),
+    _check(load().ap_selftest_wait_timeout(pool.handle, int(limit_ns), int(bool(leave_counter)), _stream(stream, pool.device)),
            "ap_selftest_wait_timeout")
 
 
@@ -489,5 +499,5 @@ def profile_enable(pool: KVPool, on: bool = True) -> None:
 def profile_collect(pool: KVPool, stream=None) -> dict:
     """{kernel name: (total ms, launches)} since the last enable/collect."""
     kt = KernelTimes()
-    _check(load().ap_profile_collect(pool.handle, _stream(stream), ctypes.byref(kt)), "ap_profile_collect")
+    _check(load().ap_profile_collect(pool.handle, _stream(stream, pool.device), ctypes.byref(kt)), "ap_profile_collect")
     return {name: (float(kt.ms[i]), int(kt.launches[i])) for i, name in enumerate(KERNEL_NAMES)}

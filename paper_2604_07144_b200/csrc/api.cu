@@ -18,6 +18,11 @@ struct DeviceGuard {
     bool ok = false;
     explicit DeviceGuard(int dev) {
         if (cudaGetDevice(&prev) != cudaSuccess) { prev = -1; (void)cudaGetLastError(); }
+        if (prev == dev) {                 // (already there: nothing to set, nothing to put back)
+            ok = true;
+            prev = -1;
+            return;
+        }
         ok = cudaSetDevice(dev) == cudaSuccess;
         if (!ok) (void)cudaGetLastError();
     }

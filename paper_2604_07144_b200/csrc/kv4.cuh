@@ -23,6 +23,7 @@ namespace ap {
 namespace kv4 {
 
 constexpr int kGroup = 32;
+constexpr float kSmallStep = 7.8886090522101181e-31f;      // 2^-100
 
 template <int D>
 struct Tile {
@@ -64,11 +65,26 @@ __device__ __forceinline__ uint32_t quantise8(const uint4 x, float &step) {
     amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
     step = group_step(amax);
     uint32_t w = 0;
+    if (step >= kSmallStep) {
+        // rint(x / s) by a product with 1 / s.  x / s = 2^n X / S with X below 2^8 and S from 16 to 31, so a quotient
+        // between 1/4 and 7 either is a half-integer or lies at least 2^-11 away from one, while the product is
+        // off by less than 2^-20: moved to the nearest multiple of 2^-13 (by adding and subtracting 1.5 2^10, whose last
+        // bit is worth that) it is on the same side of every half-integer as the quotient, and on it if the
+        // quotient is.  Adding 1.5 2^23 + 8 then rounds to an integer, ties to even, and leaves c in the low bits.
+        const float inv = __frcp_rn(step);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        int c = 8;
-        if (step > 0.f) c = min(max(__float2int_rn(__fdiv_rn(f[i], step)) + 8, 1), 15);
-        w |= (uint32_t)c << (4 * i);
+        for (int i = 0; i < 8; ++i) {
+            const float y = __fsub_rn(__fadd_rn(__fmul_rn(f[i], inv), 1536.f), 1536.f);
+            w |= (__float_as_uint(__fadd_rn(y, 12582920.f)) & 15u) << (4 * i);
+        }
+    } else {
+        // (1 / s would overflow; a step of zero or NaN: every code is 8)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            int c = 8;
+            if (step > 0.f) c = min(max(__float2int_rn(__fdiv_rn(f[i], step)) + 8, 1), 15);
+            w |= (uint32_t)c << (4 * i);
+        }
     }
     return w;
 }

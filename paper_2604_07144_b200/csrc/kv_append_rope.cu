@@ -7,6 +7,8 @@
 // The angle of a far position needs more than 32 bits: p f_i / 2 pi is formed in 64 bits, whole turns are
 // taken off there, and only the fraction goes to fp32 sine and cosine.  Those are computed once per token
 // and shared by its heads through shared memory.  The rotation is fp32 and rounds once, to bf16.
+#include <algorithm>
+
 #include "internal.h"
 #include "kv4.cuh"
 #include "ptx.cuh"
@@ -16,12 +18,14 @@ namespace ap {
 namespace {
 
 constexpr int kPassHeads = 32;      // kv heads whose rotated K waits in shared memory for quantisation
+constexpr int kAhead = 2;           // units of a thread loaded before the angles are ready
+constexpr int kMaxThreads = 256;
 
 // One block per token.  A thread's unit is 16 elements of one head row, two 16-byte chunks that turn
 // together: for half-split pairs chunk u with chunk u + R/16, for neighbouring pairs chunks 2u and 2u + 1;
 // either way they need the angles 8u .. 8u + 7.  Chunks past R are copied, two at a time.
 template <int D, bool kFour>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kMaxThreads)
 rope_append_kernel(const __grid_constant__ RopeParams rope, uint8_t *__restrict__ k_pool, uint8_t *__restrict__ v_pool,
                    const uint4 *q, const uint4 *__restrict__ k_new, const uint4 *__restrict__ v_new, uint4 *q_rot,
                    int64_t q_stride, int64_t k_stride, int64_t v_stride, const int32_t *__restrict__ append_dst,
@@ -32,21 +36,7 @@ rope_append_kernel(const __grid_constant__ RopeParams rope, uint8_t *__restrict_
     __shared__ uint4 k_rows[kFour ? kPassHeads * kChunks : 1];
     const int64_t row = blockIdx.x;
     const int32_t dst = __ldg(append_dst + row), pos = __ldg(positions + row);
-    for (int i = threadIdx.x; i < 8 * rope.units; i += blockDim.x) {
-        double turns = (double)pos * rope.turn[i];
-        turns -= rint(turns);
-        float s, c;
-        sincospif((float)(2.0 * turns), &s, &c);
-        trig[i] = make_float2(c * rope.amplitude, s * rope.amplitude);
-    }
-    ptx::griddep_launch_dependents();
-    ptx::griddep_wait();
-    __syncthreads();
     const int32_t page = dst >> 4, slot = dst & 15;
-    if (page < 0 || page >= num_pages) {
-        if (threadIdx.x == 0) ptx::record_status(status, AP_ERR_BAD_BLOCK_TABLE);
-        return;
-    }
     auto first_chunk = [&](int u) { return u >= rope.units ? 2 * u : rope.interleaved ? 2 * u : u; };
     auto second_chunk = [&](int u) { return u >= rope.units || rope.interleaved ? 2 * u + 1 : u + rope.units; };
     auto rotate = [&](int u, uint4 &x, uint4 &y) {
@@ -73,26 +63,70 @@ rope_append_kernel(const __grid_constant__ RopeParams rope, uint8_t *__restrict_
         x = make_uint4(a[0], a[1], a[2], a[3]);
         y = make_uint4(a[4], a[5], a[6], a[7]);
     };
-    // q rows, then (bf16 pool) K rows and V rows
+    // q rows, then (bf16 pool) K rows and V rows: where unit `id` reads and writes
     const int n = (Hq + (kFour ? 0 : 2 * Hkv)) * kUnits;
-    for (int id = threadIdx.x; id < n; id += blockDim.x) {
-        const int u = id % kUnits, h = id / kUnits;
-        const uint4 *src;
-        uint4 *out;
+    struct Unit { const uint4 *src; uint4 *out; int c0, c1, u; bool turns; };
+    auto unit_of = [&](int id) {
+        Unit w;
+        w.u = id % kUnits;
+        const int h = id / kUnits;
         if (h < Hq) {
-            src = q + row * q_stride + h * kChunks;
-            out = q_rot + (row * Hq + h) * kChunks;
+            w.src = q + row * q_stride + h * kChunks;
+            w.out = q_rot + (row * Hq + h) * kChunks;
         } else {
             const bool is_v = h >= Hq + Hkv;
             const int g = h - Hq - (is_v ? Hkv : 0);
-            src = (is_v ? v_new + row * v_stride : k_new + row * k_stride) + g * kChunks;
-            out = reinterpret_cast<uint4 *>(is_v ? v_pool : k_pool) + (((int64_t)page * Hkv + g) * kPageSize + slot) * kChunks;
+            w.src = (is_v ? v_new + row * v_stride : k_new + row * k_stride) + g * kChunks;
+            w.out = reinterpret_cast<uint4 *>(is_v ? v_pool : k_pool) + (((int64_t)page * Hkv + g) * kPageSize + slot) * kChunks;
         }
-        const int c0 = first_chunk(u), c1 = second_chunk(u);
-        uint4 x = src[c0], y = src[c1];
-        if (kFour || h < Hq + Hkv) rotate(u, x, y);
-        out[c0] = x;
-        out[c1] = y;
+        w.c0 = first_chunk(w.u);
+        w.c1 = second_chunk(w.u);
+        w.turns = kFour || h < Hq + Hkv;
+        return w;
+    };
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
+    if (page < 0 || page >= num_pages) {                     // (the whole block)
+        if (threadIdx.x == 0) ptx::record_status(status, AP_ERR_BAD_BLOCK_TABLE);
+        return;
+    }
+    // A thread's first kAhead units are loaded ahead of the angles, whose 64-bit arithmetic and barrier then run
+    // while the loads are in flight.
+    const int step = blockDim.x;
+    uint4 x[kAhead], y[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        const int id = threadIdx.x + i * step;
+        if (id < n) {
+            const Unit w = unit_of(id);
+            x[i] = w.src[w.c0];
+            y[i] = w.src[w.c1];
+        }
+    }
+    for (int i = threadIdx.x; i < 8 * rope.units; i += step) {
+        double turns = (double)pos * rope.turn[i];
+        turns -= rint(turns);
+        float s, c;
+        sincospif((float)(2.0 * turns), &s, &c);
+        trig[i] = make_float2(c * rope.amplitude, s * rope.amplitude);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        const int id = threadIdx.x + i * step;
+        if (id < n) {
+            const Unit w = unit_of(id);
+            if (w.turns) rotate(w.u, x[i], y[i]);
+            w.out[w.c0] = x[i];
+            w.out[w.c1] = y[i];
+        }
+    }
+    for (int id = threadIdx.x + kAhead * step; id < n; id += step) {
+        const Unit w = unit_of(id);
+        uint4 a = w.src[w.c0], b = w.src[w.c1];
+        if (w.turns) rotate(w.u, a, b);
+        w.out[w.c0] = a;
+        w.out[w.c1] = b;
     }
     if constexpr (kFour) {
         // K: rotated and rounded to bf16 in shared memory, then quantised from there, 32 heads at a time; V: quantised
@@ -136,8 +170,12 @@ template <int D, bool kFour>
 cudaError_t launch_t(const ap_kv_pool *pool, const ap_plan *plan, const RopeParams &rope, const void *q, const void *k_new,
                      const void *v_new, void *q_rot, int64_t q_stride, int64_t k_stride, int64_t v_stride, cudaStream_t stream) {
     const int Hkv = pool->desc.num_kv_heads, Hq = q ? plan->num_q_heads : 0;
+    // Few rows: a thread per unit, as wide as it goes, for latency.  Many: as many passes as needed with every thread
+    // busy in each, so that blocks are small and several share an SM.
     const int units = (Hq + 2 * Hkv) * (D / 16);
-    const unsigned threads = (unsigned)(units >= 256 ? 256 : (units + 31) / 32 * 32);
+    const int passes = plan->info.n_new <= 2 * pool->sm_count ? (units + kMaxThreads - 1) / kMaxThreads
+                                                              : std::max(kAhead, (units + kMaxThreads - 1) / kMaxThreads);
+    const unsigned threads = (unsigned)(((units + passes - 1) / passes + 31) / 32 * 32);
     return launch_overlapped(rope_append_kernel<D, kFour>, (unsigned)plan->info.n_new, threads, 0, stream, rope,
                              (uint8_t *)pool->desc.k_base, (uint8_t *)pool->desc.v_base, (const uint4 *)q, (const uint4 *)k_new,
                              (const uint4 *)v_new, (uint4 *)q_rot, q_stride / 8, k_stride / 8, v_stride / 8, plan->d_append_dst,

@@ -36,6 +36,28 @@ def test_reference_format_round_trip_and_error_bound():
         assert (np.ceil(np.abs(W.bf16_bits_to_f64(x)).reshape(40, 2, -1, 32).max(-1) / 7 / (s[..., ::32] * 17 / 16)) <= 1).all()
 
 
+def test_quotients_by_product_round_like_division():
+    """The append forms rint(x / s) as rint of x (1 / s) moved to a multiple of 2^-13.  Every 8-bit x, every 5-bit s and
+    every scale between them, in fp32 as the kernel does it, against exact fractions."""
+    from fractions import Fraction
+    f = np.float32
+    for S in range(16, 32):
+        inv = f(1) / f(S)
+        for n in range(-12, 4):
+            X = np.arange(128, 256)
+            x = (X * 2.0 ** n).astype(f)
+            x = x[x <= 7 * S]
+            y = (x * inv + f(1536)) - f(1536)
+            got = (y + f(12582912)) - f(12582912)
+            want = [round(Fraction(float(v)) / S) for v in x]             # Python rounds ties to even
+            assert got.tolist() == want
+            neg = ((-x * inv + f(1536)) - f(1536) + f(12582912)) - f(12582912)
+            assert (-neg).tolist() == want
+            # the kernel's last addition carries the 8 along: ties still go to even, and the low bits are the code
+            code = (y + f(12582920)).view(np.uint32) & 15
+            assert code.tolist() == [(w + 8) & 15 for w in want]
+
+
 def test_4bit_pool_descriptions_and_refusals():
     assert ap.kv_pool_bytes_4bit(10, 8, 128) == 10 * 8 * 1152 and ap.kv_pool_bytes_4bit(10, 2, 64) == 10 * 2 * 576
     assert ap.kv_pool_bytes_4bit(0, 8, 128) == 0 and ap.kv_pool_bytes_4bit(4, 2, 96) == 0
