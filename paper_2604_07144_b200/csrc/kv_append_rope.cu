@@ -84,15 +84,21 @@ rope_append_kernel(const __grid_constant__ RopeParams rope, uint8_t *__restrict_
         w.turns = kFour || h < Hq + Hkv;
         return w;
     };
+    const int step = blockDim.x;
+    for (int i = threadIdx.x; i < 8 * rope.units; i += step) {
+        double turns = (double)pos * rope.turn[i];
+        turns -= rint(turns);
+        float s, c;
+        sincospif((float)(2.0 * turns), &s, &c);
+        trig[i] = make_float2(c * rope.amplitude, s * rope.amplitude);
+    }
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     if (page < 0 || page >= num_pages) {                     // (the whole block)
         if (threadIdx.x == 0) ptx::record_status(status, AP_ERR_BAD_BLOCK_TABLE);
         return;
     }
-    // A thread's first kAhead units are loaded ahead of the angles, whose 64-bit arithmetic and barrier then run
-    // while the loads are in flight.
-    const int step = blockDim.x;
+    // A thread's first kAhead units are loaded ahead of the barrier that waits for the angles.
     uint4 x[kAhead], y[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
@@ -102,13 +108,6 @@ rope_append_kernel(const __grid_constant__ RopeParams rope, uint8_t *__restrict_
             x[i] = w.src[w.c0];
             y[i] = w.src[w.c1];
         }
-    }
-    for (int i = threadIdx.x; i < 8 * rope.units; i += step) {
-        double turns = (double)pos * rope.turn[i];
-        turns -= rint(turns);
-        float s, c;
-        sincospif((float)(2.0 * turns), &s, &c);
-        trig[i] = make_float2(c * rope.amplitude, s * rope.amplitude);
     }
     __syncthreads();
 #pragma unroll
