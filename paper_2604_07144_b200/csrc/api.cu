@@ -809,6 +809,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     plan->group = G;
     plan->scale = b->softmax_scale > 0.f ? b->softmax_scale : 1.0f / std::sqrt((float)d);
     plan->n_part_slots = n_slots;
+    for (const MergeEntry &m : merges) plan->max_parts = std::max(plan->max_parts, (int)m.part_count);
     plan->head_block = HB;
     plan->window = win.window;
     plan->sinks = win.sinks;

@@ -142,6 +142,7 @@ struct ap_plan {
     ap_plan_layout layout{};
     std::vector<int32_t> blob;   // host copy of the uploaded work lists
     int n_part_slots = 0;
+    int max_parts = 0;           // partials of the stream that was cut most often
     // Sliding window (0: none).  The plan's lists then count keys in compacted contexts: the pages no new
     // token of a decode row (of a prefill unit) sees are left out of its block-table entries, and bt_offset,
     // kv_len, pos0 and ctx_len refer to what is left.

@@ -477,62 +477,80 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
     cp_async_wait<0>();
 }
 
-// Merges the partials of a cut stream, one query head per block:
+// Merges the partials of a cut stream, query head by query head:
 //   lse = m* + ln sum_k exp(lse_k - m*),  o = sum_k exp(lse_k - lse) o_k,  m* = max_k lse_k.
 // A kernel of its own, overlapped with the decode kernel's end: with 64 query heads and ~20 partials each, the
-// warp that finishes a stream would still be merging for 30 us when all others are through (204 -> 221 us on 16
-// rows of 32 - 64 k tokens); here every head has four warps, eight partial rows in flight each.
-constexpr int kMergeThreads = 128;
+// warp that finishes a stream would still be merging for 30 us when all others are through (192 -> 221 us on 16
+// rows of 32 - 64 k tokens).  W warps share a head's partials (1 where streams have at most 8, else 4); the first eight
+// rows of o that a warp needs are loaded along with the lse values, so that up to 8 W partials take one round trip.
+constexpr int kMergeWarps = 4;
+constexpr int kMergeBatch = 8;
 
-template <int D>
-__global__ void __launch_bounds__(kMergeThreads)
+template <int D, int W>
+__global__ void __launch_bounds__(kMergeWarps * 32)
 kv4_merge_kernel(const MergeEntry *__restrict__ merges, const float *__restrict__ o_part, const float *__restrict__ lse_part,
-                 __nv_bfloat16 *__restrict__ out, float *__restrict__ lse_out, int Hq, int PH, int G) {
-    constexpr int kW = kMergeThreads / 32, kBatch = 8;
-    __shared__ float4 sums[kW][32];
-    const MergeEntry me = merges[blockIdx.x / PH];
-    const int ph = blockIdx.x % PH, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+                 __nv_bfloat16 *__restrict__ out, float *__restrict__ lse_out, int Hq, int PH, int G, int n_heads) {
+    __shared__ float4 sums[W > 1 ? kMergeWarps : 1][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % W;
+    const int head = min((int)blockIdx.x * (kMergeWarps / W) + warp / W, n_heads - 1);     // (a last block may repeat the last head)
+    const MergeEntry me = merges[head / PH];
+    const int ph = head % PH, n = me.part_count;
+    const bool col_ok = lane * 4 < D;
     griddep_launch_dependents();
     griddep_wait();
     const float *lse = lse_part + (size_t)me.part_begin * PH + ph;
-    const int n = me.part_count;
-    float mx = -INFINITY, sum = 0.f;
-    for (int k = lane; k < n; k += 32) mx = fmaxf(mx, __ldcg(lse + (size_t)k * PH));
+    const float4 *o = reinterpret_cast<const float4 *>(o_part + ((size_t)me.part_begin * PH + ph) * D) + lane;
+    auto load = [&](int k) { return k < n && col_ok ? __ldcg(o + (size_t)k * PH * (D / 4)) : make_float4(0.f, 0.f, 0.f, 0.f); };
+    float4 x[kMergeBatch];
+#pragma unroll
+    for (int i = 0; i < kMergeBatch; ++i) x[i] = load(part + i * W);
+    const float mine = lane < n ? __ldcg(lse + (size_t)lane * PH) : -INFINITY;
+    float mx = mine;
+    for (int k = lane + 32; k < n; k += 32) mx = fmaxf(mx, __ldcg(lse + (size_t)k * PH));
 #pragma unroll
     for (int sh = 16; sh >= 1; sh >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, sh));
-    for (int k = lane; k < n; k += 32) sum += __expf(__ldcg(lse + (size_t)k * PH) - mx);
+    float sum = __expf(mine - mx);
+    for (int k = lane + 32; k < n; k += 32) sum += __expf(__ldcg(lse + (size_t)k * PH) - mx);
 #pragma unroll
     for (int sh = 16; sh >= 1; sh >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, sh);
     const float total = mx + __logf(sum);
-    const bool col_ok = lane * 4 < D;
-    const float4 *o = reinterpret_cast<const float4 *>(o_part + ((size_t)me.part_begin * PH + ph) * D) + lane;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = warp; k0 < n; k0 += kW * kBatch) {
-        float4 x[kBatch];
-        float w[kBatch];
+    for (int k0 = part; k0 < n; k0 += W * kMergeBatch) {
+        if (k0 != part) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int k = k0 + i * kW;
-            x[i] = k < n && col_ok ? __ldcg(o + (size_t)k * PH * (D / 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            w[i] = k < n ? __expf(__ldcg(lse + (size_t)k * PH) - total) : 0.f;
+            for (int i = 0; i < kMergeBatch; ++i) x[i] = load(k0 + i * W);
         }
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            acc.x += w[i] * x[i].x; acc.y += w[i] * x[i].y; acc.z += w[i] * x[i].z; acc.w += w[i] * x[i].w;
+        for (int i = 0; i < kMergeBatch; ++i) {
+            const int k = k0 + i * W;
+            if (k >= n) break;
+            const float w = __expf(__ldcg(lse + (size_t)k * PH) - total);
+            acc.x += w * x[i].x; acc.y += w * x[i].y; acc.z += w * x[i].z; acc.w += w * x[i].w;
         }
     }
-    sums[warp][lane] = acc;
-    __syncthreads();
-    if (warp == 0 && col_ok) {
+    if constexpr (W > 1) {
+        sums[warp][lane] = acc;
+        __syncthreads();
+        if (part != 0) return;
 #pragma unroll
-        for (int i = 1; i < kW; ++i) {
-            const float4 x = sums[i][lane];
-            acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+        for (int i = 1; i < W; ++i) {
+            const float4 y = sums[warp + i][lane];
+            acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
         }
-        const size_t row = (size_t)me.q_row * Hq + (size_t)me.kv_head * G + ph;
+    }
+    const size_t row = (size_t)me.q_row * Hq + (size_t)me.kv_head * G + ph;
+    if (col_ok)
         *reinterpret_cast<uint2 *>(out + row * D + lane * 4) = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
-        if (lane == 0 && lse_out) lse_out[row] = total;
-    }
+    if (lane == 0 && lse_out) lse_out[row] = total;
+}
+
+template <int D, int W>
+cudaError_t launch_merge(const ap_plan *plan, void *out, float *lse, const float *o_part, const float *lse_part, cudaStream_t stream) {
+    const int part_heads = plan->head_block * plan->group, n_heads = (int)plan->info.merge_entries * part_heads;
+    constexpr int kPerBlock = kMergeWarps / W;
+    return launch_overlapped(kv4_merge_kernel<D, W>, (unsigned)((n_heads + kPerBlock - 1) / kPerBlock), (unsigned)(kMergeWarps * 32), 0,
+                             stream, plan->d_merge, o_part, lse_part, (__nv_bfloat16 *)out, lse, plan->num_q_heads, part_heads,
+                             plan->group, n_heads);
 }
 
 template <int D, bool kWin>
@@ -555,11 +573,9 @@ cudaError_t launch_t(const ap_kv_pool *pool, const ap_plan *plan, const void *q,
         plan->d_cta_begin, plan->d_bt_flat, o_part, lse_part, (__nv_bfloat16 *)out, lse, plan->num_q_heads,
         pool->desc.num_kv_heads, plan->group, plan->head_block, lists, pool->desc.num_pages, scale_log2, pool->status_dev,
         plan->window, plan->sinks);
-    const int part_heads = plan->head_block * plan->group;
     if (e == cudaSuccess && plan->info.merge_entries > 0)
-        e = launch_overlapped(kv4_merge_kernel<D>, (unsigned)(plan->info.merge_entries * part_heads), (unsigned)kMergeThreads, 0,
-                              stream, plan->d_merge, (const float *)o_part, (const float *)lse_part, (__nv_bfloat16 *)out, lse,
-                              plan->num_q_heads, part_heads, plan->group);
+        e = plan->max_parts <= kMergeBatch ? launch_merge<D, 1>(plan, out, lse, o_part, lse_part, stream)
+                                           : launch_merge<D, kMergeWarps>(plan, out, lse, o_part, lse_part, stream);
     return e;
 }
 
