@@ -658,12 +658,16 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
         cta_begin.reserve((size_t)max_ctas + 1);
         cta_begin.push_back(0);
         // (+ kStageTiles: about what a list loses to rounding; without it the loss drifts to the last lists)
-        int64_t cap = std::max<int64_t>((left + max_ctas - 1) / max_ctas + kStageTiles, min_share);
+        // In the 4-bit kernel an item's fixed cost weighs as much as a tenth of a list, so the items that the cuts still to
+        // come will add (one per list) are counted ahead; without that the last lists got 1.4 times the mean.
+        const int64_t cut_cost = pool->four_bit ? kItemCost : 0, rounding = pool->four_bit ? kStageTiles / 2 : kStageTiles;
+        int64_t cap = std::max<int64_t>((left + cut_cost * (max_ctas - 1) + max_ctas - 1) / max_ctas + rounding, min_share);
         auto next_cta = [&]() {
             if ((int32_t)items.size() > cta_begin.back()) cta_begin.push_back((int32_t)items.size());
             const int lists_left = max_ctas - ((int)cta_begin.size() - 1);
             cap = lists_left <= 1 ? INT64_MAX / 2
-                                  : std::max<int64_t>((left + lists_left - 1) / lists_left + kStageTiles, min_share);
+                                  : std::max<int64_t>((left + cut_cost * (lists_left - 1) + lists_left - 1) / lists_left + rounding,
+                                                      min_share);
         };
         for (int s = 0; s < B; ++s) {
             if (b->q_lens[s] != 1) continue;

@@ -223,7 +223,7 @@ int prepare_static_workspace(int device);
 
 // Decode kernel launch geometry (used by the planner to size the item lists).
 int decode_ctas_per_sm(int head_dim);
-// The 4-bit decode kernel: 16 warps on an SM, each on its own kv head of an item; a list of items belongs to HB
+// The 4-bit decode kernel: a block of 16 warps per SM, each on its own kv head of an item; a list of items belongs to HB
 // warps, HB the largest of 8, 4, 2, 1 that divides the number of kv heads.
 constexpr int kKv4WarpsPerSm = 16;
 inline int kv4_head_block(int num_kv_heads) {

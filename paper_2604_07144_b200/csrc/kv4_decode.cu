@@ -8,7 +8,9 @@
 // kernel.  An item is a range of a row's pages for a block of HB kv heads (8, 4, 2 or 1, the largest that
 // divides the pool's); each of the plan's lists belongs to HB warps of a block, one per kv head, which read
 // the HB tiles that lie together in HBM.  (With blocks of warps that share a head and fold their results at
-// an item's end, barriers and uneven shares cost 20 of 49 us on 64 rows of 128 .. 8192 tokens.)
+// an item's end, barriers and uneven shares cost 20 of 49 us on 64 rows of 128 .. 8192 tokens.  One block of 16
+// warps per SM, not two of eight: an SM's scheduler prefers its older block's warps, which ran through their
+// lists in 145 us where the younger block's took 181.)
 //
 // What bounds the kernel is the ALU pipe (LOP3, PRMT, shifts: one warp instruction in two clocks) on the
 // way from nibbles to MMA operands, so that way is short.  The bits of a byte b, put into a bf16 pattern with
@@ -32,6 +34,8 @@
 //
 // At the end of an item a warp has its head's complete (m, l, O) in registers and writes the bf16 output or, for
 // a stream cut across lists, an fp32 partial for the merge kernel.
+#include <algorithm>
+
 #include "decode_splitk.cuh"
 #include "kv4.cuh"
 
@@ -42,16 +46,16 @@ namespace {
 using namespace ptx;
 using namespace kv4;
 
-constexpr int kWarps = 8;
+constexpr int kWarps = kKv4WarpsPerSm;   // of a full block
 constexpr int kThreads = kWarps * 32;
-constexpr int kDepth = 3;                // pairs of pages in a warp's ring (K and V tile of each)
+constexpr int kDepth = 2;                // pairs of pages in a warp's ring (K and V tile of each)
 
 template <int D>
 struct Kv4Cfg {
     static constexpr int kPageBytes = 2 * Tile<D>::kBytes;        // K tile, V tile
     static constexpr int kSlotBytes = 2 * kPageBytes;
-    static constexpr int kSmemBytes = kWarps * kDepth * kSlotBytes;
-    static_assert(2 * (kSmemBytes + 1024) <= 228 * 1024, "two blocks per SM");
+    static constexpr int kRingBytes = kDepth * kSlotBytes;        // of a warp
+    static_assert(kWarps * kRingBytes <= 227 * 1024, "fits the shared memory of an SM");
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) {
@@ -117,7 +121,7 @@ __device__ __forceinline__ int ring_chunk(int c) {
 }
 
 template <int D, bool kWin>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, 1)
 kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict__ v_pool, const __nv_bfloat16 *__restrict__ q,
                   const DecodeItem *__restrict__ items, const int32_t *__restrict__ cta_begin, const int32_t *__restrict__ bt_flat,
                   float *o_part, float *lse_part, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse_out, int Hq, int Hkv,
@@ -135,7 +139,7 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
     auto uniform = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
     const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
-    const int list = blockIdx.x * (kWarps / HB) + warp / HB, my_head = warp % HB;
+    const int list = blockIdx.x * ((int)(blockDim.x >> 5) / HB) + warp / HB, my_head = warp % HB;
     if (list >= n_lists) {
         griddep_launch_dependents();
         griddep_wait();
@@ -176,7 +180,7 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
         cur_bt += 2;
         cur_left -= 2;
     };
-    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * kDepth * Cfg::kSlotBytes);
+    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * Cfg::kRingBytes);
     // a lane's share of a tile's copy: code chunks lane (and lane + 32, four lines on), and, for the first
     // lanes, a chunk of K's or V's steps
     const uint32_t c_dst = 16 * ring_chunk<D>(lane);
@@ -211,8 +215,9 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
         }
         cp_async_commit();       // (an empty group past the last pair keeps the count of groups in step)
     };
-#pragma unroll 1
-    for (int s = 0; s < kDepth; ++s) issue(s);
+    // the first pair at once, the ring's others after the first item's queries: with all of them ahead (32 MB over the
+    // GPU) the first pair's data came 2 us later
+    issue(0);
 
     // a lane's places in a tile: K words of rows g and g + 8 (four or two lines on), K steps; V words of rows
     // 2t and 2t + 1 (and 2t + 8, 2t + 9), V steps
@@ -281,6 +286,10 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
             }
             f_col[0] = __shfl_sync(0xffffffffu, f, 8 * t);
             f_col[1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+        }
+        if (n == 0) {
+#pragma unroll 1
+            for (int i = 1; i < kDepth; ++i) issue(i);
         }
         // running maximum of the scores (f_col makes exponents of 2 of them), sum and O
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
@@ -561,14 +570,17 @@ cudaError_t launch_t(const ap_kv_pool *pool, const ap_plan *plan, const void *q,
     const int dev = pool->desc.device & 63;
     if (!configured[dev]) {
         const cudaError_t e = cudaFuncSetAttribute(kv4_decode_kernel<D, kWin>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   Cfg::kSmemBytes);
+                                                   kWarps * Cfg::kRingBytes);
         if (e != cudaSuccess) return e;
         configured[dev] = true;
     }
     const float scale_log2 = plan->scale * 1.4426950408889634f;
-    const int lists = (int)plan->info.decode_ctas, per_block = kWarps / plan->head_block;
+    // few lists are spread over the SMs, one per block if they go round
+    const int HB = plan->head_block, lists = (int)plan->info.decode_ctas;
+    const int per_block = std::min(kWarps / HB, (lists + pool->sm_count - 1) / pool->sm_count);
     cudaError_t e = launch_overlapped(
-        kv4_decode_kernel<D, kWin>, (unsigned)((lists + per_block - 1) / per_block), (unsigned)kThreads, (size_t)Cfg::kSmemBytes,
+        kv4_decode_kernel<D, kWin>, (unsigned)((lists + per_block - 1) / per_block), (unsigned)(per_block * HB * 32),
+        (size_t)(per_block * HB * Cfg::kRingBytes),
         stream, (const uint8_t *)pool->desc.k_base, (const uint8_t *)pool->desc.v_base, (const __nv_bfloat16 *)q, plan->d_items,
         plan->d_cta_begin, plan->d_bt_flat, o_part, lse_part, (__nv_bfloat16 *)out, lse, plan->num_q_heads,
         pool->desc.num_kv_heads, plan->group, plan->head_block, lists, pool->desc.num_pages, scale_log2, pool->status_dev,
