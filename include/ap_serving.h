@@ -119,6 +119,7 @@ int ap_kv_pool_create(ap_kv_pool **out, const ap_pool_desc *desc);
  * prefill of a mixed iteration run one after the other (ap_kv_pool_set_side_by_side
  * has no effect).  A plan with prefill chunks needs workspace for the pages they
  * read, widened to bf16: 2 * 16 * head_dim * 2 bytes per page and kv head.
+ * A query element of 2^121 or more makes its head's result NaN.
  * ap_kv_pool_bytes_4bit: bytes of one plane; 0 if the description is invalid.
  */
 size_t ap_kv_pool_bytes_4bit(const ap_pool_desc *desc);
@@ -275,6 +276,9 @@ int ap_plan_predict(const ap_plan *plan, double hbm_gbs, double tensor_tflops, a
  *   cta_begin     [n_cta_begin]       item range of decode CTA c is [cta_begin[c], cta_begin[c+1])
  *   merge_entries [merge_entries][4]  q_row, first kv_head of the block, part_begin, part_count
  *   prefill_tiles [prefill_tiles][8]  q_row0, rows, q_head, kv_head, bt_offset, pos0, ctx_len, q_head_b (-1: none)
+ * With a window, kv_len, pos0 and ctx_len count in the compacted context (the kept pages one after the
+ * other); on a 4-bit pool the entries of prefill tiles number the widened copies of pages, in the order in
+ * which the sequences' seen pages follow one another.
  * blob: host, capacity_ints >= layout.total_ints, or NULL to query the layout only.
  */
 typedef struct ap_plan_layout {
@@ -458,8 +462,9 @@ int ap_selftest_wait_timeout(ap_kv_pool *pool, uint64_t limit_ns, int leave_coun
 
 /*
  * Per-kernel device timing for benchmarks.  While enabled, every kernel the
- * library launches for this pool is bracketed by CUDA events recorded on the
- * launching stream.  ap_profile_collect synchronises `stream`, adds up the
+ * library launches for this pool (page copies and read-backs excepted) is bracketed
+ * by CUDA events recorded on the launching stream; a rotated append counts as
+ * append, a 4-bit pool's merge as decode and its widening of pages as prefill.  ap_profile_collect synchronises `stream`, adds up the
  * elapsed times per kernel since the last enable/collect, and clears the
  * records.  Index: 0 kv_append, 1 decode split-K (which also performs the LSE
  * merge), 2 prefill, 3 the single launch that holds both parts of a mixed plan.

@@ -111,6 +111,8 @@ constexpr double kPrefillStepSingleUs = 1.35; // the same for a one-tile unit
 constexpr double kPrefillUnitUs = 5.3;       // prologue + epilogue + relaunch gap of a unit
 constexpr double kPrefillTailUs = 12.0;      // spread of the SMs' finishing times (about half a short unit) + ramp-up
 constexpr double kDecodeFixedUs = 8.0;       // first-data latency and finishing spread of the decode kernel
+constexpr double kDecode4GpuGBs = 5200.0;    // GB/s of 4-bit KV the 4-bit decode kernel gets through with all its warps
+constexpr double kWidenGpuGBs = 6000.0;      // read + written by the widening of pages for prefill
 constexpr double kAppendGBs = 4000.0;        // scatter of 256-byte rows
 constexpr double kAppendFixedUs = 3.0;
 
@@ -925,11 +927,17 @@ int ap_plan_predict(const ap_plan *plan, double hbm_gbs, double tensor_tflops, a
     e.roofline_append_us = t_op_us(0.0, w.append_bytes);
     // calibrated model (the one the planner's side-by-side decision uses)
     const int sms = plan->pool->sm_count;
+    const ap_pool_desc &d = plan->pool->desc;
     const double ctas = (double)std::max<int64_t>(plan->info.decode_ctas, 1);
-    const double decode_rate = std::min(ctas * decode_sm_gbs(plan->head_block * kPageSize * plan->pool->desc.head_dim * 2),
-                                        kDecodeGpuGBs) * 1e3;                             // bytes / us
+    const double decode_rate =                                                            // bytes / us
+        1e3 * (plan->pool->four_bit
+                   ? kDecode4GpuGBs * std::min(1.0, ctas * plan->head_block / ((double)kKv4WarpsPerSm * sms))
+                   : std::min(ctas * decode_sm_gbs(plan->head_block * kPageSize * d.head_dim * 2), kDecodeGpuGBs));
     e.model_decode_us = w.decode_bytes > 0.0 ? w.decode_bytes / decode_rate + kDecodeFixedUs : 0.0;
     e.model_prefill_us = w.prefill_sm_us > 0.0 ? w.prefill_sm_us / sms + kPrefillTailUs : 0.0;
+    if (plan->n_wide_pages > 0)
+        e.model_prefill_us += 2.0 * plan->n_wide_pages * d.num_kv_heads *
+                              (plan->pool->tile_bytes + pool_tile_bytes(d.head_dim, false)) / (kWidenGpuGBs * 1e3);
     const double append_us = w.append_bytes > 0.0 ? w.append_bytes / (kAppendGBs * 1e3) + kAppendFixedUs : 0.0;
     if (plan->side_by_side)
         e.model_step_us = append_us + kPrefillTailUs +
@@ -997,10 +1005,14 @@ int ap_kv_append_rope(ap_kv_pool *pool, const ap_plan *plan, const ap_rope_desc 
     params.units = rope->rotary_dim / 16;
     params.interleaved = rope->interleaved;
     params.amplitude = rope->amplitude == 0.f ? 1.f : rope->amplitude;
-    for (int i = 0; i < rope->rotary_dim / 2; ++i) {
-        const double f = rope->inv_freq ? rope->inv_freq[i] : std::pow(rope->base, -2.0 * i / rope->rotary_dim);
+    // base^(-2 i / R) as the i-th power of one pow: 64 of them would take as long as the launch.  The product is off by
+    // less than i 2^-52 of f_i, an angle p f_i by less than 1e-6 even at p = 2^31.
+    const double ratio = rope->inv_freq ? 1.0 : std::pow(rope->base, -2.0 / rope->rotary_dim);
+    double f = 1.0;
+    for (int i = 0; i < rope->rotary_dim / 2; ++i, f *= ratio) {
+        if (rope->inv_freq) f = rope->inv_freq[i];
         if (!std::isfinite(f)) return AP_ERR_INVALID_ARG;
-        params.turn[i] = f / 6.283185307179586476925286766559;
+        params.turn[i] = f * 0.15915494309189533576888376337251;       // / (2 pi)
     }
     auto stride_of = [](int64_t given, int heads, int dim) { return given ? given : (int64_t)heads * dim; };
     const int64_t qs = stride_of(rope->q_row_stride, Hq, d), ks = stride_of(rope->k_row_stride, Hkv, d),

@@ -10,6 +10,7 @@ from paper_2604_07144_b200 import workloads as W
 import kv4_reference as Q
 import operator_reference as R
 from harness import to_bits, to_dev
+from test_windowed_attention import _hide as hide
 
 SHAPES = [(8, 2, 64), (6, 2, 128), (5, 1, 128), (8, 8, 64), (32, 8, 128), (64, 8, 128), (3, 3, 128)]
 
@@ -139,6 +140,8 @@ def test_4bit_plan_lists():
 # ------------------------------------------------------------------ GPU --
 
 def _check_attention(batch, window=None, sinks=0, append=True, planes=None):
+    if window is not None:
+        hide(batch, window, sinks)       # table entries of unseen pages -1, unseen tokens of the others NaN
     kp, vp = planes or Q.planes_of(batch)
     make = None if window is None else (lambda pool: ap.plan_create_windowed(
         pool, batch.q_lens, batch.ctx_lens, batch.block_tables, batch.num_q_heads, window, sinks))
@@ -349,3 +352,38 @@ def test_4bit_library_planes_host_call_and_static_workspace():
     ap.plan_destroy(plan)
     for p in (big, pool):
         ap.kv_pool_destroy(p)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("four_bit", [False, True], ids=["bf16", "4bit"])
+def test_without_lse_and_with_one_workspace_for_all_layers(four_bit):
+    """lse may be NULL; a workspace that is large enough serves plans of different layers in turn (what it holds before
+    a call does not matter), and pools on two streams do not disturb one another."""
+    import torch
+    shape, n = (6, 2, 128), 4
+    batches = [_batch(shape, 50 + i, [1, 1, 60, 1], [700 + 100 * i, 33, 300, 5000]) for i in range(n)]
+    devs = []
+    for i, b in enumerate(batches):
+        make = None if i % 2 else (lambda pool, b=b: ap.plan_create_windowed(pool, b.q_lens, b.ctx_lens, b.block_tables, 6, 100, 4))
+        planes = Q.planes_of(b) if four_bit else (None, None)
+        devs.append(R.Device(b, make, k_plane=planes[0], v_plane=planes[1], four_bit=four_bit))
+    size = max(256, *(d.workspace_bytes for d in devs))
+    ws = [torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda:0") for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for d in devs:
+        ap.kv_append(d.pool, d.plan, d.k_new, d.v_new)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for i, d in enumerate(devs):
+            with torch.cuda.stream(streams[i // 2]):
+                d.out.fill_(float("nan"))
+                ap.attention_iteration(d.pool, d.plan, d.q, d.out, None, ws[i // 2], size)
+    torch.cuda.synchronize()
+    for i, (b, d) in enumerate(zip(batches, devs)):
+        assert ap.last_device_status(d.pool) == 0 and np.isnan(d.lse.cpu().numpy()).all()
+        k, v = ((Q.values(p.cpu().numpy(), 128) if four_bit else W.bf16_bits_to_f64(to_bits(p))) for p in (d.k_pool, d.v_pool))
+        window, sinks = (None, 0) if i % 2 else (100, 4)
+        ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b, window, sinks)
+        R.check(to_bits(d.out)[:b.n_new], ref[1], ref, f"layer {i}")
+        d.close()
