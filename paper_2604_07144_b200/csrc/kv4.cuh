@@ -23,7 +23,7 @@ namespace ap {
 namespace kv4 {
 
 constexpr int kGroup = 32;
-constexpr float kSmallStep = 7.8886090522101181e-31f;      // 2^-100
+constexpr uint32_t kHugeTop = 0x7B800000u, kSmallTop = 0x0E800000u;      // bits of 2^120, 2^-98
 
 template <int D>
 struct Tile {
@@ -41,50 +41,47 @@ __device__ __forceinline__ int stored_word(int chunk) {
 
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
 
-// Step of a group from the largest absolute value's bit pattern (as an unsigned integer: NaN is largest).
-__device__ __forceinline__ float group_step(uint32_t amax_bits) {
-    if (amax_bits >= 0x7B800000u) return __uint_as_float(0x7FC00000u);          // 2^120 and beyond, inf, NaN
-    const uint32_t s = __float_as_uint(__fdiv_rn(__uint_as_float(amax_bits), 7.f));
-    return __uint_as_float((s + 0x7FFFFu) & ~0x7FFFFu);
-}
-
 // Quantises eight bf16 values; the four lanes of an aligned quad hold the four chunks of a group.
-// Every lane of the warp has to call it.
+// Every lane of the warp has to call it.  No division in the common case:
+//   s    max |x| is m 2^e with m an integer from 128 to 255.  m (1 - 2^-16) / 7 lies below m / 7, and above every
+//        number of five significant bits that m / 7 is above (m and 7 times such a number differ by a 255th or not at
+//        all); where m / 7 is one itself, rounding up brings it back.  So rounding it up gives s.
+//   c    x / s = 2^n X / S with X below 2^8 and S from 16 to 31, so a quotient between 1/4 and 7 either is a half-integer
+//        or lies at least 2^-11 away from one.  x times the approximate 1 / s is off by less than 2^-19; added to
+//        1.5 2^10, whose last bit is worth 2^-13, it becomes the multiple of 2^-13 that is on the same side of every
+//        half-integer as the quotient, and on it if the quotient is.  A second addition moves it on to 1.5 2^23 + 8,
+//        rounding to an integer with ties to even, and leaves c in the low bits.
 __device__ __forceinline__ uint32_t quantise8(const uint4 x, float &step) {
-    float f[8];
     const uint32_t u[4] = {x.x, x.y, x.z, x.w};
-    uint32_t amax = 0;
+    uint32_t top = __vmaxu2(__vmaxu2(u[0] & 0x7FFF7FFFu, u[1] & 0x7FFF7FFFu), __vmaxu2(u[2] & 0x7FFF7FFFu, u[3] & 0x7FFF7FFFu));
+    top = max(top << 16, top & 0xFFFF0000u);                     // bits of max |x| (NaN is largest)
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    float f[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         f[2 * i] = __uint_as_float(u[i] << 16);
         f[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
     }
+    auto round_up = [](float v) { return __uint_as_float((__float_as_uint(v) + 0x7FFFFu) & ~0x7FFFFu); };
+    if (top - kSmallTop < kHugeTop - kSmallTop) {
+        step = round_up(__fmul_rn(__uint_as_float(top), 0.14285496f));       // (1 - 2^-16) / 7
+        float inv;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(step));
+        uint32_t c[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(f[i]) & 0x7FFFFFFFu);
-    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-    step = group_step(amax);
-    uint32_t w = 0;
-    if (step >= kSmallStep) {
-        // rint(x / s) by a product with 1 / s.  x / s = 2^n X / S with X below 2^8 and S from 16 to 31, so a quotient
-        // between 1/4 and 7 either is a half-integer or lies at least 2^-11 away from one, while the product is
-        // off by less than 2^-20: moved to the nearest multiple of 2^-13 (by adding and subtracting 1.5 2^10, whose last
-        // bit is worth that) it is on the same side of every half-integer as the quotient, and on it if the
-        // quotient is.  Adding 1.5 2^23 + 8 then rounds to an integer, ties to even, and leaves c in the low bits.
-        const float inv = __frcp_rn(step);
+        for (int i = 0; i < 8; ++i) c[i] = __float_as_uint(__fadd_rn(__fmaf_rn(f[i], inv, 1536.f), 12581384.f));
+        // two codes a byte, four bytes a word
+        const uint32_t b0 = c[1] * 16 + c[0], b1 = c[3] * 16 + c[2], b2 = c[5] * 16 + c[4], b3 = c[7] * 16 + c[6];
+        return prmt(prmt(b0, b1, 0x0040), prmt(b2, b3, 0x0040), 0x5410);
+    }
+    // no step (zero or NaN), or one whose reciprocal might overflow
+    uint32_t w = 0x88888888u;
+    step = top >= kHugeTop ? __uint_as_float(0x7FC00000u) : round_up(__fdiv_rn(__uint_as_float(top), 7.f));
+    if (step > 0.f) {
+        w = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float y = __fsub_rn(__fadd_rn(__fmul_rn(f[i], inv), 1536.f), 1536.f);
-            w |= (__float_as_uint(__fadd_rn(y, 12582920.f)) & 15u) << (4 * i);
-        }
-    } else {
-        // (1 / s would overflow; a step of zero or NaN: every code is 8)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            int c = 8;
-            if (step > 0.f) c = min(max(__float2int_rn(__fdiv_rn(f[i], step)) + 8, 1), 15);
-            w |= (uint32_t)c << (4 * i);
-        }
+        for (int i = 0; i < 8; ++i) w |= (uint32_t)min(max(__float2int_rn(__fdiv_rn(f[i], step)) + 8, 1), 15) << (4 * i);
     }
     return w;
 }

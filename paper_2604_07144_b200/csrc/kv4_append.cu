@@ -10,6 +10,16 @@ namespace {
 
 // A thread has elements 32 g + 8 t .. + 7 of every group g of one head row, for its t: the words of a row that
 // are stored next to one another (16 bytes at d = 128).  The four lanes of a quad have the row's four t.
+__device__ __forceinline__ void row_and_head(int64_t rh, int num_kv_heads, int64_t &row, int &head) {
+    if (rh < (int64_t)1 << 32) {                         // (a 64-bit division takes as long as the rest of the thread)
+        row = (uint32_t)rh / (uint32_t)num_kv_heads;
+        head = (int)((uint32_t)rh % (uint32_t)num_kv_heads);
+    } else {
+        row = rh / num_kv_heads;
+        head = (int)(rh % num_kv_heads);
+    }
+}
+
 // One thread quantises its slice of a K row and of the V row; a quad shares its groups' maxima by shuffle and its
 // first lane stores the steps.  All loads go out first: 2 d / 32 of 16 bytes a thread.
 template <int D>
@@ -21,8 +31,11 @@ __global__ void __launch_bounds__(128) kv4_append_kernel(uint8_t *__restrict__ k
     constexpr int NG = T::kGroups;
     const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     const int64_t i = idx < n_slices ? idx : n_slices - 1;      // the shuffles need whole warps; the rest stores nothing
-    const int t = (int)(i & 3), g = (int)((i >> 2) % num_kv_heads);
-    const int32_t dst = __ldg(append_dst + (i >> 2) / num_kv_heads);   // plan data: uploaded before any kernel of the step
+    const int t = (int)(i & 3);
+    int64_t row;
+    int g;
+    row_and_head(i >> 2, num_kv_heads, row, g);
+    const int32_t dst = __ldg(append_dst + row);                // plan data: uploaded before any kernel of the step
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     const int64_t vec = (i >> 2) * (D / 8) + t;
@@ -95,8 +108,11 @@ __global__ void __launch_bounds__(128) kv4_read_new_kernel(const uint8_t *__rest
     constexpr int NG = T::kGroups;
     const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     const int64_t i = idx < n_slices ? idx : n_slices - 1;
-    const int t = (int)(i & 3), g = (int)((i >> 2) % num_kv_heads);
-    const int32_t dst = __ldg(append_dst + (i >> 2) / num_kv_heads);
+    const int t = (int)(i & 3);
+    int64_t row;
+    int g;
+    row_and_head(i >> 2, num_kv_heads, row, g);
+    const int32_t dst = __ldg(append_dst + row);
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     if (idx >= n_slices) return;

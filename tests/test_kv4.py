@@ -37,26 +37,32 @@ def test_reference_format_round_trip_and_error_bound():
         assert (np.ceil(np.abs(W.bf16_bits_to_f64(x)).reshape(40, 2, -1, 32).max(-1) / 7 / (s[..., ::32] * 17 / 16)) <= 1).all()
 
 
-def test_quotients_by_product_round_like_division():
-    """The append forms rint(x / s) as rint of x (1 / s) moved to a multiple of 2^-13.  Every 8-bit x, every 5-bit s and
-    every scale between them, in fp32 as the kernel does it, against exact fractions."""
+def test_quantiser_without_divisions_is_exact():
+    """The append forms the step from a product with (1 - 2^-16) / 7 and rint(x / s) from one with an approximate 1 / s (see
+    kv4.cuh).  Every 8-bit x, every 5-bit s and every scale between them, in fp32 as the kernel does it, against
+    exact fractions; 1 / s with up to two ulps of error either way."""
     from fractions import Fraction
     f = np.float32
+    # steps: five significant bits at or above m / 7
+    m = np.arange(128, 256).astype(f)
+    t = m * f(0.14285496)
+    step = ((t.view(np.uint32) + np.uint32(0x7FFFF)) & ~np.uint32(0x7FFFF)).view(f)
+    for mi, si in zip(m, step):
+        grid = [Fraction(S) * Fraction(2) ** e for e in range(-3, 3) for S in range(16, 32)]
+        assert Fraction(float(si)) == min(g for g in grid if g >= Fraction(int(mi), 7))
+    # codes
     for S in range(16, 32):
-        inv = f(1) / f(S)
-        for n in range(-12, 4):
-            X = np.arange(128, 256)
-            x = (X * 2.0 ** n).astype(f)
-            x = x[x <= 7 * S]
-            y = (x * inv + f(1536)) - f(1536)
-            got = (y + f(12582912)) - f(12582912)
-            want = [round(Fraction(float(v)) / S) for v in x]             # Python rounds ties to even
-            assert got.tolist() == want
-            neg = ((-x * inv + f(1536)) - f(1536) + f(12582912)) - f(12582912)
-            assert (-neg).tolist() == want
-            # the kernel's last addition carries the 8 along: ties still go to even, and the low bits are the code
-            code = (y + f(12582920)).view(np.uint32) & 15
-            assert code.tolist() == [(w + 8) & 15 for w in want]
+        exact = f(1) / f(S)
+        for inv in (exact, *(np.nextafter(exact, f(d), dtype=f) for d in (0, 1)),
+                    *(np.nextafter(np.nextafter(exact, f(d), dtype=f), f(d), dtype=f) for d in (0, 1))):
+            for n in range(-12, 4):
+                x = (np.arange(128, 256) * 2.0 ** n).astype(f)
+                x = x[x <= 7 * S]
+                want = [round(Fraction(float(v)) / S) for v in x]                 # Python rounds ties to even
+                for sign in (1, -1):
+                    y = (sign * x.astype(np.float64) * np.float64(inv) + 1536.0).astype(f)       # one rounding: an FMA
+                    code = (y + f(12581384)).view(np.uint32) & 15
+                    assert code.tolist() == [8 + sign * w for w in want]
 
 
 def test_4bit_pool_descriptions_and_refusals():
