@@ -168,35 +168,38 @@ def _ptr(x) -> Optional[int]:
     """Address of a device tensor / host array / raw integer (None -> NULL)."""
     if x is None:
         return None
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        pass
     if isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        return int(x.data_ptr())
     if isinstance(x, np.ndarray):
         return int(x.ctypes.data)
     raise TypeError(f"cannot take the address of {type(x)}")
 
 
-_torch = None
+_raw_stream = None        # torch's accessor of the current stream's handle, once torch has initialised CUDA
 
 
 def _stream(stream, device: Optional[int] = None) -> Optional[int]:
     """CUDA stream handle: a torch stream, an integer, or None for torch's current stream on ``device`` (a pool's
     device; the current device where it is not given)."""
-    global _torch
+    global _raw_stream
     if stream is None:
-        if _torch is None:
+        if _raw_stream is None:
             try:
                 import torch
-                _torch = torch
             except ImportError:
                 return None
-        if not _torch.cuda.is_initialized():
-            return None                      # nobody can have chosen a stream yet
+            if not torch.cuda.is_initialized():
+                return None                  # nobody can have chosen a stream yet
+            # torch.cuda.current_stream(device).cuda_stream takes 3 us, as long as a launch
+            _raw_stream = torch._C._cuda_getCurrentRawStream
         if device is None or device < 0:
-            device = _torch.cuda.current_device()
-        # torch.cuda.current_stream(device).cuda_stream takes 3 us, as long as a launch
-        return int(_torch._C._cuda_getCurrentRawStream(device)) or None
+            import torch
+            device = torch.cuda.current_device()
+        return _raw_stream(device) or None
     if hasattr(stream, "cuda_stream"):
         return int(stream.cuda_stream) or None
     return int(stream) or None
@@ -398,7 +401,10 @@ def kv_append(pool: KVPool, plan: Plan, k_new, v_new, stream=None) -> None:
 
 def _row_stride(x) -> int:
     """Elements from one row of a [rows, heads, head_dim] tensor to the next (0: contiguous, or not a tensor)."""
-    if x is None or not hasattr(x, "stride") or x.is_contiguous():
+    try:
+        if x is None or x.is_contiguous():
+            return 0
+    except AttributeError:                   # an address
         return 0
     stride, shape = x.stride(), x.shape
     if len(shape) != 3 or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2]):
@@ -415,7 +421,7 @@ def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, r
     rotary = pool.head_dim if rotary_dim is None else int(rotary_dim)
     if freq is not None and freq.shape != (rotary // 2,):
         raise ValueError("inv_freq must have rotary_dim / 2 entries")
-    if q_rot is not None and hasattr(q_rot, "is_contiguous") and not q_rot.is_contiguous():
+    if _row_stride(q_rot):
         raise ValueError("q_rot must be contiguous")
     desc = RopeDesc(rotary, int(bool(interleaved)), float(base), _ptr(freq), float(amplitude), _row_stride(q),
                     _row_stride(k_new), _row_stride(v_new))

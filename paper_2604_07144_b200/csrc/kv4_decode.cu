@@ -32,6 +32,13 @@
 // read 16 bytes of a row per lane, V fragments 8 bytes of four rows per lane, pairs of rows interleaved with
 // PRMT.
 //
+// Measured: 16 rows of 32 - 64 k tokens at 64 / 8 heads of 128 (841 MB) 165 us, 5.1 TB/s, 0.78 of copy bandwidth (198 us in
+// a loop of seconds, where the power limit takes the clock down); 64 rows of 128 .. 8192 tokens at 32 / 8
+// heads (126 MB) 34.6 us.  Copying alone, without the arithmetic, takes 132 and 27.5 us.  331 warp
+// instructions per tile (K and V of 16 tokens): 127 on the ALU pipe and 72 HFMA2, each one per two clocks of a
+// scheduler, and 17 MMAs, one per eight.  Issue slots are 70 % busy, the ALU pipe 54 %, and neither more warps (20
+// at 96 registers) nor fewer (12) change the time.
+//
 // At the end of an item a warp has its head's complete (m, l, O) in registers and writes the bf16 output or, for
 // a stream cut across lists, an fp32 partial for the merge kernel.
 #include <algorithm>

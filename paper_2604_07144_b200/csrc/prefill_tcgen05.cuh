@@ -151,6 +151,8 @@ __device__ __noinline__ void rescale_o(uint32_t taddr, float alpha) {
 // kWin: sliding window.  The row at position p sees key v if v <= p and (v > p - window or v < sinks), in
 // positions of the unit's compacted context (the planner leaves out the pages that no row of the unit sees,
 // which lie between the sinks and the first row's window, so both tests hold for compacted positions too).
+// Masked steps (about four of a unit's ten at a window of 1024) test one bit per score: with comparisons of
+// positions 8 x 512 rows beside 120 decode rows took 167 us where they take 135.
 template <int D, bool kWin>
 __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUtensorMap &k_map, const CUtensorMap &v_map,
                                              const PrefillTile *__restrict__ tiles, const int32_t *__restrict__ bt_flat,
