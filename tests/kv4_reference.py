@@ -13,7 +13,7 @@ def tile_bytes(d):
 
 def quantise(bits):
     """bf16 bits [..., d] -> (codes uint8 [..., d], steps bf16 bits [..., d / 32])."""
-    x = W.bf16_bits_to_f64(bits).reshape(*bits.shape[:-1], -1, GROUP)
+    x = W.bf16_bits_to_f64(bits).reshape(*bits.shape[:-1], bits.shape[-1] // GROUP, GROUP)
     with np.errstate(invalid="ignore", over="ignore"):
         top = np.abs(x).max(-1)
         bad = ~(top < 2.0 ** 120)

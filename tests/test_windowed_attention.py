@@ -189,3 +189,31 @@ def test_a_window_that_covers_the_context_gives_the_plain_result():
     for out, lse in got:
         R.check(out, lse, ref)
     assert np.array_equal(got[0][0][:3], got[1][0][:3]) and np.array_equal(got[0][1][:3], got[1][1][:3])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("window", [None, BIG], ids=["plain", "windowed"])
+@pytest.mark.parametrize("mode,q_lens,ctx_lens", [
+    (6, [1, 1, 1, 1, 8, 1, 1, 1], [935, 877, 16, 1242, 706, 669, 865, 596]),
+    (3, [1, 1, 1, 1, 1, 1, 1, 44], [10, 158, 59, 13, 79, 161, 31, 86])])
+def test_items_of_a_page_or_two_read_their_own_queries(window, mode, q_lens, ctx_lens):
+    """Decode rows of a page or two between long ones, 32 query heads per item, a few SMs: the producer runs two items
+    ahead, and the query buffer of an item must not be refilled while a warp's loads from it are in flight.  The lists
+    and the order of every sum are fixed, so all runs have to agree bit for bit with one that the reference has passed."""
+    b = _batch((64, 8, 128), 15, q_lens, ctx_lens)
+    make = None if window is None else (
+        lambda pool: ap.plan_create_windowed(pool, b.q_lens, b.ctx_lens, b.block_tables, 64, window, 0))
+    for single in (True, False):
+        dev = R.Device(b, make, side_by_side=mode, single_launch=single)
+        ap.kv_append(dev.pool, dev.plan, dev.k_new, dev.v_new)
+        k, v = (W.bf16_bits_to_f64(R.to_bits(p)) for p in (dev.k_pool, dev.v_pool))
+        ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b)
+        dev.attend()
+        first = dev.results()
+        for run in range(500):
+            dev.attend()
+            if run % 4 == 3:
+                out, lse = dev.results()
+                assert np.array_equal(out, first[0]) and np.array_equal(lse, first[1]), f"run {run}, single launch {single}"
+        dev.close()
+        R.check(*first, ref)
