@@ -307,6 +307,18 @@ size_t ap_kv_pool_bytes_4bit(const ap_pool_desc *d) {
     return (size_t)d->num_pages * (size_t)d->num_kv_heads * (size_t)pool_tile_bytes(d->head_dim, true);
 }
 
+// All pages free, lowest last in the list.  False: no host memory (no exception leaves a C entry).
+static bool fill_free_list(ap_kv_pool *p) {
+    try {
+        p->free_list.resize((size_t)p->desc.num_pages);
+        p->allocated.assign((size_t)p->desc.num_pages, 0);
+    } catch (const std::bad_alloc &) {
+        return false;
+    }
+    for (int32_t i = 0; i < p->desc.num_pages; ++i) p->free_list[(size_t)i] = p->desc.num_pages - 1 - i;
+    return true;
+}
+
 static int pool_create(ap_kv_pool **out, const ap_pool_desc *desc, bool four_bit) {
     if (!out) return AP_ERR_INVALID_ARG;
     *out = nullptr;
@@ -330,9 +342,7 @@ static int pool_create(ap_kv_pool **out, const ap_pool_desc *desc, bool four_bit
         hp->tile_bytes = pool_tile_bytes(desc->head_dim, four_bit);
         hp->head_block = four_bit ? kv4_head_block(desc->num_kv_heads) : decode_head_block(desc->num_kv_heads);
         hp->sm_count = 148;
-        hp->free_list.resize((size_t)desc->num_pages);
-        for (int32_t i = 0; i < desc->num_pages; ++i) hp->free_list[(size_t)i] = desc->num_pages - 1 - i;
-        hp->allocated.assign((size_t)desc->num_pages, 0);
+        if (!fill_free_list(hp)) { delete hp; return AP_ERR_CUDA; }
         *out = hp;
         return AP_OK;
     }
@@ -395,9 +405,7 @@ static int pool_create(ap_kv_pool **out, const ap_pool_desc *desc, bool four_bit
                                         p->head_block);
             if (rc != AP_OK) break;
         }
-        p->free_list.resize((size_t)desc->num_pages);
-        for (int32_t i = 0; i < desc->num_pages; ++i) p->free_list[(size_t)i] = desc->num_pages - 1 - i;
-        p->allocated.assign((size_t)desc->num_pages, 0);
+        if (!fill_free_list(p)) rc = AP_ERR_CUDA;
     } while (false);
     if (rc != AP_OK) {
         (void)cudaGetLastError();
@@ -772,9 +780,10 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     const size_t o_wide = sec(cursor, wide_pages.size());
     const size_t total_ints = std::max<size_t>(cursor, 8);
 
+    std::vector<int32_t> blob(total_ints, 0);
     ap_plan *plan = new (std::nothrow) ap_plan();
     if (!plan) return AP_ERR_CUDA;
-    plan->blob.assign(total_ints, 0);
+    plan->blob = std::move(blob);
     int32_t *h = plan->blob.data();
     if (n_new) std::memcpy(h + o_append, append_dst.data(), (size_t)n_new * 4);
     if (n_new) std::memcpy(h + o_pos, positions.data(), (size_t)n_new * 4);
@@ -1018,6 +1027,9 @@ int ap_kv_append_rope(ap_kv_pool *pool, const ap_plan *plan, const ap_rope_desc 
     const int64_t qs = stride_of(rope->q_row_stride, Hq, d), ks = stride_of(rope->k_row_stride, Hkv, d),
                   vs = stride_of(rope->v_row_stride, Hkv, d);
     if (qs < (int64_t)Hq * d || ks < (int64_t)Hkv * d || vs < (int64_t)Hkv * d || (qs | ks | vs) % 8) return AP_ERR_INVALID_ARG;
+    // (rows further apart than any memory: the byte offsets below and in the kernel would leave 64 bits)
+    const int64_t far = (int64_t)1 << 32;
+    if (qs > far || ks > far || vs > far) return AP_ERR_INVALID_ARG;
     if ((q == nullptr) != (q_rot == nullptr)) return AP_ERR_INVALID_ARG;
     if (pool->desc.device < 0) return AP_ERR_CUDA;
     const int64_t n = plan->info.n_new;

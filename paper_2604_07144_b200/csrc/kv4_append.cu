@@ -43,8 +43,8 @@ __global__ void __launch_bounds__(128) kv4_append_kernel(uint8_t *__restrict__ k
     uint4 k[NG], v[NG];
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
-        k[j] = __ldg(k_new + vec + 4 * j);
-        v[j] = __ldg(v_new + vec + 4 * j);
+        k[j] = __ldcg(k_new + vec + 4 * j);
+        v[j] = __ldcg(v_new + vec + 4 * j);
     }
     uint32_t kw[NG], vw[NG], ks[NG], vs[NG];
 #pragma unroll
@@ -80,20 +80,21 @@ __global__ void __launch_bounds__(128) kv4_append_kernel(uint8_t *__restrict__ k
     }
 }
 
-// A slice's words and steps -> its d / 32 vectors of eight bf16 values.
+// A slice's words and steps -> its d / 32 vectors of eight bf16 values.  (From L2: the kernel may have been resident while
+// the one before wrote them, when a line in L1 can be older than that.)
 template <int D>
 __device__ __forceinline__ void read_slice(const uint8_t *row_words, const uint8_t *row_steps, uint4 (&out)[kv4::Tile<D>::kGroups]) {
     constexpr int NG = kv4::Tile<D>::kGroups;
     uint32_t w[NG], s[NG / 2];
     if constexpr (NG == 4) {
-        const uint4 a = __ldg(reinterpret_cast<const uint4 *>(row_words));
-        const uint2 b = __ldg(reinterpret_cast<const uint2 *>(row_steps));
+        const uint4 a = __ldcg(reinterpret_cast<const uint4 *>(row_words));
+        const uint2 b = __ldcg(reinterpret_cast<const uint2 *>(row_steps));
         w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
         s[0] = b.x; s[1] = b.y;
     } else {
-        const uint2 a = __ldg(reinterpret_cast<const uint2 *>(row_words));
+        const uint2 a = __ldcg(reinterpret_cast<const uint2 *>(row_words));
         w[0] = a.x; w[1] = a.y;
-        s[0] = __ldg(reinterpret_cast<const uint32_t *>(row_steps));
+        s[0] = __ldcg(reinterpret_cast<const uint32_t *>(row_steps));
     }
 #pragma unroll
     for (int j = 0; j < NG; ++j) out[j] = kv4::dequantise8(w[j], (uint16_t)(j & 1 ? s[j / 2] >> 16 : s[j / 2] & 0xFFFFu));
@@ -153,8 +154,8 @@ __global__ void __launch_bounds__(256) kv_read_new_kernel(const uint4 *__restric
         return;
     }
     const int64_t o = (((int64_t)page * num_kv_heads + g) * kPageSize + slot) * chunks + c;
-    k_out[v] = k_pool[o];
-    v_out[v] = v_pool[o];
+    k_out[v] = __ldcg(k_pool + o);
+    v_out[v] = __ldcg(v_pool + o);
 }
 
 // Widens the listed pages to bf16 pages of the same layout as a bf16 pool's, page after page in the list's

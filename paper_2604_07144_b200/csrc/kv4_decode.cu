@@ -252,7 +252,7 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
             for (int gr = 0; gr < NG; ++gr) {
                 x[gr] = make_uint4(0, 0, 0, 0);
                 if (g < G)
-                    x[gr] = __ldg(reinterpret_cast<const uint4 *>(q + ((size_t)item.q_row * Hq + (size_t)kv_head * G + g) * D + 32 * gr + 8 * t));
+                    x[gr] = __ldcg(reinterpret_cast<const uint4 *>(q + ((size_t)item.q_row * Hq + (size_t)kv_head * G + g) * D + 32 * gr + 8 * t));
                 const uint32_t w[4] = {x[gr].x, x[gr].y, x[gr].z, x[gr].w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) amax = max(amax, max((w[i] << 16) & 0x7FFFFFFFu, w[i] & 0x7FFF0000u));

@@ -101,15 +101,16 @@ rope_append_kernel(const __grid_constant__ RopeParams rope, uint8_t *__restrict_
         if (threadIdx.x == 0) ptx::record_status(status, AP_ERR_BAD_BLOCK_TABLE);
         return;
     }
-    // A thread's first kAhead units are loaded ahead of the barrier that waits for the angles.
+    // A thread's first kAhead units are loaded ahead of the barrier that waits for the angles.  (From L2: this
+    // kernel was resident while its inputs were still being written, and they are read once.)
     uint4 x[kAhead], y[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
         const int id = threadIdx.x + i * step;
         if (id < n) {
             const Unit w = unit_of(id);
-            x[i] = w.src[w.c0];
-            y[i] = w.src[w.c1];
+            x[i] = __ldcg(w.src + w.c0);
+            y[i] = __ldcg(w.src + w.c1);
         }
     }
     __syncthreads();
@@ -125,7 +126,7 @@ rope_append_kernel(const __grid_constant__ RopeParams rope, uint8_t *__restrict_
     }
     for (int id = threadIdx.x + kAhead * step; id < n; id += step) {
         const Unit w = unit_of(id);
-        uint4 a = w.src[w.c0], b = w.src[w.c1];
+        uint4 a = __ldcg(w.src + w.c0), b = __ldcg(w.src + w.c1);
         if (w.turns) rotate(w.u, a, b);
         w.out[w.c0] = a;
         w.out[w.c1] = b;
@@ -147,7 +148,7 @@ rope_append_kernel(const __grid_constant__ RopeParams rope, uint8_t *__restrict_
                 const int u = id % kUnits, g = id / kUnits;
                 const uint4 *src = k_new + row * k_stride + (h0 + g) * kChunks;
                 const int c0 = first_chunk(u), c1 = second_chunk(u);
-                uint4 x = src[c0], y = src[c1];
+                uint4 x = __ldcg(src + c0), y = __ldcg(src + c1);
                 rotate(u, x, y);
                 k_rows[g * kChunks + c0] = x;
                 k_rows[g * kChunks + c1] = y;
@@ -158,7 +159,7 @@ rope_append_kernel(const __grid_constant__ RopeParams rope, uint8_t *__restrict_
                 const int i = base + (int)threadIdx.x, at = min(i, chunks - 1), g = at / kChunks, c = at % kChunks;
                 float ks, vs;
                 const uint32_t kw = kv4::quantise8(k_rows[at], ks);
-                const uint32_t vw = kv4::quantise8(__ldg(v_new + row * v_stride + (h0 + g) * kChunks + c), vs);
+                const uint32_t vw = kv4::quantise8(__ldcg(v_new + row * v_stride + (h0 + g) * kChunks + c), vs);
                 if (i < chunks) {
                     store(k_pool, h0 + g, c, kw, ks);
                     store(v_pool, h0 + g, c, vw, vs);

@@ -78,7 +78,7 @@ def test_rope_refusals():
     for bad in (dict(rotary_dim=0), dict(rotary_dim=-16), dict(rotary_dim=80), dict(rotary_dim=17), dict(base=0.0), dict(base=-1.0),
                 dict(base=float("inf")), dict(base=float("nan")), dict(amplitude=float("nan")), dict(interleaved=2),
                 dict(q_row_stride=8 * 64 - 8), dict(k_row_stride=64), dict(v_row_stride=2 * 64 + 4), dict(q=4096), dict(q_rot=4096),
-                dict(k_row_stride=-128)):
+                dict(k_row_stride=-128), dict(q_row_stride=1 << 40), dict(v_row_stride=2 ** 63 - 8)):
         assert status(**bad) == B.AP_ERR_INVALID_ARG, bad
     assert status(rope=0) == B.AP_ERR_INVALID_ARG
     assert status(rotary_dim=24) == B.AP_ERR_UNSUPPORTED
@@ -300,3 +300,62 @@ def test_layers_of_an_iteration_captured_in_a_graph(four_bit):
             ap.plan_destroy(p)
     for p in pools:
         ap.kv_pool_destroy(p)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("four_bit", [False, True], ids=["bf16", "4bit"])
+@pytest.mark.parametrize("shape,n", [((8, 2, 64), 3), ((32, 8, 128), 40)], ids=["small", "larger"])
+def test_back_to_back_launches_see_what_the_one_before_wrote(shape, n, four_bit):
+    """Kernels overlap the end of the one before them.  32 steps with data of their own through the same pages and the same
+    rotated queries, captured without a gap: append with rotation, read back, attention.  Each has to give what it
+    gives alone, bit for bit (the order of every sum is fixed)."""
+    import torch
+    hq, hkv, d = shape
+    b = _batch(shape, 31, [1] * n, [37 + 5 * i for i in range(n)])
+    gen = torch.Generator(device="cuda:0").manual_seed(5)
+    draw = lambda heads: torch.randn((32, n, heads, d), generator=gen, device="cuda:0").to(torch.bfloat16)
+    q, k, v = draw(hq), draw(hkv), draw(hkv)
+    if four_bit:
+        pool = ap.kv_pool_create_4bit(b.num_pages, hkv, d)
+        fill = ap.plan_create(pool, b.ctx_lens, b.ctx_lens, b.block_tables, hq)
+        rows = torch.randn((int(b.ctx_lens.sum()), hkv, d), generator=gen, device="cuda:0").to(torch.bfloat16)
+        ap.kv_append(pool, fill, rows, rows)
+    else:
+        planes = [to_dev(x) for x in (b.k_pool, b.v_pool)]
+        pool = ap.kv_pool_create(b.num_pages, hkv, d, *planes)
+    plan = ap.plan_create(pool, b.q_lens, b.ctx_lens, b.block_tables, hq)
+    ws = torch.empty(max(256, ap.plan_workspace_bytes(plan)), dtype=torch.uint8, device="cuda:0")
+    q_rot = torch.empty((n, hq, d), dtype=torch.bfloat16, device="cuda:0")
+
+    def steps(sync):
+        res = [torch.empty((32, n, h, d), dtype=torch.bfloat16, device="cuda:0") for h in (hkv, hkv, hq)]
+        lse = torch.empty((32, n, hq), dtype=torch.float32, device="cuda:0")
+
+        def run():
+            for i in range(32):
+                ap.kv_append_rope(pool, plan, k[i], v[i], q[i], q_rot)
+                sync()
+                ap.kv_read_new(pool, plan, res[0][i], res[1][i])
+                sync()
+                ap.attention_iteration(pool, plan, q_rot, res[2][i], lse[i], ws)
+                sync()
+        return run, res + [lse]
+    run, alone = steps(torch.cuda.synchronize)
+    run()
+    run, chained = steps(lambda: None)
+    g, st = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(g, stream=st):
+        run()
+    for _ in range(20):
+        for x in chained:
+            x.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert ap.last_device_status(pool) == 0
+        for x, y in zip(chained, alone):
+            assert torch.equal(x, y)
+    del g
+    if four_bit:
+        ap.plan_destroy(fill)
+    ap.plan_destroy(plan)
+    ap.kv_pool_destroy(pool)
