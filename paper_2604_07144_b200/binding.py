@@ -338,7 +338,8 @@ def plan_create_windowed(pool: KVPool, q_lens, ctx_lens, block_tables, num_q_hea
     """Plan of a sliding-window layer: a new token sees its last ``window`` keys (itself among them) and the
     first ``sinks`` keys of its context.  Used like a plan of :func:`plan_create`."""
     desc, keep = _batch_desc(q_lens, ctx_lens, block_tables, num_q_heads, softmax_scale)
-    win = WindowDesc(int(window), int(sinks))
+    # (a number past 32 bits would wrap; so long a window is the whole context, and one below 1 is refused)
+    win = WindowDesc(*(max(-1, min(int(x), 2 ** 31 - 1)) for x in (window, sinks)))
     h = ctypes.c_void_p()
     _check(load().ap_plan_create_windowed(ctypes.byref(h), pool.handle, ctypes.byref(desc), ctypes.byref(win),
                                           _stream(stream, pool.device)), "ap_plan_create_windowed")
@@ -409,6 +410,8 @@ def _row_stride(x) -> int:
     stride, shape = x.stride(), x.shape
     if len(shape) != 3 or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2]):
         raise ValueError("expected [rows, heads, head_dim] with a token's heads contiguous")
+    if shape[0] > 1 and stride[0] < shape[1] * shape[2]:
+        raise ValueError("rows overlap (an expanded tensor?)")
     return int(stride[0]) if shape[0] > 1 else 0
 
 
@@ -418,7 +421,7 @@ def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, r
     """Append with the rotary embedding: K rotated by its position, V as it is, ``q`` rotated into ``q_rot``.
     Tensors [rows, heads, head_dim] may be strided by row (slices of one projection)."""
     freq = None if inv_freq is None else np.ascontiguousarray(inv_freq, dtype=np.float64)
-    rotary = pool.head_dim if rotary_dim is None else int(rotary_dim)
+    rotary = pool.head_dim if rotary_dim is None else max(-1, min(int(rotary_dim), 2 ** 31 - 1))
     if freq is not None and freq.shape != (rotary // 2,):
         raise ValueError("inv_freq must have rotary_dim / 2 entries")
     if _row_stride(q_rot):
@@ -431,6 +434,8 @@ def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, r
 
 def kv_read_new(pool: KVPool, plan: Plan, k, v, stream=None) -> None:
     """The rows of the plan's new tokens, read back as the bf16 numbers the pool holds (or, in 4 bits, stands for)."""
+    if _row_stride(k) or _row_stride(v):
+        raise ValueError("k and v must be contiguous")
     _check(load().ap_kv_read_new(pool.handle, plan.handle, _ptr(k), _ptr(v), _stream(stream, pool.device)), "ap_kv_read_new")
 
 

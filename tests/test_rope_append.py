@@ -87,6 +87,25 @@ def test_rope_refusals():
     assert status(inv_freq=freq.ctypes.data, rotary_dim=32, base=0.0) == B.AP_ERR_CUDA       # base is not looked at
     with pytest.raises(ValueError):
         ap.kv_append_rope(pool, plan, 0, 0, inv_freq=np.ones(3))
+    for far in (2 ** 32 + 64, -2 ** 32 + 64):                            # would wrap to 64
+        with pytest.raises(ap.ApError) as e:
+            ap.kv_append_rope(pool, plan, 4096, 8192, rotary_dim=far)
+        assert e.value.status == B.AP_ERR_INVALID_ARG
+    import torch
+    row = torch.zeros((1, 2, 64), dtype=torch.bfloat16)
+    rows = torch.zeros((4, 4, 64), dtype=torch.bfloat16)
+    for bad in (row.expand(4, 2, 64), rows.transpose(0, 1), rows[:, :, ::2], rows[:, ::2]):  # overlapping rows, strided heads
+        with pytest.raises(ValueError):
+            ap.kv_append_rope(pool, plan, bad, rows)
+        with pytest.raises(ValueError):
+            ap.kv_append_rope(pool, plan, rows, rows, q=bad, q_rot=rows)
+        with pytest.raises(ValueError):
+            ap.kv_read_new(pool, plan, rows, bad)
+    for strided in (rows[:, :2], rows[::2]):                             # fine as inputs, not as results
+        with pytest.raises(ValueError):
+            ap.kv_append_rope(pool, plan, rows, rows, q=rows, q_rot=strided)
+        with pytest.raises(ValueError):
+            ap.kv_read_new(pool, plan, strided, rows)
     other = ap.kv_pool_create(64, 2, 64, device=-1)
     assert status(pool_=other) == B.AP_ERR_INVALID_ARG
     ap.plan_destroy(plan)

@@ -103,7 +103,7 @@ def test_windowed_plan_lists(window, sinks):
 def test_windowed_plan_refusals_and_predictions():
     pool = ap.kv_pool_create(64, 2, 64, device=-1)
     bt = np.arange(40, dtype=np.int32)[None]
-    for window, sinks in ((0, 0), (-1, 4), (4, -1)):
+    for window, sinks in ((0, 0), (-1, 4), (4, -1), (-2 ** 32 + 9, 0), (4, -2 ** 40)):
         with pytest.raises(ap.ApError) as e:
             ap.plan_create_windowed(pool, [1], [600], bt, 8, window, sinks)
         assert e.value.status == B.AP_ERR_INVALID_ARG
@@ -124,7 +124,7 @@ def test_windowed_plan_refusals_and_predictions():
     # the work figures count visible keys: 100 + 4 of a decode row
     plan = ap.plan_create_windowed(pool, [1], [600], bt, 8, 100, 4)
     full = ap.plan_create(pool, [1], [600], bt, 8)
-    wide = ap.plan_create_windowed(pool, [1], [600], bt, 8, 600, 4)
+    wide = ap.plan_create_windowed(pool, [1], [600], bt, 8, 2 ** 32 + 5, 2 ** 33)        # (not 5 and 0)
     pw, pf = ap.plan_predict(plan), ap.plan_predict(full)
     assert pw["decode_flops"] == 4 * 8 * 64 * 104 and pf["decode_flops"] == 4 * 8 * 64 * 600
     assert pw["decode_bytes"] < pf["decode_bytes"] and ap.plan_predict(wide) == pf
