@@ -115,10 +115,13 @@ int ap_kv_pool_create(ap_kv_pool **out, const ap_pool_desc *desc);
  * not below 2^120 in magnitude, stands for NaN.
  * Everything that takes a pool takes such a pool: plans (with a window too),
  * ap_kv_append, ap_kv_append_rope, ap_kv_read_new, ap_attention_iteration,
- * ap_kv_copy_pages (between 4-bit pools), ap_serving_iteration_host.  Decode and
- * prefill of a mixed iteration run one after the other (ap_kv_pool_set_side_by_side
- * has no effect).  A plan with prefill chunks needs workspace for the pages they
- * read, widened to bf16: 2 * 16 * head_dim * 2 bytes per page and kv head.
+ * ap_kv_copy_pages (between 4-bit pools), ap_serving_iteration_host.  In a mixed
+ * iteration decode has the whole GPU and the prefill units, on the pool's second
+ * stream, take the SMs as it leaves them (mode 0 of ap_kv_pool_set_side_by_side:
+ * on the caller's stream, behind it; the other modes do not differ, and
+ * ap_plan_info.side_by_side is 0).  A plan with prefill chunks needs workspace for
+ * the pages they read, widened to bf16: 2 * 16 * head_dim * 2 bytes per page and
+ * kv head.
  * A query element of 2^121 or more makes its head's result NaN.
  * ap_kv_pool_bytes_4bit: bytes of one plane; 0 if the description is invalid.
  */
@@ -464,7 +467,8 @@ int ap_selftest_wait_timeout(ap_kv_pool *pool, uint64_t limit_ns, int leave_coun
  * Per-kernel device timing for benchmarks.  While enabled, every kernel the
  * library launches for this pool (page copies and read-backs excepted) is bracketed
  * by CUDA events recorded on the launching stream; a rotated append counts as
- * append, a 4-bit pool's merge as decode and its widening of pages as prefill.  ap_profile_collect synchronises `stream`, adds up the
+ * append, a 4-bit pool's merge as part of its decode, its widening of pages as a
+ * prefill launch of its own.  ap_profile_collect synchronises `stream`, adds up the
  * elapsed times per kernel since the last enable/collect, and clears the
  * records.  Index: 0 kv_append, 1 decode split-K (which also performs the LSE
  * merge), 2 prefill, 3 the single launch that holds both parts of a mixed plan.

@@ -159,7 +159,7 @@ int max_decode_lists(const ap_kv_pool *pool) {
 int side_by_side_decode_ctas(const ap_kv_pool *pool, const ap_batch_desc *b, const WindowView &win, int d, int Hkv, int G,
                              int max_ctas) {
     const int mode = pool->side_by_side_mode;
-    if (mode == 0 || pool->four_bit) return 0;           // (a 4-bit pool's decode and prefill kernels run one after the other)
+    if (mode == 0 || pool->four_bit) return 0;           // (a 4-bit pool's decode has the whole GPU first)
     double decode_bytes = 0.0, w_p = 0.0;
     int64_t decode_rows = 0, prefill_seqs = 0;
     const double d_scale = (double)d / 128.0;
@@ -225,22 +225,39 @@ cudaError_t launch_attention_kernels(ap_kv_pool *pool, const ap_plan *plan, cons
     float *lse_part = plan->ws.bytes ? (float *)(ws + plan->ws.lse_part_off) : nullptr;
     cudaError_t e = cudaSuccess;
     if (pool->four_bit) {
-        if (plan->info.decode_items > 0) {
-            TimedScope timed(pool, AP_KERNEL_DECODE, st);
-            e = launch_kv4_decode(pool, plan, q, out, lse, o_part, lse_part, st);
-        }
-        if (e == cudaSuccess && plan->info.prefill_tiles > 0) {
+        const bool decode = plan->info.decode_items > 0, prefill = plan->info.prefill_tiles > 0;
+        void *k = ws + plan->ws.wide_k_off, *v = ws + plan->ws.wide_v_off;
+        CUtensorMap k_map, v_map;
+        if (prefill) {
             // prefill is bound by the tensor cores and reads a page's K/V once per unit: the pages are widened to
             // bf16 once, into the workspace, and the units read them from there
-            TimedScope timed(pool, AP_KERNEL_PREFILL, st);
-            void *k = ws + plan->ws.wide_k_off, *v = ws + plan->ws.wide_v_off;
             const ap_pool_desc &d = pool->desc;
-            CUtensorMap k_map, v_map;
             if (encode_pool_tensor_map(&k_map, k, plan->n_wide_pages, d.num_kv_heads, d.head_dim, 1) != AP_OK ||
                 encode_pool_tensor_map(&v_map, v, plan->n_wide_pages, d.num_kv_heads, d.head_dim, 1) != AP_OK)
                 return cudaErrorInvalidValue;
+            TimedScope timed(pool, AP_KERNEL_PREFILL, st);
             e = launch_kv4_widen(pool, plan, k, v, st);
-            if (e == cudaSuccess) e = launch_prefill(pool, plan, q, out, lse, k_map, v_map, plan->n_wide_pages, st);
+        }
+        // With both parts the prefill units go to the second stream, of least priority: they take the SMs as the decode
+        // blocks leave them, while the last of those and the merge are still running (8 chunks of 512 and 120 rows: 182
+        // us, 190-206 on one stream; in loops of seconds, under the power limit, equal).
+        const bool fork = plan->fork_prefill;
+        cudaStream_t prefill_st = fork ? pool->side_stream : st;
+        if (e == cudaSuccess && fork) e = cudaEventRecord(pool->fork_event, st);
+        if (e == cudaSuccess && decode) {
+            TimedScope timed(pool, AP_KERNEL_DECODE, st);
+            e = launch_kv4_decode(pool, plan, q, out, lse, o_part, lse_part, st);
+        }
+        if (e == cudaSuccess && prefill) {
+            if (fork) e = cudaStreamWaitEvent(prefill_st, pool->fork_event, 0);
+            if (e == cudaSuccess) {
+                TimedScope timed(pool, AP_KERNEL_PREFILL, prefill_st);
+                e = launch_prefill(pool, plan, q, out, lse, k_map, v_map, plan->n_wide_pages, prefill_st);
+            }
+            if (fork) {
+                if (e == cudaSuccess) e = cudaEventRecord(pool->join_event, prefill_st);
+                if (e == cudaSuccess) e = cudaStreamWaitEvent(st, pool->join_event, 0);
+            }
         }
         return e;
     }
@@ -877,6 +894,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     }
     plan->side_by_side = side_ctas > 0 && !items.empty() && !tiles.empty();
     plan->single_launch = plan->side_by_side && pool->single_launch;
+    plan->fork_prefill = pool->four_bit && pool->side_by_side_mode != 0 && !items.empty() && !tiles.empty();
     info.launches_attention = plan->single_launch ? 1 : (items.empty() ? 0 : 1) + (tiles.empty() ? 0 : 1);
     if (pool->four_bit)      // decode, merge, widen, prefill
         info.launches_attention += (merges.empty() ? 0 : 1) + (tiles.empty() ? 0 : 1);

@@ -150,6 +150,7 @@ struct ap_plan {
     int n_wide_pages = 0;        // 4-bit pool: pages that prefill units read, widened to bf16 in the workspace; the
                                  // units' block-table entries number them in this order
     ap::PlanWork work{};
+    bool fork_prefill = false;   // 4-bit pool: prefill on the second stream, behind the decode kernel's blocks
     bool side_by_side = false;   // decode confined to part of the GPU, prefill on the rest at the same time
     bool single_launch = false;  // ... and both in one launch (else: two kernels on two streams)
     ap::WorkspaceLayout ws{};

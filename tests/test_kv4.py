@@ -99,7 +99,7 @@ def test_4bit_plan_lists():
     b = _batch((32, 8, 128), 3, [1, 300, 1, 0, 5, 1], [700, 1000, 9000, 20, 40, 17], with_pool=False)
     for window, sinks in ((None, 0), (200, 20), (64, 0)):
         pool = ap.kv_pool_create_4bit(b.num_pages, 8, 128, device=-1)
-        ap.kv_pool_set_side_by_side(pool, 40)                  # no effect on a 4-bit pool
+        ap.kv_pool_set_side_by_side(pool, 40)                  # no difference to the default on a 4-bit pool
         plan = (ap.plan_create(pool, b.q_lens, b.ctx_lens, b.block_tables, 32) if window is None else
                 ap.plan_create_windowed(pool, b.q_lens, b.ctx_lens, b.block_tables, 32, window, sinks))
         ex, rows = ap.plan_export(plan), b.q_indptr
@@ -393,3 +393,56 @@ def test_without_lse_and_with_one_workspace_for_all_layers(four_bit):
         ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b, window, sinks)
         R.check(to_bits(d.out)[:b.n_new], ref[1], ref, f"layer {i}")
         d.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("window", [None, 40])
+def test_4bit_mixed_dispatches_agree_and_replay(window):
+    """Prefill on the second stream behind decode, or on the caller's: the same lists, so the same bits; eager from a stream of the
+    caller's, and captured.  The out rows are poisoned and read right behind the call, which has to cover both parts."""
+    import torch
+    b = _batch((16, 4, 128), 41, [1, 130, 1, 1, 64, 1] + [1] * 20, [700, 600, 33, 5000, 64, 1] + [90 + 41 * i for i in range(20)])
+    make = (lambda p: ap.plan_create(p, b.q_lens, b.ctx_lens, b.block_tables, 16)) if window is None else (
+        lambda p: ap.plan_create_windowed(p, b.q_lens, b.ctx_lens, b.block_tables, 16, window, 3))
+    gen = torch.Generator(device="cuda:0").manual_seed(3)
+    rows = torch.randn((int(b.ctx_lens.sum()), 4, 128), generator=gen, device="cuda:0").to(torch.bfloat16)
+    q = torch.randn((b.n_new, 16, 128), generator=gen, device="cuda:0").to(torch.bfloat16)
+    results = []
+    for mode in (0, 1):
+        pool = ap.kv_pool_create_4bit(b.num_pages, 4, 128)
+        ap.kv_pool_set_side_by_side(pool, mode)
+        fill = ap.plan_create(pool, b.ctx_lens, b.ctx_lens, b.block_tables, 16)
+        ap.kv_append(pool, fill, rows, -rows)
+        plan = make(pool)
+        info = ap.plan_get_info(plan)
+        assert info["side_by_side"] == 0 and info["decode_rows"] == 24 and info["prefill_tiles"] > 0
+        ws = torch.empty(max(256, ap.plan_workspace_bytes(plan)), dtype=torch.uint8, device="cuda:0")
+        out, lse = torch.empty_like(q), torch.empty((b.n_new, 16), device="cuda:0")
+        seen = [torch.empty_like(out), torch.empty_like(lse)]
+        st, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+
+        def step():
+            ws.fill_(0xFF)
+            out.fill_(float("nan"))
+            lse.fill_(float("nan"))
+            ap.attention_iteration(pool, plan, q, out, lse, ws)
+            seen[0].copy_(out)
+            seen[1].copy_(lse)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            step()
+        st.synchronize()
+        results.append([x.clone() for x in seen])
+        with torch.cuda.graph(g, stream=st):
+            step()
+        for _ in range(10):
+            seen[0].zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            assert ap.last_device_status(pool) == 0 and torch.equal(seen[0], results[-1][0]) and torch.equal(seen[1], results[-1][1])
+        del g
+        for p in (plan, fill):
+            ap.plan_destroy(p)
+        ap.kv_pool_destroy(pool)
+    assert torch.isfinite(results[0][0].float()).all() and torch.isfinite(results[0][1]).all()
+    assert all(torch.equal(x, y) for x, y in zip(*results))
