@@ -402,17 +402,24 @@ def kv_append(pool: KVPool, plan: Plan, k_new, v_new, stream=None) -> None:
 
 def _row_stride(x) -> int:
     """Elements from one row of a [rows, heads, head_dim] tensor to the next (0: contiguous, or not a tensor)."""
+    if x is None:
+        return 0
     try:
-        if x is None or x.is_contiguous():
+        if x.is_contiguous():
             return 0
+        row, head, one = x.stride()
+        n, heads, dim = x.shape
     except AttributeError:                   # an address
         return 0
-    stride, shape = x.stride(), x.shape
-    if len(shape) != 3 or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2]):
+    except ValueError:
+        one = n = heads = dim = row = head = 0
+    if one != 1 or (heads > 1 and head != dim):
         raise ValueError("expected [rows, heads, head_dim] with a token's heads contiguous")
-    if shape[0] > 1 and stride[0] < shape[1] * shape[2]:
+    if n < 2:
+        return 0
+    if row < heads * dim:
         raise ValueError("rows overlap (an expanded tensor?)")
-    return int(stride[0]) if shape[0] > 1 else 0
+    return row
 
 
 def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, rotary_dim: Optional[int] = None,
@@ -426,7 +433,7 @@ def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, r
         raise ValueError("inv_freq must have rotary_dim / 2 entries")
     if _row_stride(q_rot):
         raise ValueError("q_rot must be contiguous")
-    desc = RopeDesc(rotary, int(bool(interleaved)), float(base), _ptr(freq), float(amplitude), _row_stride(q),
+    desc = RopeDesc(rotary, 1 if interleaved else 0, base, None if freq is None else freq.ctypes.data, amplitude, _row_stride(q),
                     _row_stride(k_new), _row_stride(v_new))
     _check(load().ap_kv_append_rope(pool.handle, plan.handle, ctypes.byref(desc), _ptr(q), _ptr(k_new), _ptr(v_new),
                                     _ptr(q_rot), _stream(stream, pool.device)), "ap_kv_append_rope")
