@@ -21,6 +21,24 @@ __device__ __forceinline__ void row_and_head(int64_t rh, int num_kv_heads, int64
     }
 }
 
+// Plain loads, not through the read-only path: the kernel was resident while the one before still wrote this data, and
+// what the wait for that kernel makes visible is what ordinary loads see.
+__device__ __forceinline__ uint4 load16(const void *p) {
+    uint4 v;
+    asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 load8(const void *p) {
+    uint2 v;
+    asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t load4(const void *p) {
+    uint32_t v;
+    asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
 // One thread quantises its slice of a K row and of the V row; a quad shares its groups' maxima by shuffle and its
 // first lane stores the steps.  All loads go out first: 2 d / 32 of 16 bytes a thread.
 template <int D>
@@ -43,8 +61,8 @@ __global__ void __launch_bounds__(128) kv4_append_kernel(uint8_t *__restrict__ k
     uint4 k[NG], v[NG];
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
-        k[j] = __ldcg(k_new + vec + 4 * j);
-        v[j] = __ldcg(v_new + vec + 4 * j);
+        k[j] = load16(k_new + vec + 4 * j);
+        v[j] = load16(v_new + vec + 4 * j);
     }
     uint32_t kw[NG], vw[NG], ks[NG], vs[NG];
 #pragma unroll
@@ -80,21 +98,20 @@ __global__ void __launch_bounds__(128) kv4_append_kernel(uint8_t *__restrict__ k
     }
 }
 
-// A slice's words and steps -> its d / 32 vectors of eight bf16 values.  (From L2: the kernel may have been resident while
-// the one before wrote them, when a line in L1 can be older than that.)
+// A slice's words and steps -> its d / 32 vectors of eight bf16 values.
 template <int D>
 __device__ __forceinline__ void read_slice(const uint8_t *row_words, const uint8_t *row_steps, uint4 (&out)[kv4::Tile<D>::kGroups]) {
     constexpr int NG = kv4::Tile<D>::kGroups;
     uint32_t w[NG], s[NG / 2];
     if constexpr (NG == 4) {
-        const uint4 a = __ldcg(reinterpret_cast<const uint4 *>(row_words));
-        const uint2 b = __ldcg(reinterpret_cast<const uint2 *>(row_steps));
+        const uint4 a = load16(row_words);
+        const uint2 b = load8(row_steps);
         w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
         s[0] = b.x; s[1] = b.y;
     } else {
-        const uint2 a = __ldcg(reinterpret_cast<const uint2 *>(row_words));
+        const uint2 a = load8(row_words);
         w[0] = a.x; w[1] = a.y;
-        s[0] = __ldcg(reinterpret_cast<const uint32_t *>(row_steps));
+        s[0] = load4(row_steps);
     }
 #pragma unroll
     for (int j = 0; j < NG; ++j) out[j] = kv4::dequantise8(w[j], (uint16_t)(j & 1 ? s[j / 2] >> 16 : s[j / 2] & 0xFFFFu));
@@ -154,8 +171,8 @@ __global__ void __launch_bounds__(256) kv_read_new_kernel(const uint4 *__restric
         return;
     }
     const int64_t o = (((int64_t)page * num_kv_heads + g) * kPageSize + slot) * chunks + c;
-    k_out[v] = __ldcg(k_pool + o);
-    v_out[v] = __ldcg(v_pool + o);
+    k_out[v] = load16(k_pool + o);
+    v_out[v] = load16(v_pool + o);
 }
 
 // Widens the listed pages to bf16 pages of the same layout as a bf16 pool's, page after page in the list's
