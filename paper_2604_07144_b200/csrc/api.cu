@@ -239,8 +239,8 @@ cudaError_t launch_attention_kernels(ap_kv_pool *pool, const ap_plan *plan, cons
             e = launch_kv4_widen(pool, plan, k, v, st);
         }
         // With both parts the prefill units go to the second stream, of least priority: they take the SMs as the decode
-        // blocks leave them, while the last of those and the merge are still running (8 chunks of 512 and 120 rows: 182
-        // us, 190-206 on one stream; in loops of seconds, under the power limit, equal).
+        // blocks leave them, while the last of those and the merge are still running (8 chunks of 512 and 120 rows:
+        // 184.7 us, 193.0 on one stream; in loops of seconds, under the power limit, equal).
         const bool fork = plan->fork_prefill;
         cudaStream_t prefill_st = fork ? pool->side_stream : st;
         if (e == cudaSuccess && fork) e = cudaEventRecord(pool->fork_event, st);
