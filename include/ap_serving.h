@@ -122,7 +122,8 @@ int ap_kv_pool_create(ap_kv_pool **out, const ap_pool_desc *desc);
  * ap_plan_info.side_by_side is 0).  A plan with prefill chunks needs workspace for
  * the pages they read, widened to bf16: 2 * 16 * head_dim * 2 bytes per page and
  * kv head.
- * A query element of 2^121 or more makes its head's result NaN.
+ * Decode rows: a query element of 2^121 or more (with a softmax_scale above 2, of
+ * 2^113 / softmax_scale or more) makes its head's result NaN.
  * ap_kv_pool_bytes_4bit: bytes of one plane; 0 if the description is invalid.
  */
 size_t ap_kv_pool_bytes_4bit(const ap_pool_desc *desc);

@@ -261,16 +261,19 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
             amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
             const int a = min(max(120 + 127 - (int)(amax >> 23), 7), 126);
             const float up = __int_as_float((a + 127) << 23);                          // 2^a
+            const float up_off = up * -7.3468396926392969e-40f;                        // -8 2^(a - 133) = -2^(a - 130)
             const float f = scale_log2 * __int_as_float((133 - a + 127) << 23);        // scale log2(e) 2^(133 - a)
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
                 const uint32_t w[4] = {x[gr].x, x[gr].y, x[gr].z, x[gr].w};
+                // (sum q is formed of the queries as they are: 32 scaled ones of 2^123 and more would overflow it)
                 float e[8], sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    e[2 * i] = __uint_as_float(w[i] << 16) * up;
-                    e[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u) * up;
-                    sum += e[2 * i] + e[2 * i + 1];
+                    const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xFFFF0000u);
+                    e[2 * i] = lo * up;
+                    e[2 * i + 1] = hi * up;
+                    sum += lo + hi;
                 }
                 qf[gr][0] = pack_bf16x2(e[0], e[4]);
                 qf[gr][1] = pack_bf16x2(e[1] * 0.0625f, e[5] * 0.0625f);
@@ -280,7 +283,7 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
                 // -8 sum q of this group in three bf16 parts (24 bits), in the units of the accumulators; element
                 // gr & 1 of the B registers whose k indices the part's steps have in the offset product
-                const float part0 = sum * -7.3468396926392969e-40f;                     // -8 2^-133 = -2^-130
+                const float part0 = sum * up_off;
                 const float hi = __uint_as_float(__float_as_uint(part0) & 0xFFFF0000u), rest = part0 - hi;
                 const float mid = __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u), lo = rest - mid;
                 auto put = [&](uint32_t &reg, float v) { reg |= (pack_bf16x2(v, 0.f) & 0xFFFFu) << (16 * (gr & 1)); };

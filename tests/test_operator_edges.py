@@ -1,0 +1,106 @@
+"""Edges of the operators on paged pools: values of every size, what masked keys may hold, what a NaN does."""
+import numpy as np
+import pytest
+
+import paper_2604_07144_b200 as ap
+from paper_2604_07144_b200 import workloads as W
+
+import kv4_reference as Q
+import operator_reference as R
+from harness import to_bits, to_dev
+
+
+def _batch(shape, seed, q_lens, ctx_lens, with_pool=True):
+    return W._assemble(f"edges_{seed}", shape, W.make_rng(seed), np.asarray(q_lens, np.int32), np.asarray(ctx_lens, np.int32),
+                       1.3, with_pool=with_pool)
+
+
+def _times(bits, factor):
+    """bf16 bits of the values times a power of two; slots without a token stay as they are."""
+    scaled = W.f32_to_bf16_bits((W.bf16_bits_to_f64(bits) * factor).astype(np.float32))
+    return np.where(bits == W.CANARY, bits, scaled)
+
+
+def _put_row(plane, page, slot, bits, four_bit):
+    if four_bit:
+        Q.put(plane, np.array([page]), np.array([slot]), bits[None])
+    else:
+        plane[page, :, slot] = bits
+
+
+def _planes(batch, four_bit):
+    """(K, V) planes as numpy, with the batch's new tokens in place."""
+    planes = list(Q.planes_of(batch)) if four_bit else [batch.k_pool.copy(), batch.v_pool.copy()]
+    page, slot = Q.new_slots(batch)
+    for plane, new in zip(planes, (batch.k_new, batch.v_new)):
+        for i in range(batch.n_new):
+            _put_row(plane, page[i], slot[i], new[i], four_bit)
+    return planes
+
+
+def _attend(batch, planes, four_bit, window=None, sinks=0):
+    """(out bits, lse, k, v): the library's attention over the planes, and the values they stand for in float64."""
+    make = None if window is None else (lambda pool: ap.plan_create_windowed(
+        pool, batch.q_lens, batch.ctx_lens, batch.block_tables, batch.num_q_heads, window, sinks))
+    dev = R.Device(batch, make, k_plane=planes[0], v_plane=planes[1], four_bit=four_bit)
+    try:
+        dev.attend()
+        out, lse = dev.results()
+    finally:
+        dev.close()
+    k, v = (Q.values(p, batch.head_dim) if four_bit else W.bf16_bits_to_f64(p) for p in planes)
+    return out, lse, k, v
+
+
+def _check_of_any_size(out_bits, lse, ref, longest, what):
+    """operator_reference.check without its absolute slack: |out - ref| <= (2^-8 + 2e-4) A plus half an ulp of bf16 at ref,
+    which is never below half a subnormal's, 2^-134; plus longest 2^-149 for sums of at most `longest` products that may
+    round to fp32's subnormals, each addition and each product by 2^-150."""
+    ref_out, ref_lse, absw = ref
+    got = W.bf16_bits_to_f64(out_bits)
+    assert np.isfinite(got).all() and np.isfinite(lse).all(), f"{what}: non-finite output"
+    a = np.abs(ref_out)
+    half_ulp = np.maximum(np.where(a > 0, 2.0 ** (np.floor(np.log2(np.maximum(a, 1e-300))) - 8), 0.0), 2.0 ** -134)
+    excess = np.abs(got - ref_out) - (absw * (2.0 ** -8 + 2e-4) + half_ulp + longest * 2.0 ** -149)
+    i = np.unravel_index(np.argmax(excess), excess.shape)
+    assert excess[i] <= 0, f"{what}: {got[i]} against {ref_out[i]} at {i} (A {absw[i]})"
+    lerr = np.abs(lse - ref_lse)
+    assert (lerr <= 2e-4 + 1e-5 * np.abs(ref_lse)).all(), f"{what}: lse off by {lerr.max()}"
+
+
+# ------------------------------------------------------------- every size --
+
+SIZES = [(0, 0, 100), (0, 0, -100), (0, 0, 117), (0, 0, -118), (0, 0, -127), (100, -100, 0), (-100, 100, 0), (117, -117, 117),
+         (-117, 113, -117)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(8, 2, 64), (6, 2, 128)], ids=str)
+@pytest.mark.parametrize("k_log2,q_log2,v_log2", SIZES)
+def test_4bit_attention_over_values_of_one_size(shape, k_log2, q_log2, v_log2):
+    """Every value of a plane, new tokens included, near one power of two, so that steps are near 2^-130 .. 2^117 and nothing
+    larger hides them; q by the inverse of K's size, so that scores stay those of N(0, 1) rows.  Decode and prefill
+    rows, with and without a window."""
+    b = _batch(shape, 61, [1, 1, 1, 20, 150], [200, 37, 2100, 64, 300])
+    b.k_pool, b.v_pool, b.q = _times(b.k_pool, 2.0 ** k_log2), _times(b.v_pool, 2.0 ** v_log2), _times(b.q, 2.0 ** q_log2)
+    b.k_new, b.v_new = _times(b.k_new, 2.0 ** k_log2), _times(b.v_new, 2.0 ** v_log2)
+    planes = _planes(b, True)
+    for window, sinks in ((None, 0), (90, 4)):
+        out, lse, k, v = _attend(b, planes, True, window, sinks)
+        ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b, window, sinks)
+        _check_of_any_size(out, lse, ref, 2100, f"window {window}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [2.0 ** 114, 2.0 ** 116, 2.0 ** 118, 2.0 ** 121 * (1 - 2.0 ** -8)], ids=lambda v: f"{v:.3g}")
+def test_4bit_queries_up_to_the_stated_limit(value):
+    """All elements of a query equal, just below the 2^121 from which a head's result is NaN; K as much smaller.  Scores: at most
+    d products of 8 |k'| (k' ~ N(0, 1) / 8), as for N(0, 1) rows."""
+    for shape in ((8, 2, 64), (6, 2, 128)):
+        b = _batch(shape, 62, [1, 1, 1, 40], [200, 33, 1500, 90])
+        b.q[:] = W.f32_to_bf16_bits(np.array([value], np.float32))[0]
+        b.k_pool, b.k_new = (_times(x, 2.0 ** -np.ceil(np.log2(value))) for x in (b.k_pool, b.k_new))
+        planes = _planes(b, True)
+        out, lse, k, v = _attend(b, planes, True)
+        ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b)
+        _check_of_any_size(out, lse, ref, 1500, f"q {value}")
