@@ -88,7 +88,8 @@ __device__ __forceinline__ uint32_t low_bits(int n) {
 // 2^x for two values on the FMA pipe (relieves the special-function unit, which would otherwise
 // bound the softmax): x = n + f with n = round(x), f in [-0.5, 0.5]; 2^f by a cubic fitted for
 // relative error (7.7e-5, well inside the bf16 rounding P gets anyway); 2^n by adding n to the
-// exponent field.  x is clamped at -125 so the exponent cannot wrap (2^-125 is zero for our purposes).
+// exponent field.  x is clamped at -125 so the exponent cannot wrap, and what 2^-125 comes out as is taken off again:
+// a masked score (x = -inf) weighs exactly 0, as on the special-function unit, whatever its V holds.
 // kFine: a quartic instead (2.7e-6), one more packed FMA; short windows average the cubic's error over few keys, and
 // it would show in lse.
 template <bool kFine>
@@ -99,20 +100,22 @@ __device__ __forceinline__ float2 exp2_poly2(float2 x) {
     const float2 t = __fadd2_rn(x, make_float2(kMagic, kMagic));
     const float2 n = __fadd2_rn(t, make_float2(-kMagic, -kMagic));
     const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
+    constexpr float kOne = kFine ? 0.9999993f : 0.99992894f;           // the polynomial at f = 0
     float2 p;
     if constexpr (kFine) {
         p = __ffma2_rn(f, make_float2(0.00957011f, 0.00957011f), make_float2(0.0559179f, 0.0559179f));
         p = __ffma2_rn(p, f, make_float2(0.24024744f, 0.24024744f));
         p = __ffma2_rn(p, f, make_float2(0.6931218f, 0.6931218f));
-        p = __ffma2_rn(p, f, make_float2(0.9999993f, 0.9999993f));
+        p = __ffma2_rn(p, f, make_float2(kOne, kOne));
     } else {
         p = __ffma2_rn(f, make_float2(0.05508868f, 0.05508868f), make_float2(0.24260405f, 0.24260405f));
         p = __ffma2_rn(p, f, make_float2(0.69327624f, 0.69327624f));
-        p = __ffma2_rn(p, f, make_float2(0.99992894f, 0.99992894f));
+        p = __ffma2_rn(p, f, make_float2(kOne, kOne));
     }
     p.x = __int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23));
     p.y = __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23));
-    return p;
+    constexpr float kClamped = kOne * 0x1p-125f;
+    return __fadd2_rn(p, make_float2(-kClamped, -kClamped));
 }
 
 // Shared-memory matrix descriptor for tcgen05.mma, 128-byte swizzle:

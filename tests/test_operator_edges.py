@@ -104,3 +104,23 @@ def test_4bit_queries_up_to_the_stated_limit(value):
         out, lse, k, v = _attend(b, planes, True)
         ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b)
         _check_of_any_size(out, lse, ref, 1500, f"q {value}")
+
+
+# ----------------------------------------------------------- masked places --
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("four_bit", [False, True], ids=["bf16", "4bit"])
+@pytest.mark.parametrize("window,sinks", [(None, 0), (24, 3)])
+def test_a_masked_key_weighs_nothing_however_large_its_v(four_bit, window, sinks):
+    """Rows of a block that do not see a key, which other rows of the same block see, get none of its V of 2^119."""
+    for shape in ((6, 2, 128), (8, 2, 64)):
+        b = _batch(shape, 63, [128, 200], [128, 500])
+        planes = _planes(b, four_bit)
+        big = np.full((shape[1], shape[2]), W.f32_to_bf16_bits(np.array([2.0 ** 119], np.float32))[0], np.uint16)
+        large = {0: range(64, 128), 1: range(400, 432)}
+        for s, keys in large.items():
+            for j in keys:
+                _put_row(planes[1], b.block_tables[s, j // 16], j % 16, big, four_bit)
+        out, lse, k, v = _attend(b, planes, four_bit, window, sinks)
+        ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b, window, sinks)
+        _check_of_any_size(out, lse, ref, 500, f"window {window}")
