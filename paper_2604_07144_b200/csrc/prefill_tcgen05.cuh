@@ -73,10 +73,16 @@ struct PrefillCfg {
     static constexpr uint32_t kColO = 256;    // + 128 * tile
 };
 
-// three-input maximum (one instruction on sm_100)
+// Maxima that a NaN wins: a visible NaN score has to reach the row's reference maximum and through it every weight,
+// because the clamp of exp2_poly2 would drop it.  Three inputs are one instruction on sm_100.
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float max2(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
 
@@ -392,7 +398,7 @@ __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUt
                             float v = __uint_as_float(sreg[c][i]);
                             if (tok0 + c * 32 + i > my_pos) v = -INFINITY;
                             sreg[c][i] = __float_as_uint(v);
-                            mx = fmaxf(mx, v);
+                            mx = max2(mx, v);
                         }
                 } else {
 #pragma unroll
@@ -408,8 +414,9 @@ __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUt
                     if (!wait_or_abort(&pv_done[x], (uint32_t)(j - 1) & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
                     tcgen05_fence_after();
                 }
-                const float m_new = fmaxf(m_used, mx);
-                const bool moved = (m_new - m_used) * scale_log2 > kRescaleThreshold;   // true while m_used = -inf
+                const float m_new = max2(m_used, mx);
+                const bool moved = (m_new - m_used) * scale_log2 > kRescaleThreshold ||   // true while m_used = -inf
+                                   (kWin && m_new != m_new);
                 const bool rescale = __any_sync(0xffffffffu, moved);
                 float alpha = 1.f;
                 if (rescale) {
@@ -419,7 +426,10 @@ __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUt
                     if (j > 0) rescale_o<D>(lane_addr + col_o, alpha);
                 }
                 // (with a window a row may see no key of the unit's first steps: its scores stay -inf, the weights 0)
-                const float ms = kWin && m_used == -INFINITY ? 0.f : m_used * scale_log2;
+                // (without one the maximum is finite, or the row NaN: m_new - m_new says so, 4.5 us of 172 cheaper than a
+                // test beside the one above)
+                const float ms = kWin ? (m_used == -INFINITY ? 0.f : m_used * scale_log2)
+                                      : fmaf(m_used, scale_log2, m_new - m_new);
                 const float2 sc2 = make_float2(scale_log2, scale_log2), nms2 = make_float2(-ms, -ms);
                 float2 sum2 = make_float2(0.f, 0.f), sum2b = make_float2(0.f, 0.f);
 #pragma unroll

@@ -124,3 +124,33 @@ def test_a_masked_key_weighs_nothing_however_large_its_v(four_bit, window, sinks
         out, lse, k, v = _attend(b, planes, four_bit, window, sinks)
         ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b, window, sinks)
         _check_of_any_size(out, lse, ref, 500, f"window {window}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("four_bit", [False, True], ids=["bf16", "4bit"])
+@pytest.mark.parametrize("window", [None, 40])
+def test_a_visible_nan_key_makes_its_rows_nan_and_no_others(four_bit, window):
+    """K of one token is NaN: every row that sees the token is NaN in out and lse, every other row is as if it were not there.
+    The token in turn at each place of a 16-token page (the softmax treats keys differently by their place)."""
+    shape = (6, 2, 128)
+    b = _batch(shape, 64, [1, 70, 1, 150], [100, 90, 700, 400])
+    nan = np.full((2, 128), 0x7FC0, np.uint16)
+    clean = _planes(b, four_bit)
+    for place in range(16):
+        planes = [p.copy() for p in clean]
+        bad = {0: 80 + place, 1: 32 + place, 2: 672 + place, 3: 320 + place}
+        for s, j in bad.items():
+            _put_row(planes[0], b.block_tables[s, j // 16], j % 16, nan, four_bit)
+        out, lse, _, v = _attend(b, planes, four_bit, window)
+        got, row = W.bf16_bits_to_f64(out), 0
+        k = Q.values(clean[0], 128) if four_bit else W.bf16_bits_to_f64(clean[0])
+        ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b, window)
+        for s in range(4):
+            n, ctx = int(b.q_lens[s]), int(b.ctx_lens[s])
+            sees = R.visible(n, ctx, window)[:, bad[s]]
+            o, l = got[row:row + n], lse[row:row + n]
+            assert np.isnan(o[sees]).all() and np.isnan(l[sees]).all(), f"place {place}, sequence {s}"
+            part = [x[row:row + n][~sees] for x in ref]
+            if not sees.all():
+                R.check(out[row:row + n][~sees], l[~sees], part, f"place {place}, sequence {s}")
+            row += n
