@@ -9,6 +9,10 @@ namespace ap {
 
 namespace {
 
+using ptx::load16;
+using ptx::load4;
+using ptx::load8;
+
 // A thread has elements 32 g + 8 t .. + 7 of every group g of one head row, for its t: the words of a row that
 // are stored next to one another (16 bytes at d = 128).  The four lanes of a quad have the row's four t.
 __device__ __forceinline__ void row_and_head(int64_t rh, int num_kv_heads, int64_t &row, int &head) {
@@ -19,24 +23,6 @@ __device__ __forceinline__ void row_and_head(int64_t rh, int num_kv_heads, int64
         row = rh / num_kv_heads;
         head = (int)(rh % num_kv_heads);
     }
-}
-
-// Plain loads, not through the read-only path: the kernel was resident while the one before still wrote this data, and
-// what the wait for that kernel makes visible is what ordinary loads see.
-__device__ __forceinline__ uint4 load16(const void *p) {
-    uint4 v;
-    asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint2 load8(const void *p) {
-    uint2 v;
-    asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint32_t load4(const void *p) {
-    uint32_t v;
-    asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
 }
 
 // One thread quantises its slice of a K row and of the V row; a quad shares its groups' maxima by shuffle and its

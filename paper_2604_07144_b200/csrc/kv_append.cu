@@ -32,8 +32,9 @@ __global__ void __launch_bounds__(256) kv_append_kernel(uint4 *__restrict__ k_po
         return;
     }
     const int64_t o = (((int64_t)page * num_kv_heads + g) * kPageSize + slot) * chunks_per_row + c;
-    k_pool[o] = __ldg(k_new + v);
-    v_pool[o] = __ldg(v_new + v);
+    const uint4 k = ptx::load16(k_new + v), w = ptx::load16(v_new + v);
+    k_pool[o] = k;
+    v_pool[o] = w;
 }
 
 }  // namespace

@@ -24,6 +24,28 @@ __device__ __forceinline__ void record_status(int *status, int code) {
     __threadfence_system();
 }
 
+// ------------------------------------------------------------ global loads --
+
+// Ordinary loads of what a step's kernels and the caller's write (inputs, pool planes).  Not through the read-only
+// path (__ldg, or what the compiler makes of const __restrict__): the kernel was resident while the one before still
+// wrote this data, and what the wait for that kernel makes visible is what ordinary loads see.  Plan lists, uploaded
+// before any kernel of the step, may take either.
+__device__ __forceinline__ uint4 load16(const void *p) {
+    uint4 v;
+    asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 load8(const void *p) {
+    uint2 v;
+    asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t load4(const void *p) {
+    uint32_t v;
+    asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
 // ---------------------------------------------------------------- mbarrier --
 
 __device__ __forceinline__ void mbar_init(uint64_t *bar, uint32_t count) {

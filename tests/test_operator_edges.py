@@ -154,3 +154,70 @@ def test_a_visible_nan_key_makes_its_rows_nan_and_no_others(four_bit, window):
             if not sees.all():
                 R.check(out[row:row + n][~sees], l[~sees], part, f"place {place}, sequence {s}")
             row += n
+
+
+# --------------------------------------------------------- overlapped launches --
+
+def test_only_plan_lists_are_read_through_the_read_only_path():
+    """A kernel may be resident while the one before still writes its inputs, and the read-only path may then hand out
+    stale lines: __ldg is for lists that were uploaded before any kernel of the step."""
+    import os
+    import re
+    from paper_2604_07144_b200 import build
+    lists = ("append_dst", "positions", "pages", "pairs", "cta_begin", "cur_bt", "bt", "bt_flat", "src", "&merges")
+    found = 0
+    for name in sorted(os.listdir(build.CSRC)):
+        text = re.sub(r"//.*", "", open(os.path.join(build.CSRC, name)).read())
+        for arg in re.findall(r"__ldg\(\s*(&?\w+)", text):
+            assert arg in lists, f"{name}: __ldg({arg} ...)"
+            found += 1
+    assert found >= 10
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,n", [((8, 2, 64), 3), ((32, 8, 128), 40), ((32, 8, 128), 900)], ids=str)
+def test_rows_read_back_from_one_pool_and_appended_to_another_at_once(shape, n):
+    """append to a 4-bit pool -> read back -> append to a bf16 pool -> read back, 24 steps with new data through the same
+    buffers, captured without a gap: the rows in the bf16 pool are those that the 4-bit pool stands for."""
+    import torch
+    hq, hkv, d = shape
+    b = _batch(shape, 65, [1] * n, [1 + (7 * i) % 60 for i in range(n)], with_pool=False)
+    gen = torch.Generator(device="cuda:0").manual_seed(7)
+    k, v = (torch.randn((24, n, hkv, d), generator=gen, device="cuda:0").to(torch.bfloat16) for _ in range(2))
+    pools = [ap.kv_pool_create_4bit(b.num_pages, hkv, d), ap.kv_pool_create(b.num_pages, hkv, d)]
+    plans = [ap.plan_create(p, b.q_lens, b.ctx_lens, b.block_tables, hq) for p in pools]
+    mid = [torch.empty((n, hkv, d), dtype=torch.bfloat16, device="cuda:0") for _ in range(2)]
+
+    def steps(sync):
+        res = [torch.zeros((24, n, hkv, d), dtype=torch.bfloat16, device="cuda:0") for _ in range(2)]
+
+        def run():
+            for i in range(24):
+                ap.kv_append(pools[0], plans[0], k[i], v[i])
+                sync()
+                ap.kv_read_new(pools[0], plans[0], mid[0], mid[1])
+                sync()
+                ap.kv_append(pools[1], plans[1], mid[0], mid[1])
+                sync()
+                ap.kv_read_new(pools[1], plans[1], res[0][i], res[1][i])
+                sync()
+        return run, res
+    run, alone = steps(torch.cuda.synchronize)
+    run()
+    assert not torch.equal(alone[0][0], alone[0][1])
+    run, chained = steps(lambda: None)
+    g, st = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(g, stream=st):
+        run()
+    for _ in range(20):
+        for x in chained + mid:
+            x.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(ap.last_device_status(p) == 0 for p in pools)
+        assert all(torch.equal(x, y) for x, y in zip(chained, alone))
+    del g
+    for p in plans:
+        ap.plan_destroy(p)
+    for p in pools:
+        ap.kv_pool_destroy(p)
