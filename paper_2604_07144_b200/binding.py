@@ -179,6 +179,14 @@ def _ptr(x) -> Optional[int]:
     raise TypeError(f"cannot take the address of {type(x)}")
 
 
+def _contiguous(*tensors) -> None:
+    """Refuses tensors that the library, which gets an address only, would read or write in the wrong places."""
+    for x in tensors:
+        test = getattr(x, "is_contiguous", None)
+        if not (test() if test is not None else not isinstance(x, np.ndarray) or x.flags.c_contiguous):
+            raise ValueError("expected a contiguous tensor")
+
+
 _raw_stream = None        # torch's accessor of the current stream's handle, once torch has initialised CUDA
 
 
@@ -396,6 +404,7 @@ def plan_export(plan: Plan) -> dict:
 # ---------------------------------------------------------------- kernels --
 
 def kv_append(pool: KVPool, plan: Plan, k_new, v_new, stream=None) -> None:
+    _contiguous(k_new, v_new)
     _check(load().ap_kv_append(pool.handle, plan.handle, _ptr(k_new), _ptr(v_new), _stream(stream, pool.device)),
            "ap_kv_append")
 
@@ -431,8 +440,7 @@ def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, r
     rotary = pool.head_dim if rotary_dim is None else max(-1, min(int(rotary_dim), 2 ** 31 - 1))
     if freq is not None and freq.shape != (rotary // 2,):
         raise ValueError("inv_freq must have rotary_dim / 2 entries")
-    if _row_stride(q_rot):
-        raise ValueError("q_rot must be contiguous")
+    _contiguous(q_rot)
     desc = RopeDesc(rotary, 1 if interleaved else 0, base, None if freq is None else freq.ctypes.data, amplitude, _row_stride(q),
                     _row_stride(k_new), _row_stride(v_new))
     _check(load().ap_kv_append_rope(pool.handle, plan.handle, ctypes.byref(desc), _ptr(q), _ptr(k_new), _ptr(v_new),
@@ -441,8 +449,7 @@ def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, r
 
 def kv_read_new(pool: KVPool, plan: Plan, k, v, stream=None) -> None:
     """The rows of the plan's new tokens, read back as the bf16 numbers the pool holds (or, in 4 bits, stands for)."""
-    if _row_stride(k) or _row_stride(v):
-        raise ValueError("k and v must be contiguous")
+    _contiguous(k, v)
     _check(load().ap_kv_read_new(pool.handle, plan.handle, _ptr(k), _ptr(v), _stream(stream, pool.device)), "ap_kv_read_new")
 
 
@@ -458,6 +465,7 @@ def kv_copy_pages(dst_pool: KVPool, src_pool: KVPool, dst_ids: Sequence[int], sr
 
 def attention_iteration(pool: KVPool, plan: Plan, q, out, lse=None, workspace=None,
                         workspace_bytes: Optional[int] = None, stream=None) -> None:
+    _contiguous(q, out, lse, workspace)
     if workspace_bytes is None:
         workspace_bytes = 0
         if workspace is not None and hasattr(workspace, "numel"):
@@ -479,6 +487,7 @@ def attention_iteration_static(pool: KVPool, plan: Plan, q, out, lse=None, strea
     partials go to a fixed 8 MiB array inside the library.  Plans that need
     more raise ``ApError`` (``AP_ERR_WORKSPACE_TOO_SMALL``).  Calls share that
     array, so two of them must not overlap on the GPU."""
+    _contiguous(q, out, lse)
     _check(load().ap_attention_iteration_static(pool.handle, plan.handle, _ptr(q), _ptr(out), _ptr(lse),
                                                 _stream(stream, pool.device)), "ap_attention_iteration_static")
 
@@ -486,6 +495,7 @@ def attention_iteration_static(pool: KVPool, plan: Plan, q, out, lse=None, strea
 def serving_iteration_host(pool: KVPool, q_lens, ctx_lens, block_tables, num_q_heads: int, q_host,
                            k_new_host, v_new_host, out_host, lse_host=None, softmax_scale: float = 0.0,
                            stream=None) -> None:
+    _contiguous(q_host, k_new_host, v_new_host, out_host, lse_host)
     desc, keep = _batch_desc(q_lens, ctx_lens, block_tables, num_q_heads, softmax_scale)
     _check(load().ap_serving_iteration_host(pool.handle, ctypes.byref(desc), _ptr(q_host), _ptr(k_new_host),
                                             _ptr(v_new_host), _ptr(out_host), _ptr(lse_host),

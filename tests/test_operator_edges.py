@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 
 import paper_2604_07144_b200 as ap
+from paper_2604_07144_b200 import binding as B
 from paper_2604_07144_b200 import workloads as W
 
 import kv4_reference as Q
@@ -221,3 +222,55 @@ def test_rows_read_back_from_one_pool_and_appended_to_another_at_once(shape, n):
         ap.plan_destroy(p)
     for p in pools:
         ap.kv_pool_destroy(p)
+
+
+# -------------------------------------------------------------------- refusals --
+
+def _host_plan(shape=(8, 2, 64), rows=4):
+    hq, hkv, d = shape
+    pool = ap.kv_pool_create(64, hkv, d, device=-1)
+    return pool, ap.plan_create(pool, [1] * rows, [20] * rows, np.arange(2 * rows, dtype=np.int32).reshape(rows, 2), hq)
+
+
+def test_strided_tensors_are_refused_where_the_library_reads_or_writes_rows_in_a_row():
+    """Slices of one projection, expanded and transposed tensors, every second row: the rotated append takes row strides,
+    nothing else does."""
+    import torch
+    pool, plan = _host_plan()
+    fused = torch.zeros((4, 12, 64), dtype=torch.bfloat16)
+    q, k = torch.zeros((4, 8, 64), dtype=torch.bfloat16), torch.zeros((4, 2, 64), dtype=torch.bfloat16)
+    lse, ws = torch.zeros((4, 8)), torch.zeros(1 << 16, dtype=torch.uint8)
+    bad_k = [fused[:, 8:10], k[:1].expand(4, 2, 64), torch.zeros((2, 4, 64), dtype=torch.bfloat16).transpose(0, 1),
+             torch.zeros((8, 2, 64), dtype=torch.bfloat16)[::2], torch.zeros((4, 2, 128), dtype=torch.bfloat16)[:, :, ::2]]
+    bad_q = [fused[:, :8], q[:1].expand(4, 8, 64), torch.zeros((8, 8, 64), dtype=torch.bfloat16)[::2]]
+    for bad in bad_k:
+        for call in (ap.kv_append, ap.kv_read_new):
+            for args in ((bad, k), (k, bad)):
+                with pytest.raises(ValueError):
+                    call(pool, plan, *args)
+    for bad in bad_q:
+        for call, more in ((ap.attention_iteration, (lse, ws)), (ap.attention_iteration_static, (lse,))):
+            for args in ((bad, q), (q, bad)):
+                with pytest.raises(ValueError):
+                    call(pool, plan, *args, *more)
+    for more in ((torch.zeros((8, 4)).t(), ws), (lse, torch.zeros(1 << 17, dtype=torch.uint8)[::2])):
+        with pytest.raises(ValueError):
+            ap.attention_iteration(pool, plan, q, q, *more)
+    with pytest.raises(ValueError):
+        ap.attention_iteration_static(pool, plan, q, q, torch.zeros((8, 4)).t())
+    rows = [np.zeros((4, h, 64), np.uint16) for h in (8, 2, 2, 8)]
+    for i in range(4):
+        args = list(rows)
+        args[i] = np.zeros((4, 2 * args[i].shape[1], 64), np.uint16)[:, ::2]
+        with pytest.raises(ValueError):
+            ap.serving_iteration_host(pool, [1] * 4, [20] * 4, np.arange(8, dtype=np.int32).reshape(4, 2), 8, *args)
+    # what is contiguous, or an address, gets as far as the library, which launches nothing for a host-only pool
+    for call in (lambda: ap.kv_append(pool, plan, k, k), lambda: ap.kv_append(pool, plan, 4096, 8192),
+                 lambda: ap.kv_read_new(pool, plan, fused[:1, 8:10].repeat(4, 1, 1), k),
+                 lambda: ap.attention_iteration(pool, plan, q, q, None, ws),
+                 lambda: ap.attention_iteration_static(pool, plan, q, q, lse)):
+        with pytest.raises(ap.ApError) as e:
+            call()
+        assert e.value.status == B.AP_ERR_CUDA
+    ap.plan_destroy(plan)
+    ap.kv_pool_destroy(pool)
