@@ -179,12 +179,65 @@ def _ptr(x) -> Optional[int]:
     raise TypeError(f"cannot take the address of {type(x)}")
 
 
-def _contiguous(*tensors) -> None:
-    """Refuses tensors that the library, which gets an address only, would read or write in the wrong places."""
-    for x in tensors:
-        test = getattr(x, "is_contiguous", None)
-        if not (test() if test is not None else not isinstance(x, np.ndarray) or x.flags.c_contiguous):
+_bf16 = _fp32 = None      # torch's dtypes, once a tensor has been seen
+
+
+def _pair(x, y, nbytes: int, device: int) -> Tuple[Optional[int], Optional[int]]:
+    """Addresses of two contiguous bf16 tensors on `device` (-1: a host-only pool's, any) that hold at least `nbytes`
+    each; the library gets addresses only, so what it would read or write elsewhere is refused here."""
+    try:
+        if (x.dtype is y.dtype is _bf16 and x.nbytes >= nbytes <= y.nbytes and x.get_device() == device == y.get_device()
+                and x.is_contiguous() and y.is_contiguous()):
+            return x.data_ptr(), y.data_ptr()
+    except AttributeError:                   # None, an address, a host array
+        pass
+    return _checked(x, nbytes, device, 2), _checked(y, nbytes, device, 2)
+
+
+def _one(x, nbytes: int, device: int) -> Optional[int]:
+    """_pair for one tensor, or None."""
+    try:
+        if x.dtype is _bf16 and x.nbytes >= nbytes and x.get_device() == device and x.is_contiguous():
+            return x.data_ptr()
+    except AttributeError:
+        pass
+    return _checked(x, nbytes, device, 2)
+
+
+def _checked(x, nbytes: int, device: int, itemsize: Optional[int], dense: bool = True) -> Optional[int]:
+    """The same at length.  `itemsize`: 2 for bf16, 4 for fp32 (or integers of that size, or bytes), None for any type."""
+    if hasattr(x, "data_ptr"):
+        global _bf16, _fp32
+        import torch
+        _bf16, _fp32 = torch.bfloat16, torch.float32
+        want = _bf16 if itemsize == 2 else _fp32
+        plain = not (x.dtype.is_floating_point or x.dtype.is_complex) and x.element_size() in (1, itemsize)
+        if itemsize is not None and x.dtype is not want and not plain:
+            raise ValueError(f"expected {want}, not {x.dtype}")
+        if device >= 0 and x.get_device() != device and not (x.get_device() < 0 and x.is_pinned()):
+            raise ValueError(f"expected a tensor on cuda:{device}, not on {x.device}")
+        if dense and not x.is_contiguous():
             raise ValueError("expected a contiguous tensor")
+        if dense and x.nbytes < nbytes:
+            raise ValueError(f"a tensor of {x.nbytes} bytes where the call takes {nbytes}")
+    elif isinstance(x, np.ndarray):
+        if not x.flags.c_contiguous:
+            raise ValueError("expected a contiguous array")
+        if x.nbytes < nbytes:
+            raise ValueError(f"an array of {x.nbytes} bytes where the call takes {nbytes}")
+    return _ptr(x)
+
+
+def _lse_rows(x, nbytes: int, device: int) -> Optional[int]:
+    """_pair for lse: one tensor of fp32, or None."""
+    if x is None:
+        return None
+    try:
+        if x.dtype is _fp32 and x.nbytes >= nbytes and x.get_device() == device and x.is_contiguous():
+            return x.data_ptr()
+    except AttributeError:
+        pass
+    return _checked(x, nbytes, device, 4)
 
 
 _raw_stream = None        # torch's accessor of the current stream's handle, once torch has initialised CUDA
@@ -195,6 +248,8 @@ def _stream(stream, device: Optional[int] = None) -> Optional[int]:
     device; the current device where it is not given)."""
     global _raw_stream
     if stream is None:
+        if _raw_stream is not None and device is not None and device >= 0:
+            return _raw_stream(device) or None
         if _raw_stream is None:
             try:
                 import torch
@@ -232,11 +287,8 @@ class KVPool:
         self.handle = handle
         self.desc = desc
         self._keepalive = keepalive
-
-    num_pages = property(lambda self: int(self.desc.num_pages))
-    num_kv_heads = property(lambda self: int(self.desc.num_kv_heads))
-    head_dim = property(lambda self: int(self.desc.head_dim))
-    device = property(lambda self: int(self.desc.device))
+        self.num_pages, self.num_kv_heads = int(desc.num_pages), int(desc.num_kv_heads)
+        self.head_dim, self.device = int(desc.head_dim), int(desc.device)
 
 
 def kv_pool_bytes(num_pages: int, num_kv_heads: int, head_dim: int, page_size: int = 16) -> int:
@@ -244,9 +296,17 @@ def kv_pool_bytes(num_pages: int, num_kv_heads: int, head_dim: int, page_size: i
     return int(load().ap_kv_pool_bytes(ctypes.byref(d)))
 
 
+def _plane(x, nbytes: int, device: int) -> Optional[int]:
+    """Address of a pool plane: at least `nbytes` on `device` (any view of memory that lies together)."""
+    if hasattr(x, "nbytes") and x.nbytes < nbytes:
+        raise ValueError(f"a plane of {x.nbytes} bytes where the pool takes {nbytes}")
+    return _checked(x, 0, device, None, dense=False) if hasattr(x, "data_ptr") else _ptr(x)
+
+
 def kv_pool_create(num_pages: int, num_kv_heads: int, head_dim: int, k_base=None, v_base=None,
                    device: int = 0, page_size: int = 16) -> KVPool:
-    d = PoolDesc(num_pages, page_size, num_kv_heads, head_dim, _ptr(k_base), _ptr(v_base), device)
+    k_at, v_at = (_plane(x, kv_pool_bytes(num_pages, num_kv_heads, head_dim, page_size), device) for x in (k_base, v_base))
+    d = PoolDesc(num_pages, page_size, num_kv_heads, head_dim, k_at, v_at, device)
     h = ctypes.c_void_p()
     _check(load().ap_kv_pool_create(ctypes.byref(h), ctypes.byref(d)), "ap_kv_pool_create")
     return KVPool(h.value, d, (k_base, v_base))
@@ -260,7 +320,8 @@ def kv_pool_bytes_4bit(num_pages: int, num_kv_heads: int, head_dim: int, page_si
 def kv_pool_create_4bit(num_pages: int, num_kv_heads: int, head_dim: int, k_base=None, v_base=None,
                         device: int = 0, page_size: int = 16) -> KVPool:
     """Pool that holds K and V in 4 bits (see ap_kv_pool_create_4bit for the planes' layout)."""
-    d = PoolDesc(num_pages, page_size, num_kv_heads, head_dim, _ptr(k_base), _ptr(v_base), device)
+    k_at, v_at = (_plane(x, kv_pool_bytes_4bit(num_pages, num_kv_heads, head_dim, page_size), device) for x in (k_base, v_base))
+    d = PoolDesc(num_pages, page_size, num_kv_heads, head_dim, k_at, v_at, device)
     h = ctypes.c_void_p()
     _check(load().ap_kv_pool_create_4bit(ctypes.byref(h), ctypes.byref(d)), "ap_kv_pool_create_4bit")
     return KVPool(h.value, d, (k_base, v_base))
@@ -313,11 +374,16 @@ def kv_pool_num_free(pool: KVPool) -> int:
 # ------------------------------------------------------------------- plan --
 
 class Plan:
-    """Handle returned by :func:`plan_create`."""
+    """Handle returned by :func:`plan_create`.  `q_bytes`, `kv_bytes`, `lse_bytes`: what the new tokens' rows take."""
 
-    def __init__(self, handle: int, pool: KVPool):
+    def __init__(self, handle: int, pool: KVPool, rows: int, num_q_heads: int):
         self.handle = handle
         self.pool = pool
+        self.rows = rows
+        self.num_q_heads = num_q_heads
+        self.q_bytes = rows * num_q_heads * pool.head_dim * 2
+        self.kv_bytes = rows * pool.num_kv_heads * pool.head_dim * 2
+        self.lse_bytes = rows * num_q_heads * 4
 
 
 def _batch_desc(q_lens, ctx_lens, block_tables, num_q_heads: int, softmax_scale: float):
@@ -337,8 +403,7 @@ def plan_create(pool: KVPool, q_lens, ctx_lens, block_tables, num_q_heads: int,
     h = ctypes.c_void_p()
     _check(load().ap_plan_create(ctypes.byref(h), pool.handle, ctypes.byref(desc), _stream(stream, pool.device)),
            "ap_plan_create")
-    del keep
-    return Plan(h.value, pool)
+    return Plan(h.value, pool, int(keep[0].sum(dtype=np.int64)), num_q_heads)
 
 
 def plan_create_windowed(pool: KVPool, q_lens, ctx_lens, block_tables, num_q_heads: int, window: int, sinks: int = 0,
@@ -351,8 +416,7 @@ def plan_create_windowed(pool: KVPool, q_lens, ctx_lens, block_tables, num_q_hea
     h = ctypes.c_void_p()
     _check(load().ap_plan_create_windowed(ctypes.byref(h), pool.handle, ctypes.byref(desc), ctypes.byref(win),
                                           _stream(stream, pool.device)), "ap_plan_create_windowed")
-    del keep
-    return Plan(h.value, pool)
+    return Plan(h.value, pool, int(keep[0].sum(dtype=np.int64)), num_q_heads)
 
 
 def plan_destroy(plan: Plan) -> None:
@@ -404,31 +468,34 @@ def plan_export(plan: Plan) -> dict:
 # ---------------------------------------------------------------- kernels --
 
 def kv_append(pool: KVPool, plan: Plan, k_new, v_new, stream=None) -> None:
-    _contiguous(k_new, v_new)
-    _check(load().ap_kv_append(pool.handle, plan.handle, _ptr(k_new), _ptr(v_new), _stream(stream, pool.device)),
-           "ap_kv_append")
+    dev = pool.device
+    status = (_lib or load()).ap_kv_append(pool.handle, plan.handle, *_pair(k_new, v_new, plan.kv_bytes, dev), _stream(stream, dev))
+    if status:
+        _check(status, "ap_kv_append")
 
 
-def _row_stride(x) -> int:
-    """Elements from one row of a [rows, heads, head_dim] tensor to the next (0: contiguous, or not a tensor)."""
-    if x is None:
-        return 0
+def _strided_rows(x, rows: int, heads: int, dim: int, nbytes: int, device: int) -> Tuple[Optional[int], int]:
+    """(address, elements from one row to the next or 0 for contiguous) of an input of the rotated append."""
     try:
         if x.is_contiguous():
-            return 0
+            return _one(x, nbytes, device), 0
         row, head, one = x.stride()
-        n, heads, dim = x.shape
-    except AttributeError:                   # an address
-        return 0
+        n, h, d = x.shape
+    except AttributeError:                   # an address, or not given
+        return _ptr(x), 0
     except ValueError:
-        one = n = heads = dim = row = head = 0
-    if one != 1 or (heads > 1 and head != dim):
+        n = h = d = row = head = one = 0
+    if one != 1 or (head != d and h > 1):
         raise ValueError("expected [rows, heads, head_dim] with a token's heads contiguous")
+    if n < rows or h != heads or d != dim:
+        raise ValueError(f"expected [{rows}, {heads}, {dim}], not {list(x.shape)}")
     if n < 2:
-        return 0
-    if row < heads * dim:
+        row = 0
+    elif row < heads * dim:
         raise ValueError("rows overlap (an expanded tensor?)")
-    return row
+    if x.dtype is _bf16 and x.get_device() == device:
+        return x.data_ptr(), row
+    return _checked(x, 0, device, 2, dense=False), row
 
 
 def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, rotary_dim: Optional[int] = None,
@@ -440,17 +507,25 @@ def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, r
     rotary = pool.head_dim if rotary_dim is None else max(-1, min(int(rotary_dim), 2 ** 31 - 1))
     if freq is not None and freq.shape != (rotary // 2,):
         raise ValueError("inv_freq must have rotary_dim / 2 entries")
-    _contiguous(q_rot)
-    desc = RopeDesc(rotary, 1 if interleaved else 0, base, None if freq is None else freq.ctypes.data, amplitude, _row_stride(q),
-                    _row_stride(k_new), _row_stride(v_new))
-    _check(load().ap_kv_append_rope(pool.handle, plan.handle, ctypes.byref(desc), _ptr(q), _ptr(k_new), _ptr(v_new),
-                                    _ptr(q_rot), _stream(stream, pool.device)), "ap_kv_append_rope")
+    dev = pool.device
+    n, hkv, d, kv_bytes = plan.rows, pool.num_kv_heads, pool.head_dim, plan.kv_bytes
+    q_at, q_stride = (None, 0) if q is None else _strided_rows(q, n, plan.num_q_heads, d, plan.q_bytes, dev)
+    k_at, k_stride = _strided_rows(k_new, n, hkv, d, kv_bytes, dev)
+    v_at, v_stride = _strided_rows(v_new, n, hkv, d, kv_bytes, dev)
+    desc = RopeDesc(rotary, 1 if interleaved else 0, base, None if freq is None else freq.ctypes.data, amplitude, q_stride,
+                    k_stride, v_stride)
+    status = (_lib or load()).ap_kv_append_rope(pool.handle, plan.handle, ctypes.byref(desc), q_at, k_at, v_at,
+                                                _one(q_rot, plan.q_bytes, dev), _stream(stream, dev))
+    if status:
+        _check(status, "ap_kv_append_rope")
 
 
 def kv_read_new(pool: KVPool, plan: Plan, k, v, stream=None) -> None:
     """The rows of the plan's new tokens, read back as the bf16 numbers the pool holds (or, in 4 bits, stands for)."""
-    _contiguous(k, v)
-    _check(load().ap_kv_read_new(pool.handle, plan.handle, _ptr(k), _ptr(v), _stream(stream, pool.device)), "ap_kv_read_new")
+    dev = pool.device
+    status = (_lib or load()).ap_kv_read_new(pool.handle, plan.handle, *_pair(k, v, plan.kv_bytes, dev), _stream(stream, dev))
+    if status:
+        _check(status, "ap_kv_read_new")
 
 
 def kv_copy_pages(dst_pool: KVPool, src_pool: KVPool, dst_ids: Sequence[int], src_ids: Sequence[int], stream=None) -> None:
@@ -465,14 +540,22 @@ def kv_copy_pages(dst_pool: KVPool, src_pool: KVPool, dst_ids: Sequence[int], sr
 
 def attention_iteration(pool: KVPool, plan: Plan, q, out, lse=None, workspace=None,
                         workspace_bytes: Optional[int] = None, stream=None) -> None:
-    _contiguous(q, out, lse, workspace)
-    if workspace_bytes is None:
-        workspace_bytes = 0
-        if workspace is not None and hasattr(workspace, "numel"):
-            workspace_bytes = int(workspace.numel() * workspace.element_size())
-    _check(load().ap_attention_iteration(pool.handle, plan.handle, _ptr(q), _ptr(out), _ptr(lse),
-                                         _ptr(workspace), workspace_bytes, _stream(stream, pool.device)),
-           "ap_attention_iteration")
+    dev = pool.device
+    try:
+        room = workspace.nbytes
+        if workspace_bytes is None:
+            workspace_bytes = room
+        elif workspace_bytes > room:
+            raise ValueError(f"a workspace of {room} bytes where the call is told {workspace_bytes}")
+        workspace = workspace.data_ptr() if workspace.get_device() == dev and workspace.is_contiguous() else (
+            _checked(workspace, 0, dev, None))
+    except AttributeError:                   # none, or an address
+        workspace_bytes = workspace_bytes or 0
+    status = (_lib or load()).ap_attention_iteration(pool.handle, plan.handle, *_pair(q, out, plan.q_bytes, dev),
+                                                     _lse_rows(lse, plan.lse_bytes, dev), workspace, workspace_bytes,
+                                                     _stream(stream, dev))
+    if status:
+        _check(status, "ap_attention_iteration")
 
 
 def static_workspace_bytes() -> int:
@@ -487,18 +570,20 @@ def attention_iteration_static(pool: KVPool, plan: Plan, q, out, lse=None, strea
     partials go to a fixed 8 MiB array inside the library.  Plans that need
     more raise ``ApError`` (``AP_ERR_WORKSPACE_TOO_SMALL``).  Calls share that
     array, so two of them must not overlap on the GPU."""
-    _contiguous(q, out, lse)
-    _check(load().ap_attention_iteration_static(pool.handle, plan.handle, _ptr(q), _ptr(out), _ptr(lse),
-                                                _stream(stream, pool.device)), "ap_attention_iteration_static")
+    dev = pool.device
+    _check(load().ap_attention_iteration_static(pool.handle, plan.handle, *_pair(q, out, plan.q_bytes, dev),
+                                                _lse_rows(lse, plan.lse_bytes, dev), _stream(stream, dev)),
+           "ap_attention_iteration_static")
 
 
 def serving_iteration_host(pool: KVPool, q_lens, ctx_lens, block_tables, num_q_heads: int, q_host,
                            k_new_host, v_new_host, out_host, lse_host=None, softmax_scale: float = 0.0,
                            stream=None) -> None:
-    _contiguous(q_host, k_new_host, v_new_host, out_host, lse_host)
     desc, keep = _batch_desc(q_lens, ctx_lens, block_tables, num_q_heads, softmax_scale)
-    _check(load().ap_serving_iteration_host(pool.handle, ctypes.byref(desc), _ptr(q_host), _ptr(k_new_host),
-                                            _ptr(v_new_host), _ptr(out_host), _ptr(lse_host),
+    rows = int(keep[0].sum(dtype=np.int64))
+    sizes = [rows * h * pool.head_dim * 2 for h in (num_q_heads, pool.num_kv_heads, pool.num_kv_heads, num_q_heads)]
+    at = [_checked(x, size, -1, 2) for x, size in zip((q_host, k_new_host, v_new_host, out_host), sizes)]
+    _check(load().ap_serving_iteration_host(pool.handle, ctypes.byref(desc), *at, _checked(lse_host, rows * num_q_heads * 4, -1, 4),
                                             _stream(stream, pool.device)), "ap_serving_iteration_host")
     del keep
 

@@ -274,3 +274,86 @@ def test_strided_tensors_are_refused_where_the_library_reads_or_writes_rows_in_a
         assert e.value.status == B.AP_ERR_CUDA
     ap.plan_destroy(plan)
     ap.kv_pool_destroy(pool)
+
+
+def test_tensors_that_are_too_small_or_of_another_type_are_refused():
+    """The library gets addresses: rows that are not there would be read past the tensor's end, and fp16 or fp32 as bf16."""
+    import torch
+    pool, plan = _host_plan()
+    bf = torch.bfloat16
+    q, k, lse, ws = torch.zeros((4, 8, 64), dtype=bf), torch.zeros((4, 2, 64), dtype=bf), torch.zeros((4, 8)), torch.zeros(1 << 16, dtype=torch.uint8)
+    rope = lambda k_new, v_new, **more: ap.kv_append_rope(pool, plan, k_new, v_new, **more)
+    for bad in (k[:3], torch.zeros((4, 1, 64), dtype=bf), k.half(), k.float(), k.double(), torch.zeros((4, 2, 64), dtype=torch.int32),
+                torch.zeros(4 * 2 * 64 - 1, dtype=bf)):
+        for call in (lambda a, b: ap.kv_append(pool, plan, a, b), lambda a, b: ap.kv_read_new(pool, plan, a, b), rope):
+            for args in ((bad, k), (k, bad)):
+                with pytest.raises(ValueError):
+                    call(*args)
+    wide = torch.zeros((5, 16, 64), dtype=bf)
+    for bad in (wide[:3, :2], wide[:, :3], wide[:, :2].half(), torch.zeros((4, 2, 128), dtype=bf)[:, :, :32]):
+        with pytest.raises(ValueError):
+            rope(bad, k)
+    for bad in (q[:3], q.float(), q.half(), torch.zeros(10, dtype=bf)):
+        for args in ((bad, q), (q, bad)):
+            with pytest.raises(ValueError):
+                ap.attention_iteration(pool, plan, *args, lse, ws)
+            with pytest.raises(ValueError):
+                ap.attention_iteration_static(pool, plan, *args, lse)
+            with pytest.raises(ValueError):
+                rope(k, k, q=args[0], q_rot=args[1])
+    for bad in (lse[:3], lse.half(), lse.double(), q):
+        with pytest.raises(ValueError):
+            ap.attention_iteration(pool, plan, q, q, bad, ws)
+        with pytest.raises(ValueError):
+            ap.attention_iteration_static(pool, plan, q, q, bad)
+    with pytest.raises(ValueError):
+        ap.attention_iteration(pool, plan, q, q, lse, ws, (1 << 16) + 1)
+    rows = [np.zeros((4, h, 64), np.uint16) for h in (8, 2, 2, 8)]
+    for i in range(4):
+        args = list(rows)
+        args[i] = args[i][:3]
+        with pytest.raises(ValueError):
+            ap.serving_iteration_host(pool, [1] * 4, [20] * 4, np.arange(8, dtype=np.int32).reshape(4, 2), 8, *args)
+    with pytest.raises(ValueError):
+        ap.serving_iteration_host(pool, [1] * 4, [20] * 4, np.arange(8, dtype=np.int32).reshape(4, 2), 8, *rows, np.zeros((3, 8), np.float32))
+    for create, size in ((ap.kv_pool_create, ap.kv_pool_bytes(8, 2, 64)), (ap.kv_pool_create_4bit, ap.kv_pool_bytes_4bit(8, 2, 64))):
+        planes = torch.zeros(size, dtype=torch.uint8), torch.zeros(size - 1, dtype=torch.uint8)
+        for args in (planes, planes[::-1]):
+            with pytest.raises(ValueError):
+                create(8, 2, 64, *args, device=-1)
+    # more rows than the plan's, other shapes of the same memory, and bit patterns are fine: the library answers
+    for call in (lambda: ap.kv_append(pool, plan, torch.zeros((9, 2, 64), dtype=bf), k.view(4, 128)),
+                 lambda: ap.kv_append(pool, plan, k.view(torch.int16), k.view(torch.uint8)),
+                 lambda: rope(wide[:, :2], wide[:4, 2:4], q=wide[:, :8], q_rot=torch.zeros((9, 8, 64), dtype=bf)),
+                 lambda: ap.attention_iteration(pool, plan, q.view(1, 4, 512), q, lse.view(torch.int32), ws, 1 << 16)):
+        with pytest.raises(ap.ApError) as e:
+            call()
+        assert e.value.status == B.AP_ERR_CUDA
+    ap.plan_destroy(plan)
+    ap.kv_pool_destroy(pool)
+
+
+@pytest.mark.gpu
+def test_tensors_of_another_device_are_refused_and_pinned_ones_are_read():
+    import torch
+    b = _batch((8, 2, 64), 66, [1, 20], [40, 20])
+    dev = R.Device(b)
+    host = [t.cpu() for t in (dev.k_new, dev.v_new, dev.q)]
+    with pytest.raises(ValueError):
+        ap.kv_append(dev.pool, dev.plan, host[0], dev.v_new)
+    with pytest.raises(ValueError):
+        ap.kv_append_rope(dev.pool, dev.plan, dev.k_new, host[1])
+    with pytest.raises(ValueError):
+        ap.attention_iteration(dev.pool, dev.plan, host[2], dev.out, dev.lse, dev.workspace)
+    with pytest.raises(ValueError):
+        ap.attention_iteration(dev.pool, dev.plan, dev.q, dev.out, dev.lse.cpu(), dev.workspace)
+    with pytest.raises(ValueError):
+        ap.attention_iteration(dev.pool, dev.plan, dev.q, dev.out, dev.lse, dev.workspace.cpu())
+    with pytest.raises(ValueError):
+        ap.kv_pool_create(b.num_pages, 2, 64, dev.k_pool.cpu(), dev.v_pool)
+    pinned = [t.pin_memory() for t in host[:2]]
+    ap.kv_append(dev.pool, dev.plan, *pinned)
+    assert ap.last_device_status(dev.pool) == 0
+    page, slot = Q.new_slots(b)
+    assert np.array_equal(to_bits(dev.k_pool)[page, :, slot], b.k_new) and np.array_equal(to_bits(dev.v_pool)[page, :, slot], b.v_new)
+    dev.close()
