@@ -275,7 +275,8 @@ int ap_plan_predict(const ap_plan *plan, double hbm_gbs, double tensor_tflops, a
  * section:
  *   append_dst    [n_new]             page*16 + slot of every new token row
  *   bt_flat       [n_bt]              used block-table entries, sequences with q_len > 0 concatenated (with a window:
- *                                     decode rows, then each block of 128 prefill rows, without the pages it does not see)
+ *                                     without the pages that no new token sees; then blocks of 128 prefill rows that leave
+ *                                     out pages between the sinks and their window)
  *   decode_items  [decode_items][8]   q_row, first kv_head of the item's block, bt_offset, page_begin, page_count, kv_len, part_slot, merge_index
  *   cta_begin     [n_cta_begin]       item range of decode CTA c is [cta_begin[c], cta_begin[c+1])
  *   merge_entries [merge_entries][4]  q_row, first kv_head of the block, part_begin, part_count

@@ -137,6 +137,14 @@ struct WindowView {
     }
 };
 
+// Where the pages of `part`, the span of a block of query rows, lie one after the other in the entries of `all`, the
+// span of all new rows of its sequence; -1 where they do not: pages between the sinks and the block's window are
+// left out, and the block needs entries of its own, at most ceil(sinks / 16) + window / 16 + 10 of them.
+inline int32_t entries_within(const PageSpan &all, const PageSpan &part) {
+    if (part.shift() == 0 || part.first == all.first) return 0;           // no gap (then `all` has none), or the same
+    return part.sink_pages == 0 ? part.first - all.first : -1;
+}
+
 // GB/s of KV one SM's decode pipeline sustains, by the size of its TMA requests (the tiles of one page
 // that an item takes in one request): the TMA unit handles ~14 M requests per second.
 inline double decode_sm_gbs(int request_bytes) {
@@ -560,12 +568,14 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
             decode_kv += seen;
             decode_bt += span.count();
         } else {
+            bt_total += span.count();
             if (win.window == 0) {
-                bt_total += need;
                 pairs += (int64_t)ql * (cl - ql) + (int64_t)ql * (ql + 1) / 2;
-            } else {                                      // every block of query rows has entries of its own
-                for (int32_t t0 = 0; t0 < ql; t0 += 128)
-                    bt_total += win.pages(cl - ql + t0, cl - ql + std::min(ql, t0 + 128)).count();
+            } else {
+                for (int32_t t0 = 0; t0 < ql; t0 += 128) {
+                    const PageSpan part = win.pages(cl - ql + t0, cl - ql + std::min(ql, t0 + 128));
+                    if (entries_within(span, part) < 0) bt_total += part.count();
+                }
                 for (int32_t t = 0; t < ql; ++t) pairs += win.keys(cl - ql + t);
             }
             prefill_kv += seen;
@@ -588,7 +598,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
         bt_flat.insert(bt_flat.end(), row + span.first, row + span.end);
         return at;
     };
-    std::vector<int32_t> bt_off((size_t)B, 0);       // a sequence's entries (with a window: a decode row's)
+    std::vector<int32_t> bt_off((size_t)B, 0);       // a sequence's entries: the pages that any new token of it sees
     // 4-bit pool: the pages that prefill units read are widened into the workspace; their units' table entries
     // number those copies.  Sequence s's are wide_first[s], ...: the pages of its span over all its new tokens.
     std::vector<int32_t> wide_pages, wide_first((size_t)B, 0);
@@ -613,8 +623,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
                 wide_pages.insert(wide_pages.end(), row, row + all.sink_pages);
                 wide_pages.insert(wide_pages.end(), row + all.first, row + all.end);
             }
-            if (ql == 1 || win.window == 0)
-                bt_off[(size_t)s] = ql > 1 && pool->four_bit ? push_wide(s, all, all) : push_table(s, all);
+            bt_off[(size_t)s] = ql > 1 && pool->four_bit ? push_wide(s, all, all) : push_table(s, all);
             const int32_t *row = b->block_tables + (size_t)s * (size_t)b->table_stride;
             for (int32_t t = 0; t < ql; ++t) {
                 const int32_t p = cl - ql + t;
@@ -756,8 +765,9 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
             int32_t bt = bt_off[(size_t)s], pos0 = cl - ql + t0, ctx = cl;
             if (win.window > 0) {
                 // the unit's own compacted context, which ends with its last row (no row sees further)
-                const PageSpan span = win.pages(pos0, pos0 + rows);
-                bt = pool->four_bit ? push_wide(s, win.pages(cl - ql, cl), span) : push_table(s, span);
+                const PageSpan span = win.pages(pos0, pos0 + rows), all = win.pages(cl - ql, cl);
+                const int32_t at = entries_within(all, span);
+                bt = at >= 0 ? bt + at : pool->four_bit ? push_wide(s, all, span) : push_table(s, span);
                 ctx = pos0 + rows - span.shift();
                 pos0 -= span.shift();
             }

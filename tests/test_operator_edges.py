@@ -357,3 +357,30 @@ def test_tensors_of_another_device_are_refused_and_pinned_ones_are_read():
     page, slot = Q.new_slots(b)
     assert np.array_equal(to_bits(dev.k_pool)[page, :, slot], b.k_new) and np.array_equal(to_bits(dev.v_pool)[page, :, slot], b.v_new)
     dev.close()
+
+
+# ------------------------------------------------------------------ plan lists --
+
+@pytest.mark.parametrize("four_bit", [False, True], ids=["bf16", "4bit"])
+def test_windowed_table_entries_grow_with_the_prompt_and_not_with_its_square(four_bit):
+    """Blocks of query rows share their sequence's entries unless pages between the sinks and their window are left out;
+    those that do leave pages out have no more entries than sinks and window ask for."""
+    ctx, hkv = 1 << 17, 2
+    table = np.random.default_rng(1).permutation(ctx // 16).astype(np.int32)[None]
+    pool = (ap.kv_pool_create_4bit if four_bit else ap.kv_pool_create)(ctx // 16, hkv, 64, device=-1)
+    blocks = ctx // 128
+    for window, sinks, most in ((2 ** 31 - 1, 0, ctx // 16), (ctx, 4, ctx // 16), (4096, 0, ctx // 16), (1, 0, ctx // 16),
+                                (5, 2 ** 31 - 1, ctx // 16), (1000, ctx // 2, ctx // 16 + blocks // 2 * (ctx // 32 + 72)),
+                                (1024, 4, ctx // 16 + blocks * 74)):
+        plan = ap.plan_create_windowed(pool, [ctx], [ctx], table, 2, window, sinks)
+        ex = ap.plan_export(plan)
+        assert len(ex["bt_flat"]) <= most, (window, sinks)
+        # every block's entries are still those of the pages it sees
+        number = np.arange(ctx // 16) if four_bit else table[0]
+        for r0, nr, qh, _, off, pos0, vctx, _ in ex["prefill_tiles"].tolist()[:: 97]:
+            page = np.arange((r0 + nr + 15) // 16)
+            first = max(0, r0 - window + 1) // 16
+            want = number[page[(page >= first) | (16 * page < sinks)]]
+            assert vctx == pos0 + nr and np.array_equal(ex["bt_flat"][off:off + (vctx + 15) // 16], want), (window, sinks, r0)
+        ap.plan_destroy(plan)
+    ap.kv_pool_destroy(pool)
