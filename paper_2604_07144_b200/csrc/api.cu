@@ -1042,14 +1042,16 @@ int ap_kv_append_rope(ap_kv_pool *pool, const ap_plan *plan, const ap_rope_desc 
     params.units = rope->rotary_dim / 16;
     params.interleaved = rope->interleaved;
     params.amplitude = rope->amplitude == 0.f ? 1.f : rope->amplitude;
-    // base^(-2 i / R) as the i-th power of one pow: 64 of them would take as long as the launch.  The product is off by
-    // less than i 2^-52 of f_i, an angle p f_i by less than 1e-6 even at p = 2^31.
-    const double ratio = rope->inv_freq ? 1.0 : std::pow(rope->base, -2.0 / rope->rotary_dim);
-    double f = 1.0;
+    // base^(-2 i / R) as the i-th power of one pow: 64 of them would take as long as the launch.  In extended precision
+    // (64 bits), where i products are off by at most (i + 1) 2^-63 of f_i; with the rounding of f_i / 2 pi to 64-bit
+    // floating point and of its product with the position an angle is off by at most 1.04 2^-52 p f_i: 5e-7 at p = 2^31 and
+    // f_i = 1, more only where base < 1 or given frequencies are above 1.
+    const long double ratio = rope->inv_freq ? 1.0L : std::pow((long double)rope->base, -2.0L / rope->rotary_dim);
+    long double f = 1.0L;
     for (int i = 0; i < rope->rotary_dim / 2; ++i, f *= ratio) {
         if (rope->inv_freq) f = rope->inv_freq[i];
-        if (!std::isfinite(f)) return AP_ERR_INVALID_ARG;
-        params.turn[i] = f * 0.15915494309189533576888376337251;       // / (2 pi)
+        params.turn[i] = (double)(f * 0.159154943091895335768883763372514362L);       // / (2 pi)
+        if (!std::isfinite(params.turn[i])) return AP_ERR_INVALID_ARG;
     }
     auto stride_of = [](int64_t given, int heads, int dim) { return given ? given : (int64_t)heads * dim; };
     const int64_t qs = stride_of(rope->q_row_stride, Hq, d), ks = stride_of(rope->k_row_stride, Hkv, d),

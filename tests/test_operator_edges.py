@@ -384,3 +384,28 @@ def test_windowed_table_entries_grow_with_the_prompt_and_not_with_its_square(fou
             assert vctx == pos0 + nr and np.array_equal(ex["bt_flat"][off:off + (vctx + 15) // 16], want), (window, sinks, r0)
         ap.plan_destroy(plan)
     ap.kv_pool_destroy(pool)
+
+
+# ------------------------------------------------------------------- rotation --
+
+def test_rotation_frequencies_by_repeated_products_are_as_good_as_stated():
+    """The rotated append forms base^(-2 i / R) / 2 pi by i products in extended precision and rounds it to 64 bits; the angle
+    at position 2^31 is then off by at most 1.04 2^-52 2^31 f_i: two roundings of 2^-53 each, one its product with the
+    position, and 64 of 2^-63.  Against 60 digits;
+    with 64-bit products base 2 missed it (1.9e-6)."""
+    from decimal import Decimal, getcontext
+    if np.finfo(np.longdouble).nmant < 63:
+        pytest.skip("no extended precision here")
+    getcontext().prec = 60
+    two_pi = Decimal("6.28318530717958647692528676655900576839433879875021164194989")
+    inv_2pi = np.longdouble("0.159154943091895335768883763372514362")
+    far = 2 ** 31
+    for base in (0.5, 1.0001, 2.0, 10000.0, 500000.0, 1e6, 1e9):
+        for rotary in (16, 48, 64, 128):
+            ratio, f = np.power(np.longdouble(base), np.longdouble(-2) / np.longdouble(rotary)), np.longdouble(1)
+            for i in range(rotary // 2):
+                exact = Decimal(base) ** (Decimal(-2 * i) / Decimal(rotary))
+                turn = float(f * inv_2pi)
+                off = abs(Decimal(far * turn) * two_pi - far * exact)          # far * turn: one rounding, as in the kernel
+                assert off <= Decimal(1.04 * 2.0 ** -52 * far) * exact, (base, rotary, i, float(off))
+                f = f * ratio
