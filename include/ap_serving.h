@@ -75,7 +75,8 @@ typedef struct ap_plan ap_plan;       /* opaque */
  * k_base/v_base: device, each ap_kv_pool_bytes() long and 16-byte aligned
  * (what a tensor map's base address needs), owned by the caller; or both NULL,
  * then the library allocates (and zero fills) and frees them.  head_dim is 64 or 128; page_size must be 16;
- * num_q_heads / num_kv_heads may be 1..8 (given per batch).
+ * num_q_heads / num_kv_heads may be 1..8 (given per batch).  num_pages: up to 2^27, and
+ * num_pages * num_kv_heads below 2^30.
  */
 typedef struct ap_pool_desc {
     int32_t num_pages;
@@ -97,7 +98,7 @@ size_t ap_kv_pool_bytes(const ap_pool_desc *desc);
  * allocator, ap_plan_create and ap_plan_export work (planning for 148 SMs);
  * every call that would launch returns AP_ERR_CUDA.
  * Errors: INVALID_ARG (bad sizes, one base NULL, misaligned), UNSUPPORTED
- * (head_dim/page_size), CUDA (no device, allocation failure). */
+ * (head_dim/page_size, too many pages), CUDA (no device, allocation failure). */
 int ap_kv_pool_create(ap_kv_pool **out, const ap_pool_desc *desc);
 
 /*
@@ -192,7 +193,7 @@ typedef struct ap_batch_desc {
  * Validation: 0 <= q_len <= ctx_len; table_stride >= ceil(ctx_len/16) for every
  * sequence with q_len > 0; every used entry in [0, num_pages)
  * (BAD_BLOCK_TABLE); no two appended token slots alias (BAD_BLOCK_TABLE);
- * head ratio 1..8 (UNSUPPORTED).  Pages shared between sequences for reading
+ * head ratio 1..8, ctx_len up to 2^31 - 256 (UNSUPPORTED).  Pages shared between sequences for reading
  * are legal.  On error *out is NULL and nothing was launched.
  */
 int ap_plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *batch, void *stream);

@@ -356,6 +356,8 @@ static int pool_create(ap_kv_pool **out, const ap_pool_desc *desc, bool four_bit
     if (((uintptr_t)desc->k_base | (uintptr_t)desc->v_base) & 15u) return AP_ERR_INVALID_ARG;
     // the tensor maps address 8-row groups with a 32-bit extent
     if ((int64_t)desc->num_pages * desc->num_kv_heads * 2 >= (int64_t)1 << 31) return AP_ERR_UNSUPPORTED;
+    // and a plan names a slot of the pool, page * 16 + slot, in 32 bits (4-bit planes of 2^27 pages fit on a GPU)
+    if (desc->num_pages > kMaxPages) return AP_ERR_UNSUPPORTED;
 
     if (desc->device < 0) {
         // host-only pool: allocator and planner work, nothing can be launched
@@ -551,6 +553,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
         const int32_t ql = b->q_lens[s], cl = b->ctx_lens[s];
         if (ql < 0 || cl < 0 || ql > cl) return AP_ERR_INVALID_ARG;
         if (ql == 0) continue;
+        if (cl > kMaxContext) return AP_ERR_UNSUPPORTED;
         const int64_t need = ((int64_t)cl + kPageSize - 1) / kPageSize;
         if (need > b->table_stride) return AP_ERR_INVALID_ARG;
         const int32_t *row = b->block_tables + (size_t)s * (size_t)b->table_stride;

@@ -14,6 +14,8 @@
 namespace ap {
 
 constexpr int kPageSize = 16;
+constexpr int kMaxPages = 1 << 27;                        // page * 16 + slot in 32 bits
+constexpr int kMaxContext = INT32_MAX - 255;              // positions up to two 128-key steps past the last one in 32 bits
 constexpr uint64_t kDefaultWaitLimitNs = 2000000000ull;   // 2 s
 constexpr int kMaxMergeEntries = 4096;   // arrival counters kept per pool (the planner makes < 2 per CTA)
 

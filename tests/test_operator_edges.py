@@ -409,3 +409,31 @@ def test_rotation_frequencies_by_repeated_products_are_as_good_as_stated():
                 off = abs(Decimal(far * turn) * two_pi - far * exact)          # far * turn: one rounding, as in the kernel
                 assert off <= Decimal(1.04 * 2.0 ** -52 * far) * exact, (base, rotary, i, float(off))
                 f = f * ratio
+
+
+# -------------------------------------------------------------- 32-bit numbers --
+
+def test_slots_and_positions_that_pass_32_bits_are_refused():
+    """A plan names a slot as page * 16 + slot and adds up to two steps of 128 keys to a position, in 32 bits."""
+    for create in (ap.kv_pool_create, ap.kv_pool_create_4bit):
+        with pytest.raises(ap.ApError) as e:
+            create((1 << 27) + 1, 1, 64, device=-1)
+        assert e.value.status == B.AP_ERR_UNSUPPORTED
+        pool = create(16, 1, 64, device=-1)
+        table = np.zeros((1, 1 << 27), np.int32)                             # (never touched: no memory of its own)
+        for q_len, window in ((1, None), (2, None), (1, 100), (300, 100)):
+            for ctx in (2 ** 31 - 1, 2 ** 31 - 255):
+                with pytest.raises(ap.ApError) as e:
+                    if window is None:
+                        ap.plan_create(pool, [q_len], [ctx], table, 1)
+                    else:
+                        ap.plan_create_windowed(pool, [q_len], [ctx], table, 1, window)
+                assert e.value.status == B.AP_ERR_UNSUPPORTED
+        # the longest one, of a window that shows only its end
+        far = 2 ** 31 - 256
+        plan = ap.plan_create_windowed(pool, [1], [far], table, 1, 40)
+        assert ap.plan_export(plan)["append_dst"].tolist() == [(far - 1) % 16]
+        ap.plan_destroy(plan)
+        # a sequence without new tokens may be described in any way
+        ap.plan_destroy(ap.plan_create(pool, [0, 1], [2 ** 31 - 1, 5], np.zeros((2, 1), np.int32), 1))
+        ap.kv_pool_destroy(pool)
