@@ -1258,7 +1258,8 @@ int ap_serving_iteration_host(ap_kv_pool *pool, const ap_batch_desc *batch, cons
     cudaStream_t st = (cudaStream_t)stream;
     if (batch->batch < 0 || batch->num_q_heads <= 0 || (batch->batch > 0 && !batch->q_lens)) return AP_ERR_INVALID_ARG;
     // The input copies do not depend on the plan, so they are issued first and run while the host
-    // plans; only their sizes (the number of new tokens) are needed up front.
+    // plans; only their sizes (the number of new tokens) are needed up front.  (When the staging buffer has to grow
+    // the plan comes first: see below.)
     size_t n = 0;
     for (int s = 0; s < batch->batch; ++s) {
         if (batch->q_lens[s] < 0) return AP_ERR_INVALID_ARG;
@@ -1285,7 +1286,13 @@ int ap_serving_iteration_host(ap_kv_pool *pool, const ap_batch_desc *batch, cons
     const size_t ws_bytes = align_up(max_slots * part_heads * d * sizeof(float), 256) +
                             align_up(max_slots * part_heads * sizeof(float), 256) + wide_bytes;
     const size_t total = 2 * q_bytes + 2 * kv_bytes + lse_bytes + ws_bytes;
+    ap_plan *plan = nullptr;
+    int rc = AP_OK;
     if (total > pool->stage_bytes) {
+        // The sizes come from a batch that nobody has looked at yet: the planner validates it before the staging buffer
+        // is given back and one of that size asked for.
+        rc = ap_plan_create(&plan, pool, batch, stream);
+        if (rc != AP_OK) return rc;
         if (pool->stage_dev) {
             (void)cudaDeviceSynchronize();
             (void)cudaFree(pool->stage_dev);
@@ -1295,6 +1302,7 @@ int ap_serving_iteration_host(ap_kv_pool *pool, const ap_batch_desc *batch, cons
         const size_t want = total + total / 4;
         if (cudaMalloc(&pool->stage_dev, want) != cudaSuccess) {
             (void)cudaGetLastError();
+            ap_plan_destroy(plan);
             return AP_ERR_CUDA;
         }
         pool->stage_bytes = want;
@@ -1309,10 +1317,10 @@ int ap_serving_iteration_host(ap_kv_pool *pool, const ap_batch_desc *batch, cons
                cudaMemcpyAsync(dv, v_new_host, n * Hkv * d * 2, cudaMemcpyHostToDevice, st) == cudaSuccess);
     if (!ok) {
         (void)cudaGetLastError();
+        if (plan) ap_plan_destroy(plan);
         return AP_ERR_CUDA;
     }
-    ap_plan *plan = nullptr;
-    int rc = ap_plan_create(&plan, pool, batch, stream);
+    if (!plan) rc = ap_plan_create(&plan, pool, batch, stream);
     if (rc != AP_OK) {               // the copies already queued only touch the staging buffer,
         (void)cudaStreamSynchronize(st);   // but they read the caller's memory: let them finish
         return rc;

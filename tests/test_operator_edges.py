@@ -437,3 +437,31 @@ def test_slots_and_positions_that_pass_32_bits_are_refused():
         # a sequence without new tokens may be described in any way
         ap.plan_destroy(ap.plan_create(pool, [0, 1], [2 ** 31 - 1, 5], np.zeros((2, 1), np.int32), 1))
         ap.kv_pool_destroy(pool)
+
+
+# ------------------------------------------------------------------- host call --
+
+@pytest.mark.gpu
+def test_the_host_call_validates_a_batch_before_it_sizes_its_staging_by_it():
+    """On a 4-bit pool the staging grows with the contexts of prefill chunks; a context that the table does not hold is
+    INVALID_ARG, whatever memory it would take, and the pool goes on as before."""
+    shape = (6, 2, 128)
+    b = _batch(shape, 67, [1, 30], [100, 60])
+    planes = _planes(b, True)
+    dev = R.Device(b, k_plane=planes[0], v_plane=planes[1], four_bit=True)
+
+    def call(q_lens, ctx_lens, table, q=b.q, k=b.k_new, v=b.v_new):
+        out, lse = np.zeros((len(q), 6, 128), np.uint16), np.zeros((len(q), 6), np.float32)
+        ap.serving_iteration_host(dev.pool, q_lens, ctx_lens, table, 6, q, k, v, out, lse)
+        return out, lse
+    first = call(b.q_lens, b.ctx_lens, b.block_tables)
+    for ctx, status in ((2 ** 31 - 257, B.AP_ERR_INVALID_ARG), (2 ** 31 - 1, B.AP_ERR_UNSUPPORTED), (1 << 24, B.AP_ERR_INVALID_ARG)):
+        with pytest.raises(ap.ApError) as e:
+            call([1, 30], [100, ctx], b.block_tables)
+        assert e.value.status == status, ctx
+    again = call(b.q_lens, b.ctx_lens, b.block_tables)
+    assert all(np.array_equal(x, y) for x, y in zip(first, again))
+    k, v = (Q.values(p, 128) for p in planes)
+    ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b)
+    R.check(*first, ref)
+    dev.close()
