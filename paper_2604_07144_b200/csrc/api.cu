@@ -83,6 +83,23 @@ int acquire_plan_buffer(ap_kv_pool *pool, size_t n_ints, PlanBuffer *out) {
     return AP_OK;
 }
 
+// Back to the pool for the next plan; freed if there is no host memory to remember it (no exception leaves a C entry).
+void give_back_plan_buffer(ap_kv_pool *pool, PlanBuffer &b) {
+    try {
+        pool->plan_buffers.push_back(b);
+    } catch (const std::bad_alloc &) {
+        release_plan_buffer(b);
+    }
+}
+
+void give_back_event(ap_kv_pool *pool, cudaEvent_t e) {
+    try {
+        pool->spare_events.push_back(e);
+    } catch (const std::bad_alloc &) {
+        (void)cudaEventDestroy(e);
+    }
+}
+
 cudaEvent_t take_event(ap_kv_pool *pool) {
     if (!pool->spare_events.empty()) {
         cudaEvent_t e = pool->spare_events.back();
@@ -217,7 +234,13 @@ struct TimedScope {
     }
     ~TimedScope() {
         if (!on) return;
-        if (cudaEventRecord(rec.stop, stream) == cudaSuccess) pool->timed.push_back(rec);
+        if (cudaEventRecord(rec.stop, stream) != cudaSuccess) return;
+        try {
+            pool->timed.push_back(rec);
+        } catch (const std::bad_alloc &) {          // (this launch goes uncounted)
+            (void)cudaEventDestroy(rec.start);
+            (void)cudaEventDestroy(rec.stop);
+        }
     }
 };
 
@@ -843,7 +866,7 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
         if (cudaMemcpyAsync(plan->buf.dev, plan->buf.host, total_ints * 4, cudaMemcpyHostToDevice, st) != cudaSuccess ||
             cudaEventRecord(plan->buf.uploaded, st) != cudaSuccess) {
             (void)cudaGetLastError();
-            pool->plan_buffers.push_back(plan->buf);
+            give_back_plan_buffer(pool, plan->buf);
             delete plan;
             return AP_ERR_CUDA;
         }
@@ -991,7 +1014,7 @@ int ap_plan_predict(const ap_plan *plan, double hbm_gbs, double tensor_tflops, a
 
 int ap_plan_destroy(ap_plan *plan) {
     if (!plan) return AP_ERR_INVALID_ARG;
-    if (plan->pool && plan->buf.dev) plan->pool->plan_buffers.push_back(plan->buf);
+    if (plan->pool && plan->buf.dev) give_back_plan_buffer(plan->pool, plan->buf);
     delete plan;
     return AP_OK;
 }
@@ -1103,8 +1126,8 @@ int ap_kv_read_new(ap_kv_pool *pool, const ap_plan *plan, void *k, void *v, void
     return AP_OK;
 }
 
-int ap_kv_copy_pages(ap_kv_pool *dst_pool, const ap_kv_pool *src_pool, int32_t n, const int32_t *dst_ids,
-                     const int32_t *src_ids, void *stream) {
+static int kv_copy_pages(ap_kv_pool *dst_pool, const ap_kv_pool *src_pool, int32_t n, const int32_t *dst_ids,
+                         const int32_t *src_ids, void *stream) {
     if (!dst_pool || !src_pool || n < 0 || (n > 0 && (!dst_ids || !src_ids))) return AP_ERR_INVALID_ARG;
     const ap_pool_desc &dd = dst_pool->desc, &sd = src_pool->desc;
     if (dd.num_kv_heads != sd.num_kv_heads || dd.head_dim != sd.head_dim || dd.page_size != sd.page_size ||
@@ -1147,8 +1170,17 @@ int ap_kv_copy_pages(ap_kv_pool *dst_pool, const ap_kv_pool *src_pool, int32_t n
         release_plan_buffer(buf);
         return AP_ERR_CUDA;
     }
-    dst_pool->plan_buffers.push_back(buf);
+    give_back_plan_buffer(dst_pool, buf);
     return AP_OK;
+}
+
+int ap_kv_copy_pages(ap_kv_pool *dst_pool, const ap_kv_pool *src_pool, int32_t n, const int32_t *dst_ids,
+                     const int32_t *src_ids, void *stream) {
+    try {
+        return kv_copy_pages(dst_pool, src_pool, n, dst_ids, src_ids, stream);
+    } catch (const std::bad_alloc &) {
+        return AP_ERR_CUDA;
+    }
 }
 
 int ap_attention_iteration(ap_kv_pool *pool, const ap_plan *plan, const void *q, void *out, float *lse,
@@ -1218,8 +1250,8 @@ int ap_profile_enable(ap_kv_pool *pool, int on) {
     if (!pool) return AP_ERR_INVALID_ARG;
     if (pool->desc.device < 0) return AP_ERR_CUDA;
     for (auto &t : pool->timed) {
-        pool->spare_events.push_back(t.start);
-        pool->spare_events.push_back(t.stop);
+        give_back_event(pool, t.start);
+        give_back_event(pool, t.stop);
     }
     pool->timed.clear();
     pool->profiling = on != 0;
@@ -1243,8 +1275,8 @@ int ap_profile_collect(ap_kv_pool *pool, void *stream, ap_kernel_times *out) {
             (void)cudaGetLastError();
             rc = AP_ERR_CUDA;
         }
-        pool->spare_events.push_back(t.start);
-        pool->spare_events.push_back(t.stop);
+        give_back_event(pool, t.start);
+        give_back_event(pool, t.stop);
     }
     pool->timed.clear();
     return rc;

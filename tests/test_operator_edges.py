@@ -465,3 +465,30 @@ def test_the_host_call_validates_a_batch_before_it_sizes_its_staging_by_it():
     ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b)
     R.check(*first, ref)
     dev.close()
+
+
+# ----------------------------------------------------------- out of host memory --
+
+def test_a_page_copy_without_host_memory_returns_a_status():
+    """In a child process whose address space may not grow: the list of destinations does not fit, and the call says so instead
+    of ending the process with an exception at a C entry."""
+    import os
+    import subprocess
+    import sys
+    child = """
+import ctypes, resource
+import numpy as np
+from paper_2604_07144_b200 import binding as B
+lib = B.load()
+desc = B.PoolDesc(1 << 26, 16, 1, 64, None, None, -1)
+pool = ctypes.c_void_p()
+assert lib.ap_kv_pool_create_4bit(ctypes.byref(pool), ctypes.byref(desc)) == 0
+ids = np.arange(4, dtype=np.int32)
+assert lib.ap_kv_copy_pages(pool, pool, 2, ids.ctypes.data, ids[2:].ctypes.data, None) == 0
+size = int(open("/proc/self/statm").read().split()[0]) * resource.getpagesize()
+resource.setrlimit(resource.RLIMIT_AS, (size + (8 << 20), resource.RLIM_INFINITY))
+print("status", lib.ap_kv_copy_pages(pool, pool, 2, ids.ctypes.data, ids[2:].ctypes.data, None))
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", child], cwd=root, capture_output=True, text=True, timeout=120)
+    assert done.returncode == 0 and done.stdout.split() == ["status", str(B.AP_ERR_CUDA)], done.stdout + done.stderr
