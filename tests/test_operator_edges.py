@@ -492,3 +492,60 @@ print("status", lib.ap_kv_copy_pages(pool, pool, 2, ids.ctypes.data, ids[2:].cty
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     done = subprocess.run([sys.executable, "-c", child], cwd=root, capture_output=True, text=True, timeout=120)
     assert done.returncode == 0 and done.stdout.split() == ["status", str(B.AP_ERR_CUDA)], done.stdout + done.stderr
+
+
+# ------------------------------------------------------------- more of the forms --
+
+def test_struct_sizes_of_the_operators_match_the_header(tmp_path):
+    import ctypes
+    import os
+    import subprocess
+    inc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    src, exe = tmp_path / "sizes.c", tmp_path / "sizes"
+    fields = ("rotary_dim", "interleaved", "base", "inv_freq", "amplitude", "q_row_stride", "k_row_stride", "v_row_stride")
+    src.write_text('#include "ap_serving.h"\n#include <stddef.h>\n#include <stdio.h>\nint main(void) {\n'
+                   '  printf("%zu %zu", sizeof(ap_rope_desc), sizeof(ap_window_desc));\n'
+                   + "".join(f'  printf(" %zu", offsetof(ap_rope_desc, {f}));\n' for f in fields)
+                   + '  printf(" %zu", offsetof(ap_window_desc, sinks));\n  return 0;\n}\n')
+    subprocess.check_call(["gcc", "-std=c99", "-Wall", "-Werror", "-I", inc, str(src), "-o", str(exe)])
+    got = [int(x) for x in subprocess.check_output([str(exe)]).split()]
+    assert got == [ctypes.sizeof(B.RopeDesc), ctypes.sizeof(B.WindowDesc), *(getattr(B.RopeDesc, f).offset for f in fields),
+                   B.WindowDesc.sinks.offset]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(8, 2, 64), (6, 2, 128), (40, 40, 64)], ids=str)
+def test_rotated_append_to_a_4bit_pool_in_place_without_q_and_with_given_frequencies(shape):
+    """q in place, q left out, given frequencies and an amplitude: what the pool stores is the quantised form of what a bf16 pool
+    stores, and q is rotated alike."""
+    b = _batch(shape, 68, [1, 20, 1], [77, 300, 5000])
+    page, slot = Q.new_slots(b)
+    freq = np.array([0.9 ** i / (1 + i % 3) for i in range(shape[2] // 2)])
+    for kw in (dict(inv_freq=freq), dict(inv_freq=freq[:16], rotary_dim=32, interleaved=True, amplitude=1.25), dict(base=2.0)):
+        for with_q in (True, False):
+            rows, q_out = [], []
+            for four_bit in (False, True):
+                planes = [Q.empty_plane(b.num_pages, shape[1], shape[2], s) for s in (1, 2)] if four_bit else (None, None)
+                dev = R.Device(b, k_plane=planes[0], v_plane=planes[1], four_bit=four_bit)
+                ap.kv_append_rope(dev.pool, dev.plan, dev.k_new, dev.v_new, **(dict(q=dev.q, q_rot=dev.q) if with_q else {}), **kw)
+                assert ap.last_device_status(dev.pool) == 0
+                q_out.append(to_bits(dev.q))
+                if four_bit:
+                    for plane, r, got in zip(planes, rows, (dev.k_pool, dev.v_pool)):
+                        Q.put(plane, page, slot, r)
+                        assert np.array_equal(got.cpu().numpy(), plane)
+                else:
+                    rows = [to_bits(p)[page, :, slot] for p in (dev.k_pool, dev.v_pool)]
+                dev.close()
+            assert np.array_equal(*q_out) and np.array_equal(q_out[0], b.q) == (not with_q)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("window,sinks", [(None, 0), (3000, 20), (700, 1000)])
+def test_4bit_prefill_of_long_contexts(window, sinks):
+    """Chunks on prefixes of thousands of tokens, alone and beside decode rows, with sinks that reach past a block's window."""
+    for shape in ((8, 2, 64), (5, 1, 128)):
+        b = _batch(shape, 69, [300, 2, 1, 130], [9000, 5001, 7000, 2500])
+        out, lse, k, v = _attend(b, _planes(b, True), True, window, sinks)
+        ref = R.attention(lambda s: R.table_rows(b, k, s), lambda s: R.table_rows(b, v, s), b, window, sinks)
+        R.check(out, lse, ref, f"window {window}")
