@@ -54,15 +54,16 @@ def _attend(batch, planes, four_bit, window=None, sinks=0):
 
 
 def _check_of_any_size(out_bits, lse, ref, longest, what):
-    """operator_reference.check without its absolute slack: |out - ref| <= (2^-8 + 2e-4) A plus half an ulp of bf16 at ref,
-    which is never below half a subnormal's, 2^-134; plus longest 2^-149 for sums of at most `longest` products that may
-    round to fp32's subnormals, each addition and each product by 2^-150."""
+    """operator_reference.check without its absolute slack: the value that is rounded to bf16 at the end is within
+    s = (2^-8 + 2e-4) A of ref, plus longest 2^-149 for sums of at most `longest` products that may round to fp32's
+    subnormals, each addition and each product by 2^-150.  The rounding adds half an ulp of bf16 at up to |ref| + s (s may
+    cross into the next binade), which is never below half a subnormal's, 2^-134."""
     ref_out, ref_lse, absw = ref
     got = W.bf16_bits_to_f64(out_bits)
     assert np.isfinite(got).all() and np.isfinite(lse).all(), f"{what}: non-finite output"
-    a = np.abs(ref_out)
-    half_ulp = np.maximum(np.where(a > 0, 2.0 ** (np.floor(np.log2(np.maximum(a, 1e-300))) - 8), 0.0), 2.0 ** -134)
-    excess = np.abs(got - ref_out) - (absw * (2.0 ** -8 + 2e-4) + half_ulp + longest * 2.0 ** -149)
+    s = absw * (2.0 ** -8 + 2e-4) + longest * 2.0 ** -149
+    half_ulp = np.maximum(2.0 ** (np.floor(np.log2(np.maximum(np.abs(ref_out) + s, 1e-300))) - 8), 2.0 ** -134)
+    excess = np.abs(got - ref_out) - (s + half_ulp)
     i = np.unravel_index(np.argmax(excess), excess.shape)
     assert excess[i] <= 0, f"{what}: {got[i]} against {ref_out[i]} at {i} (A {absw[i]})"
     lerr = np.abs(lse - ref_lse)
