@@ -12,7 +12,9 @@ import of the library fails with an error.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
+import struct
 from typing import Optional, Sequence, Tuple
 
 import numpy as np
@@ -71,6 +73,11 @@ class RopeDesc(ctypes.Structure):
     _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("base", ctypes.c_double),
                 ("inv_freq", ctypes.c_void_p), ("amplitude", ctypes.c_float), ("q_row_stride", ctypes.c_int64),
                 ("k_row_stride", ctypes.c_int64), ("v_row_stride", ctypes.c_int64)]
+
+
+#: RopeDesc in one piece: a ctypes structure takes three times as long to fill, a twentieth of a rotated append's call
+_ROPE_DESC = struct.Struct("@iidPf4xqqq")
+_FP32_MAX = 3.4028234663852886e38
 
 
 class PlanInfo(ctypes.Structure):
@@ -135,7 +142,7 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "ap_plan_create": (ctypes.c_int, [ctypes.POINTER(vp), vp, ctypes.POINTER(BatchDesc), vp]),
         "ap_kv_pool_bytes_4bit": (sz, [ctypes.POINTER(PoolDesc)]),
         "ap_kv_pool_create_4bit": (ctypes.c_int, [ctypes.POINTER(vp), ctypes.POINTER(PoolDesc)]),
-        "ap_kv_append_rope": (ctypes.c_int, [vp, vp, ctypes.POINTER(RopeDesc), vp, vp, vp, vp, vp]),
+        "ap_kv_append_rope": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp, vp]),      # (the description: bytes or a RopeDesc by reference)
         "ap_kv_read_new": (ctypes.c_int, [vp, vp, vp, vp, vp]),
         "ap_plan_create_windowed": (ctypes.c_int, [ctypes.POINTER(vp), vp, ctypes.POINTER(BatchDesc),
                                                    ctypes.POINTER(WindowDesc), vp]),
@@ -248,8 +255,6 @@ def _stream(stream, device: Optional[int] = None) -> Optional[int]:
     device; the current device where it is not given)."""
     global _raw_stream
     if stream is None:
-        if _raw_stream is not None and device is not None and device >= 0:
-            return _raw_stream(device) or None
         if _raw_stream is None:
             try:
                 import torch
@@ -469,7 +474,8 @@ def plan_export(plan: Plan) -> dict:
 
 def kv_append(pool: KVPool, plan: Plan, k_new, v_new, stream=None) -> None:
     dev = pool.device
-    status = (_lib or load()).ap_kv_append(pool.handle, plan.handle, *_pair(k_new, v_new, plan.kv_bytes, dev), _stream(stream, dev))
+    k_at, v_at = _pair(k_new, v_new, plan.kv_bytes, dev)
+    status = (_lib or load()).ap_kv_append(pool.handle, plan.handle, k_at, v_at, _stream(stream, dev))
     if status:
         _check(status, "ap_kv_append")
 
@@ -512,9 +518,11 @@ def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, r
     q_at, q_stride = (None, 0) if q is None else _strided_rows(q, n, plan.num_q_heads, d, plan.q_bytes, dev)
     k_at, k_stride = _strided_rows(k_new, n, hkv, d, kv_bytes, dev)
     v_at, v_stride = _strided_rows(v_new, n, hkv, d, kv_bytes, dev)
-    desc = RopeDesc(rotary, 1 if interleaved else 0, base, None if freq is None else freq.ctypes.data, amplitude, q_stride,
-                    k_stride, v_stride)
-    status = (_lib or load()).ap_kv_append_rope(pool.handle, plan.handle, ctypes.byref(desc), q_at, k_at, v_at,
+    if not abs(amplitude) <= _FP32_MAX:      # (NaN and what fp32 does not hold: refused by the library)
+        amplitude = math.nan
+    desc = _ROPE_DESC.pack(rotary, 1 if interleaved else 0, base, 0 if freq is None else freq.ctypes.data, amplitude, q_stride,
+                           k_stride, v_stride)
+    status = (_lib or load()).ap_kv_append_rope(pool.handle, plan.handle, desc, q_at, k_at, v_at,
                                                 _one(q_rot, plan.q_bytes, dev), _stream(stream, dev))
     if status:
         _check(status, "ap_kv_append_rope")
@@ -523,7 +531,8 @@ def kv_append_rope(pool: KVPool, plan: Plan, k_new, v_new, q=None, q_rot=None, r
 def kv_read_new(pool: KVPool, plan: Plan, k, v, stream=None) -> None:
     """The rows of the plan's new tokens, read back as the bf16 numbers the pool holds (or, in 4 bits, stands for)."""
     dev = pool.device
-    status = (_lib or load()).ap_kv_read_new(pool.handle, plan.handle, *_pair(k, v, plan.kv_bytes, dev), _stream(stream, dev))
+    k_at, v_at = _pair(k, v, plan.kv_bytes, dev)
+    status = (_lib or load()).ap_kv_read_new(pool.handle, plan.handle, k_at, v_at, _stream(stream, dev))
     if status:
         _check(status, "ap_kv_read_new")
 
@@ -551,8 +560,9 @@ def attention_iteration(pool: KVPool, plan: Plan, q, out, lse=None, workspace=No
             _checked(workspace, 0, dev, None))
     except AttributeError:                   # none, or an address
         workspace_bytes = workspace_bytes or 0
-    status = (_lib or load()).ap_attention_iteration(pool.handle, plan.handle, *_pair(q, out, plan.q_bytes, dev),
-                                                     _lse_rows(lse, plan.lse_bytes, dev), workspace, workspace_bytes,
+    q_at, out_at = _pair(q, out, plan.q_bytes, dev)
+    lse_at = None if lse is None else _lse_rows(lse, plan.lse_bytes, dev)
+    status = (_lib or load()).ap_attention_iteration(pool.handle, plan.handle, q_at, out_at, lse_at, workspace, workspace_bytes,
                                                      _stream(stream, dev))
     if status:
         _check(status, "ap_attention_iteration")

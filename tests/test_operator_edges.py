@@ -512,6 +512,27 @@ def test_struct_sizes_of_the_operators_match_the_header(tmp_path):
     got = [int(x) for x in subprocess.check_output([str(exe)]).split()]
     assert got == [ctypes.sizeof(B.RopeDesc), ctypes.sizeof(B.WindowDesc), *(getattr(B.RopeDesc, f).offset for f in fields),
                    B.WindowDesc.sinks.offset]
+    # the packed form that the binding passes
+    packed = B._ROPE_DESC.pack(64, 1, 2.5, 4096, 0.5, 8, 16, 24)
+    desc = B.RopeDesc.from_buffer_copy(packed)
+    assert len(packed) == got[0] and tuple(getattr(desc, f) for f in fields) == (64, 1, 2.5, 4096, 0.5, 8, 16, 24)
+
+
+def test_amplitudes_and_bases_that_are_no_numbers_are_refused():
+    import torch
+    pool, plan = _host_plan()
+    k = torch.zeros((4, 2, 64), dtype=torch.bfloat16)
+    for kw in (dict(amplitude=float("inf")), dict(amplitude=float("nan")), dict(amplitude=1e39), dict(amplitude=-1e300), dict(base=float("inf")),
+               dict(base=-2), dict(base=0)):
+        with pytest.raises(ap.ApError) as e:
+            ap.kv_append_rope(pool, plan, k, k, **kw)
+        assert e.value.status == B.AP_ERR_INVALID_ARG, kw
+    for kw in (dict(amplitude=np.float32(1.5), base=10000), dict(amplitude=-2, base=np.float64(7), rotary_dim=np.int64(32), interleaved=np.bool_(True))):
+        with pytest.raises(ap.ApError) as e:
+            ap.kv_append_rope(pool, plan, k, k, **kw)
+        assert e.value.status == B.AP_ERR_CUDA, kw
+    ap.plan_destroy(plan)
+    ap.kv_pool_destroy(pool)
 
 
 @pytest.mark.gpu
