@@ -228,6 +228,8 @@ def _checked(x, nbytes: int, device: int, itemsize: Optional[int], dense: bool =
         if dense and x.nbytes < nbytes:
             raise ValueError(f"a tensor of {x.nbytes} bytes where the call takes {nbytes}")
     elif isinstance(x, np.ndarray):
+        if device >= 0:
+            raise ValueError("expected a device tensor, not a host array")
         if not x.flags.c_contiguous:
             raise ValueError("expected a contiguous array")
         if x.nbytes < nbytes:
@@ -305,7 +307,7 @@ def _plane(x, nbytes: int, device: int) -> Optional[int]:
     """Address of a pool plane: at least `nbytes` on `device` (any view of memory that lies together)."""
     if hasattr(x, "nbytes") and x.nbytes < nbytes:
         raise ValueError(f"a plane of {x.nbytes} bytes where the pool takes {nbytes}")
-    return _checked(x, 0, device, None, dense=False) if hasattr(x, "data_ptr") else _ptr(x)
+    return _checked(x, 0, device, None, dense=False)
 
 
 def kv_pool_create(num_pages: int, num_kv_heads: int, head_dim: int, k_base=None, v_base=None,
@@ -488,7 +490,7 @@ def _strided_rows(x, rows: int, heads: int, dim: int, nbytes: int, device: int) 
         row, head, one = x.stride()
         n, h, d = x.shape
     except AttributeError:                   # an address, or not given
-        return _ptr(x), 0
+        return _checked(x, nbytes, device, 2), 0
     except ValueError:
         n = h = d = row = head = one = 0
     if one != 1 or (head != d and h > 1):
@@ -559,7 +561,7 @@ def attention_iteration(pool: KVPool, plan: Plan, q, out, lse=None, workspace=No
         workspace = workspace.data_ptr() if workspace.get_device() == dev and workspace.is_contiguous() else (
             _checked(workspace, 0, dev, None))
     except AttributeError:                   # none, or an address
-        workspace_bytes = workspace_bytes or 0
+        workspace, workspace_bytes = _checked(workspace, 0, dev, None), workspace_bytes or 0
     q_at, out_at = _pair(q, out, plan.q_bytes, dev)
     lse_at = None if lse is None else _lse_rows(lse, plan.lse_bytes, dev)
     status = (_lib or load()).ap_attention_iteration(pool.handle, plan.handle, q_at, out_at, lse_at, workspace, workspace_bytes,

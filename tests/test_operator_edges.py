@@ -335,6 +335,25 @@ def test_tensors_that_are_too_small_or_of_another_type_are_refused():
 
 
 @pytest.mark.gpu
+def test_host_arrays_are_refused_where_a_kernel_would_read_or_write_them():
+    b = _batch((8, 2, 64), 66, [1, 20], [40, 20])
+    dev = R.Device(b)
+    rows = np.zeros((21, 2, 64), np.uint16)
+    for call in (lambda: ap.kv_append(dev.pool, dev.plan, rows, dev.v_new), lambda: ap.kv_read_new(dev.pool, dev.plan, rows, rows),
+                 lambda: ap.kv_append_rope(dev.pool, dev.plan, dev.k_new, rows),
+                 lambda: ap.kv_append_rope(dev.pool, dev.plan, dev.k_new, dev.v_new, q=b.q, q_rot=dev.q),
+                 lambda: ap.kv_append_rope(dev.pool, dev.plan, dev.k_new, dev.v_new, q=dev.q, q_rot=b.q),
+                 lambda: ap.attention_iteration(dev.pool, dev.plan, b.q, dev.out, dev.lse, dev.workspace),
+                 lambda: ap.attention_iteration(dev.pool, dev.plan, dev.q, dev.out, np.zeros((21, 8), np.float32), dev.workspace),
+                 lambda: ap.attention_iteration(dev.pool, dev.plan, dev.q, dev.out, dev.lse, np.zeros(1 << 16, np.uint8)),
+                 lambda: ap.attention_iteration_static(dev.pool, dev.plan, dev.q, b.q),
+                 lambda: ap.kv_pool_create(b.num_pages, 2, 64, b.k_pool, b.v_pool)):
+        with pytest.raises(ValueError):
+            call()
+    dev.close()
+
+
+@pytest.mark.gpu
 def test_tensors_of_another_device_are_refused_and_pinned_ones_are_read():
     import torch
     b = _batch((8, 2, 64), 66, [1, 20], [40, 20])
