@@ -47,10 +47,10 @@ UNIT = "KV-tokens/s"
 # workload (ncu captures summarised under profiles/), keyed by (kernel, config, hash of
 # the kernel's source file the counters were taken from); a changed kernel reports null.
 NCU_TRAFFIC = {
-    # profiles/decode_splitk_config2.md: 536.5 MB read + 2.2 MB written per launch (algorithmic 535.0 MB)
-    ("decode_splitk", 2, "18ba4bb7b010e361"): 538.7e6,
-    # profiles/prefill_tcgen05_config3.md: 149.9 MB read + 16.5 MB written per launch (K/V re-reads are served by the L2)
-    ("prefill_tcgen05", 3, "cdcbd1dbdff491be"): 166.4e6,
+    # profiles/decode_splitk_config2.md: 536.6 MB read + 2.3 MB written per launch (algorithmic 535.0 MB)
+    ("decode_splitk", 2, "1b9aa6fd843646c3"): 538.8e6,
+    # profiles/prefill_tcgen05_config3.md: 148.9 MB read + 15.1 MB written per launch (K/V re-reads are served by the L2)
+    ("prefill_tcgen05", 3, "ae4bf39589d7ea14"): 164.1e6,
 }
 
 

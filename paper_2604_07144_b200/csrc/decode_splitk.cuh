@@ -234,7 +234,7 @@ __device__ __forceinline__ void combine_item(const DecodeItem item, const float 
 // kWin: sliding window.  The planner has cut the pages without a visible key out of the row's table, so of
 // the kv_len keys that are left only [sinks, kv_len - window) are hidden: the rest of the last sink page and
 // the head of the window's first page, fewer than two pages.  64 rows of 128 .. 8192 tokens with a window of 1024
-// and 4 sinks (168 MB of visible K/V, 25.6 us at copy bandwidth): 32.2 us, HBM-bound like the kernel without
+// and 4 sinks (168 MB of visible K/V, 25.6 us at copy bandwidth): 32.4 us, HBM-bound like the kernel without
 // the tests; what is above the floor is start-up and the finishing spread of a short launch.
 template <int D, bool kWin>
 __device__ __forceinline__ void decode_cta(const CUtensorMap &k_map, const CUtensorMap &v_map, const __nv_bfloat16 *__restrict__ q,
@@ -614,6 +614,7 @@ __device__ __forceinline__ void decode_cta(const CUtensorMap &k_map, const CUten
                     o[i][0] *= al0; o[i][1] *= al1; o[i][2] *= al0; o[i][3] *= al1;
                 }
                 // P^T as the B operand: transpose the two 8x8 (token x head) blocks across the warp
+                // (weights in bf16 for P V, each off by at most 2^-8 of itself; their sum takes them as they are)
                 const uint32_t b0 = movmatrix_trans(pack_bf16x2(p0_, p1_));
                 const uint32_t b1 = movmatrix_trans(pack_bf16x2(p2_, p3_));
                 // ---- O^T += V^T P^T : columns of d (16mt + g, + 8) x heads (2t, 2t+1)

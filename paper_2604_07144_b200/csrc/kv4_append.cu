@@ -1,6 +1,6 @@
 // Appending to, reading back from and widening a 4-bit pool (the format is described in kv4.cuh).  All
 // three are single passes over their data, bound by HBM: 8000 rows at 8 heads of 128, appended and read back
-// (84 MB), 16.0 us (5.2 TB/s); widening 1290 pages of 8 heads (107 MB read and written) 15.5 us.
+// (84 MB), 16.2 us (5.2 TB/s; 16.6 us in a loop of seconds); widening 1290 pages of 8 heads (107 MB read and written) 15.5 us.
 #include "internal.h"
 #include "kv4.cuh"
 #include "ptx.cuh"

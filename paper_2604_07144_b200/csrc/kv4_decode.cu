@@ -12,8 +12,8 @@
 // warps per SM, not two of eight: an SM's scheduler prefers its older block's warps, which ran through their
 // lists in 145 us where the younger block's took 181.)
 //
-// What bounds the kernel is the ALU pipe (LOP3, PRMT, shifts: one warp instruction in two clocks) on the
-// way from nibbles to MMA operands, so that way is short.  The bits of a byte b, put into a bf16 pattern with
+// Most of what an SM issues lies on the way from nibbles to MMA operands (LOP3, PRMT, shifts on the ALU pipe: one
+// warp instruction in two clocks), so that way is short.  The bits of a byte b, put into a bf16 pattern with
 // nothing above them, ARE the number b 2^-133 (bits 0 .. 6 are a subnormal's mantissa, and from bit 7, the
 // exponent's last, the scale goes on linearly).  One AND therefore turns two nibbles of a word into two bf16
 // numbers, c 2^-133 where they lie at bits 0 .. 3 of their halves and c 2^-129 at bits 4 .. 7; a shift by
@@ -32,12 +32,12 @@
 // read 16 bytes of a row per lane, V fragments 8 bytes of four rows per lane, pairs of rows interleaved with
 // PRMT.
 //
-// Measured: 16 rows of 32 - 64 k tokens at 64 / 8 heads of 128 (841 MB) 165 us, 5.1 TB/s, 0.78 of copy bandwidth (198 us in
+// Measured: 16 rows of 32 - 64 k tokens at 64 / 8 heads of 128 (841 MB) 165 us, 5.1 TB/s, 0.78 of copy bandwidth (194 us in
 // a loop of seconds, where the power limit takes the clock down); 64 rows of 128 .. 8192 tokens at 32 / 8
-// heads (126 MB) 34.6 us.  Copying alone, without the arithmetic, takes 132 and 27.5 us.  331 warp
+// heads (126 MB) 35.3 us.  Copying alone, without the arithmetic, takes 132 and 27.5 us.  331 warp
 // instructions per tile (K and V of 16 tokens): 127 on the ALU pipe and 72 HFMA2, each one per two clocks of a
-// scheduler, and 17 MMAs, one per eight.  Issue slots are 70 % busy, the ALU pipe 54 %, and neither more warps (20
-// at 96 registers) nor fewer (12) change the time.
+// scheduler, and 17 MMAs, one per eight.  No pipe is full: issue slots are 70 % busy, the ALU pipe 54 %; a warp's
+// products and its widening take turns.  More warps (20 at 96 registers: 188 us) and fewer (12: 195) are slower.
 //
 // At the end of an item a warp has its head's complete (m, l, O) in registers and writes the bf16 output or, for
 // a stream cut across lists, an fp32 partial for the merge kernel.
@@ -407,6 +407,9 @@ kv4_decode_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict_
                     o[i][0] *= al0; o[i][1] *= al1; o[i][2] *= al0; o[i][3] *= al1;
                 }
             }
+            // The weights go to the tensor cores in bf16, each off by at most 2^-8 of itself; their sum takes them as they
+            // are.  The outputs' RMS error rises from the last rounding's 0.0017 to 0.0020 .. 0.0023; weights in two
+            // parts would double the products of P V.
             const float mf0 = m0 * f_col[0], mf1 = m1 * f_col[1];
             uint32_t b0[2], b1[2];
 #pragma unroll

@@ -8,8 +8,8 @@
 // taken off there, and only the fraction goes to fp32 sine and cosine.  Those are computed once per token
 // and shared by its heads through shared memory, ahead of the wait for the kernel before.  The rotation is fp32
 // and rounds once, to bf16.
-// 8192 rows at 32 / 8 heads of 128 (201 MB): 32.2 us, 6.26 TB/s, 0.95 of copy bandwidth; 4 rows at 8 / 2 heads of 64:
-// 1.4 us in a graph.
+// 8192 rows at 32 / 8 heads of 128 (201 MB): 32.2 us, 6.25 TB/s, 0.95 of copy bandwidth (33.5 us, 0.92, in a loop of
+// seconds); 4 rows at 8 / 2 heads of 64: 1.4 us in a graph.
 #include <algorithm>
 
 #include "internal.h"
@@ -101,8 +101,8 @@ rope_append_kernel(const __grid_constant__ RopeParams rope, uint8_t *__restrict_
         if (threadIdx.x == 0) ptx::record_status(status, AP_ERR_BAD_BLOCK_TABLE);
         return;
     }
-    // A thread's first kAhead units are loaded ahead of the barrier that waits for the angles.  (From L2: this
-    // kernel was resident while its inputs were still being written, and they are read once.)
+    // A thread's first kAhead units are loaded ahead of the barrier that waits for the angles.  (Past L1, which
+    // would keep what is read once.)
     uint4 x[kAhead], y[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {

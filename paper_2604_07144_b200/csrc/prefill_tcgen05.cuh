@@ -161,7 +161,8 @@ __device__ __noinline__ void rescale_o(uint32_t taddr, float alpha) {
 // positions of the unit's compacted context (the planner leaves out the pages that no row of the unit sees,
 // which lie between the sinks and the first row's window, so both tests hold for compacted positions too).
 // Masked steps (about four of a unit's ten at a window of 1024) test one bit per score: with comparisons of
-// positions 8 x 512 rows beside 120 decode rows took 167 us where they take 135.
+// positions 8 x 512 rows beside 120 decode rows took 167 us where they took 135 (137 now, 152 in a loop of seconds, where
+// the power limit takes the clock down).
 template <int D, bool kWin>
 __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUtensorMap &k_map, const CUtensorMap &v_map,
                                              const PrefillTile *__restrict__ tiles, const int32_t *__restrict__ bt_flat,
@@ -448,6 +449,7 @@ __device__ __forceinline__ void prefill_unit(const CUtensorMap &q_map, const CUt
                             xy.x = exp2_approx(xy.x);
                             xy.y = exp2_approx(xy.y);
                         }
+                        // (the sum takes the weights as they are; P V takes them in bf16, each off by at most 2^-8 of itself)
                         sum2 = __fadd2_rn(sum2, xy);
                         preg[i] = pack_bf16x2(xy.x, xy.y);
                     }
