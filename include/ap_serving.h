@@ -370,6 +370,10 @@ int ap_kv_read_new(ap_kv_pool *pool, const ap_plan *plan, void *k, void *v, void
  * chunks: causal tiled attention on tcgen05 tensor cores).  The pool must
  * already hold the iteration's tokens.  Attention calls on the same pool must
  * not overlap on the GPU (they share the pool's merge arrival counters).
+ * A key that a row does not see has weight exactly 0 there, whatever its K holds; a
+ * visible K that makes a score NaN makes the row NaN.  In a prefill chunk the
+ * products 0 * V are still formed for keys of the same 128-key step, so a
+ * non-finite V can reach rows before it (never of another sequence).
  * q, out: device, 16-byte aligned; lse: device or NULL; workspace: device,
  * 256-byte aligned, at least ap_plan_workspace_bytes() (else
  * WORKSPACE_TOO_SMALL), contents undefined before and after.

@@ -213,6 +213,8 @@ def _one(x, nbytes: int, device: int) -> Optional[int]:
 
 def _checked(x, nbytes: int, device: int, itemsize: Optional[int], dense: bool = True) -> Optional[int]:
     """The same at length.  `itemsize`: 2 for bf16, 4 for fp32 (or integers of that size, or bytes), None for any type."""
+    if nbytes <= 0 and dense and itemsize is not None:
+        return _ptr(x)                       # a plan without new tokens: nothing is read or written
     if hasattr(x, "data_ptr"):
         global _bf16, _fp32
         import torch
@@ -232,6 +234,10 @@ def _checked(x, nbytes: int, device: int, itemsize: Optional[int], dense: bool =
             raise ValueError("expected a device tensor, not a host array")
         if not x.flags.c_contiguous:
             raise ValueError("expected a contiguous array")
+        plain = x.dtype.kind in "biu" and x.dtype.itemsize in (1, itemsize)
+        like = x.dtype == np.float32 if itemsize == 4 else x.dtype.kind == "V" and x.dtype.itemsize == 2    # (numpy's own has no bf16)
+        if itemsize is not None and not plain and not like:
+            raise ValueError(f"expected {'bf16 bits' if itemsize == 2 else 'float32'}, not {x.dtype}")
         if x.nbytes < nbytes:
             raise ValueError(f"an array of {x.nbytes} bytes where the call takes {nbytes}")
     return _ptr(x)
@@ -493,6 +499,8 @@ def _strided_rows(x, rows: int, heads: int, dim: int, nbytes: int, device: int) 
         return _checked(x, nbytes, device, 2), 0
     except ValueError:
         n = h = d = row = head = one = 0
+    if rows <= 0:
+        return _ptr(x), 0
     if one != 1 or (head != d and h > 1):
         raise ValueError("expected [rows, heads, head_dim] with a token's heads contiguous")
     if n < rows or h != heads or d != dim:

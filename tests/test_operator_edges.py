@@ -317,6 +317,16 @@ def test_tensors_that_are_too_small_or_of_another_type_are_refused():
             ap.serving_iteration_host(pool, [1] * 4, [20] * 4, np.arange(8, dtype=np.int32).reshape(4, 2), 8, *args)
     with pytest.raises(ValueError):
         ap.serving_iteration_host(pool, [1] * 4, [20] * 4, np.arange(8, dtype=np.int32).reshape(4, 2), 8, *rows, np.zeros((3, 8), np.float32))
+    table = np.arange(8, dtype=np.int32).reshape(4, 2)
+    for i, bad in ((0, np.float32), (1, np.float16), (2, np.float64), (3, np.int32), (4, np.float64), (4, np.float16), (4, np.uint16)):
+        args = rows + [np.zeros((4, 8), np.float32)]
+        args[i] = args[i].astype(bad)
+        with pytest.raises(ValueError):
+            ap.serving_iteration_host(pool, [1] * 4, [20] * 4, table, 8, *args)
+    for cast in (lambda x: x, lambda x: x.view(np.int16), lambda x: x.view(np.uint8), lambda x: torch.from_numpy(x.view(np.int16))):
+        with pytest.raises(ap.ApError) as e:
+            ap.serving_iteration_host(pool, [1] * 4, [20] * 4, table, 8, *(cast(x) for x in rows), np.zeros((4, 8), np.float32))
+        assert e.value.status == B.AP_ERR_CUDA
     for create, size in ((ap.kv_pool_create, ap.kv_pool_bytes(8, 2, 64)), (ap.kv_pool_create_4bit, ap.kv_pool_bytes_4bit(8, 2, 64))):
         planes = torch.zeros(size, dtype=torch.uint8), torch.zeros(size - 1, dtype=torch.uint8)
         for args in (planes, planes[::-1]):
@@ -332,6 +342,25 @@ def test_tensors_that_are_too_small_or_of_another_type_are_refused():
         assert e.value.status == B.AP_ERR_CUDA
     ap.plan_destroy(plan)
     ap.kv_pool_destroy(pool)
+
+
+@pytest.mark.gpu
+def test_a_plan_without_new_tokens_takes_any_tensors_and_touches_none():
+    import torch
+    b = _batch((8, 2, 64), 70, [0, 0], [40, 20])
+    dev = R.Device(b)
+    before = dev.k_pool.clone()
+    nothing = torch.empty(0, dtype=torch.bfloat16)
+    ap.kv_append(dev.pool, dev.plan, nothing, nothing)
+    ap.kv_append_rope(dev.pool, dev.plan, nothing, nothing, q=nothing, q_rot=nothing)
+    ap.kv_append_rope(dev.pool, dev.plan, dev.k_pool[:, :, 0], None)
+    ap.kv_read_new(dev.pool, dev.plan, nothing, nothing)
+    ap.attention_iteration(dev.pool, dev.plan, nothing, nothing, nothing, None)
+    ap.attention_iteration_static(dev.pool, dev.plan, None, None)
+    ap.serving_iteration_host(dev.pool, b.q_lens, b.ctx_lens, b.block_tables, 8, None, None, None, None)
+    assert ap.last_device_status(dev.pool) == 0
+    assert np.array_equal(to_bits(dev.k_pool), to_bits(before)) and torch.isnan(dev.out.float()).all() and torch.isnan(dev.lse).all()
+    dev.close()
 
 
 @pytest.mark.gpu
