@@ -468,6 +468,168 @@ int ap_kv_pool_set_wait_limit(ap_kv_pool *pool, uint64_t limit_ns);
  */
 int ap_selftest_wait_timeout(ap_kv_pool *pool, uint64_t limit_ns, int leave_counter, void *stream);
 
+/* --------------------------------------------------------- whole prompts -- */
+
+/*
+ * Attention of whole prompts, packed one after the other: token t of a prompt
+ * attends tokens 0 .. t of the same prompt.  K and V are read from the rows the
+ * projection left, not from pages, so it needs no append before it and no cache
+ * behind it (prompts to embed, rank or score; the first iteration of a request,
+ * beside its ap_kv_append; layers whose cache another GPU keeps).  The pool gives
+ * kv heads, head_dim, device, staging, status word and wait limit; its pages are
+ * not touched.  A prompt that continues a cached prefix is an ap_plan's.
+ * lens: host, [batch] tokens of each prompt, >= 0 (0: no rows); read during the
+ * call.  num_q_heads, softmax_scale: as in ap_batch_desc.  Up to 2^30 tokens in all.
+ */
+typedef struct ap_prompt_plan ap_prompt_plan; /* opaque */
+typedef struct ap_prompt_desc {
+    int32_t batch;
+    int32_t num_q_heads;
+    const int32_t *lens;
+    float softmax_scale;
+} ap_prompt_desc;
+int ap_prompt_plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *prompts, void *stream);
+int ap_prompt_plan_destroy(ap_prompt_plan *plan);
+
+typedef struct ap_prompt_info {
+    int64_t n_rows;      /* rows of q, k, v, out */
+    int64_t pairs;       /* (query row, key) pairs, one head */
+    int64_t tiles;       /* work units on the tensor cores (prompts of more than 64 tokens) */
+    int64_t short_units; /* work units of the kernel for shorter prompts */
+    int64_t launches;    /* kernels ap_prompt_attention launches */
+} ap_prompt_info;
+int ap_prompt_plan_get_info(const ap_prompt_plan *plan, ap_prompt_info *info);
+
+/*
+ * q: [n_rows][num_q_heads][head_dim] bf16, k, v: [n_rows][num_kv_heads][head_dim]
+ * bf16, device, 16-byte aligned; *_row_stride: elements from one token's row to the
+ * next, a multiple of 8 (0: contiguous), so that they may be cut out of one
+ * projection's output.  out: [n_rows][num_q_heads][head_dim] contiguous, 16-byte
+ * aligned; lse: [n_rows][num_q_heads] fp32 or NULL.  out and lse overlap no input
+ * (INVALID_ARG).  Softmax weights are rounded to bf16 for their product with V.  A key behind a row
+ * weighs exactly 0, whatever its K holds; a non-finite V can reach the rows before
+ * it of the same block of 128 rows of its prompt, never another prompt.
+ * Rows behind the last prompt are neither read nor written.
+ */
+typedef struct ap_prompt_strides {
+    int64_t q_row_stride, k_row_stride, v_row_stride;
+} ap_prompt_strides;
+int ap_prompt_attention(ap_kv_pool *pool, const ap_prompt_plan *plan, const void *q, const void *k, const void *v, void *out,
+                        float *lse, const ap_prompt_strides *strides, void *stream);
+
+/* ---------------------------------------------------- state-space layers -- */
+
+/*
+ * Layers that keep a state of fixed size per sequence instead of a KV cache, over
+ * the same batches: q_lens new tokens of each sequence, chunks beside single
+ * tokens, rows concatenated in batch order.  Where attention has block tables a
+ * sequence here has a slot, which holds, for one layer:
+ *     conv plane : [num_slots][conv_width - 1][channels]  bf16, the last inputs of
+ *                  the short convolution, oldest first
+ *     scan plane : [num_slots][channels][state_dim]       fp32
+ * channels: a multiple of 8 (else UNSUPPORTED) up to 2^20; state_dim 8, 16, 32 or
+ * 64; conv_width 2, 3 or 4 (else UNSUPPORTED).  conv_base / scan_base: device,
+ * 16-byte aligned, owned by the caller, or NULL: the library allocates (and zero
+ * fills) that plane.  device < 0 (with both bases NULL): a host-only pool, which
+ * plans and validates; calls that would launch return AP_ERR_CUDA.
+ */
+typedef struct ap_state_pool ap_state_pool; /* opaque */
+typedef struct ap_state_plan ap_state_plan; /* opaque */
+typedef struct ap_state_desc {
+    int32_t num_slots;
+    int32_t channels;
+    int32_t state_dim;
+    int32_t conv_width;
+    void *conv_base;
+    void *scan_base;
+    int32_t device;
+} ap_state_desc;
+/* Bytes of a plane; 0 if the description is invalid. */
+size_t ap_state_pool_conv_bytes(const ap_state_desc *desc);
+size_t ap_state_pool_scan_bytes(const ap_state_desc *desc);
+int ap_state_pool_create(ap_state_pool **out, const ap_state_desc *desc);
+/* Frees the handle and only what the library allocated.  Synchronises the device. */
+int ap_state_pool_destroy(ap_state_pool *pool);
+void *ap_state_pool_conv_base(const ap_state_pool *pool);
+void *ap_state_pool_scan_base(const ap_state_pool *pool);
+
+/*
+ * One iteration's batch.  q_lens, ctx_lens as in ap_batch_desc; a sequence whose
+ * context is all new (ctx_len == q_len) begins from a state of zeros, whatever its
+ * slot holds; any other goes on from its slot.  slots: host, [batch]; in
+ * [0, num_slots) and no slot twice among sequences with q_len > 0 (INVALID_ARG).
+ * Every call with the plan leaves the slots of those sequences at the state after
+ * their last new token, and other slots as they were.
+ * The plan may be used with every state pool of the same description (but for the
+ * bases): a model makes one per iteration for all its layers.  It belongs to the
+ * pool it was made with, which has to outlive it.
+ */
+typedef struct ap_state_batch {
+    int32_t batch;
+    const int32_t *q_lens;
+    const int32_t *ctx_lens;
+    const int32_t *slots;
+} ap_state_batch;
+int ap_state_plan_create(ap_state_plan **out, ap_state_pool *pool, const ap_state_batch *batch, void *stream);
+int ap_state_plan_destroy(ap_state_plan *plan);
+
+typedef struct ap_state_info {
+    int64_t n_new;         /* rows of x, out, ... */
+    int64_t single_rows;   /* sequences with one new token */
+    int64_t chunk_seqs;    /* sequences with more */
+    int64_t split_seqs;    /* of these: cut along time for the scan */
+    int64_t segments;      /* pieces they were cut into */
+    int64_t launches_scan; /* kernels ap_scan_iteration launches */
+} ap_state_info;
+int ap_state_plan_get_info(const ap_state_plan *plan, ap_state_info *info);
+
+/* Bytes of caller-provided device workspace that ap_scan_iteration needs for this
+ * plan (the states between the pieces of sequences cut along time); may be 0. */
+size_t ap_state_plan_workspace_bytes(const ap_state_plan *plan);
+
+/*
+ * Short causal convolution, channel by channel (w = conv_width):
+ *     out[t][c] = act(bias[c] + sum_{j < w} weight[c][j] x[t - w + 1 + j][c])
+ * x before a sequence's first new token comes from its slot (or is zero); the slot
+ * then holds the last w - 1 inputs, bit for bit.  silu != 0: act(y) = y / (1 + e^-y).
+ * Sums in fp32, rounded once.
+ * x: [n_new][channels] bf16, rows x_row_stride elements apart (0: contiguous; a
+ * multiple of 8); weight: [channels][w] bf16; bias: [channels] bf16 or NULL; out:
+ * [n_new][channels] bf16, rows out_row_stride elements apart.  Device, 16-byte
+ * aligned.  out overlaps no input and no slot (INVALID_ARG).
+ */
+typedef struct ap_conv_desc {
+    int32_t silu;
+    int64_t x_row_stride, out_row_stride;
+} ap_conv_desc;
+int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_conv_desc *conv, const void *x,
+                      const void *weight, const void *bias, void *out, void *stream);
+
+/*
+ * Selective state space scan, channel by channel (n < state_dim):
+ *     d      = dt[t][c] + dt_bias[c];  if softplus: d = ln(1 + e^d)
+ *     h[c][n] <- e^(d a[c][n]) h[c][n] + d x[t][c] b[t][n]
+ *     y      = sum_n c[t][n] h[c][n] + d_skip[c] x[t][c]
+ *     out[t][c] = y, or y z[t][c] / (1 + e^-z[t][c]) where z is given
+ * with h from the sequence's slot (or zero) and back to it.  fp32 throughout; out
+ * is rounded once.
+ * x, dt, z: [n_new][channels] bf16; b, c: [n_new][state_dim] bf16; each with rows
+ * *_row_stride elements apart (0: contiguous; a multiple of 8), so that they may be
+ * cut out of projections' outputs.  a: [channels][state_dim] fp32; d_skip, dt_bias:
+ * [channels] fp32 or NULL; z may be NULL.  out: [n_new][channels] bf16, rows
+ * out_row_stride elements apart.  Device, 16-byte aligned.  out overlaps no input
+ * and no slot (INVALID_ARG).  workspace: device, 256-byte aligned, at least
+ * ap_state_plan_workspace_bytes() (else WORKSPACE_TOO_SMALL), contents undefined
+ * before and after; calls that may overlap on the GPU take one each.
+ */
+typedef struct ap_scan_desc {
+    int32_t softplus;
+    int64_t x_row_stride, dt_row_stride, b_row_stride, c_row_stride, z_row_stride, out_row_stride;
+} ap_scan_desc;
+int ap_scan_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_scan_desc *scan, const void *x,
+                      const void *dt, const float *a, const void *b, const void *c, const void *z, const float *d_skip,
+                      const float *dt_bias, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ----------------------------------------------------------- diagnostics -- */
 
 /*

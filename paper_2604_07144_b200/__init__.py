@@ -13,4 +13,8 @@ from .binding import (  # noqa: F401
     plan_predict, plan_export, plan_get_info, plan_workspace_bytes, profile_collect, profile_enable,
     serving_iteration_host, status_string, kv_pool_set_wait_limit, selftest_wait_timeout, kv_pool_set_single_launch,
     plan_create_windowed, kv_pool_bytes_4bit, kv_pool_create_4bit, kv_append_rope, kv_read_new,
+    PromptPlan, prompt_plan_create, prompt_plan_destroy, prompt_plan_get_info, prompt_attention,
+    StatePool, StatePlan, state_pool_conv_bytes, state_pool_scan_bytes, state_pool_create, state_pool_destroy, state_pool_conv_base,
+    state_pool_scan_base, state_plan_create, state_plan_destroy, state_plan_get_info, state_plan_workspace_bytes,
+    conv_iteration, scan_iteration,
 )

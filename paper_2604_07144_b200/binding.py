@@ -43,6 +43,10 @@ EXPORTED_SYMBOLS = (
     "ap_static_workspace_bytes", "ap_attention_iteration_static",
     "ap_kv_pool_set_wait_limit", "ap_selftest_wait_timeout", "ap_kv_pool_set_single_launch",
     "ap_plan_create_windowed", "ap_kv_pool_bytes_4bit", "ap_kv_pool_create_4bit", "ap_kv_append_rope", "ap_kv_read_new",
+    "ap_prompt_plan_create", "ap_prompt_plan_destroy", "ap_prompt_plan_get_info", "ap_prompt_attention",
+    "ap_state_pool_conv_bytes", "ap_state_pool_scan_bytes", "ap_state_pool_create", "ap_state_pool_destroy",
+    "ap_state_pool_conv_base", "ap_state_pool_scan_base", "ap_state_plan_create", "ap_state_plan_destroy",
+    "ap_state_plan_get_info", "ap_state_plan_workspace_bytes", "ap_conv_iteration", "ap_scan_iteration",
 )
 
 
@@ -74,6 +78,49 @@ class RopeDesc(ctypes.Structure):
                 ("inv_freq", ctypes.c_void_p), ("amplitude", ctypes.c_float), ("q_row_stride", ctypes.c_int64),
                 ("k_row_stride", ctypes.c_int64), ("v_row_stride", ctypes.c_int64)]
 
+
+class PromptDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("num_q_heads", ctypes.c_int32), ("lens", ctypes.c_void_p),
+                ("softmax_scale", ctypes.c_float)]
+
+
+class PromptStrides(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("q_row_stride", "k_row_stride", "v_row_stride")]
+
+
+class PromptInfo(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("n_rows", "pairs", "tiles", "short_units", "launches")]
+
+    def as_dict(self):
+        return {n: int(getattr(self, n)) for n, _ in self._fields_}
+
+
+class StateDesc(ctypes.Structure):
+    _fields_ = [("num_slots", ctypes.c_int32), ("channels", ctypes.c_int32), ("state_dim", ctypes.c_int32),
+                ("conv_width", ctypes.c_int32), ("conv_base", ctypes.c_void_p), ("scan_base", ctypes.c_void_p),
+                ("device", ctypes.c_int32)]
+
+
+class StateBatch(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("q_lens", ctypes.c_void_p), ("ctx_lens", ctypes.c_void_p), ("slots", ctypes.c_void_p)]
+
+
+class StateInfo(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("n_new", "single_rows", "chunk_seqs", "split_seqs", "segments", "launches_scan")]
+
+    def as_dict(self):
+        return {n: int(getattr(self, n)) for n, _ in self._fields_}
+
+
+class ConvDesc(ctypes.Structure):
+    _fields_ = [("silu", ctypes.c_int32), ("x_row_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64)]
+
+
+class ScanDesc(ctypes.Structure):
+    _fields_ = [("softplus", ctypes.c_int32)] + [(n + "_row_stride", ctypes.c_int64) for n in ("x", "dt", "b", "c", "z", "out")]
+
+
+_PROMPT_STRIDES, _CONV_DESC, _SCAN_DESC = struct.Struct("@qqq"), struct.Struct("@i4xqq"), struct.Struct("@i4xqqqqqq")
 
 #: RopeDesc in one piece: a ctypes structure takes three times as long to fill, a twentieth of a rotated append's call
 _ROPE_DESC = struct.Struct("@iidPf4xqqq")
@@ -163,6 +210,23 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "ap_kv_pool_set_single_launch": (ctypes.c_int, [vp, i32]),
         "ap_kv_pool_set_wait_limit": (ctypes.c_int, [vp, u64]),
         "ap_selftest_wait_timeout": (ctypes.c_int, [vp, u64, ctypes.c_int, vp]),
+        # (descriptions of the calls that a layer makes: bytes, or a structure by reference)
+        "ap_prompt_plan_create": (ctypes.c_int, [ctypes.POINTER(vp), vp, ctypes.POINTER(PromptDesc), vp]),
+        "ap_prompt_plan_destroy": (ctypes.c_int, [vp]),
+        "ap_prompt_plan_get_info": (ctypes.c_int, [vp, ctypes.POINTER(PromptInfo)]),
+        "ap_prompt_attention": (ctypes.c_int, [vp] * 9),
+        "ap_state_pool_conv_bytes": (sz, [ctypes.POINTER(StateDesc)]),
+        "ap_state_pool_scan_bytes": (sz, [ctypes.POINTER(StateDesc)]),
+        "ap_state_pool_create": (ctypes.c_int, [ctypes.POINTER(vp), ctypes.POINTER(StateDesc)]),
+        "ap_state_pool_destroy": (ctypes.c_int, [vp]),
+        "ap_state_pool_conv_base": (vp, [vp]),
+        "ap_state_pool_scan_base": (vp, [vp]),
+        "ap_state_plan_create": (ctypes.c_int, [ctypes.POINTER(vp), vp, ctypes.POINTER(StateBatch), vp]),
+        "ap_state_plan_destroy": (ctypes.c_int, [vp]),
+        "ap_state_plan_get_info": (ctypes.c_int, [vp, ctypes.POINTER(StateInfo)]),
+        "ap_state_plan_workspace_bytes": (sz, [vp]),
+        "ap_conv_iteration": (ctypes.c_int, [vp] * 8),
+        "ap_scan_iteration": (ctypes.c_int, [vp] * 13 + [sz, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -557,25 +621,244 @@ def kv_copy_pages(dst_pool: KVPool, src_pool: KVPool, dst_ids: Sequence[int], sr
                                    _stream(stream, dst_pool.device) if dst_pool.desc.device >= 0 else None), "ap_kv_copy_pages")
 
 
-def attention_iteration(pool: KVPool, plan: Plan, q, out, lse=None, workspace=None,
-                        workspace_bytes: Optional[int] = None, stream=None) -> None:
-    dev = pool.device
+def _workspace(workspace, workspace_bytes: Optional[int], dev: int) -> Tuple[Optional[int], int]:
+    """(address, bytes) of a caller's workspace: a tensor, an address with its size, or none."""
     try:
         room = workspace.nbytes
         if workspace_bytes is None:
             workspace_bytes = room
         elif workspace_bytes > room:
             raise ValueError(f"a workspace of {room} bytes where the call is told {workspace_bytes}")
-        workspace = workspace.data_ptr() if workspace.get_device() == dev and workspace.is_contiguous() else (
-            _checked(workspace, 0, dev, None))
+        return workspace.data_ptr() if workspace.get_device() == dev and workspace.is_contiguous() else (
+            _checked(workspace, 0, dev, None)), workspace_bytes
     except AttributeError:                   # none, or an address
-        workspace, workspace_bytes = _checked(workspace, 0, dev, None), workspace_bytes or 0
+        return _checked(workspace, 0, dev, None), workspace_bytes or 0
+
+
+def attention_iteration(pool: KVPool, plan: Plan, q, out, lse=None, workspace=None,
+                        workspace_bytes: Optional[int] = None, stream=None) -> None:
+    dev = pool.device
+    workspace, workspace_bytes = _workspace(workspace, workspace_bytes, dev)
     q_at, out_at = _pair(q, out, plan.q_bytes, dev)
     lse_at = None if lse is None else _lse_rows(lse, plan.lse_bytes, dev)
     status = (_lib or load()).ap_attention_iteration(pool.handle, plan.handle, q_at, out_at, lse_at, workspace, workspace_bytes,
                                                      _stream(stream, dev))
     if status:
         _check(status, "ap_attention_iteration")
+
+
+# ---------------------------------------------------------- whole prompts --
+
+class PromptPlan:
+    """Handle returned by :func:`prompt_plan_create`."""
+
+    def __init__(self, handle: int, pool: KVPool, rows: int, num_q_heads: int):
+        self.prompt_handle = handle
+        self.pool = pool
+        self.rows = rows
+        self.num_q_heads = num_q_heads
+        self.q_bytes = rows * num_q_heads * pool.head_dim * 2
+        self.kv_bytes = rows * pool.num_kv_heads * pool.head_dim * 2
+        self.lse_bytes = rows * num_q_heads * 4
+
+
+def _host_ints(x) -> np.ndarray:
+    """A list of lengths or slots as int32; numbers past 32 bits are refused, not wrapped."""
+    a = np.asarray(x)
+    if a.ndim != 1 or (a.size and a.dtype.kind not in "iu"):
+        raise ValueError("expected a list of integers")
+    if a.size and (a.max() > 2 ** 31 - 1 or a.min() < -2 ** 31):
+        raise ValueError("a number past 32 bits")
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
+def prompt_plan_create(pool: KVPool, lens, num_q_heads: int, softmax_scale: float = 0.0, stream=None) -> PromptPlan:
+    """Plan of whole prompts of ``lens`` tokens, packed one after the other (see ap_prompt_plan_create)."""
+    lens = _host_ints(lens)
+    desc = PromptDesc(len(lens), num_q_heads, _ptr(lens), softmax_scale)
+    h = ctypes.c_void_p()
+    _check(load().ap_prompt_plan_create(ctypes.byref(h), pool.handle, ctypes.byref(desc), _stream(stream, pool.device)),
+           "ap_prompt_plan_create")
+    return PromptPlan(h.value, pool, int(lens.sum(dtype=np.int64)), num_q_heads)
+
+
+def prompt_plan_destroy(plan: PromptPlan) -> None:
+    if plan.prompt_handle:
+        _check(load().ap_prompt_plan_destroy(plan.prompt_handle), "ap_prompt_plan_destroy")
+        plan.prompt_handle = None
+
+
+def prompt_plan_get_info(plan: PromptPlan) -> dict:
+    info = PromptInfo()
+    _check(load().ap_prompt_plan_get_info(plan.prompt_handle, ctypes.byref(info)), "ap_prompt_plan_get_info")
+    return info.as_dict()
+
+
+def prompt_attention(pool: KVPool, plan: PromptPlan, q, k, v, out, lse=None, stream=None) -> None:
+    """Causal attention of whole prompts from q, k, v [rows, heads, head_dim], which may be strided by row (slices of one
+    projection); no pages, no block tables."""
+    dev, n, d = pool.device, plan.rows, pool.head_dim
+    q_at, q_stride = _strided_rows(q, n, plan.num_q_heads, d, plan.q_bytes, dev)
+    k_at, k_stride = _strided_rows(k, n, pool.num_kv_heads, d, plan.kv_bytes, dev)
+    v_at, v_stride = _strided_rows(v, n, pool.num_kv_heads, d, plan.kv_bytes, dev)
+    status = (_lib or load()).ap_prompt_attention(pool.handle, plan.prompt_handle, q_at, k_at, v_at, _one(out, plan.q_bytes, dev),
+                                                  _lse_rows(lse, plan.lse_bytes, dev),
+                                                  _PROMPT_STRIDES.pack(q_stride, k_stride, v_stride), _stream(stream, dev))
+    if status:
+        _check(status, "ap_prompt_attention")
+
+
+# ----------------------------------------------------- state-space layers --
+
+class StatePool:
+    """Handle returned by :func:`state_pool_create`."""
+
+    def __init__(self, handle: int, desc: StateDesc, keepalive=()):
+        self.state_handle = handle
+        self.desc = desc
+        self._keepalive = keepalive
+        self.num_slots, self.channels, self.device = int(desc.num_slots), int(desc.channels), int(desc.device)
+        self.state_dim, self.conv_width = int(desc.state_dim), int(desc.conv_width)
+
+
+class StatePlan:
+    """Handle returned by :func:`state_plan_create`."""
+
+    def __init__(self, handle: int, pool: StatePool, rows: int):
+        self.state_plan_handle = handle
+        self.pool = pool
+        self.rows = rows
+
+
+def state_pool_conv_bytes(num_slots: int, channels: int, state_dim: int, conv_width: int) -> int:
+    d = StateDesc(num_slots, channels, state_dim, conv_width, None, None, 0)
+    return int(load().ap_state_pool_conv_bytes(ctypes.byref(d)))
+
+
+def state_pool_scan_bytes(num_slots: int, channels: int, state_dim: int, conv_width: int) -> int:
+    d = StateDesc(num_slots, channels, state_dim, conv_width, None, None, 0)
+    return int(load().ap_state_pool_scan_bytes(ctypes.byref(d)))
+
+
+def state_pool_create(num_slots: int, channels: int, state_dim: int, conv_width: int, conv_base=None, scan_base=None,
+                      device: int = 0) -> StatePool:
+    """Slots for one layer's states: ``conv_base`` [num_slots, conv_width - 1, channels] bf16, ``scan_base``
+    [num_slots, channels, state_dim] fp32; a plane that is not given is the library's, zero filled."""
+    shape = num_slots, channels, state_dim, conv_width
+    at = []
+    for base, nbytes, size in ((conv_base, state_pool_conv_bytes(*shape), 2), (scan_base, state_pool_scan_bytes(*shape), 4)):
+        at.append(None if base is None else _checked(base, max(nbytes, 1), device, size))
+    d = StateDesc(*shape, *at, device)
+    h = ctypes.c_void_p()
+    _check(load().ap_state_pool_create(ctypes.byref(h), ctypes.byref(d)), "ap_state_pool_create")
+    return StatePool(h.value, d, (conv_base, scan_base))
+
+
+def state_pool_destroy(pool: StatePool) -> None:
+    if pool.state_handle:
+        _check(load().ap_state_pool_destroy(pool.state_handle), "ap_state_pool_destroy")
+        pool.state_handle = None
+
+
+def state_pool_conv_base(pool: StatePool) -> int:
+    return int(load().ap_state_pool_conv_base(pool.state_handle) or 0)
+
+
+def state_pool_scan_base(pool: StatePool) -> int:
+    return int(load().ap_state_pool_scan_base(pool.state_handle) or 0)
+
+
+def state_plan_create(pool: StatePool, q_lens, ctx_lens, slots, stream=None) -> StatePlan:
+    """Plan of one iteration over state slots: ``q_lens`` new tokens of each sequence, ``ctx_lens`` with them (equal: the
+    sequence begins here), its slot.  Serves every pool of the same description."""
+    q, c, s = _host_ints(q_lens), _host_ints(ctx_lens), _host_ints(slots)
+    if not len(q) == len(c) == len(s):
+        raise ValueError("q_lens, ctx_lens and slots must be of the same length")
+    desc = StateBatch(len(q), _ptr(q), _ptr(c), _ptr(s))
+    h = ctypes.c_void_p()
+    _check(load().ap_state_plan_create(ctypes.byref(h), pool.state_handle, ctypes.byref(desc), _stream(stream, pool.device)),
+           "ap_state_plan_create")
+    return StatePlan(h.value, pool, int(q.sum(dtype=np.int64)))
+
+
+def state_plan_destroy(plan: StatePlan) -> None:
+    if plan.state_plan_handle:
+        _check(load().ap_state_plan_destroy(plan.state_plan_handle), "ap_state_plan_destroy")
+        plan.state_plan_handle = None
+
+
+def state_plan_get_info(plan: StatePlan) -> dict:
+    info = StateInfo()
+    _check(load().ap_state_plan_get_info(plan.state_plan_handle, ctypes.byref(info)), "ap_state_plan_get_info")
+    return info.as_dict()
+
+
+def state_plan_workspace_bytes(plan: StatePlan) -> int:
+    return int(load().ap_state_plan_workspace_bytes(plan.state_plan_handle))
+
+
+def _matrix(x, rows: int, cols: int, device: int) -> Tuple[Optional[int], int]:
+    """(address, elements from one row to the next or 0 for contiguous) of a bf16 tensor [rows, cols] of the call."""
+    try:
+        n, c = x.shape
+        row, one = x.stride()
+        if x.dtype is _bf16 and x.get_device() == device and c == cols and n >= rows and one == 1 and row >= cols:
+            return x.data_ptr(), row if n > 1 else 0
+    except AttributeError:                   # None, an address, a host array
+        return _checked(x, rows * cols * 2, device, 2), 0
+    except ValueError:
+        n = c = row = one = 0
+    if rows <= 0:
+        return _ptr(x), 0
+    if n < rows or c != cols:
+        raise ValueError(f"expected [{rows}, {cols}], not {list(x.shape)}")
+    if (one != 1 and c > 1) or (row < cols and n > 1):
+        raise ValueError("expected rows of contiguous elements that do not overlap")
+    return _checked(x, 0, device, 2, dense=False), row if n > 1 else 0
+
+
+def _vector(x, nbytes: int, device: int, dtype_bytes: int) -> Optional[int]:
+    """Address of a contiguous parameter (bf16: 2, fp32: 4 bytes an element), or None."""
+    try:
+        if x.dtype is (_fp32 if dtype_bytes == 4 else _bf16) and x.nbytes >= nbytes and x.get_device() == device and x.is_contiguous():
+            return x.data_ptr()
+    except AttributeError:
+        pass
+    return _checked(x, nbytes, device, dtype_bytes)
+
+
+def conv_iteration(pool: StatePool, plan: StatePlan, x, weight, out, bias=None, silu: bool = True, stream=None) -> None:
+    """Short causal convolution of the plan's rows ``x`` [rows, channels] with ``weight`` [channels, conv_width]; the slots
+    take the last inputs.  ``x`` and ``out`` may be strided by row."""
+    dev, n, c = pool.device, plan.rows, pool.channels
+    x_at, xs = _matrix(x, n, c, dev)
+    out_at, os_ = _matrix(out, n, c, dev)
+    status = (_lib or load()).ap_conv_iteration(
+        pool.state_handle, plan.state_plan_handle, _CONV_DESC.pack(1 if silu else 0, xs, os_), x_at,
+        _vector(weight, c * pool.conv_width * 2, dev, 2), _vector(bias, c * 2, dev, 2), out_at, _stream(stream, dev))
+    if status:
+        _check(status, "ap_conv_iteration")
+
+
+def scan_iteration(pool: StatePool, plan: StatePlan, x, dt, a, b, c, out, z=None, d_skip=None, dt_bias=None,
+                   softplus: bool = True, workspace=None, workspace_bytes: Optional[int] = None, stream=None) -> None:
+    """Selective state space scan of the plan's rows: ``x``, ``dt``, ``z``, ``out`` [rows, channels], ``b``, ``c``
+    [rows, state_dim] (all bf16, may be strided by row), ``a`` [channels, state_dim], ``d_skip``, ``dt_bias`` [channels]
+    (fp32); the slots take the states (see ap_scan_iteration)."""
+    dev, n, ch, st = pool.device, plan.rows, pool.channels, pool.state_dim
+    workspace, room = _workspace(workspace, workspace_bytes, dev)
+    x_at, xs = _matrix(x, n, ch, dev)
+    dt_at, dts = _matrix(dt, n, ch, dev)
+    b_at, bs = _matrix(b, n, st, dev)
+    c_at, cs = _matrix(c, n, st, dev)
+    z_at, zs = (None, 0) if z is None else _matrix(z, n, ch, dev)
+    out_at, os_ = _matrix(out, n, ch, dev)
+    status = (_lib or load()).ap_scan_iteration(
+        pool.state_handle, plan.state_plan_handle, _SCAN_DESC.pack(1 if softplus else 0, xs, dts, bs, cs, zs, os_), x_at, dt_at,
+        _vector(a, ch * st * 4, dev, 4), b_at, c_at, z_at, _vector(d_skip, ch * 4, dev, 4), _vector(dt_bias, ch * 4, dev, 4), out_at,
+        workspace, room, _stream(stream, dev))
+    if status:
+        _check(status, "ap_scan_iteration")
 
 
 def static_workspace_bytes() -> int:

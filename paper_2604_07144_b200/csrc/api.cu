@@ -7,31 +7,12 @@
 #include <cstring>
 #include <new>
 
+#include "host_util.h"
 #include "internal.h"
 
 using namespace ap;
 
 namespace {
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) { prev = -1; (void)cudaGetLastError(); }
-        if (prev == dev) {                 // (already there: nothing to set, nothing to put back)
-            ok = true;
-            prev = -1;
-            return;
-        }
-        ok = cudaSetDevice(dev) == cudaSuccess;
-        if (!ok) (void)cudaGetLastError();
-    }
-    ~DeviceGuard() {
-        if (prev >= 0 && ok) (void)cudaSetDevice(prev);
-    }
-};
-
-inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // bytes of one (page, kv head) tile of a plane: 16 rows of d bf16 numbers, or of d 4-bit codes and d / 32 steps
 inline int pool_tile_bytes(int head_dim, bool four_bit) {
@@ -48,48 +29,6 @@ inline uint64_t splitmix64(uint64_t &state) {
     z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
     z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
     return z ^ (z >> 31);
-}
-
-void release_plan_buffer(PlanBuffer &b) {
-    if (b.uploaded) (void)cudaEventDestroy(b.uploaded);
-    if (b.host) (void)cudaFreeHost(b.host);
-    if (b.dev) (void)cudaFree(b.dev);
-    b = PlanBuffer{};
-}
-
-int acquire_plan_buffer(ap_kv_pool *pool, size_t n_ints, PlanBuffer *out) {
-    for (size_t i = 0; i < pool->plan_buffers.size(); ++i) {
-        if (pool->plan_buffers[i].capacity >= n_ints) {
-            *out = pool->plan_buffers[i];
-            pool->plan_buffers.erase(pool->plan_buffers.begin() + (long)i);
-            // the previous upload from this staging area must have been consumed
-            if (cudaEventSynchronize(out->uploaded) != cudaSuccess) {
-                (void)cudaGetLastError();
-                return AP_ERR_CUDA;
-            }
-            return AP_OK;
-        }
-    }
-    PlanBuffer b;
-    b.capacity = std::max<size_t>(n_ints + n_ints / 2, 4096);
-    if (cudaMallocHost((void **)&b.host, b.capacity * sizeof(int32_t)) != cudaSuccess ||
-        cudaMalloc((void **)&b.dev, b.capacity * sizeof(int32_t)) != cudaSuccess ||
-        cudaEventCreateWithFlags(&b.uploaded, cudaEventDisableTiming) != cudaSuccess) {
-        (void)cudaGetLastError();
-        release_plan_buffer(b);
-        return AP_ERR_CUDA;
-    }
-    *out = b;
-    return AP_OK;
-}
-
-// Back to the pool for the next plan; freed if there is no host memory to remember it (no exception leaves a C entry).
-void give_back_plan_buffer(ap_kv_pool *pool, PlanBuffer &b) {
-    try {
-        pool->plan_buffers.push_back(b);
-    } catch (const std::bad_alloc &) {
-        release_plan_buffer(b);
-    }
 }
 
 void give_back_event(ap_kv_pool *pool, cudaEvent_t e) {
@@ -859,14 +798,14 @@ static int plan_create(ap_plan **out, ap_kv_pool *pool, const ap_batch_desc *b, 
     if (pool->desc.device >= 0) {
         DeviceGuard guard(pool->desc.device);
         if (!guard.ok) { delete plan; return AP_ERR_CUDA; }
-        int rc = acquire_plan_buffer(pool, total_ints, &plan->buf);
+        int rc = acquire_plan_buffer(pool->plan_buffers, total_ints, &plan->buf);
         if (rc != AP_OK) { delete plan; return rc; }
         std::memcpy(plan->buf.host, h, total_ints * 4);
         cudaStream_t st = (cudaStream_t)stream;
         if (cudaMemcpyAsync(plan->buf.dev, plan->buf.host, total_ints * 4, cudaMemcpyHostToDevice, st) != cudaSuccess ||
             cudaEventRecord(plan->buf.uploaded, st) != cudaSuccess) {
             (void)cudaGetLastError();
-            give_back_plan_buffer(pool, plan->buf);
+            give_back_plan_buffer(pool->plan_buffers, plan->buf);
             delete plan;
             return AP_ERR_CUDA;
         }
@@ -1014,7 +953,7 @@ int ap_plan_predict(const ap_plan *plan, double hbm_gbs, double tensor_tflops, a
 
 int ap_plan_destroy(ap_plan *plan) {
     if (!plan) return AP_ERR_INVALID_ARG;
-    if (plan->pool && plan->buf.dev) give_back_plan_buffer(plan->pool, plan->buf);
+    if (plan->pool && plan->buf.dev) give_back_plan_buffer(plan->pool->plan_buffers, plan->buf);
     delete plan;
     return AP_OK;
 }
@@ -1157,7 +1096,7 @@ static int kv_copy_pages(ap_kv_pool *dst_pool, const ap_kv_pool *src_pool, int32
     if (!guard.ok) return AP_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)stream;
     PlanBuffer buf;
-    int rc = acquire_plan_buffer(dst_pool, pairs.size(), &buf);
+    int rc = acquire_plan_buffer(dst_pool->plan_buffers, pairs.size(), &buf);
     if (rc != AP_OK) return rc;
     std::memcpy(buf.host, pairs.data(), pairs.size() * sizeof(int32_t));
     cudaError_t e = cudaMemcpyAsync(buf.dev, buf.host, pairs.size() * sizeof(int32_t), cudaMemcpyHostToDevice, st);
@@ -1170,7 +1109,7 @@ static int kv_copy_pages(ap_kv_pool *dst_pool, const ap_kv_pool *src_pool, int32
         release_plan_buffer(buf);
         return AP_ERR_CUDA;
     }
-    give_back_plan_buffer(dst_pool, buf);
+    give_back_plan_buffer(dst_pool->plan_buffers, buf);
     return AP_OK;
 }
 

@@ -1,0 +1,649 @@
+// Causal attention of whole prompts, packed one after the other, K and V read from the projection's rows.
+//
+// Prompts of more than kShortRows tokens go to the tensor cores (tcgen05, accumulators in tensor memory), shorter ones
+// to a kernel of mma.sync tiles; a plan with both launches both.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "host_util.h"
+#include "layers.h"
+#include "prefill_tcgen05.cuh"
+
+namespace ap {
+
+namespace {
+
+using namespace ptx;
+using prefill::exp2_poly2;
+using prefill::instr_desc;
+using prefill::kKvSlots;
+using prefill::kMmaWarp;
+using prefill::kPrefillThreads;
+using prefill::kProducerWarp;
+using prefill::kRescaleThreshold;
+using prefill::kTileM;
+using prefill::kTileN;
+using prefill::kv_seq_k;
+using prefill::kv_seq_v;
+using prefill::max2;
+using prefill::max3;
+using prefill::PrefillCfg;
+using prefill::rescale_o;
+using prefill::smem_desc;
+
+constexpr int kShortRows = 64;
+
+// ----------------------------------------------------- tensor-core units --
+//
+// A unit is 128 rows of a prompt for two q heads of a kv head, over the prompt's rows up to its own last one.  Roles,
+// barriers, ring and tensor-memory columns are those of the paged prefill kernel (prefill_tcgen05.cuh): two softmax
+// groups of 128 threads, a producer warp, an MMA-issuing warp per tile, one score region that the tiles use in turn.
+// What differs is the stream: 128 rows of K (of V) come in one request of 32 KB instead of eight of 4 KB through a block
+// table, as [half][128 rows][64] with the 128-byte swizzle, and begin at any row.
+template <int D>
+__global__ void __launch_bounds__(kPrefillThreads, 1)
+prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+                      const __grid_constant__ CUtensorMap v_map, const PromptTile *__restrict__ tiles,
+                      __nv_bfloat16 *__restrict__ out, float *__restrict__ lse_out, int Hq, float scale_log2, int *status,
+                      uint64_t wait_limit_ns) {
+    using Cfg = PrefillCfg<D>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint64_t *bars = (uint64_t *)(smem + Cfg::kOffBar);
+    uint64_t *q_full = bars + 0;
+    uint64_t *kv_full = bars + 1;                // [kKvSlots]
+    uint64_t *kv_empty = kv_full + kKvSlots;     // [kKvSlots]
+    uint64_t *s_full = kv_empty + kKvSlots;      // [2] per tile
+    uint64_t *p_full = s_full + 2;               // [2]
+    uint64_t *pv_done = p_full + 2;              // [2] O_x += P_x V of a step has completed
+    uint64_t *s_out = pv_done + 2;               // [2] tile x's scores have been copied out of the shared region
+    uint32_t *tmem_slot = (uint32_t *)(s_out + 2);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const PromptTile tile = tiles[blockIdx.x];
+    const int n_tiles = tile.q_head_b >= 0 ? 2 : 1;
+    const int pos0 = tile.row0 - tile.start;     // position of the first row in its prompt
+    const int kv_len = pos0 + tile.rows;         // keys the last valid row sees
+    const int n_steps = (kv_len + kTileN - 1) / kTileN;
+
+    if (threadIdx.x == 0) {
+        mbar_init(q_full, 1);
+        for (int s = 0; s < kKvSlots; ++s) {
+            mbar_init(&kv_full[s], 1);
+            mbar_init(&kv_empty[s], n_tiles);    // one commit per issuing warp
+        }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(&s_full[x], 1);
+            mbar_init(&p_full[x], 4);            // one arrival per softmax warp
+            mbar_init(&pv_done[x], 1);
+            mbar_init(&s_out[x], 4);
+        }
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == kMmaWarp) {
+        tmem_alloc(tmem_slot, Cfg::kTmemCols);
+        tmem_relinquish();
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    griddep_launch_dependents();
+    griddep_wait();                              // the preamble reads only the plan
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == kProducerWarp) {
+            // -------------------------------------------------- producer --
+            if (lane == 0) {
+                prefetch_tensormap(&q_map);
+                prefetch_tensormap(&k_map);
+                prefetch_tensormap(&v_map);
+                mbar_arrive_expect_tx(q_full, (uint32_t)(n_tiles * Cfg::kQBytes));
+                tma_load_3d(smem + Cfg::kOffQ, &q_map, q_full, 0, tile.row0, tile.q_head * Cfg::kHalves);
+                if (n_tiles == 2)
+                    tma_load_3d(smem + Cfg::kOffQ + Cfg::kQBytes, &q_map, q_full, 0, tile.row0, tile.q_head_b * Cfg::kHalves);
+                // ring order K_0, K_1, V_0, K_2, V_1, ...: entry n goes to slot n % kKvSlots
+                const int n_entries = 2 * n_steps;
+                for (int n = 0; n < n_entries; ++n) {
+                    const bool is_k = n == 0 || ((n & 1) && n < n_entries - 1);
+                    const int j = is_k ? (n + 1) / 2 : (n == n_entries - 1 ? n_steps - 1 : n / 2 - 1);
+                    const int s = n % kKvSlots;
+                    if (!wait_or_abort(&kv_empty[s], ((uint32_t)(n / kKvSlots) & 1u) ^ 1u, abort_flag, wait_limit_ns)) {
+                        record_status(status, AP_ERR_TIMEOUT);
+                        *abort_flag = 1;
+                        break;
+                    }
+                    // (rows past the packed batch's last read as zeros; they count)
+                    mbar_arrive_expect_tx(&kv_full[s], (uint32_t)Cfg::kKvTileBytes);
+                    tma_load_3d(smem + Cfg::kOffK + s * Cfg::kKvTileBytes, is_k ? &k_map : &v_map, &kv_full[s], 0,
+                                tile.start + j * kTileN, tile.kv_head * Cfg::kHalves);
+                }
+            }
+            __syncwarp();
+        } else if (warp == kMmaWarp || (warp == kMmaWarp + 1 && n_tiles == 2)) {
+            // ----------------------------------------------- MMA issuers --
+            const int x = warp - kMmaWarp;
+            const uint32_t leader = elect_one();
+            constexpr uint32_t kIdescQK = instr_desc(kTileM, kTileN, false);
+            constexpr uint32_t kIdescPV = instr_desc(kTileM, D, true);
+            bool ok = wait_or_abort(q_full, 0, abort_flag, wait_limit_ns);
+            // All three operands lie as [half][128 rows][64], 8-row groups 1024 B apart, halves 16 KB apart.
+            constexpr uint32_t kHalfBytes = kTileN * 128;
+            const uint64_t q_desc0 = smem_desc(smem_u32(smem + Cfg::kOffQ + x * Cfg::kQBytes), 16, 1024);
+            const uint64_t k_desc0 = smem_desc(smem_u32(smem + Cfg::kOffK), 16, 1024);
+            const uint64_t v_desc0 = smem_desc(smem_u32(smem + Cfg::kOffK), kHalfBytes, 1024);
+            const uint32_t q_lo = (uint32_t)q_desc0, q_hi = (uint32_t)(q_desc0 >> 32);
+            const uint32_t k_lo = (uint32_t)k_desc0, k_hi = (uint32_t)(k_desc0 >> 32);
+            const uint32_t v_lo = (uint32_t)v_desc0, v_hi = (uint32_t)(v_desc0 >> 32);
+            const uint32_t t_s = tmem + Cfg::kColS, t_p = tmem + Cfg::kColP + x * 64, t_o = tmem + Cfg::kColO + x * 128;
+            auto issue_qk = [&](int slot) {
+                const uint32_t b0 = k_lo + (uint32_t)((slot * Cfg::kKvTileBytes) >> 4);
+#pragma unroll
+                for (int kh = 0; kh < D / 64; ++kh)
+                    umma_ss_x4(leader, t_s, q_lo + ((kh * kHalfBytes) >> 4), q_hi, b0 + ((kh * kHalfBytes) >> 4), k_hi, kIdescQK,
+                               kh > 0 ? 1u : 0u, 32u >> 4, 32u >> 4);
+                umma_commit(leader, &s_full[x]);
+                umma_commit(leader, &kv_empty[slot]);
+            };
+            auto issue_pv = [&](int slot, bool first_step) {
+                const uint32_t b0 = v_lo + (uint32_t)((slot * Cfg::kKvTileBytes) >> 4);
+                constexpr uint32_t kVStep = (2 * 1024) >> 4;                       // 16 keys of V
+#pragma unroll
+                for (int kq = 0; kq < kTileN / 64; ++kq)
+                    umma_ts_x4(leader, t_o, t_p + kq * 32, b0 + kq * 4 * kVStep, v_hi, kIdescPV, (first_step && kq == 0) ? 0u : 1u, 8u,
+                               kVStep);
+                umma_commit(leader, &pv_done[x]);
+                umma_commit(leader, &kv_empty[slot]);
+            };
+            // The score region passes from tile to tile through two barriers with one waiter each: S_x(step) may be
+            // issued once the scores written before it have been copied out.
+            auto wait_s_free = [&](int step) {
+                if (n_tiles == 2 && x == 1) return wait_or_abort(&s_out[0], (uint32_t)step & 1u, abort_flag, wait_limit_ns);
+                if (step == 0) return true;
+                return wait_or_abort(&s_out[n_tiles - 1], (uint32_t)(step - 1) & 1u, abort_flag, wait_limit_ns);
+            };
+            if (ok) ok = wait_or_abort(&kv_full[0], 0, abort_flag, wait_limit_ns);
+            if (ok) ok = wait_s_free(0);
+            if (ok) {
+                tcgen05_fence_after();
+                issue_qk(0);
+            }
+            for (int j = 0; ok && j < n_steps; ++j) {
+                const int nv = kv_seq_v(j, n_steps), nk = kv_seq_k(j + 1);
+                if (j + 1 < n_steps) {           // the next scores of the tile go ahead of this step's P V
+                    if (!wait_or_abort(&kv_full[nk % kKvSlots], (uint32_t)(nk / kKvSlots) & 1u, abort_flag, wait_limit_ns) ||
+                        !wait_s_free(j + 1)) { ok = false; break; }
+                    tcgen05_fence_after();
+                    issue_qk(nk % kKvSlots);
+                }
+                if (!wait_or_abort(&kv_full[nv % kKvSlots], (uint32_t)(nv / kKvSlots) & 1u, abort_flag, wait_limit_ns) ||
+                    !wait_or_abort(&p_full[x], (uint32_t)j & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
+                // In the last step tile A's group clears the V rows past the unit's last key before it hands P_A over;
+                // tile B's product reads the same V tile and has to see that too.
+                if (x == 1 && j == n_steps - 1 && kv_len < n_steps * kTileN &&
+                    !wait_or_abort(&p_full[0], (uint32_t)j & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
+                tcgen05_fence_after();
+                issue_pv(nv % kKvSlots, j == 0);
+            }
+            if (!ok && leader) {
+                record_status(status, AP_ERR_TIMEOUT);
+                *abort_flag = 1;
+            }
+            __syncwarp();
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        // ------------------------------------------------------- softmax --
+        const int x = warp >> 2;                                     // tile A or B
+        if (x < n_tiles) {
+            const int r = threadIdx.x & 127;                         // query row = TMEM lane
+            const int q_head = x == 0 ? tile.q_head : tile.q_head_b;
+            const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+            const uint32_t col_s = Cfg::kColS, col_p = Cfg::kColP + x * 64, col_o = Cfg::kColO + x * 128;
+            const int my_pos = min(pos0 + r, kv_len - 1);            // last key this row sees
+            float m_used = -INFINITY, l = 0.f;
+            bool ok = true;
+            for (int j = 0; j < n_steps; ++j) {
+                // S_x(j) complete: copy this row's 128 scores out and give the region back at once
+                if (!wait_or_abort(&s_full[x], (uint32_t)j & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
+                tcgen05_fence_after();
+                uint32_t sreg[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(lane_addr + col_s + c * 32, sreg[c]);
+                tmem_ld_wait();
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s_out[x]);
+                const int tok0 = j * kTileN;
+                float mx = -INFINITY;
+                if (tok0 + kTileN - 1 > pos0) {
+                    // diagonal or last step: one bit per key says whether the row sees it
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t seen = prefill::low_bits(my_pos + 1 - (tok0 + c * 32));
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!(seen >> i & 1u)) sreg[c][i] = 0xFF800000u;            // -inf
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2)
+                        mx = max3(mx, __uint_as_float(sreg[c][i]), __uint_as_float(sreg[c][i + 1]));
+                // P_x and O_x belong to the tensor pipe until O_x += P_x V of the step before is done
+                if (j > 0) {
+                    if (!wait_or_abort(&pv_done[x], (uint32_t)(j - 1) & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
+                    tcgen05_fence_after();
+                }
+                // Keep the old reference max unless some row of the warp moved by more than the threshold: P stays
+                // bounded by 2^threshold and O needs no rescale most steps.
+                const float m_new = max2(m_used, mx);
+                const bool rescale = __any_sync(0xffffffffu, (m_new - m_used) * scale_log2 > kRescaleThreshold);   // (true on the first step)
+                float alpha = 1.f;
+                if (rescale) {
+                    alpha = exp2_approx((m_used - m_new) * scale_log2);   // 0 on the first step
+                    m_used = m_new;
+                    if (j > 0) rescale_o<D>(lane_addr + col_o, alpha);
+                }
+                const float ms = fmaf(m_used, scale_log2, m_new - m_new);   // (a NaN score makes the row NaN)
+                const float2 sc2 = make_float2(scale_log2, scale_log2), nms2 = make_float2(-ms, -ms);
+                float2 sum2 = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t preg[32];                                  // 64 keys as bf16 pairs
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        float2 xy = __ffma2_rn(make_float2(__uint_as_float(sreg[2 * c + (i >> 4)][(2 * i) & 31]),
+                                                           __uint_as_float(sreg[2 * c + (i >> 4)][(2 * i + 1) & 31])),
+                                               sc2, nms2);
+                        // one pair in eight goes to the FMA pipe instead of the special-function unit
+                        if ((i & 7) == 7) {
+                            xy = exp2_poly2<true>(xy);
+                        } else {
+                            xy.x = exp2_approx(xy.x);
+                            xy.y = exp2_approx(xy.y);
+                        }
+                        // (the sum takes the weights as they are; P V takes them in bf16, each off by at most 2^-8 of itself)
+                        sum2 = __fadd2_rn(sum2, xy);
+                        preg[i] = pack_bf16x2(xy.x, xy.y);
+                    }
+                    tmem_st_32x32b_x32(lane_addr + col_p + c * 32, preg);
+                }
+                l = l * alpha + (sum2.x + sum2.y);
+                tmem_st_wait();
+                if (x == 0 && j == n_steps - 1 && kv_len < n_steps * kTileN) {
+                    // rows past the unit's last key belong to nobody it serves (the next prompt's, or none): 0 * V must be 0
+                    const int nv = kv_seq_v(j, n_steps), s = nv % kKvSlots;
+                    if (!wait_or_abort(&kv_full[s], (uint32_t)(nv / kKvSlots) & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
+                    uint8_t *v_tile = smem + Cfg::kOffK + s * Cfg::kKvTileBytes;
+                    const int first = kv_len - tok0;
+                    for (int idx = r; idx < (kTileN - first) * (D / 8); idx += 128) {
+                        const int key = first + idx / (D / 8), ch = idx % (D / 8);
+                        *(uint4 *)(v_tile + (ch >> 3) * (kTileN * 128) + key * 128 + ((ch & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                }
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[x]);
+            }
+            if (ok && wait_or_abort(&pv_done[x], (uint32_t)(n_steps - 1) & 1u, abort_flag, wait_limit_ns)) {
+                tcgen05_fence_after();
+                const float inv = 1.f / l;
+                const bool valid = r < tile.rows;
+                __nv_bfloat16 *orow = out + ((size_t)(tile.row0 + r) * Hq + q_head) * D;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t oreg[32];
+                    tmem_ld_32x32b_x32(lane_addr + col_o + c * 32, oreg);
+                    tmem_ld_wait();
+                    if (valid) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            uint4 v;
+                            v.x = pack_bf16x2(__uint_as_float(oreg[i]) * inv, __uint_as_float(oreg[i + 1]) * inv);
+                            v.y = pack_bf16x2(__uint_as_float(oreg[i + 2]) * inv, __uint_as_float(oreg[i + 3]) * inv);
+                            v.z = pack_bf16x2(__uint_as_float(oreg[i + 4]) * inv, __uint_as_float(oreg[i + 5]) * inv);
+                            v.w = pack_bf16x2(__uint_as_float(oreg[i + 6]) * inv, __uint_as_float(oreg[i + 7]) * inv);
+                            *(uint4 *)(orow + c * 32 + i) = v;
+                        }
+                    }
+                }
+                if (valid && lse_out)
+                    lse_out[(size_t)(tile.row0 + r) * Hq + q_head] = (m_used * scale_log2 + log2f(l)) * 0.6931471805599453f;
+            } else {
+                record_status(status, AP_ERR_TIMEOUT);
+                *abort_flag = 1;
+            }
+        }
+    }
+
+    tcgen05_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) tmem_dealloc(tmem, Cfg::kTmemCols);
+}
+
+// ---------------------------------------------------------- short prompts --
+//
+// A block is a prompt's rows and one kv head: K and V in shared memory once, then each warp takes 16 rows of a q head at
+// a time (mma.sync m16n8k16: a 128-row tile of the tensor cores would be empty for the most part, and a unit's prologue
+// and epilogue cost 5 us).  All scores of a row are in registers, so the softmax takes one pass.
+constexpr int kShortWarps = 4;
+
+template <int D>
+struct ShortSmem {
+    static constexpr int kStride = D * 2 + 16;                        // bytes of a row: 8 rows of an ldmatrix in 8 bank groups
+    uint8_t k[kShortRows * kStride], v[kShortRows * kStride];
+    uint8_t q[kShortWarps][16 * kStride];                             // a warp's rows; then its results on their way out
+};
+
+template <int D>
+__global__ void __launch_bounds__(32 * kShortWarps)
+prompt_short_kernel(const ShortPrompt *__restrict__ prompts, const uint16_t *q, const uint16_t *k, const uint16_t *v, uint16_t *out,
+                    float *lse_out, int Hq, int Hkv, int64_t qs, int64_t ks, int64_t vs, float scale_log2) {
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    ShortSmem<D> &sm = *(ShortSmem<D> *)smem_raw;
+    constexpr int kStride = ShortSmem<D>::kStride, kChunks = D / 8;
+    const ShortPrompt p = prompts[blockIdx.x / Hkv];
+    const int kv_head = (int)blockIdx.x % Hkv, G = Hq / Hkv;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int blocks = (p.rows + 15) / 16;                            // blocks of 16 rows
+    griddep_launch_dependents();
+    griddep_wait();
+    for (int i = threadIdx.x; i < blocks * 16 * kChunks; i += 32 * kShortWarps) {
+        const int row = i / kChunks, ch = i % kChunks;
+        uint4 a = make_uint4(0, 0, 0, 0), b = a;                      // (rows past the prompt: zeros, whatever the next one holds)
+        if (row < p.rows) {
+            a = load16(k + (p.start + (int64_t)row) * ks + kv_head * D + ch * 8);
+            b = load16(v + (p.start + (int64_t)row) * vs + kv_head * D + ch * 8);
+        }
+        *(uint4 *)(sm.k + row * kStride + ch * 16) = a;
+        *(uint4 *)(sm.v + row * kStride + ch * 16) = b;
+    }
+    __syncthreads();
+    uint8_t *mine = sm.q[warp];
+    const uint32_t q_addr = smem_u32(mine) + (lane & 15) * kStride + (lane >> 4) * 16;
+    const uint32_t k_addr = smem_u32(sm.k) + ((lane & 7) + (lane >> 4) * 8) * kStride + ((lane >> 3) & 1) * 16;
+    const uint32_t v_addr = smem_u32(sm.v) + (lane & 15) * kStride + (lane >> 4) * 16;
+    for (int item = warp; item < blocks * G; item += kShortWarps) {
+        // (the later blocks, with more keys, first)
+        const int rb = blocks - 1 - item / G, head = kv_head * G + item % G;
+        const int row0 = rb * 16;
+        for (int i = lane; i < 16 * kChunks; i += 32) {
+            const int row = i / kChunks, ch = i % kChunks;
+            uint4 a = make_uint4(0, 0, 0, 0);
+            if (row0 + row < p.rows) a = load16(q + (p.start + (int64_t)(row0 + row)) * qs + head * D + ch * 8);
+            *(uint4 *)(mine + row * kStride + ch * 16) = a;
+        }
+        __syncwarp();
+        uint32_t qf[D / 16][4];
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) ldmatrix_x4(qf[c], q_addr + c * 32);
+        // S: blocks of 16 keys up to the rows' own
+        float s[kShortRows / 8][4];
+#pragma unroll
+        for (int kb = 0; kb < kShortRows / 16; ++kb) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[2 * kb][e] = s[2 * kb + 1][e] = 0.f;
+            if (kb <= rb) {
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    uint32_t kf[4];
+                    ldmatrix_x4(kf, k_addr + kb * 16 * kStride + c * 32);
+                    mma_bf16_16816(s[2 * kb], qf[c][0], qf[c][1], qf[c][2], qf[c][3], kf[0], kf[1]);
+                    mma_bf16_16816(s[2 * kb + 1], qf[c][0], qf[c][1], qf[c][2], qf[c][3], kf[2], kf[3]);
+                }
+            }
+        }
+        // a lane holds rows lane / 4 and lane / 4 + 8, keys 8 n + 2 (lane % 4) and the next
+        const int r0 = row0 + (lane >> 2), key0 = 2 * (lane & 3);
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < kShortRows / 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (8 * n + key0 + (e & 1) > r0 + 8 * (e >> 1)) s[n][e] = -INFINITY;
+                m[e >> 1] = prefill::max2(m[e >> 1], s[n][e]);
+            }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            m[h] = prefill::max2(m[h], __shfl_xor_sync(0xffffffffu, m[h], 1));
+            m[h] = prefill::max2(m[h], __shfl_xor_sync(0xffffffffu, m[h], 2));
+        }
+        float o[D / 8][4];
+#pragma unroll
+        for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < kShortRows / 16; ++kb) {
+            if (kb > rb) continue;
+            uint32_t pf[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                               // (rows lane / 4, + 8) x (keys 0-7, 8-15) of the block
+                float w[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int h = i & 1;
+                    w[e] = exp2_approx((s[2 * kb + (i >> 1)][2 * h + e] - m[h]) * scale_log2);
+                    l[h] += w[e];
+                }
+                pf[i] = pack_bf16x2(w[0], w[1]);                        // (off by at most 2^-8 of itself; the sum takes it as it is)
+            }
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+                uint32_t vf[4];
+                ldmatrix_x4_trans(vf, v_addr + kb * 16 * kStride + c * 32);
+                mma_bf16_16816(o[2 * c], pf[0], pf[1], pf[2], pf[3], vf[0], vf[1]);
+                mma_bf16_16816(o[2 * c + 1], pf[0], pf[1], pf[2], pf[3], vf[2], vf[3]);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+            const int row = r0 + 8 * h;
+            if (lse_out && (lane & 3) == 0 && row < p.rows)
+                lse_out[(p.start + (int64_t)row) * Hq + head] = (m[h] * scale_log2 + log2f(l[h])) * 0.6931471805599453f;
+            const float inv = 1.f / l[h];
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n)
+                *(uint32_t *)(mine + ((lane >> 2) + 8 * h) * kStride + n * 16 + (lane & 3) * 4) =
+                    pack_bf16x2(o[n][2 * h] * inv, o[n][2 * h + 1] * inv);
+        }
+        __syncwarp();
+        for (int i = lane; i < 16 * kChunks; i += 32) {
+            const int row = i / kChunks, ch = i % kChunks;
+            if (row0 + row < p.rows)
+                *(uint4 *)(out + ((p.start + (int64_t)(row0 + row)) * Hq + head) * D + ch * 8) = *(const uint4 *)(mine + row * kStride + ch * 16);
+        }
+        __syncwarp();
+    }
+}
+
+template <int D>
+cudaError_t launch_prompt_t(const ap_kv_pool *pool, const ap_prompt_plan *plan, const void *q, const void *k, const void *v,
+                            void *out, float *lse, const ap_prompt_strides &st, cudaStream_t stream) {
+    using Cfg = PrefillCfg<D>;
+    static bool configured[64] = {};
+    const int dev = pool->desc.device & 63;
+    if (!configured[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(prompt_tcgen05_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(prompt_short_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(ShortSmem<D>));
+        if (e != cudaSuccess) return e;
+        configured[dev] = true;
+    }
+    const int Hq = plan->num_q_heads, Hkv = pool->desc.num_kv_heads;
+    const float scale_log2 = plan->scale * 1.4426950408889634f;
+    cudaError_t e = cudaSuccess;
+    if (plan->info.tiles > 0) {
+        CUtensorMap q_map, k_map, v_map;
+        if (encode_rows_tensor_map(&q_map, q, plan->info.n_rows, Hq, D, st.q_row_stride) != AP_OK ||
+            encode_rows_tensor_map(&k_map, k, plan->info.n_rows, Hkv, D, st.k_row_stride) != AP_OK ||
+            encode_rows_tensor_map(&v_map, v, plan->info.n_rows, Hkv, D, st.v_row_stride) != AP_OK)
+            return cudaErrorInvalidValue;
+        e = launch_overlapped(prompt_tcgen05_kernel<D>, (unsigned)plan->info.tiles, (unsigned)kPrefillThreads, (size_t)Cfg::kSmemBytes,
+                              stream, q_map, k_map, v_map, plan->d_tiles, (__nv_bfloat16 *)out, lse, Hq, scale_log2, pool->status_dev,
+                              pool->wait_limit_ns);
+    }
+    if (e == cudaSuccess && plan->info.short_units > 0)
+        e = launch_overlapped(prompt_short_kernel<D>, (unsigned)plan->info.short_units, 32u * kShortWarps, sizeof(ShortSmem<D>), stream,
+                              plan->d_short, (const uint16_t *)q, (const uint16_t *)k, (const uint16_t *)v, (uint16_t *)out, lse, Hq, Hkv,
+                              st.q_row_stride, st.k_row_stride, st.v_row_stride, scale_log2);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+int plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *b, void *stream) {
+    if (!out) return AP_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!pool || !b || b->batch < 0 || b->num_q_heads <= 0 || (b->batch > 0 && !b->lens)) return AP_ERR_INVALID_ARG;
+    const int Hkv = pool->desc.num_kv_heads, Hq = b->num_q_heads, d = pool->desc.head_dim;
+    if (Hq % Hkv != 0) return AP_ERR_INVALID_ARG;
+    const int G = Hq / Hkv;
+    if (G > 8) return AP_ERR_UNSUPPORTED;
+    int64_t rows = 0, pairs = 0, tiles_n = 0, shorts_n = 0;
+    for (int s = 0; s < b->batch; ++s) {
+        const int32_t n = b->lens[s];
+        if (n < 0) return AP_ERR_INVALID_ARG;
+        rows += n;
+        pairs += (int64_t)n * ((int64_t)n + 1) / 2;
+        if (n > kShortRows) tiles_n += ((int64_t)n + kTileM - 1) / kTileM * Hkv * ((G + 1) / 2);
+        else if (n > 0) ++shorts_n;
+    }
+    // (row numbers of a last tile's keys, past the end of the batch, stay within 32 bits)
+    if (rows > (int64_t)1 << 30 || tiles_n > (int64_t)1 << 27 || shorts_n * Hkv >= (int64_t)1 << 31) return AP_ERR_UNSUPPORTED;
+    std::vector<PromptTile> tiles;
+    std::vector<ShortPrompt> shorts;
+    tiles.reserve((size_t)tiles_n);
+    shorts.reserve((size_t)shorts_n);
+    int32_t start = 0;
+    for (int s = 0; s < b->batch; ++s) {
+        const int32_t n = b->lens[s];
+        if (n > kShortRows) {
+            for (int32_t t0 = 0; t0 < n; t0 += kTileM)
+                for (int kv = 0; kv < Hkv; ++kv)
+                    for (int g = 0; g < G; g += 2)
+                        tiles.push_back({start + t0, std::min(kTileM, n - t0), start, kv * G + g, g + 1 < G ? kv * G + g + 1 : -1, kv, {0, 0}});
+        } else if (n > 0) {
+            shorts.push_back({start, n});
+        }
+        start += n;
+    }
+    // longest first: blocks are handed out in order.  Units of the same steps stay together (they share K and V in the L2).
+    std::stable_sort(tiles.begin(), tiles.end(), [](const PromptTile &x, const PromptTile &y) {
+        return (x.row0 - x.start + x.rows + kTileN - 1) / kTileN > (y.row0 - y.start + y.rows + kTileN - 1) / kTileN;
+    });
+    std::stable_sort(shorts.begin(), shorts.end(), [](const ShortPrompt &x, const ShortPrompt &y) { return x.rows > y.rows; });
+
+    ap_prompt_plan *plan = new (std::nothrow) ap_prompt_plan();
+    if (!plan) return AP_ERR_CUDA;
+    const size_t tile_ints = tiles.size() * (sizeof(PromptTile) / 4), ints = tile_ints + shorts.size() * (sizeof(ShortPrompt) / 4);
+    if (pool->desc.device >= 0 && ints > 0) {
+        DeviceGuard guard(pool->desc.device);
+        if (!guard.ok) { delete plan; return AP_ERR_CUDA; }
+        const int rc = acquire_plan_buffer(pool->plan_buffers, ints, &plan->buf);
+        if (rc != AP_OK) { delete plan; return rc; }
+        if (!tiles.empty()) std::memcpy(plan->buf.host, tiles.data(), tiles.size() * sizeof(PromptTile));
+        if (!shorts.empty()) std::memcpy(plan->buf.host + tile_ints, shorts.data(), shorts.size() * sizeof(ShortPrompt));
+        cudaStream_t st = (cudaStream_t)stream;
+        if (cudaMemcpyAsync(plan->buf.dev, plan->buf.host, ints * 4, cudaMemcpyHostToDevice, st) != cudaSuccess ||
+            cudaEventRecord(plan->buf.uploaded, st) != cudaSuccess) {
+            (void)cudaGetLastError();
+            give_back_plan_buffer(pool->plan_buffers, plan->buf);
+            delete plan;
+            return AP_ERR_CUDA;
+        }
+        plan->d_tiles = (const PromptTile *)plan->buf.dev;
+        plan->d_short = (const ShortPrompt *)(plan->buf.dev + tile_ints);
+    }
+    plan->pool = pool;
+    plan->num_q_heads = Hq;
+    plan->scale = b->softmax_scale > 0.f ? b->softmax_scale : 1.0f / std::sqrt((float)d);
+    plan->info.n_rows = rows;
+    plan->info.pairs = pairs;
+    plan->info.tiles = (int64_t)tiles.size();
+    plan->info.short_units = (int64_t)shorts.size() * Hkv;
+    plan->info.launches = (tiles.empty() ? 0 : 1) + (shorts.empty() ? 0 : 1);
+    *out = plan;
+    return AP_OK;
+}
+
+}  // namespace
+
+cudaError_t launch_prompt(const ap_kv_pool *pool, const ap_prompt_plan *plan, const void *q, const void *k, const void *v,
+                          void *out, float *lse, const ap_prompt_strides &strides, cudaStream_t stream) {
+    if (pool->desc.head_dim == 128) return launch_prompt_t<128>(pool, plan, q, k, v, out, lse, strides, stream);
+    return launch_prompt_t<64>(pool, plan, q, k, v, out, lse, strides, stream);
+}
+
+}  // namespace ap
+
+using namespace ap;
+
+extern "C" {
+
+int ap_prompt_plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *prompts, void *stream) {
+    try {
+        return plan_create(out, pool, prompts, stream);
+    } catch (const std::bad_alloc &) {
+        return AP_ERR_CUDA;
+    }
+}
+
+int ap_prompt_plan_destroy(ap_prompt_plan *plan) {
+    if (!plan) return AP_ERR_INVALID_ARG;
+    if (plan->buf.dev) give_back_plan_buffer(plan->pool->plan_buffers, plan->buf);
+    delete plan;
+    return AP_OK;
+}
+
+int ap_prompt_plan_get_info(const ap_prompt_plan *plan, ap_prompt_info *info) {
+    if (!plan || !info) return AP_ERR_INVALID_ARG;
+    *info = plan->info;
+    return AP_OK;
+}
+
+int ap_prompt_attention(ap_kv_pool *pool, const ap_prompt_plan *plan, const void *q, const void *k, const void *v, void *out,
+                        float *lse, const ap_prompt_strides *strides, void *stream) {
+    if (!pool || !plan || plan->pool != pool || !strides) return AP_ERR_INVALID_ARG;
+    const int64_t d = pool->desc.head_dim, Hq = plan->num_q_heads, Hkv = pool->desc.num_kv_heads, n = plan->info.n_rows;
+    ap_prompt_strides st = *strides;
+    if (st.q_row_stride == 0) st.q_row_stride = Hq * d;
+    if (st.k_row_stride == 0) st.k_row_stride = Hkv * d;
+    if (st.v_row_stride == 0) st.v_row_stride = Hkv * d;
+    const int64_t far = (int64_t)1 << 32;
+    if (st.q_row_stride < Hq * d || st.k_row_stride < Hkv * d || st.v_row_stride < Hkv * d ||
+        (st.q_row_stride | st.k_row_stride | st.v_row_stride) % 8 || st.q_row_stride > far || st.k_row_stride > far || st.v_row_stride > far)
+        return AP_ERR_INVALID_ARG;
+    if (pool->desc.device < 0) return AP_ERR_CUDA;
+    if (n == 0) return AP_OK;
+    if (!q || !k || !v || !out || (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15u) || ((uintptr_t)lse & 3u))
+        return AP_ERR_INVALID_ARG;
+    auto meets = [&](const void *p, int64_t stride, int64_t cols, const void *o, int64_t bytes) {
+        const uintptr_t a = (uintptr_t)p, e = a + (uintptr_t)((n - 1) * stride + cols) * 2, o0 = (uintptr_t)o;
+        return o && a < o0 + (uintptr_t)bytes && o0 < e;
+    };
+    for (int i = 0; i < 2; ++i) {
+        const void *o = i ? (const void *)lse : out;
+        const int64_t bytes = i ? n * Hq * 4 : n * Hq * d * 2;
+        if (meets(q, st.q_row_stride, Hq * d, o, bytes) || meets(k, st.k_row_stride, Hkv * d, o, bytes) ||
+            meets(v, st.v_row_stride, Hkv * d, o, bytes))
+            return AP_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(pool->desc.device);
+    if (!guard.ok) return AP_ERR_CUDA;
+    if (launch_prompt(pool, plan, q, k, v, out, lse, st, (cudaStream_t)stream) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return AP_ERR_CUDA;
+    }
+    return AP_OK;
+}
+
+}  // extern "C"

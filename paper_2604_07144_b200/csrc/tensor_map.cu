@@ -5,7 +5,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
-#include "internal.h"
+#include "layers.h"
 
 namespace ap {
 
@@ -59,23 +59,27 @@ int encode_pool_tensor_map(CUtensorMap *map, void *base, int num_pages, int num_
     return r == CUDA_SUCCESS ? AP_OK : AP_ERR_CUDA;
 }
 
-// q [n_rows][Hq][d] bf16:
-//   dim0: 64 elements; dim1: rows (stride Hq*d*2); dim2: Hq*d/64 column blocks (stride 128 bytes).
+// q [n_rows][Hq][d] bf16 (or k, v with their heads; rows `row_stride` elements apart):
+//   dim0: 64 elements; dim1: rows (stride row_stride*2); dim2: Hq*d/64 column blocks (stride 128 bytes).
 // A box of (64, 128, d/64) at (0, row0, head*d/64) is a 128-row query tile of
 // one head, landing as [half][128 rows][64] (16 swizzle atoms per half).
 // Rows past n_rows read as zero.
-int encode_q_tensor_map(CUtensorMap *map, const void *q, int64_t n_rows, int num_q_heads, int head_dim) {
+int encode_rows_tensor_map(CUtensorMap *map, const void *base, int64_t n_rows, int heads, int head_dim, int64_t row_stride) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return AP_ERR_CUDA;
     const cuuint64_t halves = (cuuint64_t)head_dim / 64;
-    cuuint64_t dims[3] = {64, (cuuint64_t)n_rows, (cuuint64_t)num_q_heads * halves};
-    cuuint64_t strides[2] = {(cuuint64_t)num_q_heads * (cuuint64_t)head_dim * 2, 128};
+    cuuint64_t dims[3] = {64, (cuuint64_t)n_rows, (cuuint64_t)heads * halves};
+    cuuint64_t strides[2] = {(cuuint64_t)row_stride * 2, 128};
     cuuint32_t box[3] = {64, 128, (cuuint32_t)halves};
     cuuint32_t estr[3] = {1, 1, 1};
-    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(q), dims, strides, box, estr,
+    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? AP_OK : AP_ERR_CUDA;
+}
+
+int encode_q_tensor_map(CUtensorMap *map, const void *q, int64_t n_rows, int num_q_heads, int head_dim) {
+    return encode_rows_tensor_map(map, q, n_rows, num_q_heads, head_dim, (int64_t)num_q_heads * head_dim);
 }
 
 }  // namespace ap
