@@ -79,7 +79,7 @@ struct ap_state_plan {
 namespace ap {
 
 constexpr int kConvRun = 16;      // rows that a thread of the convolution walks
-constexpr int kScanTile = 32;     // rows that a block of the scan stages at a time; pieces are multiples of it
+constexpr int kScanTile = 32;     // pieces of a sequence are multiples of it, as it is of the rows that the scan stages at a time
 
 struct ScanArgs {                 // by value to the kernels
     const uint16_t *x, *dt, *b, *c, *z;       // bf16
@@ -92,7 +92,7 @@ struct ScanArgs {                 // by value to the kernels
     int channels, softplus;
 };
 
-int scan_block_channels(int state_dim);       // channels a block of the scan takes
+int scan_warp_channels(int state_dim);        // channels that a warp of the scan takes
 cudaError_t launch_conv(const ap_state_pool *pool, const ap_state_plan *plan, const ap_conv_desc &conv, const void *x,
                         const void *weight, const void *bias, void *out, cudaStream_t stream);
 cudaError_t launch_scan(const ap_state_pool *pool, const ap_state_plan *plan, const ScanArgs &args, cudaStream_t stream);

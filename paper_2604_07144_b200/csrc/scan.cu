@@ -7,9 +7,13 @@
 // (token, channel, state): at 16 states the special-function unit (16 a clock and SM) bounds it, ahead of HBM.  A single
 // token costs its state, read and written: HBM.
 //
-// Work split.  A quad of lanes takes kCh channels (four at 16 states); a lane holds N / 4 states of each of them.  Against
-// a lane per channel this halves what the lanes read from shared memory per update (b and c serve four channels, d and
-// d x four lanes) and leaves every lane with one channel's sum, by exchanging partial sums inside the quad.
+// Work split of prompts.  H states of a channel are a lane's, L = N / H lanes make a channel, and a warp walks 32 / L channels
+// alone: no barrier but its own.  The steps of a tile of rows are worked out once, spread over the lanes, and so are the
+// gates: partial sums of L rows are exchanged so that each lane ends with the sum of one.  What all channels share, b and c,
+// stands in shared memory in fp32; x, dt and z come by asynchronous copies, a tile ahead.  Few states a lane make many
+// warps, which is what hides the chain from load to exponential to sum.
+#include <type_traits>
+
 #include "layers.h"
 #include "ptx.cuh"
 
@@ -19,18 +23,30 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kScanWarps = 4, kScanThreads = 32 * kScanWarps;
-
+// Single tokens: a quad of lanes takes kCh channels, each lane N / 4 states of every one of them.
 template <int N>
-struct Scan {
+struct Step {
     static constexpr int kHeld = N / 4;                        // states a lane holds of a channel
     static constexpr int kCh = kHeld <= 4 ? 4 : 16 / kHeld;    // channels of a quad: 16 states a lane at most
-    static constexpr int kBlockCh = kScanWarps * 8 * kCh;
+    static constexpr int kThreads = 128;
+    static constexpr int kBlockCh = kThreads / 4 * kCh;
     static constexpr int kVec = kHeld < 4 ? kHeld : 4;         // states that lie together: lane q has 4 kVec i + kVec q + e
     static constexpr int kVecs = kHeld / kVec;
-    static constexpr int kGroups = kBlockCh / 8;               // 16-byte groups of a row's channels
-    static constexpr int kRowsAtOnce = kScanThreads / kGroups; // rows that the block stages at once
-    static constexpr int kPasses = kScanTile / kRowsAtOnce;
+};
+
+// Prompts: a lane has H states of one channel.
+constexpr int kTile = 16;                                      // rows staged at a time
+constexpr int kGroup = 8;                                      // rows walked in one piece of code
+constexpr int kWalkBlocks = 7;                               // of an SM
+template <int N, int H>
+struct Walk {
+    static constexpr int kLanes = N / H;                       // lanes of a channel
+    static constexpr int kCh = 32 / kLanes;                    // channels of a warp
+    // warps of a block, blocks of an SM
+    static constexpr int kWarps = 2, kBlocks = 8;
+    // staging: a lane takes two channels next to one another
+    static constexpr int kTwos = kCh / 2, kRowsAtOnce = 32 / kTwos, kPasses = kTile / kRowsAtOnce;
+    static_assert(H % 4 == 0 && kCh >= 4 && kTile % kRowsAtOnce == 0, "");
 };
 
 __device__ __forceinline__ float2 widen2(uint32_t v) {
@@ -54,12 +70,54 @@ __device__ __forceinline__ float softplus(float x) {
     return fmaf(p, u, fmaxf(x, 0.f));                          // (a NaN comes through u)
 }
 
-__device__ __forceinline__ float gate(float y, float z) { return y * __fdividef(z, 1.f + exp2_approx(-1.4426950408889634f * z)); }
+// The same for two values, on packed fp32.
+__device__ __forceinline__ float2 softplus2(float2 x) {
+    const float2 t = __fmul2_rn(make_float2(fabsf(x.x), fabsf(x.y)), make_float2(-1.4426950408889634f, -1.4426950408889634f));
+    const float2 u = make_float2(exp2_approx(t.x), exp2_approx(t.y));
+    auto two = [](float c) { return make_float2(c, c); };
+    float2 p = __ffma2_rn(two(-0.0032440212f), u, two(0.0198514443f));
+    p = __ffma2_rn(p, u, two(-0.0569594987f));
+    p = __ffma2_rn(p, u, two(0.106036514f));
+    p = __ffma2_rn(p, u, two(-0.153055906f));
+    p = __ffma2_rn(p, u, two(0.196759388f));
+    p = __ffma2_rn(p, u, two(-0.249541342f));
+    p = __ffma2_rn(p, u, two(0.333299637f));
+    p = __ffma2_rn(p, u, two(-0.499999017f));
+    p = __ffma2_rn(p, u, two(1.f));
+    return __ffma2_rn(p, u, make_float2(fmaxf(x.x, 0.f), fmaxf(x.y, 0.f)));
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) {   // a NaN wins
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float d;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+
+__device__ __forceinline__ float reciprocal(float x) {         // to one step of fp32; 0 for infinity
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ float2 as_floats(uint2 v) { return make_float2(__uint_as_float(v.x), __uint_as_float(v.y)); }
+
+__device__ __forceinline__ float2 gate2(float2 y, float2 z) {
+    float2 e = __fmul2_rn(z, make_float2(-1.4426950408889634f, -1.4426950408889634f));
+    e = __fadd2_rn(make_float2(exp2_approx(e.x), exp2_approx(e.y)), make_float2(1.f, 1.f));
+    return __fmul2_rn(y, __fmul2_rn(z, make_float2(reciprocal(e.x), reciprocal(e.y))));
+}
+
+__device__ __forceinline__ float gate(float y, float z) { return y * (z * reciprocal(1.f + exp2_approx(-1.4426950408889634f * z))); }
 
 // kHeld consecutive-by-vector fp32 values of a lane: states 4 kVec i + kVec q + e
 template <int N>
-__device__ __forceinline__ void load_states(const float *row, int q, float (&h)[Scan<N>::kHeld]) {
-    using S = Scan<N>;
+__device__ __forceinline__ void load_states(const float *row, int q, float (&h)[Step<N>::kHeld]) {
+    using S = Step<N>;
 #pragma unroll
     for (int i = 0; i < S::kVecs; ++i) {
         const float *p = row + 4 * S::kVec * i + S::kVec * q;
@@ -75,8 +133,8 @@ __device__ __forceinline__ void load_states(const float *row, int q, float (&h)[
 }
 
 template <int N>
-__device__ __forceinline__ void store_states(float *row, int q, const float (&h)[Scan<N>::kHeld]) {
-    using S = Scan<N>;
+__device__ __forceinline__ void store_states(float *row, int q, const float (&h)[Step<N>::kHeld]) {
+    using S = Step<N>;
 #pragma unroll
     for (int i = 0; i < S::kVecs; ++i) {
         float *p = row + 4 * S::kVec * i + S::kVec * q;
@@ -105,226 +163,289 @@ __device__ __forceinline__ float quad_sum(const float (&y)[kCh], int q) {
     }
 }
 
-template <int N>
-struct ScanSmem {
-    float d[kScanTile][Scan<N>::kBlockCh];       // steps
-    float dx[kScanTile][Scan<N>::kBlockCh];      // step times input
-    float y[kScanTile][Scan<N>::kBlockCh];       // d_skip x, then the row's result before the gate
-    float b[kScanTile][N], c[kScanTile][N];
+// 2^x for two values on the FMA pipe: n = round(x), f = x - n in [-0.5, 0.5], 2^f = 1 + f g(f) with a quartic g fitted for
+// relative error (4.3e-7: 2^f is off by 2.2e-7 at most, and by f 4.3e-7 for small f, where decays that last are multiplied
+// thousands of times), 2^n by adding n to the exponent field.  For |x| <= kPolyRange.
+constexpr float kPolyRange = 120.f;
+__device__ __forceinline__ float2 exp2_pair(float2 x) {
+    const float2 magic = make_float2(12582912.f, 12582912.f);              // 1.5 * 2^23: x + magic holds round(x) in its low bits
+    const float2 t = __fadd2_rn(x, magic);
+    const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
+    const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
+    float2 p = __ffma2_rn(f, make_float2(0.00133335381f, 0.00133335381f), make_float2(0.00966624543f, 0.00966624543f));
+    p = __ffma2_rn(p, f, make_float2(0.0555050038f, 0.0555050038f));
+    p = __ffma2_rn(p, f, make_float2(0.240223512f, 0.240223512f));
+    p = __ffma2_rn(p, f, make_float2(0.693147123f, 0.693147123f));
+    p = __ffma2_rn(p, f, make_float2(1.f, 1.f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
+                       __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+
+// One pair of states in kPolyEvery takes the FMA pipe for its exponential.
+constexpr int kPolyEvery = 8;
+constexpr int kHeldStates = 8;
+
+template <int N, int H>
+struct WalkSmem {                                              // a warp's own
+    alignas(16) uint16_t x[kTile][Walk<N, H>::kCh], dt[kTile][Walk<N, H>::kCh], z[kTile][Walk<N, H>::kCh];
+    alignas(16) uint16_t b_in[kTile][N], c_in[kTile][N];
+    alignas(16) float b[kTile][N], c[kTile][N];
+    alignas(16) float2 step[kTile][Walk<N, H>::kCh];           // d and d x
+    alignas(16) float y[kTile][Walk<N, H>::kCh];              // d_skip x, then the row's result before the gate
+    float bias[Walk<N, H>::kCh], skip[Walk<N, H>::kCh];
 };
 
-// One piece of a sequence for kBlockCh channels.  Rows are staged kScanTile at a time: x and dt (16-byte groups of
-// channels, all threads) become d, d x and d_skip x in shared memory; the quads walk the rows; the gate is applied on the
-// way out.  The next tile's loads are in flight while the rows of this one are walked.
-template <int N, bool kStateOnly>
-__device__ __forceinline__ void scan_unit(const StateUnit &unit, int cb, const ScanArgs &g, ScanSmem<N> &sm) {
-    using S = Scan<N>;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = lane & 3;
-    const int64_t D = g.channels;
-    // staging: this thread's group of channels and first row
-    const int grp = tid % S::kGroups, row_in = tid / S::kGroups;
-    const int64_t sc = (int64_t)cb * S::kBlockCh + grp * 8;
-    const bool s_in = sc < D;                                  // (channels come in eights)
-    float bias[8] = {}, skip[8] = {};
-    if (s_in && g.dt_bias) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) bias[i] = __uint_as_float(load4(g.dt_bias + sc + i));
-    }
-    if (!kStateOnly && s_in && g.d_skip) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) skip[i] = __uint_as_float(load4(g.d_skip + sc + i));
-    }
-    // walking: this lane's channels and states
-    const int lc = warp * 8 * S::kCh + (lane >> 2) * S::kCh;   // the quad's first channel in the block
-    const int64_t wc = (int64_t)cb * S::kBlockCh + lc;
-    float h[S::kCh][S::kHeld], a2[S::kCh][S::kHeld], total[S::kCh];
-#pragma unroll
-    for (int c = 0; c < S::kCh; ++c) {
-        total[c] = 0.f;
-#pragma unroll
-        for (int i = 0; i < S::kHeld; ++i) h[c][i] = a2[c][i] = 0.f;
-        if (wc + c >= D) continue;
-        load_states<N>(g.a + (wc + c) * N, q, a2[c]);
-#pragma unroll
-        for (int i = 0; i < S::kHeld; ++i) a2[c][i] *= 1.4426950408889634f;
-        if (unit.seg > 0 && !kStateOnly) {
-            // the state behind the pieces before this one: each piece's own, and what is left of the state before it
-            load_states<N>(g.seg_state + ((int64_t)unit.seg_first * D + wc + c) * N, q, h[c]);
-            for (int s = 1; s < unit.seg; ++s) {
-                const int64_t at = (int64_t)(unit.seg_first + s) * D + wc + c;
-                const float step = __uint_as_float(load4(g.seg_dt + at));
-                float own[S::kHeld];
-                load_states<N>(g.seg_state + at * N, q, own);
-#pragma unroll
-                for (int i = 0; i < S::kHeld; ++i) h[c][i] = fmaf(exp2_approx(step * a2[c][i]), h[c][i], own[i]);
-            }
-        } else if ((unit.flags & kUnitFirst) && (unit.flags & kUnitKept)) {
-            load_states<N>(g.state + ((int64_t)unit.slot * D + wc + c) * N, q, h[c]);
-        }
-    }
+template <int kBytes>
+__device__ __forceinline__ void copy_async(void *to, const void *from) {  // global to shared
+    if constexpr (kBytes == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(to)), "l"(from), "n"(kBytes) : "memory");
+}
 
-    uint4 xr[S::kPasses], tr[S::kPasses], zr[S::kPasses];
-    constexpr int kBcGroups = N / 8;                           // 16-byte groups of a row of b (of c)
-    constexpr int kBcLoads = (kScanTile * kBcGroups + kScanThreads - 1) / kScanThreads;
-    uint4 br[kBcLoads], cr[kBcLoads];
-    auto load_tile = [&](int t0) {
+// One piece of a sequence for a warp's channels.
+template <int N, int H, bool kStateOnly>
+__device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, const ScanArgs &g, WalkSmem<N, H> &sm) {
+    using S = Walk<N, H>;
+    constexpr int K = H / 2, L = S::kLanes;
+    const int lane = threadIdx.x & 31;
+    const int64_t D = g.channels;
+    // walking: this lane's channel, and which of its states
+    const int part = lane / S::kCh, cl = lane % S::kCh;
+    const int64_t ch = c0 + cl;
+    const bool in = ch < D;
+    const int rows_all = unit.rows;
+    const int64_t row0 = unit.row0;
+    float2 h[K], a2[K];
+    float widest = 0.f;                                        // largest |a log2 e| of the warp
+    auto load_held = [&](const float *row, float2 (&to)[K]) {  // this lane's states of a channel's row
 #pragma unroll
-        for (int p = 0; p < S::kPasses; ++p) {
-            const int t = t0 + p * S::kRowsAtOnce + row_in;
-            xr[p] = tr[p] = make_uint4(0, 0, 0, 0);
-            if (s_in && t < unit.rows) {
-                xr[p] = load16(g.x + (unit.row0 + (int64_t)t) * g.xs + sc);
-                tr[p] = load16(g.dt + (unit.row0 + (int64_t)t) * g.dts + sc);
-            }
-        }
-#pragma unroll
-        for (int p = 0; p < kBcLoads; ++p) {
-            const int i = p * kScanThreads + tid, t = t0 + i / kBcGroups;
-            br[p] = cr[p] = make_uint4(0, 0, 0, 0);
-            if (i < kScanTile * kBcGroups && t < unit.rows) {
-                br[p] = load16(g.b + (unit.row0 + (int64_t)t) * g.bs + i % kBcGroups * 8);
-                if (!kStateOnly) cr[p] = load16(g.c + (unit.row0 + (int64_t)t) * g.cs + i % kBcGroups * 8);
-            }
+        for (int i = 0; i < K; i += 2) {
+            const uint4 v = load16(row + part * H + 2 * i);
+            to[i] = make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
+            to[i + 1] = make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
         }
     };
-    load_tile(0);
-    for (int t0 = 0; t0 < unit.rows; t0 += kScanTile) {
-        const int rows = min(kScanTile, unit.rows - t0);
 #pragma unroll
-        for (int p = 0; p < S::kPasses; ++p) {
-            const int r = p * S::kRowsAtOnce + row_in;
-            const uint32_t xw[4] = {xr[p].x, xr[p].y, xr[p].z, xr[p].w}, tw[4] = {tr[p].x, tr[p].y, tr[p].z, tr[p].w};
-            float *d = &sm.d[r][grp * 8], *dx = &sm.dx[r][grp * 8], *y = &sm.y[r][grp * 8];
+    for (int k = 0; k < K; ++k) h[k] = a2[k] = make_float2(0.f, 0.f);
+    if (in) {
+        load_held(g.a + ch * N, a2);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 x = widen2(xw[i]);
-                float2 s = widen2(tw[i]);
-                s.x += bias[2 * i], s.y += bias[2 * i + 1];
-                if (g.softplus) s.x = softplus(s.x), s.y = softplus(s.y);
-                *(float2 *)(d + 2 * i) = s;
-                *(float2 *)(dx + 2 * i) = make_float2(s.x * x.x, s.y * x.y);
-                if (!kStateOnly) *(float2 *)(y + 2 * i) = make_float2(skip[2 * i] * x.x, skip[2 * i + 1] * x.y);
-            }
+        for (int k = 0; k < K; ++k) {
+            a2[k] = __fmul2_rn(a2[k], make_float2(1.4426950408889634f, 1.4426950408889634f));
+            // (finite: rows past the end have steps of 0, and e^(0 a) has to be 1)
+            a2[k] = make_float2(max_nan(min_nan(a2[k].x, 3e38f), -3e38f), max_nan(min_nan(a2[k].y, 3e38f), -3e38f));
+            widest = max_nan(widest, max_nan(fabsf(a2[k].x), fabsf(a2[k].y)));
         }
+        if (unit.seg > 0 && !kStateOnly) {
+            // the state behind the pieces before this one: each piece's own, and what is left of the state before it
+            load_held(g.seg_state + ((int64_t)unit.seg_first * D + ch) * N, h);
+            for (int s = 1; s < unit.seg; ++s) {
+                const int64_t at = (int64_t)(unit.seg_first + s) * D + ch;
+                const float step = __uint_as_float(load4(g.seg_dt + at));
+                float2 own[K];
+                load_held(g.seg_state + at * N, own);
 #pragma unroll
-        for (int p = 0; p < kBcLoads; ++p) {
-            const int i = p * kScanThreads + tid;
-            if (i < kScanTile * kBcGroups) {
-                float *bd = &sm.b[i / kBcGroups][i % kBcGroups * 8], *cd = &sm.c[i / kBcGroups][i % kBcGroups * 8];
-                const uint32_t bw[4] = {br[p].x, br[p].y, br[p].z, br[p].w}, cw[4] = {cr[p].x, cr[p].y, cr[p].z, cr[p].w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    *(float2 *)(bd + 2 * k) = widen2(bw[k]);
-                    if (!kStateOnly) *(float2 *)(cd + 2 * k) = widen2(cw[k]);
-                }
+                for (int k = 0; k < K; ++k)
+                    h[k] = __ffma2_rn(make_float2(exp2_approx(step * a2[k].x), exp2_approx(step * a2[k].y)), h[k], own[k]);
             }
+        } else if ((unit.flags & kUnitFirst) && (unit.flags & kUnitKept)) {
+            load_held(g.state + ((int64_t)unit.slot * D + ch) * N, h);
         }
-        __syncthreads();
-        if (t0 + kScanTile < unit.rows) load_tile(t0 + kScanTile);
-        if (!kStateOnly && g.z) {
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) widest = max_nan(widest, __shfl_xor_sync(0xffffffffu, widest, o));
+
+    // staging: this lane's two channels and first row
+    const int two = lane % S::kTwos * 2, row_in = lane / S::kTwos;
+    const bool s_in = c0 + two < D;                            // (channels come in eights)
+    if (row_in == 0) {
+        float2 bias = make_float2(0.f, 0.f), skip = bias;
+        if (s_in && g.dt_bias) bias = as_floats(load8(g.dt_bias + c0 + two));
+        if (!kStateOnly && s_in && g.d_skip) skip = as_floats(load8(g.d_skip + c0 + two));
+        *(float2 *)&sm.bias[two] = bias, *(float2 *)&sm.skip[two] = skip;
+    }
+    float2 total = make_float2(0.f, 0.f);
+
+    // Asynchronous copies of a tile's rows, `cols` numbers each from column `col` on, kSize numbers a copy.  Rows past the
+    // unit are left as they are, and not used.
+    auto copy_rows = [&](auto size, auto to, int cols, const uint16_t *from, int64_t stride, int64_t col, int64_t end, int t0) {
+        constexpr int kSize = decltype(size)::value;
+        const int chunks = cols / kSize;
+#pragma unroll
+        for (int i = 0; i < (kTile * chunks + 31) / 32; ++i) {
+            const int at = i * 32 + lane, r = at / chunks, e = at % chunks * kSize;
+            if (at < kTile * chunks && t0 + r < rows_all && col + e < end)
+                copy_async<2 * kSize>(to + at * kSize, from + (row0 + t0 + r) * stride + col + e);
+        }
+    };
+    constexpr std::integral_constant<int, (S::kCh >= 8 ? 8 : S::kCh)> kAsync;
+    constexpr std::integral_constant<int, 8> kEight;
+    auto copy_in = [&](int t0) {
+        copy_rows(kAsync, &sm.x[0][0], S::kCh, g.x, g.xs, c0, D, t0);
+        copy_rows(kAsync, &sm.dt[0][0], S::kCh, g.dt, g.dts, c0, D, t0);
+        copy_rows(kEight, &sm.b_in[0][0], N, g.b, g.bs, 0, N, t0);
+        if (!kStateOnly) copy_rows(kEight, &sm.c_in[0][0], N, g.c, g.cs, 0, N, t0);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    copy_in(0);
+    for (int t0 = 0; t0 < rows_all; t0 += kTile) {
+        const int rows = min(kTile, rows_all - t0);
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
+        // the gates are wanted last: they come while the rows are walked
+        if (!kStateOnly && g.z) copy_rows(kAsync, &sm.z[0][0], S::kCh, g.z, g.zs, c0, D, t0);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        // b and c in fp32 (rows past the end: zeros, which their steps of 0 multiply)
+#pragma unroll
+        for (int i = lane; i < kTile * N / 8; i += 32) {
+            const bool past = i * 8 / N >= rows;
+            auto widen8 = [&](const uint16_t *from, float *to) {
+                uint4 v = *(const uint4 *)from;
+                if (past) v = make_uint4(0, 0, 0, 0);
+                const float2 a = widen2(v.x), b = widen2(v.y), c = widen2(v.z), d = widen2(v.w);
+                *(float4 *)to = make_float4(a.x, a.y, b.x, b.y);
+                *(float4 *)(to + 4) = make_float4(c.x, c.y, d.x, d.y);
+            };
+            widen8(&sm.b_in[0][0] + i * 8, &sm.b[0][0] + i * 8);
+            if (!kStateOnly) widen8(&sm.c_in[0][0] + i * 8, &sm.c[0][0] + i * 8);
+        }
+        // every row's step and step times input
+        float longest = 0.f;
+        {
+            const float2 bias = *(const float2 *)&sm.bias[two], skip = *(const float2 *)&sm.skip[two];
 #pragma unroll
             for (int p = 0; p < S::kPasses; ++p) {
-                const int t = t0 + p * S::kRowsAtOnce + row_in;
-                zr[p] = make_uint4(0, 0, 0, 0);
-                if (s_in && t < unit.rows) zr[p] = load16(g.z + (unit.row0 + (int64_t)t) * g.zs + sc);
+                const int r = p * S::kRowsAtOnce + row_in;
+                float2 d = __fadd2_rn(widen2(*(const uint32_t *)&sm.dt[r][two]), bias);
+                if (g.softplus) d = softplus2(d);
+                const float2 x = widen2(*(const uint32_t *)&sm.x[r][two]);
+                float2 dx = __fmul2_rn(d, x);
+                if (!kStateOnly) *(float2 *)&sm.y[r][two] = __fmul2_rn(skip, x);
+                if (r >= rows || !s_in) d = dx = make_float2(0.f, 0.f);      // (past the end the state stays as it is)
+                longest = max_nan(longest, max_nan(fabsf(d.x), fabsf(d.y)));
+                if (kStateOnly) total = __fadd2_rn(total, d);
+                *(float4 *)&sm.step[r][two] = make_float4(d.x, dx.x, d.y, dx.y);
             }
         }
-#pragma unroll 2
-        for (int r = 0; r < rows; ++r) {
-            float d[S::kCh], dx[S::kCh], b[S::kHeld], cc[S::kHeld];
-            if constexpr (S::kCh == 4) {
-                const float4 u = *(const float4 *)&sm.d[r][lc], v = *(const float4 *)&sm.dx[r][lc];
-                d[0] = u.x, d[1] = u.y, d[2] = u.z, d[3] = u.w;
-                dx[0] = v.x, dx[1] = v.y, dx[2] = v.z, dx[3] = v.w;
-            } else {
+        // (far also where a step or an a is NaN)
+        const bool far = __any_sync(0xffffffffu, !(longest * widest <= kPolyRange));
+        __syncwarp();
+        copy_in(t0 + kTile);                                   // (past the end: an empty group)
+        auto walk = [&](auto poly) {
+#pragma unroll 1
+            for (int r0 = 0; r0 < rows; r0 += kGroup) {
+                float y[kGroup];
 #pragma unroll
-                for (int c = 0; c < S::kCh; ++c) d[c] = sm.d[r][lc + c], dx[c] = sm.dx[r][lc + c];
-            }
+                for (int r = 0; r < kGroup; ++r) {
+                    const float2 step = sm.step[r0 + r][cl];
+                    const float2 d2 = make_float2(step.x, step.x), dx2 = make_float2(step.y, step.y);
+                    float2 b[K], c[K], sum = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int i = 0; i < S::kVecs; ++i) {
+                    for (int k = 0; k < K; k += 2) {
+                        const float4 u = *(const float4 *)&sm.b[r0 + r][part * H + 2 * k];
+                        b[k] = make_float2(u.x, u.y), b[k + 1] = make_float2(u.z, u.w);
+                        if (!kStateOnly) {
+                            const float4 v = *(const float4 *)&sm.c[r0 + r][part * H + 2 * k];
+                            c[k] = make_float2(v.x, v.y), c[k + 1] = make_float2(v.z, v.w);
+                        }
+                    }
 #pragma unroll
-                for (int e = 0; e < S::kVec; ++e) {
-                    b[i * S::kVec + e] = sm.b[r][4 * S::kVec * i + S::kVec * q + e];
-                    if (!kStateOnly) cc[i * S::kVec + e] = sm.c[r][4 * S::kVec * i + S::kVec * q + e];
+                    for (int k = 0; k < K; ++k) {
+                        float2 e = __fmul2_rn(d2, a2[k]);
+                        if (decltype(poly)::value && (r * K + k) % kPolyEvery == kPolyEvery - 1) {
+                            e = exp2_pair(e);
+                        } else {
+                            e.x = exp2_approx(e.x);
+                            e.y = exp2_approx(e.y);
+                        }
+                        h[k] = __ffma2_rn(e, h[k], __fmul2_rn(dx2, b[k]));
+                        if (!kStateOnly) sum = k == 0 ? __fmul2_rn(h[k], c[k]) : __ffma2_rn(h[k], c[k], sum);
+                    }
+                    y[r] = sum.x + sum.y;
+                }
+                if constexpr (!kStateOnly) {
+                    // the lanes of a channel exchange halves of their rows until each has whole sums
+                    constexpr int kShare = L > kGroup ? L / kGroup : 1;       // lanes that have the same row
+                    int mine = 0;
+#pragma unroll
+                    for (int o = L / 2, n = kGroup / 2; o > 0; o /= 2, n /= 2) {
+                        const bool high = part & o;
+                        if (n > 0) {
+#pragma unroll
+                            for (int i = 0; i < n; ++i) {
+                                const float keep = high ? y[i + n] : y[i], give = high ? y[i] : y[i + n];
+                                y[i] = keep + __shfl_xor_sync(0xffffffffu, give, o * S::kCh);
+                            }
+                            mine += high ? n : 0;
+                        } else {
+                            y[0] += __shfl_xor_sync(0xffffffffu, y[0], o * S::kCh);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < (kGroup > L ? kGroup / L : 1); ++i)
+                        if (part % kShare == 0) sm.y[r0 + mine + i][cl] += y[i];
                 }
             }
-            float y[S::kCh];
-#pragma unroll
-            for (int c = 0; c < S::kCh; ++c) {
-                float2 sum = make_float2(0.f, 0.f);
-                const float2 d2 = make_float2(d[c], d[c]), dx2 = make_float2(dx[c], dx[c]);
-#pragma unroll
-                for (int i = 0; i < S::kHeld; i += 2) {
-                    float2 e = __fmul2_rn(d2, make_float2(a2[c][i], a2[c][i + 1]));
-                    e.x = exp2_approx(e.x);
-                    e.y = exp2_approx(e.y);
-                    const float2 in = __fmul2_rn(dx2, make_float2(b[i], b[i + 1]));
-                    const float2 hn = __ffma2_rn(e, make_float2(h[c][i], h[c][i + 1]), in);
-                    h[c][i] = hn.x, h[c][i + 1] = hn.y;
-                    if (!kStateOnly) sum = __ffma2_rn(hn, make_float2(cc[i], cc[i + 1]), sum);
-                }
-                y[c] = sum.x + sum.y;
-                if (kStateOnly) total[c] += d[c];
-            }
-            if constexpr (!kStateOnly) {
-                const float mine = quad_sum<S::kCh>(y, q);
-                if (S::kCh == 4 || q % (4 / S::kCh) == 0) sm.y[r][lc + q * S::kCh / 4] += mine;
-            }
-        }
-        __syncthreads();
+        };
+        if (far) walk(std::false_type());
+        else walk(std::true_type());
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncwarp();
         if constexpr (!kStateOnly) {
 #pragma unroll
             for (int p = 0; p < S::kPasses; ++p) {
                 const int r = p * S::kRowsAtOnce + row_in;
-                if (!s_in || r >= rows) continue;
-                const float *y = &sm.y[r][grp * 8];
-                const uint32_t zw[4] = {zr[p].x, zr[p].y, zr[p].z, zr[p].w};
-                uint32_t o[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float2 v = *(const float2 *)(y + 2 * i);
-                    if (g.z) {
-                        const float2 z = widen2(zw[i]);
-                        v = make_float2(gate(v.x, z.x), gate(v.y, z.y));
-                    }
-                    o[i] = pack_bf16x2(v.x, v.y);
-                }
-                *(uint4 *)(g.out + (unit.row0 + (int64_t)(t0 + r)) * g.os + sc) = make_uint4(o[0], o[1], o[2], o[3]);
+                float2 y = *(const float2 *)&sm.y[r][two];
+                if (g.z) y = gate2(y, widen2(*(const uint32_t *)&sm.z[r][two]));
+                if (s_in && r < rows) *(uint32_t *)(g.out + (row0 + t0 + r) * g.os + c0 + two) = pack_bf16x2(y.x, y.y);
             }
         }
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     // the state behind the rows: the sequence's, or what the pieces after this one begin with
+    if (in) {
+        auto store_held = [&](float *row) {
 #pragma unroll
-    for (int c = 0; c < S::kCh; ++c) {
-        if (wc + c >= D) continue;
-        if (unit.flags & kUnitLast) {
-            store_states<N>(g.state + ((int64_t)unit.slot * D + wc + c) * N, q, h[c]);
-        } else if (kStateOnly || unit.seg == 0) {
-            const int64_t at = (int64_t)(unit.seg_first + unit.seg) * D + wc + c;
-            store_states<N>(g.seg_state + at * N, q, h[c]);
-            if (kStateOnly && q == 0) g.seg_dt[at] = total[c];
+            for (int i = 0; i < K; i += 2)
+                *(float4 *)(row + part * H + 2 * i) = make_float4(h[i].x, h[i].y, h[i + 1].x, h[i + 1].y);
+        };
+        if (unit.flags & kUnitLast)
+            store_held(g.state + ((int64_t)unit.slot * D + ch) * N);
+        else if (kStateOnly || unit.seg == 0)
+            store_held(g.seg_state + ((int64_t)(unit.seg_first + unit.seg) * D + ch) * N);
+    }
+    if (kStateOnly) {
+#pragma unroll
+        for (int o = S::kTwos; o < 32; o *= 2) {
+            total.x += __shfl_xor_sync(0xffffffffu, total.x, o);
+            total.y += __shfl_xor_sync(0xffffffffu, total.y, o);
         }
+        if (s_in && row_in == 0) *(float2 *)(g.seg_dt + (int64_t)(unit.seg_first + unit.seg) * D + c0 + two) = total;
     }
 }
 
-template <int N>
-__global__ void __launch_bounds__(kScanThreads)
-scan_kernel(const StateUnit *__restrict__ units, int blocks_c, const ScanArgs g) {
+template <int N, int H>
+__global__ void __launch_bounds__(32 * Walk<N, H>::kWarps, Walk<N, H>::kBlocks)
+scan_kernel(const StateUnit *__restrict__ units, int64_t n_warps, int blocks_c, const ScanArgs g) {
     extern __shared__ __align__(16) uint8_t raw[];
-    ScanSmem<N> &sm = *(ScanSmem<N> *)raw;
-    const int u = (int)blockIdx.x / blocks_c, cb = (int)blockIdx.x % blocks_c;
-    const StateUnit unit = units[u];
+    const int warp = threadIdx.x >> 5;
+    const int64_t at = (int64_t)blockIdx.x * Walk<N, H>::kWarps + warp;
     griddep_launch_dependents();
+    if (at >= n_warps) return;
+    const StateUnit unit = units[at / blocks_c];
+    const int64_t c0 = at % blocks_c * Walk<N, H>::kCh;
     griddep_wait();
-    if (unit.flags & kUnitStateOnly) scan_unit<N, true>(unit, cb, g, sm);
-    else scan_unit<N, false>(unit, cb, g, sm);
+    WalkSmem<N, H> &sm = ((WalkSmem<N, H> *)raw)[warp];
+    if (unit.flags & kUnitStateOnly) walk_unit<N, H, true>(unit, c0, g, sm);
+    else walk_unit<N, H, false>(unit, c0, g, sm);
 }
 
 // Sequences with one new token: everything in registers, lane q of a quad works out channel q * kCh / 4's step and result.
 template <int N>
-__global__ void __launch_bounds__(kScanThreads)
+__global__ void __launch_bounds__(Step<N>::kThreads)
 scan_step_kernel(const StateUnit *__restrict__ units, int blocks_c, const ScanArgs g) {
-    using S = Scan<N>;
+    using S = Step<N>;
     const int u = (int)blockIdx.x / blocks_c, cb = (int)blockIdx.x % blocks_c;
     const int lane = threadIdx.x & 31, q = lane & 3;
     const StateUnit unit = units[u];
@@ -380,35 +501,33 @@ scan_step_kernel(const StateUnit *__restrict__ units, int blocks_c, const ScanAr
     }
 }
 
+template <int N, int H>
+cudaError_t launch_walk(const ap_state_pool *pool, const StateUnit *units, int n, const ScanArgs &args, cudaStream_t stream) {
+    constexpr int kWarps = Walk<N, H>::kWarps;
+    constexpr size_t kSmem = kWarps * sizeof(WalkSmem<N, H>);
+    static_assert(kSmem <= 48 << 10, "within what a kernel may have unasked");
+    const int blocks_c = (pool->desc.channels + Walk<N, H>::kCh - 1) / Walk<N, H>::kCh;
+    const int64_t warps = (int64_t)n * blocks_c;
+    return launch_overlapped(scan_kernel<N, H>, (unsigned)((warps + kWarps - 1) / kWarps), 32u * kWarps, kSmem, stream, units,
+                             warps, blocks_c, args);
+}
+
 template <int N>
 cudaError_t launch_scan_t(const ap_state_pool *pool, const ap_state_plan *plan, const ScanArgs &args, cudaStream_t stream) {
-    static bool configured[64] = {};
-    const int dev = pool->desc.device & 63;
-    if (!configured[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(scan_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)sizeof(ScanSmem<N>));
-        if (e != cudaSuccess) return e;
-        configured[dev] = true;
-    }
-    const int blocks_c = (pool->desc.channels + Scan<N>::kBlockCh - 1) / Scan<N>::kBlockCh;
+    auto launch = [&](const StateUnit *units, int n) { return launch_walk<N, (N < kHeldStates ? N : kHeldStates)>(pool, units, n, args, stream); };
     cudaError_t e = cudaSuccess;
-    if (plan->n_first > 0)
-        e = launch_overlapped(scan_kernel<N>, (unsigned)(plan->n_first * blocks_c), (unsigned)kScanThreads, sizeof(ScanSmem<N>),
-                              stream, plan->d_first, blocks_c, args);
-    if (e == cudaSuccess && plan->n_second > 0)
-        e = launch_overlapped(scan_kernel<N>, (unsigned)(plan->n_second * blocks_c), (unsigned)kScanThreads, sizeof(ScanSmem<N>),
-                              stream, plan->d_second, blocks_c, args);
+    if (plan->n_first > 0) e = launch(plan->d_first, plan->n_first);
+    if (e == cudaSuccess && plan->n_second > 0) e = launch(plan->d_second, plan->n_second);
+    const int step_blocks = (pool->desc.channels + Step<N>::kBlockCh - 1) / Step<N>::kBlockCh;
     if (e == cudaSuccess && plan->n_single > 0)
-        e = launch_overlapped(scan_step_kernel<N>, (unsigned)(plan->n_single * blocks_c), (unsigned)kScanThreads, 0, stream,
-                              plan->d_single, blocks_c, args);
+        e = launch_overlapped(scan_step_kernel<N>, (unsigned)(plan->n_single * step_blocks), (unsigned)Step<N>::kThreads, 0, stream,
+                              plan->d_single, step_blocks, args);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
 
-int scan_block_channels(int state_dim) {
-    return state_dim == 64 ? Scan<64>::kBlockCh : state_dim == 32 ? Scan<32>::kBlockCh : Scan<16>::kBlockCh;
-}
+int scan_warp_channels(int state_dim) { return state_dim <= 16 ? 32 : state_dim == 32 ? 16 : 8; }
 
 cudaError_t launch_scan(const ap_state_pool *pool, const ap_state_plan *plan, const ScanArgs &args, cudaStream_t stream) {
     switch (pool->desc.state_dim) {

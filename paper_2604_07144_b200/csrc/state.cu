@@ -11,17 +11,20 @@ using namespace ap;
 
 namespace {
 
-// The scan's cut along time.  A block walks its rows one after the other, so few long sequences leave SMs idle.  Cut into
+// The scan's cut along time.  A warp walks its rows one after the other, so few long sequences leave SMs idle.  Cut into
 // pieces, all but the first and the last are walked twice (once for the state behind them, once for their rows) and there
-// are two launches.  Blocks of unsplit sequences cover the GPU from one block an SM on.
+// are two launches.
+constexpr int kCutBelow = 4, kResident = 14, kLeastPiece = 64;
+
 struct Cut {
     int32_t piece;       // rows of a piece, 0: no sequence is cut
 };
 
 Cut choose_cut(int sms, int blocks_c, int64_t chunk_seqs, int64_t chunk_rows) {
-    if (chunk_seqs * blocks_c >= sms) return {0};
-    const int64_t want = 4 * (int64_t)sms;                                     // blocks that are resident together
-    const int64_t rows = std::max<int64_t>(64, chunk_rows * blocks_c / want);
+    const int64_t warps = chunk_seqs * blocks_c;
+    if (warps >= kCutBelow * (int64_t)sms) return {0};
+    // pieces for as many warps as are resident together (a launch leaves one piece of each sequence out)
+    const int64_t rows = std::max<int64_t>(kLeastPiece, chunk_rows * blocks_c / (kResident * (int64_t)sms + warps));
     return {(int32_t)std::min<int64_t>(1 << 30, (rows + kScanTile - 1) / kScanTile * kScanTile)};
 }
 
@@ -84,7 +87,7 @@ int plan_create(ap_state_plan **out, ap_state_pool *pool, const ap_state_batch *
     }
     if (n_new > (int64_t)1 << 30) return AP_ERR_UNSUPPORTED;
 
-    const int blocks_c = (d.channels + scan_block_channels(d.state_dim) - 1) / scan_block_channels(d.state_dim);
+    const int blocks_c = (d.channels + scan_warp_channels(d.state_dim) - 1) / scan_warp_channels(d.state_dim);
     const Cut cut = choose_cut(pool->sm_count, blocks_c, chunk_seqs, chunk_rows);
     std::vector<StateUnit> conv, first, second, single;
     int64_t row = 0, segments = 0, split_seqs = 0;
