@@ -2,10 +2,10 @@
 //
 //   out[t][c] = act(bias[c] + sum_j weight[c][j] x[t - W + 1 + j][c])
 //
-// HBM-bound: x is read and out written once.  A thread takes 8 channels (16 bytes of a row) of a unit of up to kConvRun
-// rows and slides the window over them in registers, so a row is loaded once per unit and W - 1 rows twice.  The thread
-// of a sequence's first unit reads the slot (the inputs before the first row) and then writes it (the last W - 1 inputs):
-// the same thread does both, so no block reads what another has overwritten.
+// HBM-bound: x is read and out written once.  A thread takes 4 channels (8 bytes of a row) of a unit, a run of
+// rows of a sequence, and slides the window over them in registers, in fp32, kAhead rows loaded at a time; a row is loaded once per unit
+// and W - 1 rows twice.  The thread of a sequence's first unit reads the slot (the inputs before the first row) and then
+// writes it (the last W - 1 inputs): the same thread does both, so no block reads what another has overwritten.
 #include "layers.h"
 #include "ptx.cuh"
 
@@ -15,114 +15,116 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kConvThreads = 128;
+constexpr int kAhead = 4;                                 // rows loaded together
 
-__device__ __forceinline__ void widen8(uint4 v, float (&f)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
+struct Four {                                             // four channels in fp32
+    float2 lo, hi;
+};
+__device__ __forceinline__ Four widen4(uint2 v) {
+    return {make_float2(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u)),
+            make_float2(__uint_as_float(v.y << 16), __uint_as_float(v.y & 0xFFFF0000u))};
+}
+// y / (1 + e^-y)
+__device__ __forceinline__ float2 silu2(float2 y) {
+    float2 e = __fmul2_rn(y, make_float2(-1.4426950408889634f, -1.4426950408889634f));
+    e = __fadd2_rn(make_float2(exp2_approx(e.x), exp2_approx(e.y)), make_float2(1.f, 1.f));
+    return __fmul2_rn(y, make_float2(rcp_approx(e.x), rcp_approx(e.y)));
 }
 
-template <int W>
-__global__ void __launch_bounds__(kConvThreads)
-conv_kernel(const StateUnit *__restrict__ units, int n_units, int groups, const uint16_t *x, const uint16_t *weight,
-            const uint16_t *bias, uint16_t *out, uint16_t *slots, int64_t xs, int64_t os, int silu) {
-    const int64_t at = (int64_t)blockIdx.x * kConvThreads + threadIdx.x;
-    const int u = (int)(at / groups);
-    const int64_t c0 = (at - (int64_t)u * groups) * 8;
-    const int64_t channels = (int64_t)groups * 8;
+template <int W, bool kSilu>
+__global__ void __launch_bounds__(kConvThreads, 7)
+conv_kernel(const StateUnit *__restrict__ units, int blocks_c, int64_t channels, const uint16_t *x, const uint16_t *weight,
+            const uint16_t *bias, uint16_t *out, uint16_t *slots, int64_t xs, int64_t os) {
+    const StateUnit unit = units[(int)blockIdx.x / blocks_c];
+    const int64_t c0 = ((int64_t)((int)blockIdx.x % blocks_c) * kConvThreads + threadIdx.x) * 4;
     griddep_launch_dependents();
-    if (u >= n_units) return;
-    const StateUnit unit = units[u];
+    if (c0 >= channels) return;
     griddep_wait();
-    float w[W][8];
-    {
-        uint32_t raw[4 * W];                              // 8 channels' W weights, next to one another
+    const uint16_t *xr = x + (int64_t)unit.row0 * xs + c0;
+    uint2 next[kAhead];
+    const uint16_t *ahead = xr;                           // the row to load next
+    auto load_rows = [&](int t0) {
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const uint4 v = load16(weight + c0 * W + 8 * i);
-            raw[4 * i] = v.x, raw[4 * i + 1] = v.y, raw[4 * i + 2] = v.z, raw[4 * i + 3] = v.w;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < W; ++j) {
-                const int k = i * W + j;
-                w[j][i] = __uint_as_float(k & 1 ? raw[k >> 1] & 0xFFFF0000u : raw[k >> 1] << 16);
-            }
-    }
-    float base[8] = {};
-    if (bias) widen8(load16(bias + c0), base);
-    const uint16_t *xc = x + c0;
-    uint4 seen[W - 1];                                    // the W - 1 inputs before the next row
+        for (int i = 0; i < kAhead; ++i, ahead += xs)
+            if (t0 + i < unit.rows) next[i] = load8(ahead);
+    };
+    load_rows(0);
+    uint2 before[W - 1];                                  // the W - 1 inputs before the first row
     if (unit.flags & kUnitFirst) {
         uint16_t *slot = slots + (int64_t)unit.slot * (W - 1) * channels + c0;
-#pragma unroll
-        for (int j = 0; j < W - 1; ++j)
-            seen[j] = (unit.flags & kUnitKept) ? load16(slot + j * channels) : make_uint4(0, 0, 0, 0);
-        const int64_t end = (int64_t)unit.row0 + unit.seq_rows;
+        uint2 last[W - 1];                                // the last W - 1 inputs of the sequence
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {
+            before[j] = last[j] = make_uint2(0, 0);
             const int back = W - 1 - j;                   // rows from the end
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (back <= unit.seq_rows) {
-                v = load16(xc + (end - back) * xs);
-            } else if (unit.flags & kUnitKept) {          // fewer new rows than the window: what was there moves up
-                v = load16(slot + (j + unit.seq_rows) * channels);          // (a place that is written after this one)
-            }
-            *(uint4 *)(slot + j * channels) = v;
+            if (unit.flags & kUnitKept) before[j] = load8(slot + j * channels);
+            if (back <= unit.seq_rows) last[j] = load8(xr + (int64_t)(unit.seq_rows - back) * xs);
+            else if (unit.flags & kUnitKept) last[j] = load8(slot + (j + unit.seq_rows) * channels);   // (fewer rows than the window)
         }
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) *(uint2 *)(slot + j * channels) = last[j];
     } else {
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j) seen[j] = load16(xc + ((int64_t)unit.row0 - (W - 1) + j) * xs);
+        for (int j = 0; j < W - 1; ++j) before[j] = load8(xr + (j - (W - 1)) * xs);
     }
-    const uint16_t *xr = xc + (int64_t)unit.row0 * xs;
-    uint16_t *o = out + (int64_t)unit.row0 * os + c0;
-    constexpr int kAhead = 4;                             // rows loaded together
-    for (int t0 = 0; t0 < unit.rows; t0 += kAhead) {
-        uint4 next[kAhead];
+    Four w[W], base = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    {
+        uint32_t raw[2 * W];                              // 4 channels' W weights, next to one another
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-            if (t0 + i < unit.rows) next[i] = load16(xr + (int64_t)(t0 + i) * xs);
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (t0 + i >= unit.rows) break;
-            float y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = base[e];
-#pragma unroll
-            for (int j = 0; j < W; ++j) {
-                float v[8];
-                widen8(j < W - 1 ? seen[j] : next[i], v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = fmaf(w[j][e], v[e], y[e]);
-            }
-            if (silu) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = __fdividef(y[e], 1.f + exp2_approx(-1.4426950408889634f * y[e]));
-            }
-            *(uint4 *)(o + (int64_t)(t0 + i) * os) = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]),
-                                                                 pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-#pragma unroll
-            for (int j = 0; j + 1 < W - 1; ++j) seen[j] = seen[j + 1];
-            seen[W - 2] = next[i];
+        for (int i = 0; i < W; ++i) {
+            const uint2 v = load8(weight + c0 * W + 4 * i);
+            raw[2 * i] = v.x, raw[2 * i + 1] = v.y;
         }
+        auto number = [&](int c, int j) {
+            const int k = c * W + j;
+            return __uint_as_float(k & 1 ? raw[k >> 1] & 0xFFFF0000u : raw[k >> 1] << 16);
+        };
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[j] = {make_float2(number(0, j), number(1, j)), make_float2(number(2, j), number(3, j))};
+        if (bias) base = widen4(load8(bias + c0));
     }
+    Four seen[W - 1];
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) seen[j] = widen4(before[j]);
+    uint16_t *o = out + (int64_t)unit.row0 * os + c0;
+    auto row = [&](uint2 in) {
+        const Four v = widen4(in);
+        Four y = base;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const Four &u = j < W - 1 ? seen[j] : v;
+            y.lo = __ffma2_rn(w[j].lo, u.lo, y.lo);
+            y.hi = __ffma2_rn(w[j].hi, u.hi, y.hi);
+        }
+        if (kSilu) y.lo = silu2(y.lo), y.hi = silu2(y.hi);
+        *(uint2 *)o = make_uint2(pack_bf16x2(y.lo.x, y.lo.y), pack_bf16x2(y.hi.x, y.hi.y));
+        o += os;
+#pragma unroll
+        for (int j = 0; j + 1 < W - 1; ++j) seen[j] = seen[j + 1];
+        seen[W - 2] = v;
+    };
+    int t0 = 0;
+    for (; t0 + kAhead <= unit.rows; t0 += kAhead) {       // (whole groups: no test between rows, and the window moves for nothing)
+        uint2 now[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) now[i] = next[i];
+        load_rows(t0 + kAhead);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) row(now[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (t0 + i < unit.rows) row(next[i]);
 }
 
 template <int W>
 cudaError_t launch_conv_t(const ap_state_pool *pool, const ap_state_plan *plan, const ap_conv_desc &conv, const void *x,
                           const void *weight, const void *bias, void *out, cudaStream_t stream) {
-    const int groups = pool->desc.channels / 8;
-    const int64_t threads = (int64_t)plan->n_conv * groups;
-    const cudaError_t e = launch_overlapped(conv_kernel<W>, (unsigned)((threads + kConvThreads - 1) / kConvThreads),
-                                            (unsigned)kConvThreads, 0, stream, plan->d_conv, plan->n_conv, groups,
-                                            (const uint16_t *)x, (const uint16_t *)weight, (const uint16_t *)bias,
-                                            (uint16_t *)out, (uint16_t *)pool->desc.conv_base, conv.x_row_stride,
-                                            conv.out_row_stride, conv.silu);
+    const int blocks_c = (pool->desc.channels / 4 + kConvThreads - 1) / kConvThreads;
+    const cudaError_t e = launch_overlapped(conv.silu ? conv_kernel<W, true> : conv_kernel<W, false>, (unsigned)(plan->n_conv * blocks_c),
+                                            (unsigned)kConvThreads, 0, stream, plan->d_conv, blocks_c, (int64_t)pool->desc.channels,
+                                            (const uint16_t *)x, (const uint16_t *)weight, (const uint16_t *)bias, (uint16_t *)out,
+                                            (uint16_t *)pool->desc.conv_base, conv.x_row_stride, conv.out_row_stride);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

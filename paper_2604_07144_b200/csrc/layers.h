@@ -70,7 +70,7 @@ struct ap_state_plan {
     ap::PlanBuffer buf{};
     ap_state_info info{};
     size_t workspace_bytes = 0;
-    int n_conv = 0;               // units of the convolution: runs of at most kConvRun rows
+    int n_conv = 0;               // units of the convolution: runs of rows
     int n_first = 0, n_second = 0;   // units of the scan's first launch, of its second
     int n_single = 0;             // sequences with one row
     const ap::StateUnit *d_conv = nullptr, *d_first = nullptr, *d_second = nullptr, *d_single = nullptr;
@@ -78,7 +78,7 @@ struct ap_state_plan {
 
 namespace ap {
 
-constexpr int kConvRun = 16;      // rows that a thread of the convolution walks
+constexpr int kConvThreads = 128; // each takes 4 channels
 constexpr int kScanTile = 32;     // pieces of a sequence are multiples of it, as it is of the rows that the scan stages at a time
 
 struct ScanArgs {                 // by value to the kernels

@@ -23,6 +23,8 @@ namespace {
 
 using namespace ptx;
 
+constexpr int kStepBlocks = 6, kStepRows = 2;                  // blocks of an SM before a block takes a second sequence; most of them
+
 // Single tokens: a quad of lanes takes kCh channels, each lane N / 4 states of every one of them.
 template <int N>
 struct Step {
@@ -37,7 +39,6 @@ struct Step {
 // Prompts: a lane has H states of one channel.
 constexpr int kTile = 16;                                      // rows staged at a time
 constexpr int kGroup = 8;                                      // rows walked in one piece of code
-constexpr int kWalkBlocks = 7;                               // of an SM
 template <int N, int H>
 struct Walk {
     static constexpr int kLanes = N / H;                       // lanes of a channel
@@ -98,50 +99,15 @@ __device__ __forceinline__ float min_nan(float a, float b) {
     return d;
 }
 
-__device__ __forceinline__ float reciprocal(float x) {         // to one step of fp32; 0 for infinity
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 __device__ __forceinline__ float2 as_floats(uint2 v) { return make_float2(__uint_as_float(v.x), __uint_as_float(v.y)); }
 
 __device__ __forceinline__ float2 gate2(float2 y, float2 z) {
     float2 e = __fmul2_rn(z, make_float2(-1.4426950408889634f, -1.4426950408889634f));
     e = __fadd2_rn(make_float2(exp2_approx(e.x), exp2_approx(e.y)), make_float2(1.f, 1.f));
-    return __fmul2_rn(y, __fmul2_rn(z, make_float2(reciprocal(e.x), reciprocal(e.y))));
+    return __fmul2_rn(y, __fmul2_rn(z, make_float2(rcp_approx(e.x), rcp_approx(e.y))));
 }
 
-__device__ __forceinline__ float gate(float y, float z) { return y * (z * reciprocal(1.f + exp2_approx(-1.4426950408889634f * z))); }
-
-// kHeld consecutive-by-vector fp32 values of a lane: states 4 kVec i + kVec q + e
-template <int N>
-__device__ __forceinline__ void load_states(const float *row, int q, float (&h)[Step<N>::kHeld]) {
-    using S = Step<N>;
-#pragma unroll
-    for (int i = 0; i < S::kVecs; ++i) {
-        const float *p = row + 4 * S::kVec * i + S::kVec * q;
-        if constexpr (S::kVec == 4) {
-            const uint4 v = load16(p);
-            h[4 * i] = __uint_as_float(v.x), h[4 * i + 1] = __uint_as_float(v.y);
-            h[4 * i + 2] = __uint_as_float(v.z), h[4 * i + 3] = __uint_as_float(v.w);
-        } else {
-            const uint2 v = load8(p);
-            h[0] = __uint_as_float(v.x), h[1] = __uint_as_float(v.y);
-        }
-    }
-}
-
-template <int N>
-__device__ __forceinline__ void store_states(float *row, int q, const float (&h)[Step<N>::kHeld]) {
-    using S = Step<N>;
-#pragma unroll
-    for (int i = 0; i < S::kVecs; ++i) {
-        float *p = row + 4 * S::kVec * i + S::kVec * q;
-        if constexpr (S::kVec == 4) *(float4 *)p = make_float4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
-        else *(float2 *)p = make_float2(h[0], h[1]);
-    }
-}
+__device__ __forceinline__ float gate(float y, float z) { return y * (z * rcp_approx(1.f + exp2_approx(-1.4426950408889634f * z))); }
 
 // Sums a quad's partial sums: lane q ends with the sum of channel q * kCh / 4.
 template <int kCh>
@@ -441,63 +407,108 @@ scan_kernel(const StateUnit *__restrict__ units, int64_t n_warps, int blocks_c, 
     else walk_unit<N, H, false>(unit, c0, g, sm);
 }
 
-// Sequences with one new token: everything in registers, lane q of a quad works out channel q * kCh / 4's step and result.
+// Sequences with one new token: everything in registers.  Quad Q of a warp has channels Q, Q + 8, ... (so that a load of all
+// its lanes is one run of memory); lane q works out the step and the result of the quad's channel q * kCh / 4.
+// A block takes `rows` sequences for its channels, whose a it loads once.
 template <int N>
-__global__ void __launch_bounds__(Step<N>::kThreads)
-scan_step_kernel(const StateUnit *__restrict__ units, int blocks_c, const ScanArgs g) {
+__global__ void __launch_bounds__(Step<N>::kThreads, 8)
+scan_step_kernel(const StateUnit *__restrict__ units, int n_units, int rows, int blocks_c, const ScanArgs g) {
     using S = Step<N>;
-    const int u = (int)blockIdx.x / blocks_c, cb = (int)blockIdx.x % blocks_c;
+    const int u0 = (int)blockIdx.x / blocks_c * rows, cb = (int)blockIdx.x % blocks_c, u1 = min(u0 + rows, n_units);
     const int lane = threadIdx.x & 31, q = lane & 3;
-    const StateUnit unit = units[u];
-    const int64_t D = g.channels, row = unit.row0;
-    const int64_t wc = (int64_t)cb * S::kBlockCh + (threadIdx.x >> 5) * 8 * S::kCh + (lane >> 2) * S::kCh;
-    griddep_launch_dependents();
-    griddep_wait();
-    float *state = g.state + ((int64_t)unit.slot * D + wc) * N;
-    float h[S::kCh][S::kHeld] = {};
-    if (unit.flags & kUnitKept) {
-#pragma unroll
-        for (int c = 0; c < S::kCh; ++c)
-            if (wc + c < D) load_states<N>(state + c * N, q, h[c]);
-    }
-    const int64_t own = wc + q * S::kCh / 4;               // this lane's channel
+    const int64_t D = g.channels;
+    const int64_t wc = (int64_t)cb * S::kBlockCh + (threadIdx.x >> 5) * 8 * S::kCh + (lane >> 2);    // the quad's first
+    const int64_t own = wc + q * S::kCh / 4 * 8;           // this lane's channel
     const bool in = own < D;
-    auto number = [&](const uint16_t *p, int64_t at) { return __uint_as_float((uint32_t)*(const volatile uint16_t *)(p + at) << 16); };
-    const float x = in ? number(g.x, row * g.xs + own) : 0.f;
-    float d = in ? number(g.dt, row * g.dts + own) : 0.f;
-    if (in && g.dt_bias) d += __uint_as_float(load4(g.dt_bias + own));
-    if (g.softplus) d = softplus(d);
-    float b[S::kHeld], cc[S::kHeld];
+    const int64_t left = D - (wc - (lane >> 2));           // channels come in eights: the warp's c-th eight is there if 8 c < left
+    griddep_launch_dependents();
+    if (left <= 0) return;
+    griddep_wait();
+    auto load_held = [&](const float *p, float2 (&to)[S::kHeld / 2]) {        // this lane's states of a channel
 #pragma unroll
-    for (int i = 0; i < S::kVecs; ++i)
-#pragma unroll
-        for (int e = 0; e < S::kVec; e += 2) {
-            const int n = 4 * S::kVec * i + S::kVec * q + e;
-            const float2 bv = widen2(load4(g.b + row * g.bs + n)), cv = widen2(load4(g.c + row * g.cs + n));
-            b[i * S::kVec + e] = bv.x, b[i * S::kVec + e + 1] = bv.y;
-            cc[i * S::kVec + e] = cv.x, cc[i * S::kVec + e + 1] = cv.y;
+        for (int i = 0; i < S::kVecs; ++i) {
+            if constexpr (S::kVec == 4) {
+                const uint4 v = load16(p + 16 * i);
+                to[2 * i] = as_floats(make_uint2(v.x, v.y)), to[2 * i + 1] = as_floats(make_uint2(v.z, v.w));
+            } else {
+                to[0] = as_floats(load8(p));
+            }
         }
-    float y[S::kCh];
+    };
+    constexpr int P = S::kHeld / 2;
+    float2 a2[S::kCh][P];
 #pragma unroll
     for (int c = 0; c < S::kCh; ++c) {
-        const int from = (lane & ~3) | (c * (4 / S::kCh));
-        const float dc = __shfl_sync(0xffffffffu, d, from), dxc = dc * __shfl_sync(0xffffffffu, x, from);
-        y[c] = 0.f;
-        if (wc + c >= D) continue;
-        float a[S::kHeld];
-        load_states<N>(g.a + (wc + c) * N, q, a);
 #pragma unroll
-        for (int i = 0; i < S::kHeld; ++i) {
-            h[c][i] = fmaf(exp2_approx(dc * (1.4426950408889634f * a[i])), h[c][i], dxc * b[i]);
-            y[c] = fmaf(cc[i], h[c][i], y[c]);
-        }
-        store_states<N>(state + c * N, q, h[c]);
+        for (int i = 0; i < P; ++i) a2[c][i] = make_float2(0.f, 0.f);
+        if (8 * c < left) load_held(g.a + (wc + 8 * c) * N + q * S::kVec, a2[c]);
     }
-    float sum = quad_sum<S::kCh>(y, q);
-    if (in && (S::kCh == 4 || q % (4 / S::kCh) == 0)) {
-        if (g.d_skip) sum = fmaf(__uint_as_float(load4(g.d_skip + own)), x, sum);
-        if (g.z) sum = gate(sum, number(g.z, row * g.zs + own));
-        *(__nv_bfloat16 *)(g.out + row * g.os + own) = __float2bfloat16_rn(sum);
+    const float bias = in && g.dt_bias ? __uint_as_float(load4(g.dt_bias + own)) : 0.f;
+    const float skip = in && g.d_skip ? __uint_as_float(load4(g.d_skip + own)) : 0.f;
+    auto number = [](uint16_t v) { return __uint_as_float((uint32_t)v << 16); };
+#pragma unroll 1
+    for (int u = u0; u < u1; ++u) {
+        const int64_t row = units[u].row0;
+        float *state = g.state + ((int64_t)units[u].slot * D + wc) * N + q * S::kVec;
+        const bool kept = units[u].flags & kUnitKept;
+        float2 h[S::kCh][P];
+#pragma unroll
+        for (int c = 0; c < S::kCh; ++c) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) h[c][i] = make_float2(0.f, 0.f);
+            if (kept && 8 * c < left) load_held(state + 8 * c * N, h[c]);
+        }
+        float x = 0.f, d = 0.f, z = 0.f;
+        if (in) {
+            x = number(load2(g.x + row * g.xs + own));
+            d = number(load2(g.dt + row * g.dts + own));
+            if (g.z) z = number(load2(g.z + row * g.zs + own));
+        }
+        float2 b[P], cc[P];
+#pragma unroll
+        for (int i = 0; i < S::kVecs; ++i) {
+            const uint16_t *bp = g.b + row * g.bs + 4 * S::kVec * i + S::kVec * q, *cp = g.c + row * g.cs + 4 * S::kVec * i + S::kVec * q;
+            if constexpr (S::kVec == 4) {
+                const uint2 bv = load8(bp), cv = load8(cp);
+                b[2 * i] = widen2(bv.x), b[2 * i + 1] = widen2(bv.y), cc[2 * i] = widen2(cv.x), cc[2 * i + 1] = widen2(cv.y);
+            } else {
+                b[0] = widen2(load4(bp)), cc[0] = widen2(load4(cp));
+            }
+        }
+        d += bias;
+        if (g.softplus) d = softplus(d);
+        const float dx = d * x;
+        d *= 1.4426950408889634f;
+        float y[S::kCh];
+#pragma unroll
+        for (int c = 0; c < S::kCh; ++c) {
+            const int from = (lane & ~3) | (c * (4 / S::kCh));
+            const float dc = __shfl_sync(0xffffffffu, d, from), dxc = __shfl_sync(0xffffffffu, dx, from);
+            const float2 d2 = make_float2(dc, dc), dx2 = make_float2(dxc, dxc);
+            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                float2 e = __fmul2_rn(d2, a2[c][i]);
+                e.x = exp2_approx(e.x), e.y = exp2_approx(e.y);
+                h[c][i] = __ffma2_rn(e, h[c][i], __fmul2_rn(dx2, b[i]));
+                sum = __ffma2_rn(h[c][i], cc[i], sum);
+            }
+            y[c] = sum.x + sum.y;
+            if (8 * c < left) {
+#pragma unroll
+                for (int i = 0; i < S::kVecs; ++i) {
+                    float *p = state + 8 * c * N + 16 * i;
+                    if constexpr (S::kVec == 4) *(float4 *)p = make_float4(h[c][2 * i].x, h[c][2 * i].y, h[c][2 * i + 1].x, h[c][2 * i + 1].y);
+                    else *(float2 *)p = h[c][0];
+                }
+            }
+        }
+        float sum = quad_sum<S::kCh>(y, q);
+        if (in && (S::kCh == 4 || q % (4 / S::kCh) == 0)) {
+            sum = fmaf(skip, x, sum);
+            if (g.z) sum = gate(sum, z);
+            *(__nv_bfloat16 *)(g.out + row * g.os + own) = __float2bfloat16_rn(sum);
+        }
     }
 }
 
@@ -518,10 +529,14 @@ cudaError_t launch_scan_t(const ap_state_pool *pool, const ap_state_plan *plan, 
     cudaError_t e = cudaSuccess;
     if (plan->n_first > 0) e = launch(plan->d_first, plan->n_first);
     if (e == cudaSuccess && plan->n_second > 0) e = launch(plan->d_second, plan->n_second);
-    const int step_blocks = (pool->desc.channels + Step<N>::kBlockCh - 1) / Step<N>::kBlockCh;
-    if (e == cudaSuccess && plan->n_single > 0)
-        e = launch_overlapped(scan_step_kernel<N>, (unsigned)(plan->n_single * step_blocks), (unsigned)Step<N>::kThreads, 0, stream,
-                              plan->d_single, step_blocks, args);
+    if (e == cudaSuccess && plan->n_single > 0) {
+        // a's share of what is read falls with the sequences of a block; blocks enough for the GPU come first
+        const int blocks_c = (pool->desc.channels + Step<N>::kBlockCh - 1) / Step<N>::kBlockCh;
+        const int64_t spare = (int64_t)plan->n_single * blocks_c / ((int64_t)kStepBlocks * pool->sm_count);
+        const int rows = spare < 2 ? 1 : spare > kStepRows ? kStepRows : (int)spare;
+        e = launch_overlapped(scan_step_kernel<N>, (unsigned)((plan->n_single + rows - 1) / rows * blocks_c), (unsigned)Step<N>::kThreads, 0,
+                              stream, plan->d_single, plan->n_single, rows, blocks_c, args);
+    }
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

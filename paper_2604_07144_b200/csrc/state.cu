@@ -14,6 +14,7 @@ namespace {
 // The scan's cut along time.  A warp walks its rows one after the other, so few long sequences leave SMs idle.  Cut into
 // pieces, all but the first and the last are walked twice (once for the state behind them, once for their rows) and there
 // are two launches.
+constexpr int kConvBlocks = 14;
 constexpr int kCutBelow = 4, kResident = 14, kLeastPiece = 64;
 
 struct Cut {
@@ -26,6 +27,14 @@ Cut choose_cut(int sms, int blocks_c, int64_t chunk_seqs, int64_t chunk_rows) {
     // pieces for as many warps as are resident together (a launch leaves one piece of each sequence out)
     const int64_t rows = std::max<int64_t>(kLeastPiece, chunk_rows * blocks_c / (kResident * (int64_t)sms + warps));
     return {(int32_t)std::min<int64_t>(1 << 30, (rows + kScanTile - 1) / kScanTile * kScanTile)};
+}
+
+// Rows of a unit of the convolution.  A thread's start (weights, the rows before) costs as much as several rows; short runs
+// make blocks enough for few rows.
+int32_t conv_run(int sms, int blocks_c, int64_t rows) {
+    int32_t run = 32;
+    while (run > 4 && rows * blocks_c < (int64_t)kConvBlocks * sms * run) run /= 2;
+    return run;
 }
 
 bool same_shape(const ap_state_desc &a, const ap_state_desc &b) {
@@ -89,6 +98,8 @@ int plan_create(ap_state_plan **out, ap_state_pool *pool, const ap_state_batch *
 
     const int blocks_c = (d.channels + scan_warp_channels(d.state_dim) - 1) / scan_warp_channels(d.state_dim);
     const Cut cut = choose_cut(pool->sm_count, blocks_c, chunk_seqs, chunk_rows);
+    const int conv_blocks_c = (d.channels / 4 + kConvThreads - 1) / kConvThreads;
+    const int32_t run = conv_run(pool->sm_count, conv_blocks_c, n_new);
     std::vector<StateUnit> conv, first, second, single;
     int64_t row = 0, segments = 0, split_seqs = 0;
     for (int s = 0; s < b->batch; ++s) {
@@ -99,7 +110,7 @@ int plan_create(ap_state_plan **out, ap_state_pool *pool, const ap_state_batch *
             return StateUnit{(int32_t)(row + t0), rows, b->slots[s], flags | kept | (t0 == 0 ? kUnitFirst : 0) | (t0 + rows == ql ? kUnitLast : 0),
                              0, 0, ql, 0};
         };
-        for (int32_t t0 = 0; t0 < ql; t0 += std::min(kConvRun, ql - t0)) conv.push_back(unit(t0, std::min(kConvRun, ql - t0), 0));
+        for (int32_t t0 = 0; t0 < ql; t0 += std::min(run, ql - t0)) conv.push_back(unit(t0, std::min(run, ql - t0), 0));
         if (ql == 1) {
             single.push_back(unit(0, 1, 0));
         } else if (cut.piece == 0 || ql < 2 * cut.piece) {
@@ -127,7 +138,7 @@ int plan_create(ap_state_plan **out, ap_state_pool *pool, const ap_state_batch *
     std::stable_sort(first.begin(), first.end(), longer);
     std::stable_sort(second.begin(), second.end(), longer);
     const int64_t most = (int64_t)std::max({first.size(), second.size(), single.size()}) * blocks_c;
-    if (most >= (int64_t)1 << 31 || (int64_t)conv.size() * (d.channels / 8) / 64 >= (int64_t)1 << 31) return AP_ERR_UNSUPPORTED;
+    if (most >= (int64_t)1 << 31 || (int64_t)conv.size() * conv_blocks_c >= (int64_t)1 << 31) return AP_ERR_UNSUPPORTED;
 
     ap_state_plan *plan = new (std::nothrow) ap_state_plan();
     if (!plan) return AP_ERR_CUDA;
