@@ -39,11 +39,13 @@ struct PromptTile {
 };
 static_assert(sizeof(PromptTile) == 32, "PromptTile layout");
 
-// One unit of the kernel for short prompts: all rows of a prompt, one kv head.
+// One unit of the kernel for short prompts (and one kv head): blocks of 16 rows of a prompt.
 struct ShortPrompt {
-    int32_t start;
-    int32_t rows;        // 1..64
+    int32_t start;       // first row of the prompt
+    int32_t rows;        // rows of the prompt
+    int32_t block0, block1;
 };
+static_assert(sizeof(ShortPrompt) == 16, "ShortPrompt layout");
 
 }  // namespace ap
 

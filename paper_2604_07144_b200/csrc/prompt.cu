@@ -331,17 +331,23 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
 
 // ---------------------------------------------------------- short prompts --
 //
-// A block is a prompt's rows and one kv head: K and V in shared memory once, then each warp takes 16 rows of a q head at
-// a time (mma.sync m16n8k16: a 128-row tile of the tensor cores would be empty for the most part, and a unit's prologue
-// and epilogue cost 5 us).  All scores of a row are in registers, so the softmax takes one pass.
+// A block takes some blocks of 16 rows of a prompt for one kv head, as many as make kShortWarps items of (16 rows, q head), and
+// each warp an item at a time (mma.sync m16n8k16: a 128-row tile of the tensor cores would be empty for the most part, and a
+// unit's prologue and epilogue cost 5 us).  K and V up to the last of the rows stand in shared memory, with each warp's
+// first Q all in flight together.  All scores of a row are in registers, so the softmax takes one pass.
 constexpr int kShortWarps = 4;
 
 template <int D>
 struct ShortSmem {
     static constexpr int kStride = D * 2 + 16;                        // bytes of a row: 8 rows of an ldmatrix in 8 bank groups
-    uint8_t k[kShortRows * kStride], v[kShortRows * kStride];
-    uint8_t q[kShortWarps][16 * kStride];                             // a warp's rows; then its results on their way out
+    alignas(16) uint8_t q[kShortWarps][16 * kStride];                 // a warp's rows; then its results on their way out
+    alignas(16) uint8_t k[kShortRows * kStride], v[kShortRows * kStride];
 };
+
+// 16 bytes global -> shared, asynchronous; zeros (and `from` is not read) where `there` is false
+__device__ __forceinline__ void copy16_or_zero(void *to, const void *from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
 
 template <int D>
 __global__ void __launch_bounds__(32 * kShortWarps)
@@ -353,35 +359,41 @@ prompt_short_kernel(const ShortPrompt *__restrict__ prompts, const uint16_t *q, 
     const ShortPrompt p = prompts[blockIdx.x / Hkv];
     const int kv_head = (int)blockIdx.x % Hkv, G = Hq / Hkv;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int blocks = (p.rows + 15) / 16;                            // blocks of 16 rows
+    const int keys = p.block1 * 16;                                   // rows of K and V that the block's rows see
     griddep_launch_dependents();
     griddep_wait();
-    for (int i = threadIdx.x; i < blocks * 16 * kChunks; i += 32 * kShortWarps) {
-        const int row = i / kChunks, ch = i % kChunks;
-        uint4 a = make_uint4(0, 0, 0, 0), b = a;                      // (rows past the prompt: zeros, whatever the next one holds)
-        if (row < p.rows) {
-            a = load16(k + (p.start + (int64_t)row) * ks + kv_head * D + ch * 8);
-            b = load16(v + (p.start + (int64_t)row) * vs + kv_head * D + ch * 8);
-        }
-        *(uint4 *)(sm.k + row * kStride + ch * 16) = a;
-        *(uint4 *)(sm.v + row * kStride + ch * 16) = b;
-    }
-    __syncthreads();
     uint8_t *mine = sm.q[warp];
+    auto load_q = [&](int item) {
+        const int row0 = (p.block1 - 1 - item / G) * 16, head = kv_head * G + item % G;
+        for (int i = lane; i < 16 * kChunks; i += 32) {
+            const int row = i / kChunks, ch = i % kChunks;
+            const bool there = row0 + row < p.rows;
+            copy16_or_zero(mine + row * kStride + ch * 16, q + (p.start + (int64_t)(there ? row0 + row : 0)) * qs + head * D + ch * 8, there);
+        }
+    };
+    const int items = (p.block1 - p.block0) * G;
+    if (warp < items) load_q(warp);
+    for (int i = threadIdx.x; i < keys * kChunks; i += 32 * kShortWarps) {
+        const int row = i / kChunks, ch = i % kChunks;
+        const bool there = row < p.rows;                              // (rows past the prompt: zeros, whatever the next one holds)
+        const int64_t at = p.start + (int64_t)(there ? row : 0);
+        copy16_or_zero(sm.k + row * kStride + ch * 16, k + at * ks + kv_head * D + ch * 8, there);
+        copy16_or_zero(sm.v + row * kStride + ch * 16, v + at * vs + kv_head * D + ch * 8, there);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
     const uint32_t q_addr = smem_u32(mine) + (lane & 15) * kStride + (lane >> 4) * 16;
     const uint32_t k_addr = smem_u32(sm.k) + ((lane & 7) + (lane >> 4) * 8) * kStride + ((lane >> 3) & 1) * 16;
     const uint32_t v_addr = smem_u32(sm.v) + (lane & 15) * kStride + (lane >> 4) * 16;
-    for (int item = warp; item < blocks * G; item += kShortWarps) {
+    for (int item = warp; item < items; item += kShortWarps) {
         // (the later blocks, with more keys, first)
-        const int rb = blocks - 1 - item / G, head = kv_head * G + item % G;
+        const int rb = p.block1 - 1 - item / G, head = kv_head * G + item % G;
         const int row0 = rb * 16;
-        for (int i = lane; i < 16 * kChunks; i += 32) {
-            const int row = i / kChunks, ch = i % kChunks;
-            uint4 a = make_uint4(0, 0, 0, 0);
-            if (row0 + row < p.rows) a = load16(q + (p.start + (int64_t)(row0 + row)) * qs + head * D + ch * 8);
-            *(uint4 *)(mine + row * kStride + ch * 16) = a;
+        if (item != warp) {
+            load_q(item);
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            __syncwarp();
         }
-        __syncwarp();
         uint32_t qf[D / 16][4];
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) ldmatrix_x4(qf[c], q_addr + c * 32);
@@ -508,6 +520,7 @@ int plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *b,
     if (Hq % Hkv != 0) return AP_ERR_INVALID_ARG;
     const int G = Hq / Hkv;
     if (G > 8) return AP_ERR_UNSUPPORTED;
+    const int short_blocks = std::max(1, kShortWarps / G);                    // blocks of 16 rows of a unit
     int64_t rows = 0, pairs = 0, tiles_n = 0, shorts_n = 0;
     for (int s = 0; s < b->batch; ++s) {
         const int32_t n = b->lens[s];
@@ -515,7 +528,7 @@ int plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *b,
         rows += n;
         pairs += (int64_t)n * ((int64_t)n + 1) / 2;
         if (n > kShortRows) tiles_n += ((int64_t)n + kTileM - 1) / kTileM * Hkv * ((G + 1) / 2);
-        else if (n > 0) ++shorts_n;
+        else if (n > 0) shorts_n += ((n + 15) / 16 + short_blocks - 1) / short_blocks;
     }
     // (row numbers of a last tile's keys, past the end of the batch, stay within 32 bits)
     if (rows > (int64_t)1 << 30 || tiles_n > (int64_t)1 << 27 || shorts_n * Hkv >= (int64_t)1 << 31) return AP_ERR_UNSUPPORTED;
@@ -532,7 +545,8 @@ int plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *b,
                     for (int g = 0; g < G; g += 2)
                         tiles.push_back({start + t0, std::min(kTileM, n - t0), start, kv * G + g, g + 1 < G ? kv * G + g + 1 : -1, kv, {0, 0}});
         } else if (n > 0) {
-            shorts.push_back({start, n});
+            const int blocks = (n + 15) / 16;
+            for (int b1 = blocks; b1 > 0; b1 -= short_blocks) shorts.push_back({start, n, std::max(0, b1 - short_blocks), b1});
         }
         start += n;
     }
@@ -540,7 +554,7 @@ int plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *b,
     std::stable_sort(tiles.begin(), tiles.end(), [](const PromptTile &x, const PromptTile &y) {
         return (x.row0 - x.start + x.rows + kTileN - 1) / kTileN > (y.row0 - y.start + y.rows + kTileN - 1) / kTileN;
     });
-    std::stable_sort(shorts.begin(), shorts.end(), [](const ShortPrompt &x, const ShortPrompt &y) { return x.rows > y.rows; });
+    std::stable_sort(shorts.begin(), shorts.end(), [](const ShortPrompt &x, const ShortPrompt &y) { return x.block1 > y.block1; });
 
     ap_prompt_plan *plan = new (std::nothrow) ap_prompt_plan();
     if (!plan) return AP_ERR_CUDA;
