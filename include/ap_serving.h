@@ -599,11 +599,14 @@ size_t ap_state_plan_workspace_bytes(const ap_state_plan *plan);
  * aligned.  out overlaps no input and no slot (INVALID_ARG).
  */
 typedef struct ap_conv_desc {
-    int32_t silu;
+    int32_t silu; /* 0 or 1 */
     int64_t x_row_stride, out_row_stride;
+    const void *x;
+    const void *weight;
+    const void *bias; /* or NULL */
+    void *out;
 } ap_conv_desc;
-int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_conv_desc *conv, const void *x,
-                      const void *weight, const void *bias, void *out, void *stream);
+int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_conv_desc *conv, void *stream);
 
 /*
  * Selective state space scan, channel by channel (n < state_dim):
@@ -615,20 +618,29 @@ int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_c
  * is rounded once.
  * x, dt, z: [n_new][channels] bf16; b, c: [n_new][state_dim] bf16; each with rows
  * *_row_stride elements apart (0: contiguous; a multiple of 8), so that they may be
- * cut out of projections' outputs.  a: [channels][state_dim] fp32; d_skip, dt_bias:
- * [channels] fp32 or NULL; z may be NULL.  out: [n_new][channels] bf16, rows
- * out_row_stride elements apart.  Device, 16-byte aligned.  out overlaps no input
- * and no slot (INVALID_ARG).  workspace: device, 256-byte aligned, at least
- * ap_state_plan_workspace_bytes() (else WORKSPACE_TOO_SMALL), contents undefined
- * before and after; calls that may overlap on the GPU take one each.
+ * cut out of projections' outputs.  a: [channels][state_dim] fp32, finite (beyond
+ * 2e38 in magnitude as 2e38); d_skip, dt_bias: [channels] fp32 or NULL; z may be
+ * NULL.  out: [n_new][channels] bf16, rows out_row_stride elements apart.  Device,
+ * 16-byte aligned.  out overlaps no input and no slot (INVALID_ARG).  workspace:
+ * device, 256-byte aligned, at least ap_state_plan_workspace_bytes() (else
+ * WORKSPACE_TOO_SMALL), contents undefined before and after; calls that may
+ * overlap on the GPU take one each.
  */
 typedef struct ap_scan_desc {
-    int32_t softplus;
+    int32_t softplus; /* 0 or 1 */
     int64_t x_row_stride, dt_row_stride, b_row_stride, c_row_stride, z_row_stride, out_row_stride;
+    const void *x;
+    const void *dt;
+    const void *b;
+    const void *c;
+    const void *z; /* or NULL */
+    void *out;
+    const float *a;
+    const float *d_skip;  /* or NULL */
+    const float *dt_bias; /* or NULL */
 } ap_scan_desc;
-int ap_scan_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_scan_desc *scan, const void *x,
-                      const void *dt, const float *a, const void *b, const void *c, const void *z, const float *d_skip,
-                      const float *dt_bias, void *out, void *workspace, size_t workspace_bytes, void *stream);
+int ap_scan_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_scan_desc *scan, void *workspace,
+                      size_t workspace_bytes, void *stream);
 
 /* ----------------------------------------------------------- diagnostics -- */
 

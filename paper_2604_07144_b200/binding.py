@@ -113,14 +113,16 @@ class StateInfo(ctypes.Structure):
 
 
 class ConvDesc(ctypes.Structure):
-    _fields_ = [("silu", ctypes.c_int32), ("x_row_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64)]
+    _fields_ = [("silu", ctypes.c_int32), ("x_row_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64)] + [
+        (n, ctypes.c_void_p) for n in ("x", "weight", "bias", "out")]
 
 
 class ScanDesc(ctypes.Structure):
-    _fields_ = [("softplus", ctypes.c_int32)] + [(n + "_row_stride", ctypes.c_int64) for n in ("x", "dt", "b", "c", "z", "out")]
+    _fields_ = [("softplus", ctypes.c_int32)] + [(n + "_row_stride", ctypes.c_int64) for n in ("x", "dt", "b", "c", "z", "out")] + [
+        (n, ctypes.c_void_p) for n in ("x", "dt", "b", "c", "z", "out", "a", "d_skip", "dt_bias")]
 
 
-_PROMPT_STRIDES, _CONV_DESC, _SCAN_DESC = struct.Struct("@qqq"), struct.Struct("@i4xqq"), struct.Struct("@i4xqqqqqq")
+_PROMPT_STRIDES, _CONV_DESC, _SCAN_DESC = struct.Struct("@qqq"), struct.Struct("@i4xqqPPPP"), struct.Struct("@i4xqqqqqqPPPPPPPPP")
 
 #: RopeDesc in one piece: a ctypes structure takes three times as long to fill, a twentieth of a rotated append's call
 _ROPE_DESC = struct.Struct("@iidPf4xqqq")
@@ -225,8 +227,8 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "ap_state_plan_destroy": (ctypes.c_int, [vp]),
         "ap_state_plan_get_info": (ctypes.c_int, [vp, ctypes.POINTER(StateInfo)]),
         "ap_state_plan_workspace_bytes": (sz, [vp]),
-        "ap_conv_iteration": (ctypes.c_int, [vp] * 8),
-        "ap_scan_iteration": (ctypes.c_int, [vp] * 13 + [sz, vp]),
+        "ap_conv_iteration": (ctypes.c_int, [vp] * 4),
+        "ap_scan_iteration": (ctypes.c_int, [vp] * 4 + [sz, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -719,15 +721,17 @@ class StatePool:
         self._keepalive = keepalive
         self.num_slots, self.channels, self.device = int(desc.num_slots), int(desc.channels), int(desc.device)
         self.state_dim, self.conv_width = int(desc.state_dim), int(desc.conv_width)
+        self.a_bytes, self.weight_bytes = 4 * self.channels * self.state_dim, 2 * self.channels * self.conv_width
 
 
 class StatePlan:
-    """Handle returned by :func:`state_plan_create`."""
+    """Handle returned by :func:`state_plan_create`.  `row_bytes`, `bc_bytes`: what the new tokens' channels, and b or c, take."""
 
     def __init__(self, handle: int, pool: StatePool, rows: int):
         self.state_plan_handle = handle
         self.pool = pool
         self.rows = rows
+        self.row_bytes, self.bc_bytes = 2 * rows * pool.channels, 2 * rows * pool.state_dim
 
 
 def state_pool_conv_bytes(num_slots: int, channels: int, state_dim: int, conv_width: int) -> int:
@@ -797,45 +801,52 @@ def state_plan_workspace_bytes(plan: StatePlan) -> int:
     return int(load().ap_state_plan_workspace_bytes(plan.state_plan_handle))
 
 
-def _matrix(x, rows: int, cols: int, device: int) -> Tuple[Optional[int], int]:
-    """(address, elements from one row to the next or 0 for contiguous) of a bf16 tensor [rows, cols] of the call."""
+def _matrix(x, rows: int, cols: int, nbytes: int, device: int) -> Tuple[int, int]:
+    """(address, elements from one row to the next or 0 for contiguous) of a bf16 tensor [rows, cols] of the call; `nbytes`:
+    what it takes contiguous."""
     try:
-        n, c = x.shape
-        row, one = x.stride()
-        if x.dtype is _bf16 and x.get_device() == device and c == cols and n >= rows and one == 1 and row >= cols:
-            return x.data_ptr(), row if n > 1 else 0
-    except AttributeError:                   # None, an address, a host array
-        return _checked(x, rows * cols * 2, device, 2), 0
-    except ValueError:
-        n = c = row = one = 0
-    if rows <= 0:
-        return _ptr(x), 0
-    if n < rows or c != cols:
+        if x.dtype is _bf16 and x.get_device() == device:
+            if x.is_contiguous():
+                if x.nbytes == nbytes or (x.nbytes > nbytes and x.shape[-1] == cols):      # (other shapes of the same memory pass)
+                    return x.data_ptr(), 0
+            else:
+                n, c = x.shape
+                row, one = x.stride()
+                if c == cols and n >= rows and one == 1 and row >= cols and n > 1:
+                    return x.data_ptr(), row
+    except (AttributeError, ValueError):     # None, an address, a host array; another number of dimensions
+        pass
+    if rows <= 0 or not hasattr(x, "data_ptr") or (x.is_contiguous() and x.nbytes <= nbytes):
+        return _checked(x, nbytes, device, 2) or 0, 0
+    if x.dim() != 2 or x.shape[0] < rows or x.shape[1] != cols:
         raise ValueError(f"expected [{rows}, {cols}], not {list(x.shape)}")
-    if (one != 1 and c > 1) or (row < cols and n > 1):
+    row, one = x.stride()
+    if (one != 1 and cols > 1) or (row < cols and x.shape[0] > 1):
         raise ValueError("expected rows of contiguous elements that do not overlap")
-    return _checked(x, 0, device, 2, dense=False), row if n > 1 else 0
+    return _checked(x, 0, device, 2, dense=False), row if x.shape[0] > 1 else 0
 
 
-def _vector(x, nbytes: int, device: int, dtype_bytes: int) -> Optional[int]:
-    """Address of a contiguous parameter (bf16: 2, fp32: 4 bytes an element), or None."""
+def _floats(x, nbytes: int, device: int) -> int:
+    """Address of a contiguous fp32 parameter of the call, or 0 for None."""
+    if x is None:
+        return 0
     try:
-        if x.dtype is (_fp32 if dtype_bytes == 4 else _bf16) and x.nbytes >= nbytes and x.get_device() == device and x.is_contiguous():
+        if x.dtype is _fp32 and x.nbytes >= nbytes and x.get_device() == device and x.is_contiguous():
             return x.data_ptr()
     except AttributeError:
         pass
-    return _checked(x, nbytes, device, dtype_bytes)
+    return _checked(x, nbytes, device, 4) or 0
 
 
 def conv_iteration(pool: StatePool, plan: StatePlan, x, weight, out, bias=None, silu: bool = True, stream=None) -> None:
     """Short causal convolution of the plan's rows ``x`` [rows, channels] with ``weight`` [channels, conv_width]; the slots
     take the last inputs.  ``x`` and ``out`` may be strided by row."""
-    dev, n, c = pool.device, plan.rows, pool.channels
-    x_at, xs = _matrix(x, n, c, dev)
-    out_at, os_ = _matrix(out, n, c, dev)
-    status = (_lib or load()).ap_conv_iteration(
-        pool.state_handle, plan.state_plan_handle, _CONV_DESC.pack(1 if silu else 0, xs, os_), x_at,
-        _vector(weight, c * pool.conv_width * 2, dev, 2), _vector(bias, c * 2, dev, 2), out_at, _stream(stream, dev))
+    dev, n, c, nbytes = pool.device, plan.rows, pool.channels, plan.row_bytes
+    x_at, xs = _matrix(x, n, c, nbytes, dev)
+    out_at, os_ = _matrix(out, n, c, nbytes, dev)
+    desc = _CONV_DESC.pack(1 if silu else 0, xs, os_, x_at, _one(weight, pool.weight_bytes, dev) or 0,
+                           0 if bias is None else _one(bias, 2 * c, dev), out_at)
+    status = (_lib or load()).ap_conv_iteration(pool.state_handle, plan.state_plan_handle, desc, _stream(stream, dev))
     if status:
         _check(status, "ap_conv_iteration")
 
@@ -845,18 +856,21 @@ def scan_iteration(pool: StatePool, plan: StatePlan, x, dt, a, b, c, out, z=None
     """Selective state space scan of the plan's rows: ``x``, ``dt``, ``z``, ``out`` [rows, channels], ``b``, ``c``
     [rows, state_dim] (all bf16, may be strided by row), ``a`` [channels, state_dim], ``d_skip``, ``dt_bias`` [channels]
     (fp32); the slots take the states (see ap_scan_iteration)."""
-    dev, n, ch, st = pool.device, plan.rows, pool.channels, pool.state_dim
-    workspace, room = _workspace(workspace, workspace_bytes, dev)
-    x_at, xs = _matrix(x, n, ch, dev)
-    dt_at, dts = _matrix(dt, n, ch, dev)
-    b_at, bs = _matrix(b, n, st, dev)
-    c_at, cs = _matrix(c, n, st, dev)
-    z_at, zs = (None, 0) if z is None else _matrix(z, n, ch, dev)
-    out_at, os_ = _matrix(out, n, ch, dev)
-    status = (_lib or load()).ap_scan_iteration(
-        pool.state_handle, plan.state_plan_handle, _SCAN_DESC.pack(1 if softplus else 0, xs, dts, bs, cs, zs, os_), x_at, dt_at,
-        _vector(a, ch * st * 4, dev, 4), b_at, c_at, z_at, _vector(d_skip, ch * 4, dev, 4), _vector(dt_bias, ch * 4, dev, 4), out_at,
-        workspace, room, _stream(stream, dev))
+    dev, n, ch, st, nbytes = pool.device, plan.rows, pool.channels, pool.state_dim, plan.row_bytes
+    x_at, xs = _matrix(x, n, ch, nbytes, dev)
+    dt_at, dts = _matrix(dt, n, ch, nbytes, dev)
+    b_at, bs = _matrix(b, n, st, plan.bc_bytes, dev)
+    c_at, cs = _matrix(c, n, st, plan.bc_bytes, dev)
+    z_at, zs = (0, 0) if z is None else _matrix(z, n, ch, nbytes, dev)
+    out_at, os_ = _matrix(out, n, ch, nbytes, dev)
+    desc = _SCAN_DESC.pack(1 if softplus else 0, xs, dts, bs, cs, zs, os_, x_at, dt_at, b_at, c_at, z_at, out_at,
+                           _floats(a, pool.a_bytes, dev), _floats(d_skip, 4 * ch, dev), _floats(dt_bias, 4 * ch, dev))
+    if workspace is None:
+        workspace_bytes = 0
+    else:
+        workspace, workspace_bytes = _workspace(workspace, workspace_bytes, dev)
+    status = (_lib or load()).ap_scan_iteration(pool.state_handle, plan.state_plan_handle, desc, workspace, workspace_bytes,
+                                                _stream(stream, dev))
     if status:
         _check(status, "ap_scan_iteration")
 

@@ -118,24 +118,22 @@ conv_kernel(const StateUnit *__restrict__ units, int blocks_c, int64_t channels,
 }
 
 template <int W>
-cudaError_t launch_conv_t(const ap_state_pool *pool, const ap_state_plan *plan, const ap_conv_desc &conv, const void *x,
-                          const void *weight, const void *bias, void *out, cudaStream_t stream) {
+cudaError_t launch_conv_t(const ap_state_pool *pool, const ap_state_plan *plan, const ap_conv_desc &conv, cudaStream_t stream) {
     const int blocks_c = (pool->desc.channels / 4 + kConvThreads - 1) / kConvThreads;
     const cudaError_t e = launch_overlapped(conv.silu ? conv_kernel<W, true> : conv_kernel<W, false>, (unsigned)(plan->n_conv * blocks_c),
                                             (unsigned)kConvThreads, 0, stream, plan->d_conv, blocks_c, (int64_t)pool->desc.channels,
-                                            (const uint16_t *)x, (const uint16_t *)weight, (const uint16_t *)bias, (uint16_t *)out,
+                                            (const uint16_t *)conv.x, (const uint16_t *)conv.weight, (const uint16_t *)conv.bias, (uint16_t *)conv.out,
                                             (uint16_t *)pool->desc.conv_base, conv.x_row_stride, conv.out_row_stride);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_conv(const ap_state_pool *pool, const ap_state_plan *plan, const ap_conv_desc &conv, const void *x,
-                        const void *weight, const void *bias, void *out, cudaStream_t stream) {
+cudaError_t launch_conv(const ap_state_pool *pool, const ap_state_plan *plan, const ap_conv_desc &conv, cudaStream_t stream) {
     switch (pool->desc.conv_width) {
-        case 2: return launch_conv_t<2>(pool, plan, conv, x, weight, bias, out, stream);
-        case 3: return launch_conv_t<3>(pool, plan, conv, x, weight, bias, out, stream);
-        default: return launch_conv_t<4>(pool, plan, conv, x, weight, bias, out, stream);
+        case 2: return launch_conv_t<2>(pool, plan, conv, stream);
+        case 3: return launch_conv_t<3>(pool, plan, conv, stream);
+        default: return launch_conv_t<4>(pool, plan, conv, stream);
     }
 }
 

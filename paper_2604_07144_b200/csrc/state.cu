@@ -270,8 +270,7 @@ int ap_state_plan_get_info(const ap_state_plan *plan, ap_state_info *info) {
 
 size_t ap_state_plan_workspace_bytes(const ap_state_plan *plan) { return plan ? plan->workspace_bytes : 0; }
 
-int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_conv_desc *conv, const void *x,
-                      const void *weight, const void *bias, void *out, void *stream) {
+int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_conv_desc *conv, void *stream) {
     if (!pool || !plan || !conv || !same_shape(pool->desc, plan->desc)) return AP_ERR_INVALID_ARG;
     const int64_t D = pool->desc.channels, n = plan->info.n_new;
     ap_conv_desc c = *conv;
@@ -280,6 +279,7 @@ int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_c
         return AP_ERR_INVALID_ARG;
     if (pool->desc.device < 0) return AP_ERR_CUDA;
     if (n == 0) return AP_OK;
+    const void *x = c.x, *weight = c.weight, *bias = c.bias, *out = c.out;
     if (!x || !weight || !out || !aligned16(x) || !aligned16(weight) || !aligned16(bias) || !aligned16(out)) return AP_ERR_INVALID_ARG;
     const Rows o{out, c.out_row_stride, D, 2};
     const int64_t slots = pool->desc.num_slots, w = pool->desc.conv_width;
@@ -294,16 +294,15 @@ int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_c
         return AP_ERR_INVALID_ARG;
     DeviceGuard guard(pool->desc.device);
     if (!guard.ok) return AP_ERR_CUDA;
-    if (launch_conv(pool, plan, c, x, weight, bias, out, (cudaStream_t)stream) != cudaSuccess) {
+    if (launch_conv(pool, plan, c, (cudaStream_t)stream) != cudaSuccess) {
         (void)cudaGetLastError();
         return AP_ERR_CUDA;
     }
     return AP_OK;
 }
 
-int ap_scan_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_scan_desc *scan, const void *x,
-                      const void *dt, const float *a, const void *b, const void *c, const void *z, const float *d_skip,
-                      const float *dt_bias, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+int ap_scan_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_scan_desc *scan, void *workspace,
+                      size_t workspace_bytes, void *stream) {
     if (!pool || !plan || !scan || !same_shape(pool->desc, plan->desc)) return AP_ERR_INVALID_ARG;
     const int64_t D = pool->desc.channels, N = pool->desc.state_dim, n = plan->info.n_new;
     ScanArgs g{};
@@ -314,8 +313,10 @@ int ap_scan_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_s
         return AP_ERR_INVALID_ARG;
     if (pool->desc.device < 0) return AP_ERR_CUDA;
     if (n == 0) return AP_OK;
+    const void *x = scan->x, *dt = scan->dt, *b = scan->b, *c = scan->c, *z = scan->z, *out = scan->out;
+    const float *a = scan->a, *d_skip = scan->d_skip, *dt_bias = scan->dt_bias;
     if (!x || !dt || !a || !b || !c || !out) return AP_ERR_INVALID_ARG;
-    for (const void *p : {x, dt, (const void *)a, b, c, z, (const void *)d_skip, (const void *)dt_bias, (const void *)out})
+    for (const void *p : {x, dt, b, c, z, out, (const void *)a, (const void *)d_skip, (const void *)dt_bias})
         if (!aligned16(p)) return AP_ERR_INVALID_ARG;
     if (plan->workspace_bytes > 0) {
         if (!workspace || workspace_bytes < plan->workspace_bytes) return AP_ERR_WORKSPACE_TOO_SMALL;

@@ -181,17 +181,16 @@ def test_call_refusals():
     lib = B.load()
 
     def conv(pool_=pool, desc=True, **kw):
-        d = B.ConvDesc(1, 0, 0)
+        d = B.ConvDesc(1, 0, 0, 4096, 8192, None, 1 << 20)
         for k, v in kw.items():
             setattr(d, k, v)
-        return lib.ap_conv_iteration(pool_.state_handle, plan.state_plan_handle, ctypes.byref(d) if desc else None, 4096, 8192, None, 1 << 20, None)
+        return lib.ap_conv_iteration(pool_.state_handle, plan.state_plan_handle, ctypes.byref(d) if desc else None, None)
 
     def scan(pool_=pool, desc=True, **kw):
-        d = B.ScanDesc(1, 0, 0, 0, 0, 0, 0)
+        d = B.ScanDesc(1, 0, 0, 0, 0, 0, 0, *[4096] * 5, 1 << 20, *[4096] * 3)
         for k, v in kw.items():
             setattr(d, k, v)
-        return lib.ap_scan_iteration(pool_.state_handle, plan.state_plan_handle, ctypes.byref(d) if desc else None, *[4096] * 8, 1 << 20,
-                                     None, 0, None)
+        return lib.ap_scan_iteration(pool_.state_handle, plan.state_plan_handle, ctypes.byref(d) if desc else None, None, 0, None)
     assert conv() == scan() == B.AP_ERR_CUDA                            # valid, but the pool is host-only
     assert conv(pool_=other) == scan(pool_=other) == B.AP_ERR_INVALID_ARG
     assert conv(desc=False) == scan(desc=False) == B.AP_ERR_INVALID_ARG
