@@ -93,6 +93,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // a NaN wins
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 __device__ __forceinline__ float min_nan(float a, float b) {
     float d;
     asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
@@ -169,6 +174,30 @@ __device__ __forceinline__ void copy_async(void *to, const void *from) {  // glo
         asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(to)), "l"(from), "n"(kBytes) : "memory");
 }
 
+// A warp's copies of the rows of one tensor, kCols numbers each, kSize numbers a copy.
+template <int kCols, int kSize>
+struct Copy {
+    static constexpr int kChunks = kCols / kSize, kRows = 32 / kChunks;           // copies of a row, rows of a round
+    static constexpr int kRounds = (kTile + kRows - 1) / kRows;
+    const uint16_t *from;      // this lane's first piece of the tile's rows
+    uint16_t *to;
+    int64_t stride;
+    int row, rows;             // this lane's first row; rows there are (0: none for this lane)
+    __device__ __forceinline__ Copy(int lane, uint16_t *tile, const uint16_t *base, int64_t stride, int64_t row0, int64_t col, int64_t end, int rows)
+        : stride(stride), row(lane / kChunks) {
+        const int e = lane % kChunks * kSize;
+        from = base + (row0 + row) * stride + col + e;
+        to = tile + row * kCols + e;
+        this->rows = col + e < end && row < kTile ? rows : 0;
+    }
+    __device__ __forceinline__ void tile(int t0) {
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i)
+            if (t0 + row + i * kRows < rows) copy_async<2 * kSize>(to + i * kRows * kCols, from + i * kRows * stride);
+        from += kTile * stride;
+    }
+};
+
 // One piece of a sequence for a warp's channels.
 template <int N, int H, bool kStateOnly>
 __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, const ScanArgs &g, WalkSmem<N, H> &sm) {
@@ -232,26 +261,22 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
         *(float2 *)&sm.bias[two] = bias, *(float2 *)&sm.skip[two] = skip;
     }
     float2 total = make_float2(0.f, 0.f);
+    uint16_t *out = g.out + (row0 + row_in) * g.os + c0 + two;
+    const int out_rows = s_in ? rows_all : 0;
 
-    // Asynchronous copies of a tile's rows, `cols` numbers each from column `col` on, kSize numbers a copy.  Rows past the
-    // unit are left as they are, and not used.
-    auto copy_rows = [&](auto size, auto to, int cols, const uint16_t *from, int64_t stride, int64_t col, int64_t end, int t0) {
-        constexpr int kSize = decltype(size)::value;
-        const int chunks = cols / kSize;
-#pragma unroll
-        for (int i = 0; i < (kTile * chunks + 31) / 32; ++i) {
-            const int at = i * 32 + lane, r = at / chunks, e = at % chunks * kSize;
-            if (at < kTile * chunks && t0 + r < rows_all && col + e < end)
-                copy_async<2 * kSize>(to + at * kSize, from + (row0 + t0 + r) * stride + col + e);
-        }
-    };
-    constexpr std::integral_constant<int, (S::kCh >= 8 ? 8 : S::kCh)> kAsync;
-    constexpr std::integral_constant<int, 8> kEight;
+    // Asynchronous copies of a tile's rows into shared memory, a tile a call.  Rows past the unit are left as they are, and not
+    // used.
+    constexpr int kAsync = S::kCh >= 8 ? 8 : S::kCh;           // channels of a copy
+    Copy<S::kCh, kAsync> copy_x(lane, &sm.x[0][0], g.x, g.xs, row0, c0, D, rows_all);
+    Copy<S::kCh, kAsync> copy_dt(lane, &sm.dt[0][0], g.dt, g.dts, row0, c0, D, rows_all);
+    Copy<S::kCh, kAsync> copy_z(lane, &sm.z[0][0], g.z, g.zs, row0, c0, D, kStateOnly || !g.z ? 0 : rows_all);
+    Copy<N, 8> copy_b(lane, &sm.b_in[0][0], g.b, g.bs, row0, 0, N, rows_all);
+    Copy<N, 8> copy_c(lane, &sm.c_in[0][0], g.c, g.cs, row0, 0, N, kStateOnly ? 0 : rows_all);
     auto copy_in = [&](int t0) {
-        copy_rows(kAsync, &sm.x[0][0], S::kCh, g.x, g.xs, c0, D, t0);
-        copy_rows(kAsync, &sm.dt[0][0], S::kCh, g.dt, g.dts, c0, D, t0);
-        copy_rows(kEight, &sm.b_in[0][0], N, g.b, g.bs, 0, N, t0);
-        if (!kStateOnly) copy_rows(kEight, &sm.c_in[0][0], N, g.c, g.cs, 0, N, t0);
+        copy_x.tile(t0);
+        copy_dt.tile(t0);
+        copy_b.tile(t0);
+        if (!kStateOnly) copy_c.tile(t0);
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     copy_in(0);
@@ -260,7 +285,7 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncwarp();
         // the gates are wanted last: they come while the rows are walked
-        if (!kStateOnly && g.z) copy_rows(kAsync, &sm.z[0][0], S::kCh, g.z, g.zs, c0, D, t0);
+        if (!kStateOnly) copy_z.tile(t0);
         asm volatile("cp.async.commit_group;" ::: "memory");
         // b and c in fp32 (rows past the end: zeros, which their steps of 0 multiply)
 #pragma unroll
@@ -288,8 +313,8 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
                 const float2 x = widen2(*(const uint32_t *)&sm.x[r][two]);
                 float2 dx = __fmul2_rn(d, x);
                 if (!kStateOnly) *(float2 *)&sm.y[r][two] = __fmul2_rn(skip, x);
-                if (r >= rows || !s_in) d = dx = make_float2(0.f, 0.f);      // (past the end the state stays as it is)
-                longest = max_nan(longest, max_nan(fabsf(d.x), fabsf(d.y)));
+                if (rows < kTile && r >= rows) d = dx = make_float2(0.f, 0.f);      // (past the end the state stays as it is)
+                longest = max3_nan(longest, fabsf(d.x), fabsf(d.y));
                 if (kStateOnly) total = __fadd2_rn(total, d);
                 *(float4 *)&sm.step[r][two] = make_float4(d.x, dx.x, d.y, dx.y);
             }
@@ -364,8 +389,9 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
                 const int r = p * S::kRowsAtOnce + row_in;
                 float2 y = *(const float2 *)&sm.y[r][two];
                 if (g.z) y = gate2(y, widen2(*(const uint32_t *)&sm.z[r][two]));
-                if (s_in && r < rows) *(uint32_t *)(g.out + (row0 + t0 + r) * g.os + c0 + two) = pack_bf16x2(y.x, y.y);
+                if (r < out_rows - t0) *(uint32_t *)(out + p * S::kRowsAtOnce * g.os) = pack_bf16x2(y.x, y.y);
             }
+            out += kTile * g.os;
         }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
