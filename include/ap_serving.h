@@ -529,9 +529,10 @@ int ap_prompt_attention(ap_kv_pool *pool, const ap_prompt_plan *plan, const void
  *     scan plane : [num_slots][channels][state_dim]       fp32
  * channels: a multiple of 8 (else UNSUPPORTED) up to 2^20; state_dim 8, 16, 32 or
  * 64; conv_width 2, 3 or 4 (else UNSUPPORTED).  conv_base / scan_base: device,
- * 16-byte aligned, owned by the caller, or NULL: the library allocates (and zero
- * fills) that plane.  device < 0 (with both bases NULL): a host-only pool, which
- * plans and validates; calls that would launch return AP_ERR_CUDA.
+ * 16-byte aligned, owned by the caller; both NULL: the library allocates (and zero
+ * fills) both planes; one NULL: the layer has no such plane, and the call that needs
+ * it returns INVALID_ARG.  device < 0 (with both bases NULL): a host-only pool,
+ * which plans and validates; calls that would launch return AP_ERR_CUDA.
  */
 typedef struct ap_state_pool ap_state_pool; /* opaque */
 typedef struct ap_state_plan ap_state_plan; /* opaque */

@@ -747,7 +747,8 @@ def state_pool_scan_bytes(num_slots: int, channels: int, state_dim: int, conv_wi
 def state_pool_create(num_slots: int, channels: int, state_dim: int, conv_width: int, conv_base=None, scan_base=None,
                       device: int = 0) -> StatePool:
     """Slots for one layer's states: ``conv_base`` [num_slots, conv_width - 1, channels] bf16, ``scan_base``
-    [num_slots, channels, state_dim] fp32; a plane that is not given is the library's, zero filled."""
+    [num_slots, channels, state_dim] fp32.  With neither given both are the library's, zero filled; with one, the layer has
+    no other."""
     shape = num_slots, channels, state_dim, conv_width
     at = []
     for base, nbytes, size in ((conv_base, state_pool_conv_bytes(*shape), 2), (scan_base, state_pool_scan_bytes(*shape), 4)):

@@ -44,7 +44,7 @@ struct Walk {
     static constexpr int kLanes = N / H;                       // lanes of a channel
     static constexpr int kCh = 32 / kLanes;                    // channels of a warp
     // warps of a block, blocks of an SM
-    static constexpr int kWarps = 2, kBlocks = 8;
+    static constexpr int kWarps = 1, kBlocks = 16;
     // staging: a lane takes two channels next to one another
     static constexpr int kTwos = kCh / 2, kRowsAtOnce = 32 / kTwos, kPasses = kTile / kRowsAtOnce;
     static_assert(H % 4 == 0 && kCh >= 4 && kTile % kRowsAtOnce == 0, "");

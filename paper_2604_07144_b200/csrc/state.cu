@@ -213,8 +213,9 @@ int ap_state_pool_create(ap_state_pool **out, const ap_state_desc *desc) {
     if (desc->device >= 0) {
         DeviceGuard guard(desc->device);
         bool ok = guard.ok && cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, desc->device) == cudaSuccess;
+        const bool allocate = !desc->conv_base && !desc->scan_base;
         auto plane = [&](void **base, bool *owns, size_t bytes) {
-            if (!ok || *base) return;
+            if (!ok || !allocate) return;
             *owns = true;
             ok = cudaMalloc(base, bytes) == cudaSuccess && cudaMemset(*base, 0, bytes) == cudaSuccess;
         };
@@ -279,6 +280,7 @@ int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_c
         return AP_ERR_INVALID_ARG;
     if (pool->desc.device < 0) return AP_ERR_CUDA;
     if (n == 0) return AP_OK;
+    if (!pool->desc.conv_base) return AP_ERR_INVALID_ARG;
     const void *x = c.x, *weight = c.weight, *bias = c.bias, *out = c.out;
     if (!x || !weight || !out || !aligned16(x) || !aligned16(weight) || !aligned16(bias) || !aligned16(out)) return AP_ERR_INVALID_ARG;
     const Rows o{out, c.out_row_stride, D, 2};
@@ -313,6 +315,7 @@ int ap_scan_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_s
         return AP_ERR_INVALID_ARG;
     if (pool->desc.device < 0) return AP_ERR_CUDA;
     if (n == 0) return AP_OK;
+    if (!pool->desc.scan_base) return AP_ERR_INVALID_ARG;
     const void *x = scan->x, *dt = scan->dt, *b = scan->b, *c = scan->c, *z = scan->z, *out = scan->out;
     const float *a = scan->a, *d_skip = scan->d_skip, *dt_bias = scan->dt_bias;
     if (!x || !dt || !a || !b || !c || !out) return AP_ERR_INVALID_ARG;

@@ -376,6 +376,29 @@ def test_iterations_that_follow_one_another(states):
 
 
 @pytest.mark.gpu
+def test_a_layer_with_one_plane():
+    import torch
+    x = torch.ones(2, 64, dtype=torch.bfloat16, device="cuda")
+    w, a, b = (torch.zeros(64, 4, dtype=torch.bfloat16, device="cuda"), torch.zeros(64, 8, device="cuda"),
+               torch.zeros(2, 8, dtype=torch.bfloat16, device="cuda"))
+    for planes, works in ((dict(conv_base=torch.zeros(3, 3, 64, dtype=torch.bfloat16, device="cuda")), "conv"),
+                          (dict(scan_base=torch.zeros(3, 64, 8, device="cuda")), "scan")):
+        pool = ap.state_pool_create(3, 64, 8, 4, **planes)
+        plan = ap.state_plan_create(pool, [2], [2], [1])
+        for name, call in (("conv", lambda: ap.conv_iteration(pool, plan, x, w, torch.empty_like(x))),
+                           ("scan", lambda: ap.scan_iteration(pool, plan, x, x, a, b, b, torch.empty_like(x)))):
+            if name == works:
+                call()
+            else:
+                with pytest.raises(ap.ApError) as e:
+                    call()
+                assert e.value.status == B.AP_ERR_INVALID_ARG
+        torch.cuda.synchronize()
+        ap.state_plan_destroy(plan)
+        ap.state_pool_destroy(pool)
+
+
+@pytest.mark.gpu
 def test_captured_replayed_and_on_another_stream():
     import torch
     c = Case(800, 64, 16, 4, [300, 1, 40], [300, 4, 40]).open()
