@@ -597,7 +597,7 @@ size_t ap_state_plan_workspace_bytes(const ap_state_plan *plan);
  * x: [n_new][channels] bf16, rows x_row_stride elements apart (0: contiguous; a
  * multiple of 8); weight: [channels][w] bf16; bias: [channels] bf16 or NULL; out:
  * [n_new][channels] bf16, rows out_row_stride elements apart.  Device, 16-byte
- * aligned.  out overlaps no input and no slot (INVALID_ARG).
+ * aligned.  out overlaps no input, and neither overlaps the slots (INVALID_ARG).
  */
 typedef struct ap_conv_desc {
     int32_t silu; /* 0 or 1 */
@@ -622,7 +622,8 @@ int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_c
  * cut out of projections' outputs.  a: [channels][state_dim] fp32, finite (beyond
  * 2e38 in magnitude as 2e38); d_skip, dt_bias: [channels] fp32 or NULL; z may be
  * NULL.  out: [n_new][channels] bf16, rows out_row_stride elements apart.  Device,
- * 16-byte aligned.  out overlaps no input and no slot (INVALID_ARG).  workspace:
+ * 16-byte aligned.  out overlaps no input, and neither overlaps the slots or the
+ * workspace (INVALID_ARG).  workspace:
  * device, 256-byte aligned, at least ap_state_plan_workspace_bytes() (else
  * WORKSPACE_TOO_SMALL), contents undefined before and after; calls that may
  * overlap on the GPU take one each.

@@ -568,7 +568,14 @@ cudaError_t launch_scan_t(const ap_state_pool *pool, const ap_state_plan *plan, 
 
 }  // namespace
 
-int scan_warp_channels(int state_dim) { return state_dim <= 16 ? 32 : state_dim == 32 ? 16 : 8; }
+int scan_warp_channels(int state_dim) {
+    switch (state_dim) {
+        case 8: return Walk<8, kHeldStates>::kCh;
+        case 16: return Walk<16, kHeldStates>::kCh;
+        case 32: return Walk<32, kHeldStates>::kCh;
+        default: return Walk<64, kHeldStates>::kCh;
+    }
+}
 
 cudaError_t launch_scan(const ap_state_pool *pool, const ap_state_plan *plan, const ScanArgs &args, cudaStream_t stream) {
     switch (pool->desc.state_dim) {

@@ -15,7 +15,7 @@ namespace {
 // pieces, all but the first and the last are walked twice (once for the state behind them, once for their rows) and there
 // are two launches.
 constexpr int kConvBlocks = 14;
-constexpr int kCutBelow = 4, kResident = 14, kLeastPiece = 64;
+constexpr int kCutBelow = 12, kResident = 28, kLeastPiece = 64;
 
 struct Cut {
     int32_t piece;       // rows of a piece, 0: no sequence is cut
@@ -291,8 +291,10 @@ int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_c
         const uintptr_t o0 = (uintptr_t)out, o1 = o0 + (uintptr_t)((n - 1) * o.stride + D) * 2;
         return r.p && r0 < o1 && o0 < r1;
     };
-    if (overlap(o, Rows{x, c.x_row_stride, D, 2}, n) || meets(flat(weight, D * w, 2)) || meets(flat(bias, D, 2)) ||
-        meets(flat(pool->desc.conv_base, slots * (w - 1) * D, 2)))
+    const Rows plane = flat(pool->desc.conv_base, slots * (w - 1) * D, 2);
+    if (overlap(o, Rows{x, c.x_row_stride, D, 2}, n) || meets(flat(weight, D * w, 2)) || meets(flat(bias, D, 2)) || meets(plane) ||
+        overlap(plane, Rows{x, (n - 1) * c.x_row_stride + D, (n - 1) * c.x_row_stride + D, 2}, 1) ||
+        overlap(plane, flat(weight, D * w, 2), 1) || overlap(plane, flat(bias, D, 2), 1))
         return AP_ERR_INVALID_ARG;
     DeviceGuard guard(pool->desc.device);
     if (!guard.ok) return AP_ERR_CUDA;
@@ -333,6 +335,18 @@ int ap_scan_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_s
         meets(dt_bias, D * 4) || meets(pool->desc.scan_base, (int64_t)pool->desc.num_slots * D * N * 4) ||
         meets(plan->workspace_bytes ? workspace : nullptr, (int64_t)plan->workspace_bytes))
         return AP_ERR_INVALID_ARG;
+    // nor does what the call keeps for itself overlap an input
+    const int64_t planes = (int64_t)pool->desc.num_slots * D * N;
+    for (const Rows &kept : {Rows{pool->desc.scan_base, planes, planes, 4},
+                             Rows{plan->workspace_bytes ? workspace : nullptr, (int64_t)plan->workspace_bytes, (int64_t)plan->workspace_bytes, 1}}) {
+        auto in = [&](const void *p, int64_t stride, int64_t cols, int size) {
+            const int64_t all = (n - 1) * stride + cols;
+            return overlap(kept, Rows{p, all, all, size}, 1);
+        };
+        if (in(x, g.xs, D, 2) || in(dt, g.dts, D, 2) || in(z, g.zs, D, 2) || in(b, g.bs, N, 2) || in(c, g.cs, N, 2) ||
+            in(a, 0, D * N, 4) || in(d_skip, 0, D, 4) || in(dt_bias, 0, D, 4))
+            return AP_ERR_INVALID_ARG;
+    }
     g.x = (const uint16_t *)x, g.dt = (const uint16_t *)dt, g.b = (const uint16_t *)b, g.c = (const uint16_t *)c;
     g.z = (const uint16_t *)z, g.a = a, g.d_skip = d_skip, g.dt_bias = dt_bias, g.out = (uint16_t *)out;
     g.state = (float *)pool->desc.scan_base;

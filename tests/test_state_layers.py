@@ -336,6 +336,13 @@ def test_strided_rows_and_larger_tensors():
     ap.scan_iteration(c.pool, c.plan, xz[:, :136], dev(c.dt), dev(c.a), proj[:, 24:40], proj[:, 40:], xz[:, 136:], workspace=c.workspace())
     with pytest.raises(ap.ApError):
         ap.conv_iteration(c.pool, c.plan, dev(c.x), dev(c.weight), ap.state_pool_conv_base(c.pool))
+    with pytest.raises(ap.ApError):
+        ap.conv_iteration(c.pool, c.plan, ap.state_pool_conv_base(c.pool), dev(c.weight), c.blank())
+    for name in ("x", "dt", "b"):
+        kw = dict(x=dev(c.x), dt=dev(c.dt), b=proj[:, 24:40])
+        kw[name] = ap.state_pool_scan_base(c.pool)
+        with pytest.raises(ap.ApError):
+            ap.scan_iteration(c.pool, c.plan, a=dev(c.a), c=proj[:, 40:], out=c.blank(), workspace=c.workspace(), **kw)
     torch.cuda.synchronize()
     c.close()
 
