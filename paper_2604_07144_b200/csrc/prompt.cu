@@ -69,7 +69,20 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
     const int kv_len = pos0 + tile.rows;         // keys the last valid row sees
     const int n_steps = (kv_len + kTileN - 1) / kTileN;
 
-    if (threadIdx.x == 0) {
+    auto load_kv = [&](int n, bool is_k, int j) {
+        const int s = n % kKvSlots;
+        // (rows past the packed batch's last read as zeros; they count)
+        mbar_arrive_expect_tx(&kv_full[s], (uint32_t)Cfg::kKvTileBytes);
+        tma_load_3d(smem + Cfg::kOffK + s * Cfg::kKvTileBytes, is_k ? &k_map : &v_map, &kv_full[s], 0, tile.start + j * kTileN,
+                    tile.kv_head * Cfg::kHalves);
+    };
+    // entry n of the ring, in the order K_0, K_1, V_0, K_2, V_1, ...; it goes to slot n % kKvSlots
+    const int n_entries = 2 * n_steps;
+    auto load_entry = [&](int n) {
+        const bool is_k = n == 0 || ((n & 1) && n < n_entries - 1);
+        load_kv(n, is_k, is_k ? (n + 1) / 2 : (n == n_entries - 1 ? n_steps - 1 : n / 2 - 1));
+    };
+    if (warp == kProducerWarp && lane == 0) {
         mbar_init(q_full, 1);
         for (int s = 0; s < kKvSlots; ++s) {
             mbar_init(&kv_full[s], 1);
@@ -83,6 +96,14 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
         }
         *abort_flag = 0;
         fence_barrier_init();
+        griddep_wait();                          // (what comes before reads only the plan)
+        // the first copies are under way while the block gets its tensor memory and meets
+        mbar_arrive_expect_tx(q_full, (uint32_t)(n_tiles * Cfg::kQBytes));
+        tma_load_3d(smem + Cfg::kOffQ, &q_map, q_full, 0, tile.row0, tile.q_head * Cfg::kHalves);
+        load_entry(0);
+        if (n_tiles == 2)
+            tma_load_3d(smem + Cfg::kOffQ + Cfg::kQBytes, &q_map, q_full, 0, tile.row0, tile.q_head_b * Cfg::kHalves);
+        for (int n = 1; n < min(n_entries, kKvSlots); ++n) load_entry(n);
     }
     if (warp == kMmaWarp) {
         tmem_alloc(tmem_slot, Cfg::kTmemCols);
@@ -93,35 +114,20 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
     tcgen05_fence_after();
     const uint32_t tmem = *tmem_slot;
     griddep_launch_dependents();
-    griddep_wait();                              // the preamble reads only the plan
+    griddep_wait();
 
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kProducerWarp) {
             // -------------------------------------------------- producer --
             if (lane == 0) {
-                prefetch_tensormap(&q_map);
-                prefetch_tensormap(&k_map);
-                prefetch_tensormap(&v_map);
-                mbar_arrive_expect_tx(q_full, (uint32_t)(n_tiles * Cfg::kQBytes));
-                tma_load_3d(smem + Cfg::kOffQ, &q_map, q_full, 0, tile.row0, tile.q_head * Cfg::kHalves);
-                if (n_tiles == 2)
-                    tma_load_3d(smem + Cfg::kOffQ + Cfg::kQBytes, &q_map, q_full, 0, tile.row0, tile.q_head_b * Cfg::kHalves);
-                // ring order K_0, K_1, V_0, K_2, V_1, ...: entry n goes to slot n % kKvSlots
-                const int n_entries = 2 * n_steps;
-                for (int n = 0; n < n_entries; ++n) {
-                    const bool is_k = n == 0 || ((n & 1) && n < n_entries - 1);
-                    const int j = is_k ? (n + 1) / 2 : (n == n_entries - 1 ? n_steps - 1 : n / 2 - 1);
-                    const int s = n % kKvSlots;
-                    if (!wait_or_abort(&kv_empty[s], ((uint32_t)(n / kKvSlots) & 1u) ^ 1u, abort_flag, wait_limit_ns)) {
+                for (int n = kKvSlots; n < n_entries; ++n) {
+                    if (!wait_or_abort(&kv_empty[n % kKvSlots], ((uint32_t)(n / kKvSlots) & 1u) ^ 1u, abort_flag, wait_limit_ns)) {
                         record_status(status, AP_ERR_TIMEOUT);
                         *abort_flag = 1;
                         break;
                     }
-                    // (rows past the packed batch's last read as zeros; they count)
-                    mbar_arrive_expect_tx(&kv_full[s], (uint32_t)Cfg::kKvTileBytes);
-                    tma_load_3d(smem + Cfg::kOffK + s * Cfg::kKvTileBytes, is_k ? &k_map : &v_map, &kv_full[s], 0,
-                                tile.start + j * kTileN, tile.kv_head * Cfg::kHalves);
+                    load_entry(n);
                 }
             }
             __syncwarp();
@@ -297,23 +303,32 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
                 tcgen05_fence_after();
                 const float inv = 1.f / l;
                 const bool valid = r < tile.rows;
-                __nv_bfloat16 *orow = out + ((size_t)(tile.row0 + r) * Hq + q_head) * D;
+                // A thread has a row: straight to memory every store would touch 32 rows.  The warp's rows go through this
+                // tile's Q (all products with it are through), 16-byte pieces of row r at piece ^ (r & 7), and out as whole rows.
+                uint8_t *rows = smem + Cfg::kOffQ + x * Cfg::kQBytes + (warp & 3) * 32 * (D * 2);
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t oreg[32];
                     tmem_ld_32x32b_x32(lane_addr + col_o + c * 32, oreg);
                     tmem_ld_wait();
-                    if (valid) {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            uint4 v;
-                            v.x = pack_bf16x2(__uint_as_float(oreg[i]) * inv, __uint_as_float(oreg[i + 1]) * inv);
-                            v.y = pack_bf16x2(__uint_as_float(oreg[i + 2]) * inv, __uint_as_float(oreg[i + 3]) * inv);
-                            v.z = pack_bf16x2(__uint_as_float(oreg[i + 4]) * inv, __uint_as_float(oreg[i + 5]) * inv);
-                            v.w = pack_bf16x2(__uint_as_float(oreg[i + 6]) * inv, __uint_as_float(oreg[i + 7]) * inv);
-                            *(uint4 *)(orow + c * 32 + i) = v;
-                        }
+                    for (int i = 0; i < 32; i += 8) {
+                        uint4 v;
+                        v.x = pack_bf16x2(__uint_as_float(oreg[i]) * inv, __uint_as_float(oreg[i + 1]) * inv);
+                        v.y = pack_bf16x2(__uint_as_float(oreg[i + 2]) * inv, __uint_as_float(oreg[i + 3]) * inv);
+                        v.z = pack_bf16x2(__uint_as_float(oreg[i + 4]) * inv, __uint_as_float(oreg[i + 5]) * inv);
+                        v.w = pack_bf16x2(__uint_as_float(oreg[i + 6]) * inv, __uint_as_float(oreg[i + 7]) * inv);
+                        *(uint4 *)(rows + lane * (D * 2) + (((c * 4 + i / 8) ^ (lane & 7)) << 4)) = v;
                     }
+                }
+                __syncwarp();
+                constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces;   // 16-byte pieces of a row, rows of a store
+                __nv_bfloat16 *to = out + ((size_t)(tile.row0 + (warp & 3) * 32 + lane / kPieces) * Hq + q_head) * D + lane % kPieces * 8;
+#pragma unroll
+                for (int i = 0; i < 32; i += kAtOnce, to += (size_t)kAtOnce * Hq * D) {
+                    const int row = i + lane / kPieces;
+                    if ((warp & 3) * 32 + row < tile.rows)
+                        *(uint4 *)to = *(const uint4 *)(rows + row * (D * 2) + ((lane % kPieces ^ (row & 7)) << 4));
                 }
                 if (valid && lse_out)
                     lse_out[(size_t)(tile.row0 + r) * Hq + q_head] = (m_used * scale_log2 + log2f(l)) * 0.6931471805599453f;
