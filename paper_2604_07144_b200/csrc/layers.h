@@ -49,13 +49,21 @@ static_assert(sizeof(ShortPrompt) == 16, "ShortPrompt layout");
 
 }  // namespace ap
 
+namespace ap {
+struct PromptLists {              // units of prompt attention, block i's from begin[i] to begin[i + 1]
+    const PromptTile *tiles = nullptr;
+    const int32_t *begin = nullptr;
+    int blocks = 0;
+};
+}  // namespace ap
+
 struct ap_prompt_plan {
     ap_kv_pool *pool = nullptr;
     ap::PlanBuffer buf{};
     int num_q_heads = 0;
     float scale = 0.f;
     ap_prompt_info info{};
-    const ap::PromptTile *d_tiles = nullptr;
+    ap::PromptLists lists[2];     // units of one tile, of two
     const ap::ShortPrompt *d_short = nullptr;
 };
 

@@ -5,7 +5,9 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <functional>
 #include <new>
+#include <utility>
 
 #include "host_util.h"
 #include "layers.h"
@@ -18,7 +20,6 @@ namespace {
 using namespace ptx;
 using prefill::exp2_poly2;
 using prefill::instr_desc;
-using prefill::kKvSlots;
 using prefill::kMmaWarp;
 using prefill::kPrefillThreads;
 using prefill::kProducerWarp;
@@ -34,79 +35,80 @@ using prefill::rescale_o;
 using prefill::smem_desc;
 
 constexpr int kShortRows = 64;
+constexpr int kUnitSteps = 2;             // what a unit costs beside its steps, in steps
 
 // ----------------------------------------------------- tensor-core units --
 //
-// A unit is 128 rows of a prompt for two q heads of a kv head, over the prompt's rows up to its own last one.  Roles,
-// barriers, ring and tensor-memory columns are those of the paged prefill kernel (prefill_tcgen05.cuh): two softmax
-// groups of 128 threads, a producer warp, an MMA-issuing warp per tile, one score region that the tiles use in turn.
-// What differs is the stream: 128 rows of K (of V) come in one request of 32 KB instead of eight of 4 KB through a block
-// table, as [half][128 rows][64] with the 128-byte swizzle, and begin at any row.
+// A unit is 128 rows of a prompt for two q heads of a kv head (or one), over the prompt's rows up to its own last one.  Roles and
+// tensor-memory columns are those of the paged prefill kernel (prefill_tcgen05.cuh): two softmax groups of 128 threads, a
+// producer warp, an MMA-issuing warp per tile, one score region that the tiles use in turn.  What differs:
+//   - 128 rows of K (of V) come in one request of 32 KB instead of eight of 4 KB through a block table, as
+//     [half][128 rows][64] with the 128-byte swizzle, and begin at any row.
+//   - A block stays and works through a list of units (the host deals them out, longest first, to the least loaded block).
+//     Barriers and ring run on across units: while a unit's last weights and results are under way, the next one's Q, K and
+//     V come in and its first scores are formed.  With a block a unit those were 3700 clocks of start and 1700 of gap
+//     between blocks, of 12600 for a unit of one step.
+//   - Results leave through shared memory as whole rows (a thread has a row: straight to memory each store touched 32).
 template <int D>
+struct PromptCfg {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kQBytes = kTileM * D * 2, kKvTileBytes = kTileN * D * 2;
+    static constexpr int kSlots = 4;                                  // of the ring of K and V tiles
+    static constexpr int kStageBytes = 32 * 128;                      // a warp's rows on their way out, 64 columns at a time
+    static constexpr int kOffQ = 0;                                   // [2] tiles A, B
+    static constexpr int kOffK = 2 * kQBytes;
+    static constexpr int kOffStage = kOffK + kSlots * kKvTileBytes;
+    static constexpr int kOffBar = kOffStage + 8 * kStageBytes;
+    static constexpr int kSmemBytes = 1024 + kOffBar + 256;
+};
+
+template <int D, int kTiles>
 __global__ void __launch_bounds__(kPrefillThreads, 1)
 prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
                       const __grid_constant__ CUtensorMap v_map, const PromptTile *__restrict__ tiles,
-                      __nv_bfloat16 *__restrict__ out, float *__restrict__ lse_out, int Hq, float scale_log2, int *status,
-                      uint64_t wait_limit_ns) {
-    using Cfg = PrefillCfg<D>;
+                      const int32_t *__restrict__ begin, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse_out, int Hq,
+                      float scale_log2, int *status, uint64_t wait_limit_ns) {
+    using Cfg = PromptCfg<D>;
+    using Cols = PrefillCfg<D>;
+    constexpr int kSlots = Cfg::kSlots;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint64_t *bars = (uint64_t *)(smem + Cfg::kOffBar);
-    uint64_t *q_full = bars + 0;
-    uint64_t *kv_full = bars + 1;                // [kKvSlots]
-    uint64_t *kv_empty = kv_full + kKvSlots;     // [kKvSlots]
-    uint64_t *s_full = kv_empty + kKvSlots;      // [2] per tile
+    uint64_t *q_full = bars + 0;                 // a unit's Q is there
+    uint64_t *q_empty = bars + 1;                // its last scores are formed
+    uint64_t *kv_full = bars + 2;                // [kSlots]
+    uint64_t *kv_empty = kv_full + kSlots;       // [kSlots]
+    uint64_t *s_full = kv_empty + kSlots;        // [2] per tile
     uint64_t *p_full = s_full + 2;               // [2]
     uint64_t *pv_done = p_full + 2;              // [2] O_x += P_x V of a step has completed
     uint64_t *s_out = pv_done + 2;               // [2] tile x's scores have been copied out of the shared region
-    uint32_t *tmem_slot = (uint32_t *)(s_out + 2);
+    uint64_t *o_empty = s_out + 2;               // [2] a unit's O_x has been read
+    uint32_t *tmem_slot = (uint32_t *)(o_empty + 2);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const PromptTile tile = tiles[blockIdx.x];
-    const int n_tiles = tile.q_head_b >= 0 ? 2 : 1;
-    const int pos0 = tile.row0 - tile.start;     // position of the first row in its prompt
-    const int kv_len = pos0 + tile.rows;         // keys the last valid row sees
-    const int n_steps = (kv_len + kTileN - 1) / kTileN;
+    const int first = begin[blockIdx.x], end = begin[blockIdx.x + 1];
+    auto steps_of = [](const PromptTile &t) { return (t.row0 - t.start + t.rows + kTileN - 1) / kTileN; };
 
-    auto load_kv = [&](int n, bool is_k, int j) {
-        const int s = n % kKvSlots;
-        // (rows past the packed batch's last read as zeros; they count)
-        mbar_arrive_expect_tx(&kv_full[s], (uint32_t)Cfg::kKvTileBytes);
-        tma_load_3d(smem + Cfg::kOffK + s * Cfg::kKvTileBytes, is_k ? &k_map : &v_map, &kv_full[s], 0, tile.start + j * kTileN,
-                    tile.kv_head * Cfg::kHalves);
-    };
-    // entry n of the ring, in the order K_0, K_1, V_0, K_2, V_1, ...; it goes to slot n % kKvSlots
-    const int n_entries = 2 * n_steps;
-    auto load_entry = [&](int n) {
-        const bool is_k = n == 0 || ((n & 1) && n < n_entries - 1);
-        load_kv(n, is_k, is_k ? (n + 1) / 2 : (n == n_entries - 1 ? n_steps - 1 : n / 2 - 1));
-    };
-    if (warp == kProducerWarp && lane == 0) {
+    if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
-        for (int s = 0; s < kKvSlots; ++s) {
+        mbar_init(q_empty, kTiles);
+        for (int s = 0; s < kSlots; ++s) {
             mbar_init(&kv_full[s], 1);
-            mbar_init(&kv_empty[s], n_tiles);    // one commit per issuing warp
+            mbar_init(&kv_empty[s], kTiles);     // one commit per issuing warp
         }
         for (int x = 0; x < 2; ++x) {
             mbar_init(&s_full[x], 1);
             mbar_init(&p_full[x], 4);            // one arrival per softmax warp
             mbar_init(&pv_done[x], 1);
             mbar_init(&s_out[x], 4);
+            mbar_init(&o_empty[x], 4);
         }
         *abort_flag = 0;
         fence_barrier_init();
-        griddep_wait();                          // (what comes before reads only the plan)
-        // the first copies are under way while the block gets its tensor memory and meets
-        mbar_arrive_expect_tx(q_full, (uint32_t)(n_tiles * Cfg::kQBytes));
-        tma_load_3d(smem + Cfg::kOffQ, &q_map, q_full, 0, tile.row0, tile.q_head * Cfg::kHalves);
-        load_entry(0);
-        if (n_tiles == 2)
-            tma_load_3d(smem + Cfg::kOffQ + Cfg::kQBytes, &q_map, q_full, 0, tile.row0, tile.q_head_b * Cfg::kHalves);
-        for (int n = 1; n < min(n_entries, kKvSlots); ++n) load_entry(n);
     }
     if (warp == kMmaWarp) {
-        tmem_alloc(tmem_slot, Cfg::kTmemCols);
+        tmem_alloc(tmem_slot, Cols::kTmemCols);
         tmem_relinquish();
     }
     tcgen05_fence_before();
@@ -114,30 +116,51 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
     tcgen05_fence_after();
     const uint32_t tmem = *tmem_slot;
     griddep_launch_dependents();
-    griddep_wait();
+    griddep_wait();                              // the preamble reads only the plan
 
+    // Every role walks the block's units.  u: units so far, n: steps of them; ring entry e is in slot e % kSlots.
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kProducerWarp) {
             // -------------------------------------------------- producer --
             if (lane == 0) {
-                for (int n = kKvSlots; n < n_entries; ++n) {
-                    if (!wait_or_abort(&kv_empty[n % kKvSlots], ((uint32_t)(n / kKvSlots) & 1u) ^ 1u, abort_flag, wait_limit_ns)) {
-                        record_status(status, AP_ERR_TIMEOUT);
-                        *abort_flag = 1;
-                        break;
+                prefetch_tensormap(&q_map);
+                prefetch_tensormap(&k_map);
+                prefetch_tensormap(&v_map);
+                bool ok = true;
+                uint32_t e = 0, u = 0;
+                for (int i = first; ok && i < end; ++i, ++u) {
+                    const PromptTile tile = tiles[i];
+                    const int n_steps = steps_of(tile), n_entries = 2 * n_steps;
+                    if (u > 0 && !wait_or_abort(q_empty, (u - 1) & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
+                    mbar_arrive_expect_tx(q_full, (uint32_t)(kTiles * Cfg::kQBytes));
+                    tma_load_3d(smem + Cfg::kOffQ, &q_map, q_full, 0, tile.row0, tile.q_head * Cfg::kHalves);
+                    if (kTiles == 2)
+                        tma_load_3d(smem + Cfg::kOffQ + Cfg::kQBytes, &q_map, q_full, 0, tile.row0, tile.q_head_b * Cfg::kHalves);
+                    // a unit's entries in the order K_0, K_1, V_0, K_2, V_1, ...
+                    for (int m = 0; m < n_entries; ++m, ++e) {
+                        const bool is_k = m == 0 || ((m & 1) && m < n_entries - 1);
+                        const int j = is_k ? (m + 1) / 2 : (m == n_entries - 1 ? n_steps - 1 : m / 2 - 1);
+                        const uint32_t s = e % kSlots;
+                        if (!wait_or_abort(&kv_empty[s], (e / kSlots & 1u) ^ 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
+                        // (rows past the packed batch's last read as zeros; they count)
+                        mbar_arrive_expect_tx(&kv_full[s], (uint32_t)Cfg::kKvTileBytes);
+                        tma_load_3d(smem + Cfg::kOffK + s * Cfg::kKvTileBytes, is_k ? &k_map : &v_map, &kv_full[s], 0,
+                                    tile.start + j * kTileN, tile.kv_head * Cfg::kHalves);
                     }
-                    load_entry(n);
+                }
+                if (!ok) {
+                    record_status(status, AP_ERR_TIMEOUT);
+                    *abort_flag = 1;
                 }
             }
             __syncwarp();
-        } else if (warp == kMmaWarp || (warp == kMmaWarp + 1 && n_tiles == 2)) {
+        } else if (warp == kMmaWarp || (warp == kMmaWarp + 1 && kTiles == 2)) {
             // ----------------------------------------------- MMA issuers --
             const int x = warp - kMmaWarp;
             const uint32_t leader = elect_one();
             constexpr uint32_t kIdescQK = instr_desc(kTileM, kTileN, false);
             constexpr uint32_t kIdescPV = instr_desc(kTileM, D, true);
-            bool ok = wait_or_abort(q_full, 0, abort_flag, wait_limit_ns);
             // All three operands lie as [half][128 rows][64], 8-row groups 1024 B apart, halves 16 KB apart.
             constexpr uint32_t kHalfBytes = kTileN * 128;
             const uint64_t q_desc0 = smem_desc(smem_u32(smem + Cfg::kOffQ + x * Cfg::kQBytes), 16, 1024);
@@ -146,55 +169,59 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
             const uint32_t q_lo = (uint32_t)q_desc0, q_hi = (uint32_t)(q_desc0 >> 32);
             const uint32_t k_lo = (uint32_t)k_desc0, k_hi = (uint32_t)(k_desc0 >> 32);
             const uint32_t v_lo = (uint32_t)v_desc0, v_hi = (uint32_t)(v_desc0 >> 32);
-            const uint32_t t_s = tmem + Cfg::kColS, t_p = tmem + Cfg::kColP + x * 64, t_o = tmem + Cfg::kColO + x * 128;
-            auto issue_qk = [&](int slot) {
-                const uint32_t b0 = k_lo + (uint32_t)((slot * Cfg::kKvTileBytes) >> 4);
+            const uint32_t t_s = tmem + Cols::kColS, t_p = tmem + Cols::kColP + x * 64, t_o = tmem + Cols::kColO + x * 128;
+            bool ok = true;
+            auto wait = [&](uint64_t *bar, uint32_t phase) {
+                if (ok) ok = wait_or_abort(bar, phase & 1u, abort_flag, wait_limit_ns);
+            };
+            // S = Q_x K^T with K in ring entry `e`, the tile's use number `use` of the score region.  The region passes from
+            // tile to tile through two barriers with one waiter each: scores may be formed once those before them have been
+            // copied out.
+            auto issue_qk = [&](uint32_t e, uint32_t use) {
+                const uint32_t s = e % kSlots;
+                wait(&kv_full[s], e / kSlots);
+                if (kTiles == 2 && x == 1) wait(&s_out[0], use);
+                else if (use > 0) wait(&s_out[kTiles - 1], use - 1);
+                if (!ok) return;
+                tcgen05_fence_after();
+                const uint32_t b0 = k_lo + ((s * Cfg::kKvTileBytes) >> 4);
 #pragma unroll
                 for (int kh = 0; kh < D / 64; ++kh)
                     umma_ss_x4(leader, t_s, q_lo + ((kh * kHalfBytes) >> 4), q_hi, b0 + ((kh * kHalfBytes) >> 4), k_hi, kIdescQK,
                                kh > 0 ? 1u : 0u, 32u >> 4, 32u >> 4);
                 umma_commit(leader, &s_full[x]);
-                umma_commit(leader, &kv_empty[slot]);
+                umma_commit(leader, &kv_empty[s]);
             };
-            auto issue_pv = [&](int slot, bool first_step) {
-                const uint32_t b0 = v_lo + (uint32_t)((slot * Cfg::kKvTileBytes) >> 4);
-                constexpr uint32_t kVStep = (2 * 1024) >> 4;                       // 16 keys of V
-#pragma unroll
-                for (int kq = 0; kq < kTileN / 64; ++kq)
-                    umma_ts_x4(leader, t_o, t_p + kq * 32, b0 + kq * 4 * kVStep, v_hi, kIdescPV, (first_step && kq == 0) ? 0u : 1u, 8u,
-                               kVStep);
-                umma_commit(leader, &pv_done[x]);
-                umma_commit(leader, &kv_empty[slot]);
-            };
-            // The score region passes from tile to tile through two barriers with one waiter each: S_x(step) may be
-            // issued once the scores written before it have been copied out.
-            auto wait_s_free = [&](int step) {
-                if (n_tiles == 2 && x == 1) return wait_or_abort(&s_out[0], (uint32_t)step & 1u, abort_flag, wait_limit_ns);
-                if (step == 0) return true;
-                return wait_or_abort(&s_out[n_tiles - 1], (uint32_t)(step - 1) & 1u, abort_flag, wait_limit_ns);
-            };
-            if (ok) ok = wait_or_abort(&kv_full[0], 0, abort_flag, wait_limit_ns);
-            if (ok) ok = wait_s_free(0);
-            if (ok) {
-                tcgen05_fence_after();
-                issue_qk(0);
-            }
-            for (int j = 0; ok && j < n_steps; ++j) {
-                const int nv = kv_seq_v(j, n_steps), nk = kv_seq_k(j + 1);
-                if (j + 1 < n_steps) {           // the next scores of the tile go ahead of this step's P V
-                    if (!wait_or_abort(&kv_full[nk % kKvSlots], (uint32_t)(nk / kKvSlots) & 1u, abort_flag, wait_limit_ns) ||
-                        !wait_s_free(j + 1)) { ok = false; break; }
+            uint32_t e0 = 0, n = 0, u = 0;
+            for (int i = first; ok && i < end; ++i, ++u) {
+                const PromptTile tile = tiles[i];
+                const int n_steps = steps_of(tile);
+                wait(q_full, u);
+                issue_qk(e0, n);
+                if (n_steps == 1 && ok) umma_commit(leader, q_empty);
+                for (int j = 0; ok && j < n_steps; ++j) {
+                    if (j + 1 < n_steps) {           // the next scores of the tile go ahead of this step's P V
+                        issue_qk(e0 + (uint32_t)kv_seq_k(j + 1), n + j + 1);
+                        if (j + 2 == n_steps && ok) umma_commit(leader, q_empty);
+                    }
+                    const uint32_t ev = e0 + (uint32_t)kv_seq_v(j, n_steps), s = ev % kSlots;
+                    wait(&kv_full[s], ev / kSlots);
+                    wait(&p_full[x], n + j);
+                    if (j == 0 && u > 0) wait(&o_empty[x], u - 1);
+                    if (!ok) break;
                     tcgen05_fence_after();
-                    issue_qk(nk % kKvSlots);
+                    // O_x += P_x V, 16 keys an instruction: 8 columns of P, 2 groups of 8 rows of V
+                    const uint32_t b0 = v_lo + ((s * Cfg::kKvTileBytes) >> 4);
+                    constexpr uint32_t kVStep = (2 * 1024) >> 4;
+#pragma unroll
+                    for (int kq = 0; kq < kTileN / 64; ++kq)
+                        umma_ts_x4(leader, t_o, t_p + kq * 32, b0 + kq * 4 * kVStep, v_hi, kIdescPV, (j == 0 && kq == 0) ? 0u : 1u, 8u,
+                                   kVStep);
+                    umma_commit(leader, &pv_done[x]);
+                    umma_commit(leader, &kv_empty[s]);
                 }
-                if (!wait_or_abort(&kv_full[nv % kKvSlots], (uint32_t)(nv / kKvSlots) & 1u, abort_flag, wait_limit_ns) ||
-                    !wait_or_abort(&p_full[x], (uint32_t)j & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
-                // In the last step tile A's group clears the V rows past the unit's last key before it hands P_A over;
-                // tile B's product reads the same V tile and has to see that too.
-                if (x == 1 && j == n_steps - 1 && kv_len < n_steps * kTileN &&
-                    !wait_or_abort(&p_full[0], (uint32_t)j & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
-                tcgen05_fence_after();
-                issue_pv(nv % kKvSlots, j == 0);
+                e0 += 2 * n_steps;
+                n += n_steps;
             }
             if (!ok && leader) {
                 record_status(status, AP_ERR_TIMEOUT);
@@ -206,133 +233,148 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ------------------------------------------------------- softmax --
         const int x = warp >> 2;                                     // tile A or B
-        if (x < n_tiles) {
+        if (x < kTiles) {
             const int r = threadIdx.x & 127;                         // query row = TMEM lane
-            const int q_head = x == 0 ? tile.q_head : tile.q_head_b;
             const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-            const uint32_t col_s = Cfg::kColS, col_p = Cfg::kColP + x * 64, col_o = Cfg::kColO + x * 128;
-            const int my_pos = min(pos0 + r, kv_len - 1);            // last key this row sees
-            float m_used = -INFINITY, l = 0.f;
+            const uint32_t col_s = Cols::kColS, col_p = Cols::kColP + x * 64, col_o = Cols::kColO + x * 128;
             bool ok = true;
-            for (int j = 0; j < n_steps; ++j) {
-                // S_x(j) complete: copy this row's 128 scores out and give the region back at once
-                if (!wait_or_abort(&s_full[x], (uint32_t)j & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
-                tcgen05_fence_after();
-                uint32_t sreg[4][32];
+            uint32_t n = 0, e0 = 0;
+            for (int i = first; ok && i < end; ++i) {
+                const PromptTile tile = tiles[i];
+                const int pos0 = tile.row0 - tile.start;             // position of the first row in its prompt
+                const int kv_len = pos0 + tile.rows, n_steps = steps_of(tile);
+                const int q_head = x == 0 ? tile.q_head : tile.q_head_b;
+                const int my_pos = min(pos0 + r, kv_len - 1);        // last key this row sees
+                float m_used = -INFINITY, l = 0.f;
+                for (int j = 0; j < n_steps; ++j) {
+                    // S_x(j) complete: copy this row's 128 scores out and give the region back at once
+                    if (!wait_or_abort(&s_full[x], (n + j) & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
+                    tcgen05_fence_after();
+                    uint32_t sreg[4][32];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(lane_addr + col_s + c * 32, sreg[c]);
+                    for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(lane_addr + col_s + c * 32, sreg[c]);
+                    tmem_ld_wait();
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&s_out[x]);
+                    const int tok0 = j * kTileN;
+                    float mx = -INFINITY;
+                    if (tok0 + kTileN - 1 > pos0) {
+                        // diagonal or last step: one bit per key says whether the row sees it
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const uint32_t seen = prefill::low_bits(my_pos + 1 - (tok0 + c * 32));
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (!(seen >> k & 1u)) sreg[c][k] = 0xFF800000u;            // -inf
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int k = 0; k < 32; k += 2)
+                            mx = max3(mx, __uint_as_float(sreg[c][k]), __uint_as_float(sreg[c][k + 1]));
+                    // P_x and O_x belong to the tensor pipe until O_x += P_x V of the step before is done
+                    if (j > 0) {
+                        if (!wait_or_abort(&pv_done[x], (n + j - 1) & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
+                        tcgen05_fence_after();
+                    }
+                    // Keep the old reference max unless some row of the warp moved by more than the threshold: P stays
+                    // bounded by 2^threshold and O needs no rescale most steps.
+                    const float m_new = max2(m_used, mx);
+                    const bool rescale = __any_sync(0xffffffffu, (m_new - m_used) * scale_log2 > kRescaleThreshold);   // (true on the first step)
+                    float alpha = 1.f;
+                    if (rescale) {
+                        alpha = exp2_approx((m_used - m_new) * scale_log2);   // 0 on the first step
+                        m_used = m_new;
+                        if (j > 0) rescale_o<D>(lane_addr + col_o, alpha);
+                    }
+                    const float ms = fmaf(m_used, scale_log2, m_new - m_new);   // (a NaN score makes the row NaN)
+                    const float2 sc2 = make_float2(scale_log2, scale_log2), nms2 = make_float2(-ms, -ms);
+                    float2 sum2 = make_float2(0.f, 0.f);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t preg[32];                                  // 64 keys as bf16 pairs
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            float2 xy = __ffma2_rn(make_float2(__uint_as_float(sreg[2 * c + (k >> 4)][(2 * k) & 31]),
+                                                               __uint_as_float(sreg[2 * c + (k >> 4)][(2 * k + 1) & 31])),
+                                                   sc2, nms2);
+                            // one pair in eight goes to the FMA pipe instead of the special-function unit
+                            if ((k & 7) == 7) {
+                                xy = exp2_poly2<true>(xy);
+                            } else {
+                                xy.x = exp2_approx(xy.x);
+                                xy.y = exp2_approx(xy.y);
+                            }
+                            // (the sum takes the weights as they are; P V takes them in bf16, each off by at most 2^-8 of itself)
+                            sum2 = __fadd2_rn(sum2, xy);
+                            preg[k] = pack_bf16x2(xy.x, xy.y);
+                        }
+                        tmem_st_32x32b_x32(lane_addr + col_p + c * 32, preg);
+                    }
+                    l = l * alpha + (sum2.x + sum2.y);
+                    tmem_st_wait();
+                    if (j == n_steps - 1 && kv_len < n_steps * kTileN) {
+                        // Rows past the unit's last key belong to nobody it serves (the next prompt's, or none): 0 * V must be 0.
+                        // Both tiles' groups clear them (the same zeros) before they hand their own P over: a tile that waited
+                        // for the other's hand-over could find it two phases on.
+                        const uint32_t ev = e0 + (uint32_t)kv_seq_v(j, n_steps), s = ev % kSlots;
+                        if (!wait_or_abort(&kv_full[s], ev / kSlots & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
+                        uint8_t *v_tile = smem + Cfg::kOffK + s * Cfg::kKvTileBytes;
+                        const int past = kv_len - tok0;
+                        for (int idx = r; idx < (kTileN - past) * (D / 8); idx += 128) {
+                            const int key = past + idx / (D / 8), ch = idx % (D / 8);
+                            *(uint4 *)(v_tile + (ch >> 3) * (kTileN * 128) + key * 128 + ((ch & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_proxy_async_smem();
+                    }
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_full[x]);
+                }
+                if (ok) ok = wait_or_abort(&pv_done[x], (n + n_steps - 1) & 1u, abort_flag, wait_limit_ns);
+                if (!ok) break;
+                tcgen05_fence_after();
+                uint32_t oreg[D / 32][32];
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) tmem_ld_32x32b_x32(lane_addr + col_o + c * 32, oreg[c]);
                 tmem_ld_wait();
                 tcgen05_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&s_out[x]);
-                const int tok0 = j * kTileN;
-                float mx = -INFINITY;
-                if (tok0 + kTileN - 1 > pos0) {
-                    // diagonal or last step: one bit per key says whether the row sees it
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const uint32_t seen = prefill::low_bits(my_pos + 1 - (tok0 + c * 32));
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (!(seen >> i & 1u)) sreg[c][i] = 0xFF800000u;            // -inf
-                    }
-                }
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2)
-                        mx = max3(mx, __uint_as_float(sreg[c][i]), __uint_as_float(sreg[c][i + 1]));
-                // P_x and O_x belong to the tensor pipe until O_x += P_x V of the step before is done
-                if (j > 0) {
-                    if (!wait_or_abort(&pv_done[x], (uint32_t)(j - 1) & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
-                    tcgen05_fence_after();
-                }
-                // Keep the old reference max unless some row of the warp moved by more than the threshold: P stays
-                // bounded by 2^threshold and O needs no rescale most steps.
-                const float m_new = max2(m_used, mx);
-                const bool rescale = __any_sync(0xffffffffu, (m_new - m_used) * scale_log2 > kRescaleThreshold);   // (true on the first step)
-                float alpha = 1.f;
-                if (rescale) {
-                    alpha = exp2_approx((m_used - m_new) * scale_log2);   // 0 on the first step
-                    m_used = m_new;
-                    if (j > 0) rescale_o<D>(lane_addr + col_o, alpha);
-                }
-                const float ms = fmaf(m_used, scale_log2, m_new - m_new);   // (a NaN score makes the row NaN)
-                const float2 sc2 = make_float2(scale_log2, scale_log2), nms2 = make_float2(-ms, -ms);
-                float2 sum2 = make_float2(0.f, 0.f);
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t preg[32];                                  // 64 keys as bf16 pairs
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        float2 xy = __ffma2_rn(make_float2(__uint_as_float(sreg[2 * c + (i >> 4)][(2 * i) & 31]),
-                                                           __uint_as_float(sreg[2 * c + (i >> 4)][(2 * i + 1) & 31])),
-                                               sc2, nms2);
-                        // one pair in eight goes to the FMA pipe instead of the special-function unit
-                        if ((i & 7) == 7) {
-                            xy = exp2_poly2<true>(xy);
-                        } else {
-                            xy.x = exp2_approx(xy.x);
-                            xy.y = exp2_approx(xy.y);
-                        }
-                        // (the sum takes the weights as they are; P V takes them in bf16, each off by at most 2^-8 of itself)
-                        sum2 = __fadd2_rn(sum2, xy);
-                        preg[i] = pack_bf16x2(xy.x, xy.y);
-                    }
-                    tmem_st_32x32b_x32(lane_addr + col_p + c * 32, preg);
-                }
-                l = l * alpha + (sum2.x + sum2.y);
-                tmem_st_wait();
-                if (x == 0 && j == n_steps - 1 && kv_len < n_steps * kTileN) {
-                    // rows past the unit's last key belong to nobody it serves (the next prompt's, or none): 0 * V must be 0
-                    const int nv = kv_seq_v(j, n_steps), s = nv % kKvSlots;
-                    if (!wait_or_abort(&kv_full[s], (uint32_t)(nv / kKvSlots) & 1u, abort_flag, wait_limit_ns)) { ok = false; break; }
-                    uint8_t *v_tile = smem + Cfg::kOffK + s * Cfg::kKvTileBytes;
-                    const int first = kv_len - tok0;
-                    for (int idx = r; idx < (kTileN - first) * (D / 8); idx += 128) {
-                        const int key = first + idx / (D / 8), ch = idx % (D / 8);
-                        *(uint4 *)(v_tile + (ch >> 3) * (kTileN * 128) + key * 128 + ((ch & 7) << 4)) = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_proxy_async_smem();
-                }
-                tcgen05_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[x]);
-            }
-            if (ok && wait_or_abort(&pv_done[x], (uint32_t)(n_steps - 1) & 1u, abort_flag, wait_limit_ns)) {
-                tcgen05_fence_after();
+                if (lane == 0) mbar_arrive(&o_empty[x]);             // (the next unit's products may begin)
                 const float inv = 1.f / l;
-                const bool valid = r < tile.rows;
-                // A thread has a row: straight to memory every store would touch 32 rows.  The warp's rows go through this
-                // tile's Q (all products with it are through), 16-byte pieces of row r at piece ^ (r & 7), and out as whole rows.
-                uint8_t *rows = smem + Cfg::kOffQ + x * Cfg::kQBytes + (warp & 3) * 32 * (D * 2);
+                // 64 columns of the warp's rows at a time: 16-byte pieces of row r at piece ^ (r & 7), then out as whole rows
+                uint8_t *rows = smem + Cfg::kOffStage + warp * Cfg::kStageBytes;
+                __nv_bfloat16 *to = out + ((size_t)(tile.row0 + (warp & 3) * 32 + (lane >> 3)) * Hq + q_head) * D + (lane & 7) * 8;
+                const int rows_left = tile.rows - (warp & 3) * 32;
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t oreg[32];
-                    tmem_ld_32x32b_x32(lane_addr + col_o + c * 32, oreg);
-                    tmem_ld_wait();
+                for (int half = 0; half < D / 64; ++half) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
+                    for (int c = 0; c < 8; ++c) {
+                        const uint32_t *o = &oreg[2 * half + c / 4][c % 4 * 8];
                         uint4 v;
-                        v.x = pack_bf16x2(__uint_as_float(oreg[i]) * inv, __uint_as_float(oreg[i + 1]) * inv);
-                        v.y = pack_bf16x2(__uint_as_float(oreg[i + 2]) * inv, __uint_as_float(oreg[i + 3]) * inv);
-                        v.z = pack_bf16x2(__uint_as_float(oreg[i + 4]) * inv, __uint_as_float(oreg[i + 5]) * inv);
-                        v.w = pack_bf16x2(__uint_as_float(oreg[i + 6]) * inv, __uint_as_float(oreg[i + 7]) * inv);
-                        *(uint4 *)(rows + lane * (D * 2) + (((c * 4 + i / 8) ^ (lane & 7)) << 4)) = v;
+                        v.x = pack_bf16x2(__uint_as_float(o[0]) * inv, __uint_as_float(o[1]) * inv);
+                        v.y = pack_bf16x2(__uint_as_float(o[2]) * inv, __uint_as_float(o[3]) * inv);
+                        v.z = pack_bf16x2(__uint_as_float(o[4]) * inv, __uint_as_float(o[5]) * inv);
+                        v.w = pack_bf16x2(__uint_as_float(o[6]) * inv, __uint_as_float(o[7]) * inv);
+                        *(uint4 *)(rows + lane * 128 + ((c ^ (lane & 7)) << 4)) = v;
                     }
-                }
-                __syncwarp();
-                constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces;   // 16-byte pieces of a row, rows of a store
-                __nv_bfloat16 *to = out + ((size_t)(tile.row0 + (warp & 3) * 32 + lane / kPieces) * Hq + q_head) * D + lane % kPieces * 8;
+                    __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 32; i += kAtOnce, to += (size_t)kAtOnce * Hq * D) {
-                    const int row = i + lane / kPieces;
-                    if ((warp & 3) * 32 + row < tile.rows)
-                        *(uint4 *)to = *(const uint4 *)(rows + row * (D * 2) + ((lane % kPieces ^ (row & 7)) << 4));
+                    for (int k = 0; k < 32; k += 4) {
+                        const int row = k + (lane >> 3);
+                        if (row < rows_left)
+                            *(uint4 *)(to + (size_t)k * Hq * D + half * 64) = *(const uint4 *)(rows + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+                    }
+                    __syncwarp();
                 }
-                if (valid && lse_out)
+                if (r < tile.rows && lse_out)
                     lse_out[(size_t)(tile.row0 + r) * Hq + q_head] = (m_used * scale_log2 + log2f(l)) * 0.6931471805599453f;
-            } else {
+                n += n_steps;
+                e0 += 2 * n_steps;
+            }
+            if (!ok) {
                 record_status(status, AP_ERR_TIMEOUT);
                 *abort_flag = 1;
             }
@@ -341,7 +383,7 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
 
     tcgen05_fence_before();
     __syncthreads();
-    if (warp == kMmaWarp) tmem_dealloc(tmem, Cfg::kTmemCols);
+    if (warp == kMmaWarp) tmem_dealloc(tmem, Cols::kTmemCols);
 }
 
 // ---------------------------------------------------------- short prompts --
@@ -497,11 +539,13 @@ prompt_short_kernel(const ShortPrompt *__restrict__ prompts, const uint16_t *q, 
 template <int D>
 cudaError_t launch_prompt_t(const ap_kv_pool *pool, const ap_prompt_plan *plan, const void *q, const void *k, const void *v,
                             void *out, float *lse, const ap_prompt_strides &st, cudaStream_t stream) {
-    using Cfg = PrefillCfg<D>;
+    using Cfg = PromptCfg<D>;
     static bool configured[64] = {};
     const int dev = pool->desc.device & 63;
     if (!configured[dev]) {
-        cudaError_t e = cudaFuncSetAttribute(prompt_tcgen05_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
+        cudaError_t e = cudaFuncSetAttribute(prompt_tcgen05_kernel<D, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(prompt_tcgen05_kernel<D, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(prompt_short_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(ShortSmem<D>));
         if (e != cudaSuccess) return e;
@@ -516,15 +560,45 @@ cudaError_t launch_prompt_t(const ap_kv_pool *pool, const ap_prompt_plan *plan, 
             encode_rows_tensor_map(&k_map, k, plan->info.n_rows, Hkv, D, st.k_row_stride) != AP_OK ||
             encode_rows_tensor_map(&v_map, v, plan->info.n_rows, Hkv, D, st.v_row_stride) != AP_OK)
             return cudaErrorInvalidValue;
-        e = launch_overlapped(prompt_tcgen05_kernel<D>, (unsigned)plan->info.tiles, (unsigned)kPrefillThreads, (size_t)Cfg::kSmemBytes,
-                              stream, q_map, k_map, v_map, plan->d_tiles, (__nv_bfloat16 *)out, lse, Hq, scale_log2, pool->status_dev,
-                              pool->wait_limit_ns);
+        for (int t = 2; t >= 1 && e == cudaSuccess; --t) {
+            const PromptLists &l = plan->lists[t - 1];
+            if (l.blocks > 0)
+                e = launch_overlapped(t == 2 ? prompt_tcgen05_kernel<D, 2> : prompt_tcgen05_kernel<D, 1>, (unsigned)l.blocks,
+                                      (unsigned)kPrefillThreads, (size_t)Cfg::kSmemBytes, stream, q_map, k_map, v_map, l.tiles, l.begin,
+                                      (__nv_bfloat16 *)out, lse, Hq, scale_log2, pool->status_dev, pool->wait_limit_ns);
+        }
     }
     if (e == cudaSuccess && plan->info.short_units > 0)
         e = launch_overlapped(prompt_short_kernel<D>, (unsigned)plan->info.short_units, 32u * kShortWarps, sizeof(ShortSmem<D>), stream,
                               plan->d_short, (const uint16_t *)q, (const uint16_t *)k, (const uint16_t *)v, (uint16_t *)out, lse, Hq, Hkv,
                               st.q_row_stride, st.k_row_stride, st.v_row_stride, scale_log2);
     return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+// Units to blocks, one block an SM: the longest first, each to the block with the least to do.  A unit takes its steps and
+// about two more (results out, first softmax).
+void deal_out(std::vector<PromptTile> &tiles, int sms, std::vector<PromptTile> *dealt, std::vector<int32_t> *begin) {
+    if (tiles.empty()) return;
+    auto steps = [](const PromptTile &t) { return (t.row0 - t.start + t.rows + kTileN - 1) / kTileN; };
+    std::stable_sort(tiles.begin(), tiles.end(), [&](const PromptTile &x, const PromptTile &y) { return steps(x) > steps(y); });
+    const size_t blocks = std::min<size_t>(tiles.size(), (size_t)std::max(1, sms));
+    std::vector<std::pair<int64_t, int32_t>> load;       // (steps so far, block), the least on top
+    for (size_t i = 0; i < blocks; ++i) load.push_back({0, (int32_t)i});
+    std::vector<int32_t> of(tiles.size()), count(blocks, 0);
+    auto more = std::greater<std::pair<int64_t, int32_t>>();
+    std::make_heap(load.begin(), load.end(), more);
+    for (size_t i = 0; i < tiles.size(); ++i) {
+        std::pop_heap(load.begin(), load.end(), more);
+        of[i] = load.back().second;
+        ++count[(size_t)of[i]];
+        load.back().first += steps(tiles[i]) + kUnitSteps;
+        std::push_heap(load.begin(), load.end(), more);
+    }
+    begin->assign(blocks + 1, 0);
+    for (size_t i = 0; i < blocks; ++i) (*begin)[i + 1] = (*begin)[i] + count[i];
+    std::vector<int32_t> next(begin->begin(), begin->end() - 1);
+    dealt->resize(tiles.size());
+    for (size_t i = 0; i < tiles.size(); ++i) (*dealt)[(size_t)next[(size_t)of[i]]++] = tiles[i];
 }
 
 int plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *b, void *stream) {
@@ -547,9 +621,8 @@ int plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *b,
     }
     // (row numbers of a last tile's keys, past the end of the batch, stay within 32 bits)
     if (rows > (int64_t)1 << 30 || tiles_n > (int64_t)1 << 27 || shorts_n * Hkv >= (int64_t)1 << 31) return AP_ERR_UNSUPPORTED;
-    std::vector<PromptTile> tiles;
+    std::vector<PromptTile> tiles[2];                    // units of one tile, of two
     std::vector<ShortPrompt> shorts;
-    tiles.reserve((size_t)tiles_n);
     shorts.reserve((size_t)shorts_n);
     int32_t start = 0;
     for (int s = 0; s < b->batch; ++s) {
@@ -557,30 +630,42 @@ int plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *b,
         if (n > kShortRows) {
             for (int32_t t0 = 0; t0 < n; t0 += kTileM)
                 for (int kv = 0; kv < Hkv; ++kv)
-                    for (int g = 0; g < G; g += 2)
-                        tiles.push_back({start + t0, std::min(kTileM, n - t0), start, kv * G + g, g + 1 < G ? kv * G + g + 1 : -1, kv, {0, 0}});
+                    for (int g = 0; g < G; g += 2) {
+                        const bool two = g + 1 < G;
+                        tiles[two].push_back({start + t0, std::min(kTileM, n - t0), start, kv * G + g, two ? kv * G + g + 1 : -1, kv, {0, 0}});
+                    }
         } else if (n > 0) {
             const int blocks = (n + 15) / 16;
             for (int b1 = blocks; b1 > 0; b1 -= short_blocks) shorts.push_back({start, n, std::max(0, b1 - short_blocks), b1});
         }
         start += n;
     }
-    // longest first: blocks are handed out in order.  Units of the same steps stay together (they share K and V in the L2).
-    std::stable_sort(tiles.begin(), tiles.end(), [](const PromptTile &x, const PromptTile &y) {
-        return (x.row0 - x.start + x.rows + kTileN - 1) / kTileN > (y.row0 - y.start + y.rows + kTileN - 1) / kTileN;
-    });
     std::stable_sort(shorts.begin(), shorts.end(), [](const ShortPrompt &x, const ShortPrompt &y) { return x.block1 > y.block1; });
+    std::vector<PromptTile> dealt[2];
+    std::vector<int32_t> begin[2];
+    for (int t = 0; t < 2; ++t) deal_out(tiles[t], pool->sm_count, &dealt[t], &begin[t]);
 
     ap_prompt_plan *plan = new (std::nothrow) ap_prompt_plan();
     if (!plan) return AP_ERR_CUDA;
-    const size_t tile_ints = tiles.size() * (sizeof(PromptTile) / 4), ints = tile_ints + shorts.size() * (sizeof(ShortPrompt) / 4);
+    size_t ints = shorts.size() * (sizeof(ShortPrompt) / 4), at[2];
+    for (int t = 0; t < 2; ++t) {
+        at[t] = ints;                                    // the units, then where each block's begin
+        ints += (dealt[t].size() * (sizeof(PromptTile) / 4) + begin[t].size() + 7) / 8 * 8;
+    }
     if (pool->desc.device >= 0 && ints > 0) {
         DeviceGuard guard(pool->desc.device);
         if (!guard.ok) { delete plan; return AP_ERR_CUDA; }
         const int rc = acquire_plan_buffer(pool->plan_buffers, ints, &plan->buf);
         if (rc != AP_OK) { delete plan; return rc; }
-        if (!tiles.empty()) std::memcpy(plan->buf.host, tiles.data(), tiles.size() * sizeof(PromptTile));
-        if (!shorts.empty()) std::memcpy(plan->buf.host + tile_ints, shorts.data(), shorts.size() * sizeof(ShortPrompt));
+        if (!shorts.empty()) std::memcpy(plan->buf.host, shorts.data(), shorts.size() * sizeof(ShortPrompt));
+        plan->d_short = (const ShortPrompt *)plan->buf.dev;
+        for (int t = 0; t < 2; ++t) {
+            if (dealt[t].empty()) continue;
+            const size_t tile_ints = dealt[t].size() * (sizeof(PromptTile) / 4);
+            std::memcpy(plan->buf.host + at[t], dealt[t].data(), tile_ints * 4);
+            std::memcpy(plan->buf.host + at[t] + tile_ints, begin[t].data(), begin[t].size() * 4);
+            plan->lists[t] = {(const PromptTile *)(plan->buf.dev + at[t]), plan->buf.dev + at[t] + tile_ints, (int)begin[t].size() - 1};
+        }
         cudaStream_t st = (cudaStream_t)stream;
         if (cudaMemcpyAsync(plan->buf.dev, plan->buf.host, ints * 4, cudaMemcpyHostToDevice, st) != cudaSuccess ||
             cudaEventRecord(plan->buf.uploaded, st) != cudaSuccess) {
@@ -589,17 +674,15 @@ int plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *b,
             delete plan;
             return AP_ERR_CUDA;
         }
-        plan->d_tiles = (const PromptTile *)plan->buf.dev;
-        plan->d_short = (const ShortPrompt *)(plan->buf.dev + tile_ints);
     }
     plan->pool = pool;
     plan->num_q_heads = Hq;
     plan->scale = b->softmax_scale > 0.f ? b->softmax_scale : 1.0f / std::sqrt((float)d);
     plan->info.n_rows = rows;
     plan->info.pairs = pairs;
-    plan->info.tiles = (int64_t)tiles.size();
+    plan->info.tiles = (int64_t)(dealt[0].size() + dealt[1].size());
     plan->info.short_units = (int64_t)shorts.size() * Hkv;
-    plan->info.launches = (tiles.empty() ? 0 : 1) + (shorts.empty() ? 0 : 1);
+    plan->info.launches = (dealt[0].empty() ? 0 : 1) + (dealt[1].empty() ? 0 : 1) + (shorts.empty() ? 0 : 1);
     *out = plan;
     return AP_OK;
 }

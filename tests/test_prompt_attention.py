@@ -70,7 +70,7 @@ def test_refusals():
             ap.prompt_plan_create(pool, bad, 8)
     plan = ap.prompt_plan_create(pool, [3, 0, 200, 64, 65], 6)
     info = ap.prompt_plan_get_info(plan)
-    assert info["n_rows"] == 332 and info["pairs"] == sum(n * (n + 1) // 2 for n in (3, 200, 64, 65)) and info["launches"] == 2
+    assert info["n_rows"] == 332 and info["pairs"] == sum(n * (n + 1) // 2 for n in (3, 200, 64, 65)) and info["launches"] == 3
     assert info["tiles"] == 3 * 2 * 2 and info["short_units"] == 5 * 2     # (heads 0-2: two units; blocks of 16 rows; two kv heads)
 
     def status(pool_=pool, strides=True, **kw):
