@@ -52,7 +52,7 @@ struct Walk {
     static constexpr int kWarps = 1, kBlocks = 16;
     // staging: a lane takes two channels next to one another
     static constexpr int kTwos = kCh / 2, kRowsAtOnce = 32 / kTwos, kPasses = kTile / kRowsAtOnce;
-    static_assert(H % 4 == 0 && kCh >= 4 && kTile % kRowsAtOnce == 0, "");
+    static_assert(H == 8 && kCh >= 4 && kTile % kRowsAtOnce == 0, "eight states a lane: a 16-byte piece of b");
 };
 
 __device__ __forceinline__ float2 widen2(uint32_t v) {
@@ -166,11 +166,12 @@ constexpr int kHeldStates = 8;
 
 template <int N, int H>
 struct WalkSmem {                                              // a warp's own
-    alignas(16) uint16_t x[kTile][Walk<N, H>::kCh], dt[kTile][Walk<N, H>::kCh], z[kTile][Walk<N, H>::kCh];
+    alignas(16) uint16_t x[2][kTile][Walk<N, H>::kCh];         // (read again with the gates, while the next tile's comes in)
+    alignas(16) uint16_t dt[kTile][Walk<N, H>::kCh], z[kTile][Walk<N, H>::kCh];
     alignas(16) uint16_t b_in[kTile][N], c_in[kTile][N];
-    alignas(16) float b[kTile][N], c[kTile][N];
+    float4 b[2][kTile][N / 8], c[2][kTile][N / 8];             // [h]: states 8 i + 4 h .. + 3
     alignas(16) float2 step[kTile][Walk<N, H>::kCh];           // d and d x
-    alignas(16) float y[kTile][Walk<N, H>::kCh];              // d_skip x, then the row's result before the gate
+    alignas(16) float y[kTile][Walk<N, H>::kCh];
     float bias[Walk<N, H>::kCh], skip[Walk<N, H>::kCh];
 };
 
@@ -198,10 +199,10 @@ struct Copy {
         to = tile + row * kCols + e;
         this->rows = col + e < end && row < kTile ? rows : 0;
     }
-    __device__ __forceinline__ void tile(int t0) {
+    __device__ __forceinline__ void tile(int t0, int place = 0) {         // (place: of tiles next to one another)
 #pragma unroll
         for (int i = 0; i < kRounds; ++i)
-            if (t0 + row + i * kRows < rows) copy_async<2 * kSize>(to + i * kRows * kCols, from + i * kRows * stride);
+            if (t0 + row + i * kRows < rows) copy_async<2 * kSize>(to + (place * kTile + i * kRows) * kCols, from + i * kRows * stride);
         from += kTile * stride;
     }
 };
@@ -275,13 +276,13 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
     // Asynchronous copies of a tile's rows into shared memory, a tile a call.  Rows past the unit are left as they are, and not
     // used.
     constexpr int kAsync = S::kCh >= 8 ? 8 : S::kCh;           // channels of a copy
-    Copy<S::kCh, kAsync> copy_x(lane, &sm.x[0][0], g.x, g.xs, row0, c0, D, rows_all);
+    Copy<S::kCh, kAsync> copy_x(lane, &sm.x[0][0][0], g.x, g.xs, row0, c0, D, rows_all);
     Copy<S::kCh, kAsync> copy_dt(lane, &sm.dt[0][0], g.dt, g.dts, row0, c0, D, rows_all);
     Copy<S::kCh, kAsync> copy_z(lane, &sm.z[0][0], g.z, g.zs, row0, c0, D, kStateOnly || !g.z ? 0 : rows_all);
     Copy<N, 8> copy_b(lane, &sm.b_in[0][0], g.b, g.bs, row0, 0, N, rows_all);
     Copy<N, 8> copy_c(lane, &sm.c_in[0][0], g.c, g.cs, row0, 0, N, kStateOnly ? 0 : rows_all);
     auto copy_in = [&](int t0) {
-        copy_x.tile(t0);
+        copy_x.tile(t0, t0 / kTile & 1);
         copy_dt.tile(t0);
         copy_b.tile(t0);
         if (!kStateOnly) copy_c.tile(t0);
@@ -289,7 +290,7 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
     };
     copy_in(0);
     for (int t0 = 0; t0 < rows_all; t0 += kTile) {
-        const int rows = min(kTile, rows_all - t0);
+        const int rows = min(kTile, rows_all - t0), place = t0 / kTile & 1;
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncwarp();
         // the gates are wanted last: they come while the rows are walked
@@ -299,28 +300,26 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
 #pragma unroll
         for (int i = lane; i < kTile * N / 8; i += 32) {
             const bool past = i * 8 / N >= rows;
-            auto widen8 = [&](const uint16_t *from, float *to) {
+            auto widen8 = [&](const uint16_t *from, float4 *to) {
                 uint4 v = *(const uint4 *)from;
                 if (past) v = make_uint4(0, 0, 0, 0);
                 const float2 a = widen2(v.x), b = widen2(v.y), c = widen2(v.z), d = widen2(v.w);
-                *(float4 *)to = make_float4(a.x, a.y, b.x, b.y);
-                *(float4 *)(to + 4) = make_float4(c.x, c.y, d.x, d.y);
+                to[0] = make_float4(a.x, a.y, b.x, b.y);
+                to[kTile * N / 8] = make_float4(c.x, c.y, d.x, d.y);
             };
-            widen8(&sm.b_in[0][0] + i * 8, &sm.b[0][0] + i * 8);
-            if (!kStateOnly) widen8(&sm.c_in[0][0] + i * 8, &sm.c[0][0] + i * 8);
+            widen8(&sm.b_in[0][0] + i * 8, &sm.b[0][0][0] + i);
+            if (!kStateOnly) widen8(&sm.c_in[0][0] + i * 8, &sm.c[0][0][0] + i);
         }
         // every row's step and step times input
         float longest = 0.f;
         {
-            const float2 bias = *(const float2 *)&sm.bias[two], skip = *(const float2 *)&sm.skip[two];
+            const float2 bias = *(const float2 *)&sm.bias[two];
 #pragma unroll
             for (int p = 0; p < S::kPasses; ++p) {
                 const int r = p * S::kRowsAtOnce + row_in;
                 float2 d = __fadd2_rn(widen2(*(const uint32_t *)&sm.dt[r][two]), bias);
                 if (g.softplus) d = softplus2(d);
-                const float2 x = widen2(*(const uint32_t *)&sm.x[r][two]);
-                float2 dx = __fmul2_rn(d, x);
-                if (!kStateOnly) *(float2 *)&sm.y[r][two] = __fmul2_rn(skip, x);
+                float2 dx = __fmul2_rn(d, widen2(*(const uint32_t *)&sm.x[place][r][two]));
                 if (rows < kTile && r >= rows) d = dx = make_float2(0.f, 0.f);      // (past the end the state stays as it is)
                 longest = max3_nan(longest, fabsf(d.x), fabsf(d.y));
                 if (kStateOnly) total = __fadd2_rn(total, d);
@@ -342,10 +341,10 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
                     float2 b[K], c[K], sum = make_float2(0.f, 0.f);
 #pragma unroll
                     for (int k = 0; k < K; k += 2) {
-                        const float4 u = *(const float4 *)&sm.b[r0 + r][part * H + 2 * k];
+                        const float4 u = sm.b[k / 2][r0 + r][part];
                         b[k] = make_float2(u.x, u.y), b[k + 1] = make_float2(u.z, u.w);
                         if (!kStateOnly) {
-                            const float4 v = *(const float4 *)&sm.c[r0 + r][part * H + 2 * k];
+                            const float4 v = sm.c[k / 2][r0 + r][part];
                             c[k] = make_float2(v.x, v.y), c[k + 1] = make_float2(v.z, v.w);
                         }
                     }
@@ -364,26 +363,27 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
                     y[r] = sum.x + sum.y;
                 }
                 if constexpr (!kStateOnly) {
-                    // the lanes of a channel exchange halves of their rows until each has whole sums
+                    // the lanes of a channel exchange every other row of theirs until each has whole sums: of rows
+                    // mine, mine + L, ..., so that the lanes' rows of a store lie next to one another
                     constexpr int kShare = L > kGroup ? L / kGroup : 1;       // lanes that have the same row
                     int mine = 0;
 #pragma unroll
-                    for (int o = L / 2, n = kGroup / 2; o > 0; o /= 2, n /= 2) {
+                    for (int o = L / 2, n = kGroup / 2, bit = 1; o > 0; o /= 2, n /= 2, bit *= 2) {
                         const bool high = part & o;
                         if (n > 0) {
 #pragma unroll
                             for (int i = 0; i < n; ++i) {
-                                const float keep = high ? y[i + n] : y[i], give = high ? y[i] : y[i + n];
+                                const float keep = high ? y[2 * i + 1] : y[2 * i], give = high ? y[2 * i] : y[2 * i + 1];
                                 y[i] = keep + __shfl_xor_sync(0xffffffffu, give, o * S::kCh);
                             }
-                            mine += high ? n : 0;
+                            mine += high ? bit : 0;
                         } else {
                             y[0] += __shfl_xor_sync(0xffffffffu, y[0], o * S::kCh);
                         }
                     }
 #pragma unroll
                     for (int i = 0; i < (kGroup > L ? kGroup / L : 1); ++i)
-                        if (part % kShare == 0) sm.y[r0 + mine + i][cl] += y[i];
+                        if (part % kShare == 0) sm.y[r0 + mine + i * L][cl] = y[i];
                 }
             }
         };
@@ -392,10 +392,11 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
         asm volatile("cp.async.wait_group 1;" ::: "memory");
         __syncwarp();
         if constexpr (!kStateOnly) {
+            const float2 skip = *(const float2 *)&sm.skip[two];
 #pragma unroll
             for (int p = 0; p < S::kPasses; ++p) {
                 const int r = p * S::kRowsAtOnce + row_in;
-                float2 y = *(const float2 *)&sm.y[r][two];
+                float2 y = __ffma2_rn(skip, widen2(*(const uint32_t *)&sm.x[place][r][two]), *(const float2 *)&sm.y[r][two]);
                 if (g.z) y = gate2(y, widen2(*(const uint32_t *)&sm.z[r][two]));
                 if (r < out_rows - t0) *(uint32_t *)(out + p * S::kRowsAtOnce * g.os) = pack_bf16x2(y.x, y.y);
             }
