@@ -6,8 +6,9 @@
 // sequence, and slides the window over them in registers, in fp32, kAhead rows loaded at a time; a row is loaded once per unit
 // and W - 1 rows twice.  The thread of a sequence's first unit reads the slot (the inputs before the first row) and then
 // writes it (the last W - 1 inputs): the same thread does both, so no block reads what another has overwritten.
-// 8 x 1024 rows of 8192 channels: 50.0 us, 5.4 TB/s of 6.6 (x's rows 32 KB apart); the exponentials and reciprocals of the
-// activation keep the special-function unit 64 % busy.  Eight rows ahead, or eight blocks an SM, spill: 83 and 65 us.
+// 8 x 1024 rows of 8192 channels: 49.7 us, 5.4 TB/s of 6.6 (x's rows 32 KB apart); the exponentials and reciprocals of the
+// activation keep the special-function unit 65 % busy.  Eight rows ahead with registers for them (5 blocks an SM) 57.7 us, six
+// 51.2; eight blocks an SM spill: 65.
 #include "layers.h"
 #include "ptx.cuh"
 

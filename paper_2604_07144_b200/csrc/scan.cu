@@ -5,9 +5,9 @@
 //
 // A sequence's tokens follow one another, channels and states are independent.  A prompt costs an exponential per
 // (token, channel, state): at 16 states the special-function unit (16 a clock and SM) bounds it, ahead of HBM: 8 x 1024 rows
-// of 8192 channels are 1.07 G exponentials, 240 us of that unit alone, and 83 us of HBM.  Measured: 373 us (the unit 65 % busy,
-// issue slots and shared-memory wavefronts as much: 121 instructions per 32 channels and row).  A single token costs its
-// state, read and written: 128 sequences of 8192 channels 26.8 us, 5.3 TB/s.
+// of 8192 channels are 1.07 G exponentials, 240 us of that unit alone, and 83 us of HBM.  Measured: 361 us (the unit 69 % busy,
+// load/store wavefronts 68 %, issue slots 59 %: 115 instructions per 32 channels and row).  A single token costs its
+// state, read and written: 128 sequences of 8192 channels 26.7 us, 5.4 TB/s.
 //
 // Work split of prompts.  H states of a channel are a lane's, L = N / H lanes make a channel, and a warp walks 32 / L channels
 // alone: no barrier but its own.  Rows come in tiles of 16 by asynchronous copies, a tile ahead.  Steps and gates are worked
@@ -26,7 +26,7 @@ namespace {
 using namespace ptx;
 
 // Single tokens: a block takes a second sequence once there are kStepBlocks blocks an SM: a's share of what is read halves
-// (128 sequences: 26.5 us, with one 28.0, with four 26.8, with sixteen 30.3).
+// (128 sequences: 26.7 us, with one 28.1, with four 26.9, with sixteen 30.3).
 constexpr int kStepBlocks = 6, kStepRows = 2;
 
 // Single tokens: a quad of lanes takes kCh channels, each lane N / 4 states of every one of them.
@@ -42,13 +42,13 @@ struct Step {
 
 // Prompts: a lane has H states of one channel.
 constexpr int kTile = 16;                                      // rows staged at a time
-constexpr int kGroup = 8;                                      // rows walked in one piece of code (four: 387 us for 383)
+constexpr int kGroup = 8;                                      // rows walked in one piece of code (four: 369 us for 361, sixteen 373)
 template <int N, int H>
 struct Walk {
     static constexpr int kLanes = N / H;                       // lanes of a channel
     static constexpr int kCh = 32 / kLanes;                    // channels of a warp
-    // Warps of a block, blocks of an SM: 16 warps of 128 registers.  (Two warps a block: 383 us for 373, places come free
-    // later; 18 and 20 warps of fewer registers spill: 433 and 489.)
+    // Warps of a block, blocks of an SM: 16 warps of 128 registers.  (Two warps a block: 376 us for 361, places come free
+    // later; 18 and 20 warps of fewer registers spill: 433 and 489 where 16 took 383.)
     static constexpr int kWarps = 1, kBlocks = 16;
     // staging: a lane takes two channels next to one another
     static constexpr int kTwos = kCh / 2, kRowsAtOnce = 32 / kTwos, kPasses = kTile / kRowsAtOnce;
@@ -157,8 +157,8 @@ __device__ __forceinline__ float2 exp2_pair(float2 x) {
                        __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 
-// One pair of states in kPolyEvery takes the FMA pipe for its exponential (8 x 1024 rows: none 412 us, one in eight 383, in
-// sixteen 382; one in four, before other steps, 461 where one in eight took 435).
+// One pair of states in kPolyEvery takes the FMA pipe for its exponential (8 x 1024 rows: one in eight 361 us, none 363, in four
+// 382; 8192 rows of 4096 channels, where half the walks form states alone: 314, 323, 326).
 constexpr int kPolyEvery = 8;
 // States that a lane holds.  With 16 a lane has a channel, and the 14 warps an SM of 8 x 1024 rows of 8192 channels do not
 // hide their chains (447 us where 8 took 394); with 4 the lanes' own work doubles (498 us).

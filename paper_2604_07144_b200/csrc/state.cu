@@ -13,9 +13,9 @@ namespace {
 
 // The scan's cut along time.  A warp walks its rows one after the other, so few long sequences leave SMs idle.  Cut into
 // pieces, all but the first and the last are walked twice (once for the state behind them, once for their rows) and there
-// are two launches.  It pays below kCutBelow warps an SM (6 x 1024 rows of 4096 channels, 10.4 warps an SM: 203 us cut, 214
-// not), with pieces for kResident warps an SM, two rounds of those that are there together (8192 rows of 4096 channels: 322
-// us; 16: 356, 24: 337, 32: 333, 40: 330).
+// are two launches.  It pays below kCutBelow warps an SM (6 x 1024 rows of 4096 channels, 10.4 warps an SM: 198 us cut, 209
+// not), with pieces for kResident warps an SM, two rounds of those that are there together (8192 rows of 4096 channels: 314
+// us; 16: 327, 24: 328, 32: 326).
 constexpr int kCutBelow = 12, kResident = 28, kLeastPiece = 64;
 
 struct Cut {
@@ -31,7 +31,7 @@ Cut choose_cut(int sms, int blocks_c, int64_t chunk_seqs, int64_t chunk_rows) {
 }
 
 // Rows of a unit of the convolution.  A thread's start (weights, the rows before) costs as much as several rows: 8 x 1024 rows
-// of 8192 channels take 50.0 us in runs of 32 or 64, 52.7 in runs of 16.  Shorter runs make kConvBlocks blocks an SM for few rows.
+// of 8192 channels take 49.7 us in runs of 32 or 64, 52.2 in runs of 16.  Shorter runs make kConvBlocks blocks an SM for few rows.
 constexpr int kConvBlocks = 14;
 int32_t conv_run(int sms, int blocks_c, int64_t rows) {
     int32_t run = 32;
