@@ -479,7 +479,9 @@ int ap_selftest_wait_timeout(ap_kv_pool *pool, uint64_t limit_ns, int leave_coun
  * kv heads, head_dim, device, staging, status word and wait limit; its pages are
  * not touched.  A prompt that continues a cached prefix is an ap_plan's.
  * lens: host, [batch] tokens of each prompt, >= 0 (0: no rows); read during the
- * call.  num_q_heads, softmax_scale: as in ap_batch_desc.  Up to 2^30 tokens in all.
+ * call.  num_q_heads, softmax_scale: as in ap_batch_desc.  Up to 2^30 tokens in all
+ * (else UNSUPPORTED).  The plan belongs to the pool it was made with, which has to
+ * outlive it.
  */
 typedef struct ap_prompt_plan ap_prompt_plan; /* opaque */
 typedef struct ap_prompt_desc {
@@ -506,7 +508,7 @@ int ap_prompt_plan_get_info(const ap_prompt_plan *plan, ap_prompt_info *info);
  * next, a multiple of 8 (0: contiguous), so that they may be cut out of one
  * projection's output.  out: [n_rows][num_q_heads][head_dim] contiguous, 16-byte
  * aligned; lse: [n_rows][num_q_heads] fp32 or NULL.  out and lse overlap no input
- * (INVALID_ARG).  Softmax weights are rounded to bf16 for their product with V.  A key behind a row
+ * and not one another (INVALID_ARG).  Softmax weights are rounded to bf16 for their product with V.  A key behind a row
  * weighs exactly 0, whatever its K holds; a non-finite V can reach the rows before
  * it of the same block of 128 rows of its prompt, never another prompt.
  * Rows behind the last prompt are neither read nor written.
@@ -529,8 +531,8 @@ int ap_prompt_attention(ap_kv_pool *pool, const ap_prompt_plan *plan, const void
  *     scan plane : [num_slots][channels][state_dim]       fp32
  * channels: a multiple of 8 (else UNSUPPORTED) up to 2^20; state_dim 8, 16, 32 or
  * 64; conv_width 2, 3 or 4 (else UNSUPPORTED).  conv_base / scan_base: device,
- * 16-byte aligned, owned by the caller; both NULL: the library allocates (and zero
- * fills) both planes; one NULL: the layer has no such plane, and the call that needs
+ * 16-byte aligned, not overlapping (INVALID_ARG), owned by the caller; both NULL: the library allocates (and zero
+ * fills, before it returns) both planes; one NULL: the layer has no such plane, and the call that needs
  * it returns INVALID_ARG.  device < 0 (with both bases NULL): a host-only pool,
  * which plans and validates; calls that would launch return AP_ERR_CUDA.
  */
@@ -622,8 +624,8 @@ int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_c
  * cut out of projections' outputs.  a: [channels][state_dim] fp32, finite (beyond
  * 2e38 in magnitude as 2e38); d_skip, dt_bias: [channels] fp32 or NULL; z may be
  * NULL.  out: [n_new][channels] bf16, rows out_row_stride elements apart.  Device,
- * 16-byte aligned.  out overlaps no input, and neither overlaps the slots or the
- * workspace (INVALID_ARG).  workspace:
+ * 16-byte aligned.  out overlaps no input, neither overlaps the slots or the
+ * workspace, nor do these one another (INVALID_ARG).  workspace:
  * device, 256-byte aligned, at least ap_state_plan_workspace_bytes() (else
  * WORKSPACE_TOO_SMALL), contents undefined before and after; calls that may
  * overlap on the GPU take one each.
@@ -651,7 +653,7 @@ int ap_scan_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_s
  * library launches for this pool (page copies and read-backs excepted) is bracketed
  * by CUDA events recorded on the launching stream; a rotated append counts as
  * append, a 4-bit pool's merge as part of its decode, its widening of pages as a
- * prefill launch of its own.  ap_profile_collect synchronises `stream`, adds up the
+ * prefill launch of its own, each kernel of ap_prompt_attention as a prefill launch.  ap_profile_collect synchronises `stream`, adds up the
  * elapsed times per kernel since the last enable/collect, and clears the
  * records.  Index: 0 kv_append, 1 decode split-K (which also performs the LSE
  * merge), 2 prefill, 3 the single launch that holds both parts of a mixed plan.

@@ -39,17 +39,6 @@ void give_back_event(ap_kv_pool *pool, cudaEvent_t e) {
     }
 }
 
-cudaEvent_t take_event(ap_kv_pool *pool) {
-    if (!pool->spare_events.empty()) {
-        cudaEvent_t e = pool->spare_events.back();
-        pool->spare_events.pop_back();
-        return e;
-    }
-    cudaEvent_t e = nullptr;
-    if (cudaEventCreate(&e) != cudaSuccess) { (void)cudaGetLastError(); return nullptr; }
-    return e;
-}
-
 // Side-by-side execution of a mixed iteration.  Decode is bound by HBM when it has the whole GPU
 // (~41 GB/s per SM at 148 SMs) but one SM's decode pipeline sustains more (its ring keeps ~100 KB in
 // flight over a ~1.2 us memory latency; with items that span a block of kv heads the TMA requests are
@@ -157,31 +146,6 @@ int side_by_side_decode_ctas(const ap_kv_pool *pool, const ap_batch_desc *b, con
     if (t_serial - t_side < 10.0 || t_serial - t_side < 0.05 * t_serial) return 0;
     return k;
 }
-
-// Brackets one kernel launch with events when profiling is on.
-struct TimedScope {
-    ap_kv_pool *pool;
-    cudaStream_t stream;
-    TimedLaunch rec{};
-    bool on = false;
-    TimedScope(ap_kv_pool *p, int kernel, cudaStream_t st) : pool(p), stream(st) {
-        if (!p->profiling) return;
-        rec.kernel = kernel;
-        rec.start = take_event(p);
-        rec.stop = take_event(p);
-        on = rec.start && rec.stop && cudaEventRecord(rec.start, st) == cudaSuccess;
-    }
-    ~TimedScope() {
-        if (!on) return;
-        if (cudaEventRecord(rec.stop, stream) != cudaSuccess) return;
-        try {
-            pool->timed.push_back(rec);
-        } catch (const std::bad_alloc &) {          // (this launch goes uncounted)
-            (void)cudaEventDestroy(rec.start);
-            (void)cudaEventDestroy(rec.stop);
-        }
-    }
-};
 
 }  // namespace
 

@@ -71,4 +71,40 @@ inline void give_back_plan_buffer(std::vector<PlanBuffer> &spare, PlanBuffer &b)
     }
 }
 
+inline cudaEvent_t take_event(ap_kv_pool *pool) {
+    if (!pool->spare_events.empty()) {
+        cudaEvent_t e = pool->spare_events.back();
+        pool->spare_events.pop_back();
+        return e;
+    }
+    cudaEvent_t e = nullptr;
+    if (cudaEventCreate(&e) != cudaSuccess) { (void)cudaGetLastError(); return nullptr; }
+    return e;
+}
+
+// Brackets one kernel launch with events when profiling is on.
+struct TimedScope {
+    ap_kv_pool *pool;
+    cudaStream_t stream;
+    TimedLaunch rec{};
+    bool on = false;
+    TimedScope(ap_kv_pool *p, int kernel, cudaStream_t st) : pool(p), stream(st) {
+        if (!p->profiling) return;
+        rec.kernel = kernel;
+        rec.start = take_event(p);
+        rec.stop = take_event(p);
+        on = rec.start && rec.stop && cudaEventRecord(rec.start, st) == cudaSuccess;
+    }
+    ~TimedScope() {
+        if (!on) return;
+        if (cudaEventRecord(rec.stop, stream) != cudaSuccess) return;
+        try {
+            pool->timed.push_back(rec);
+        } catch (const std::bad_alloc &) {          // (this launch goes uncounted)
+            (void)cudaEventDestroy(rec.start);
+            (void)cudaEventDestroy(rec.stop);
+        }
+    }
+};
+
 }  // namespace ap

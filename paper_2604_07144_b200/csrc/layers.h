@@ -105,7 +105,7 @@ struct ScanArgs {                 // by value to the kernels
 int scan_warp_channels(int state_dim);        // channels that a warp of the scan takes
 cudaError_t launch_conv(const ap_state_pool *pool, const ap_state_plan *plan, const ap_conv_desc &conv, cudaStream_t stream);
 cudaError_t launch_scan(const ap_state_pool *pool, const ap_state_plan *plan, const ScanArgs &args, cudaStream_t stream);
-cudaError_t launch_prompt(const ap_kv_pool *pool, const ap_prompt_plan *plan, const void *q, const void *k, const void *v,
+cudaError_t launch_prompt(ap_kv_pool *pool, const ap_prompt_plan *plan, const void *q, const void *k, const void *v,
                           void *out, float *lse, const ap_prompt_strides &strides, cudaStream_t stream);
 
 // rows of [n_rows][heads][head_dim] bf16, `row_stride` elements apart: box of 128 rows of a head (see tensor_map.cu)

@@ -38,6 +38,7 @@ using prefill::smem_desc;
 // (with room for 128 rows) and 39.9.
 constexpr int kShortRows = 64;
 constexpr int kUnitSteps = 2;             // what a unit costs beside its steps, in steps
+constexpr uint64_t kDrainNs = 100000000;  // bound of the waits for copies and products under way, after a wait that ran out
 
 // ----------------------------------------------------- tensor-core units --
 //
@@ -91,6 +92,8 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
     uint64_t *o_empty = s_out + 2;               // [2] a unit's O_x has been read
     uint32_t *tmem_slot = (uint32_t *)(o_empty + 2);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+    volatile uint32_t *issued = tmem_slot + 2;   // the producer's: ring entries, units
+    uint64_t *drained = (uint64_t *)(tmem_slot + 4);   // [2] after a wait that ran out: tile x's products have ended
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int first = begin[blockIdx.x], end = begin[blockIdx.x + 1];
@@ -109,6 +112,7 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
             mbar_init(&pv_done[x], 1);
             mbar_init(&s_out[x], 4);
             mbar_init(&o_empty[x], 4);
+            mbar_init(&drained[x], 1);
         }
         *abort_flag = 0;
         fence_barrier_init();
@@ -155,6 +159,8 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
                                     tile.start + j * kTileN, tile.kv_head * Cfg::kHalves);
                     }
                 }
+                issued[0] = e;
+                issued[1] = u;                           // (a unit given up among its entries counts: its Q is under way)
                 if (!ok) {
                     record_status(status, AP_ERR_TIMEOUT);
                     *abort_flag = 1;
@@ -389,6 +395,21 @@ prompt_tcgen05_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_co
 
     tcgen05_fence_before();
     __syncthreads();
+    if (*abort_flag) {
+        // Given up: what is under way still writes shared and tensor memory, and ends before they are given back.
+        volatile int none = 0;
+        if (warp == kMmaWarp || (warp == kMmaWarp + 1 && kTiles == 2)) {
+            uint64_t *mine = &drained[warp - kMmaWarp];
+            umma_commit(elect_one(), mine);
+            (void)wait_or_abort(mine, 0, &none, kDrainNs);
+        } else if (warp == kProducerWarp && lane == 0) {
+            const uint32_t entries = issued[0], units = issued[1];
+            for (uint32_t e = entries < (uint32_t)kSlots ? 0 : entries - kSlots; e < entries; ++e)
+                (void)wait_or_abort(&kv_full[e % kSlots], e / kSlots & 1u, &none, kDrainNs);
+            if (units > 0) (void)wait_or_abort(q_full, (units - 1) & 1u, &none, kDrainNs);
+        }
+        __syncthreads();
+    }
     if (warp == kMmaWarp) tmem_dealloc(tmem, Cols::kTmemCols);
 }
 
@@ -543,7 +564,7 @@ prompt_short_kernel(const ShortPrompt *__restrict__ prompts, const uint16_t *q, 
 }
 
 template <int D>
-cudaError_t launch_prompt_t(const ap_kv_pool *pool, const ap_prompt_plan *plan, const void *q, const void *k, const void *v,
+cudaError_t launch_prompt_t(ap_kv_pool *pool, const ap_prompt_plan *plan, const void *q, const void *k, const void *v,
                             void *out, float *lse, const ap_prompt_strides &st, cudaStream_t stream) {
     using Cfg = PromptCfg<D>;
     static bool configured[64] = {};
@@ -568,16 +589,19 @@ cudaError_t launch_prompt_t(const ap_kv_pool *pool, const ap_prompt_plan *plan, 
             return cudaErrorInvalidValue;
         for (int t = 2; t >= 1 && e == cudaSuccess; --t) {
             const PromptLists &l = plan->lists[t - 1];
-            if (l.blocks > 0)
-                e = launch_overlapped(t == 2 ? prompt_tcgen05_kernel<D, 2> : prompt_tcgen05_kernel<D, 1>, (unsigned)l.blocks,
-                                      (unsigned)kPrefillThreads, (size_t)Cfg::kSmemBytes, stream, q_map, k_map, v_map, l.tiles, l.begin,
-                                      (__nv_bfloat16 *)out, lse, Hq, scale_log2, pool->status_dev, pool->wait_limit_ns);
+            if (l.blocks == 0) continue;
+            TimedScope ts(pool, AP_KERNEL_PREFILL, stream);
+            e = launch_overlapped(t == 2 ? prompt_tcgen05_kernel<D, 2> : prompt_tcgen05_kernel<D, 1>, (unsigned)l.blocks,
+                                  (unsigned)kPrefillThreads, (size_t)Cfg::kSmemBytes, stream, q_map, k_map, v_map, l.tiles, l.begin,
+                                  (__nv_bfloat16 *)out, lse, Hq, scale_log2, pool->status_dev, pool->wait_limit_ns);
         }
     }
-    if (e == cudaSuccess && plan->info.short_units > 0)
+    if (e == cudaSuccess && plan->info.short_units > 0) {
+        TimedScope ts(pool, AP_KERNEL_PREFILL, stream);
         e = launch_overlapped(prompt_short_kernel<D>, (unsigned)plan->info.short_units, 32u * kShortWarps, sizeof(ShortSmem<D>), stream,
                               plan->d_short, (const uint16_t *)q, (const uint16_t *)k, (const uint16_t *)v, (uint16_t *)out, lse, Hq, Hkv,
                               st.q_row_stride, st.k_row_stride, st.v_row_stride, scale_log2);
+    }
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -695,7 +719,7 @@ int plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *b,
 
 }  // namespace
 
-cudaError_t launch_prompt(const ap_kv_pool *pool, const ap_prompt_plan *plan, const void *q, const void *k, const void *v,
+cudaError_t launch_prompt(ap_kv_pool *pool, const ap_prompt_plan *plan, const void *q, const void *k, const void *v,
                           void *out, float *lse, const ap_prompt_strides &strides, cudaStream_t stream) {
     if (pool->desc.head_dim == 128) return launch_prompt_t<128>(pool, plan, q, k, v, out, lse, strides, stream);
     return launch_prompt_t<64>(pool, plan, q, k, v, out, lse, strides, stream);
@@ -755,6 +779,8 @@ int ap_prompt_attention(ap_kv_pool *pool, const ap_prompt_plan *plan, const void
             meets(v, st.v_row_stride, Hkv * d, o, bytes))
             return AP_ERR_INVALID_ARG;
     }
+    if (lse && (uintptr_t)lse < (uintptr_t)out + (uintptr_t)(n * Hq * d * 2) && (uintptr_t)out < (uintptr_t)lse + (uintptr_t)(n * Hq * 4))
+        return AP_ERR_INVALID_ARG;
     DeviceGuard guard(pool->desc.device);
     if (!guard.ok) return AP_ERR_CUDA;
     if (launch_prompt(pool, plan, q, k, v, out, lse, st, (cudaStream_t)stream) != cudaSuccess) {

@@ -229,3 +229,58 @@ def test_a_hybrid_iteration_run_together_and_captured():
     ap.prompt_plan_destroy(prompts)
     ap.kv_pool_destroy(pool)
     c.close()
+
+
+@pytest.mark.gpu
+def test_two_streams_overlaps_and_the_profile():
+    """One plan on two streams at once; results over results or inputs are refused; every kernel is in the profile."""
+    import torch
+    lens, hq, hkv, d = [200, 20, 65, 1, 300], 6, 2, 64
+    sets = [inputs(seed, lens, hq, hkv, d, extra=0) for seed in (61, 62)]
+    n = sets[0][0]
+    pool = ap.kv_pool_create(1, hkv, d)
+    plan = ap.prompt_plan_create(pool, lens, hq)
+    tensors = [[dev(t) for t in s[1:]] for s in sets]
+    results = [(torch.empty(n, hq, d, dtype=torch.bfloat16, device="cuda"), torch.empty(n, hq, device="cuda")) for _ in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for t, r, st in zip(tensors, results, streams):
+        with torch.cuda.stream(st):
+            ap.prompt_attention(pool, plan, *t, *r)
+    torch.cuda.synchronize()
+    for s, (out, lse) in zip(sets, results):
+        check(out, lse, *s, lens)
+    q, k, v = tensors[0]
+    out, lse = results[0]
+    both = torch.empty(n * hq * (d // 2 + 1), device="cuda")
+    shared = both[:n * hq * d // 2].view(torch.bfloat16).view(n, hq, d), both[n * hq * d // 2 - 4:n * hq * d // 2 - 4 + n * hq].view(n, hq)
+    for a in ((q, k, v, q, lse), (q, k, v, out, k.view(-1)[:2 * n * hq].view(torch.float32).view(n, hq)), (q, k, v, *shared)):
+        with pytest.raises(ap.ApError) as e:
+            ap.prompt_attention(pool, plan, *a)
+        assert e.value.status == B.AP_ERR_INVALID_ARG
+    ap.profile_enable(pool)
+    ap.prompt_attention(pool, plan, q, k, v, out, lse)
+    times = ap.profile_collect(pool)
+    assert sum(launches for _, launches in times.values()) == ap.prompt_plan_get_info(plan)["launches"] == 3
+    assert sum(ms for ms, _ in times.values()) > 0
+    ap.profile_enable(pool, False)
+    assert ap.last_device_status(pool) == 0
+    ap.prompt_plan_destroy(plan)
+    ap.kv_pool_destroy(pool)
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    """q, k and v in rows 2^26 elements apart, for both kernels."""
+    import torch
+    lens, hq, hkv, d = [5, 66], 2, 1, 64
+    n, q, k, v = inputs(71, lens, hq, hkv, d, extra=0)
+    wide = torch.empty((n, 1 << 26), dtype=torch.bfloat16, device="cuda")
+    at, views = (1 << 26) - 256, []
+    for t, heads in ((q, hq), (k, hkv), (v, hkv)):
+        view = wide[:, at:at + heads * d].unflatten(1, (heads, d))
+        view.copy_(dev(t))
+        views.append(view)
+        at += heads * d
+    out, lse = run(lens, hq, hkv, d, *views)
+    check(out, lse, n, q, k, v, lens)
