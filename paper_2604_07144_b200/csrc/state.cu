@@ -208,6 +208,10 @@ int ap_state_pool_create(ap_state_pool **out, const ap_state_desc *desc) {
     if (!supported(desc)) return AP_ERR_UNSUPPORTED;
     if (!aligned16(desc->conv_base) || !aligned16(desc->scan_base)) return AP_ERR_INVALID_ARG;
     if (desc->device < 0 && (desc->conv_base || desc->scan_base)) return AP_ERR_INVALID_ARG;
+    if (desc->conv_base && desc->scan_base) {              // (planes that share a byte)
+        const uintptr_t c = (uintptr_t)desc->conv_base, s = (uintptr_t)desc->scan_base;
+        if (c < s + ap_state_pool_scan_bytes(desc) && s < c + ap_state_pool_conv_bytes(desc)) return AP_ERR_INVALID_ARG;
+    }
     ap_state_pool *p = new (std::nothrow) ap_state_pool();
     if (!p) return AP_ERR_CUDA;
     p->desc = *desc;
@@ -223,6 +227,8 @@ int ap_state_pool_create(ap_state_pool **out, const ap_state_desc *desc) {
         };
         plane(&p->desc.conv_base, &p->owns_conv, ap_state_pool_conv_bytes(desc));
         plane(&p->desc.scan_base, &p->owns_scan, ap_state_pool_scan_bytes(desc));
+        // (the zeros are there before a stream that does not wait for the default one can read or write the slots)
+        if (ok && allocate) ok = cudaStreamSynchronize(0) == cudaSuccess;
         if (!ok) {
             (void)cudaGetLastError();
             ap_state_pool_destroy(p);
@@ -339,8 +345,10 @@ int ap_scan_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_s
         return AP_ERR_INVALID_ARG;
     // nor does what the call keeps for itself overlap an input
     const int64_t planes = (int64_t)pool->desc.num_slots * D * N;
-    for (const Rows &kept : {Rows{pool->desc.scan_base, planes, planes, 4},
-                             Rows{plan->workspace_bytes ? workspace : nullptr, (int64_t)plan->workspace_bytes, (int64_t)plan->workspace_bytes, 1}}) {
+    const Rows slots{pool->desc.scan_base, planes, planes, 4};
+    const Rows pieces{plan->workspace_bytes ? workspace : nullptr, (int64_t)plan->workspace_bytes, (int64_t)plan->workspace_bytes, 1};
+    if (overlap(slots, pieces, 1)) return AP_ERR_INVALID_ARG;
+    for (const Rows &kept : {slots, pieces}) {
         auto in = [&](const void *p, int64_t stride, int64_t cols, int size) {
             const int64_t all = (n - 1) * stride + cols;
             return overlap(kept, Rows{p, all, all, size}, 1);

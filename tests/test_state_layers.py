@@ -140,7 +140,9 @@ def test_plan_and_pool_refusals():
         return st
     assert pool_status() == 0
     for bad in (dict(num_slots=0), dict(channels=0), dict(channels=-8), dict(state_dim=0), dict(conv_width=0), dict(num_slots=-1),
-                dict(conv_base=4096), dict(scan_base=4096), dict(conv_base=8, device=0), dict(scan_base=24, device=0)):
+                dict(conv_base=4096), dict(scan_base=4096), dict(conv_base=8, device=0), dict(scan_base=24, device=0),
+                dict(conv_base=1 << 20, scan_base=(1 << 20) + 4 * 3 * 64 * 2 - 16, device=0),                 # planes that share 16 bytes
+                dict(conv_base=(1 << 20) + 4 * 64 * 16 * 4 - 16, scan_base=1 << 20, device=0)):
         assert pool_status(**bad) == B.AP_ERR_INVALID_ARG, bad
     for bad in (dict(channels=12), dict(channels=(1 << 20) + 8), dict(state_dim=4), dict(state_dim=24), dict(state_dim=128),
                 dict(conv_width=1), dict(conv_width=5)):
@@ -439,3 +441,134 @@ def test_captured_replayed_and_on_another_stream():
     side.synchronize()
     assert np.array_equal(host(out)[:c.n], first[0][:c.n])
     c.close()
+
+
+@pytest.mark.gpu
+def test_what_overlaps_is_refused_and_nothing_written():
+    import torch
+    c = Case(810, 64, 16, 4, [400], [400]).open()
+    need = ap.state_plan_workspace_bytes(c.plan)
+    assert need > 0
+    x, dt, a, b, cc, out = dev(c.x), dev(c.dt), dev(c.a), dev(c.b), dev(c.c), c.blank()
+    big = torch.full((need + c.state.nbytes + x.nbytes + 512,), 0x7F, dtype=torch.uint8, device="cuda")
+    base = -big.data_ptr() % 256
+    inside = big[base:base + c.state.nbytes].view(torch.float32).view(c.state.shape)
+    pool = ap.state_pool_create(c.num_slots, 64, 16, 4, scan_base=inside)
+    start = (c.num_slots - 1) * 64 * 16 * 4 // 256 * 256                                   # (the workspace begins in the last slot)
+    good = dict(x=x, dt=dt, a=a, b=b, c=cc, out=out, workspace=c.workspace())
+
+    def refused(pool, **kw):
+        with pytest.raises(ap.ApError) as e:
+            ap.scan_iteration(pool, c.plan, **{**good, **kw})
+        assert e.value.status == B.AP_ERR_INVALID_ARG, list(kw)
+    refused(pool, workspace=big[base + start:base + start + need])
+    refused(c.pool, out=x)
+    over = big[base:base + x.nbytes].view(torch.bfloat16).view(c.rows, 64)                # (its first rows lie in the slots)
+    refused(pool, x=over)
+    refused(pool, out=over)
+    refused(c.pool, b=good["workspace"].view(torch.bfloat16)[:16 * c.rows].view(c.rows, 16))
+    with pytest.raises(ap.ApError):
+        ap.conv_iteration(c.pool, c.plan, x, dev(c.weight), x)
+    torch.cuda.synchronize()
+    assert (big == 0x7F).all() and (host(out) == NAN).all()
+    assert np.array_equal(host(c.d_state).view(np.int32), c.state.view(np.int32)) and np.array_equal(host(c.d_conv), c.conv)
+    ap.state_pool_destroy(pool)
+    c.close()
+
+
+@pytest.mark.gpu
+def test_one_plan_for_two_layers_at_once():
+    """Two layers' calls on two streams, one plan: each its slots, its workspace, its result; then as two graphs."""
+    import torch
+    lens, ctx = [500, 1, 33, 200], [500, 7, 40, 200]
+    one, two = Case(820, 64, 16, 4, lens, ctx).open(), Case(821, 64, 16, 4, lens, ctx)
+    two.slots = one.slots
+    rng = np.random.default_rng(822)
+    two.conv, two.state, two.live, two.touched = bits(rng, *one.conv.shape), one.state[::-1].copy(), one.live, one.touched
+    two.conv[~two.live], two.state[~two.live] = NAN, np.nan
+    two.state[two.live] = rng.standard_normal(two.state[two.live].shape).astype(np.float32)
+    two.d_conv, two.d_state = dev(two.conv), dev(two.state)
+    two.pool = ap.state_pool_create(two.num_slots, 64, 16, 4, two.d_conv, two.d_state)
+    two.plan = one.plan
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    args = [[dev(t) for t in (c.x, c.dt, c.a, c.b, c.c)] for c in (one, two)]
+    space, outs = [c.workspace() for c in (one, two)], [c.blank() for c in (one, two)]
+    torch.cuda.synchronize()
+
+    def call(i):
+        c = (one, two)[i]
+        ap.scan_iteration(c.pool, c.plan, *args[i], outs[i], workspace=space[i])
+    for i in range(2):
+        with torch.cuda.stream(streams[i]):
+            call(i)
+    torch.cuda.synchronize()
+    for c, out in zip((one, two), outs):
+        c.check_scan(out, piece=64)
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for i in range(2):
+        with torch.cuda.graph(graphs[i], stream=streams[i]):
+            call(i)
+    first = [host(o) for o in outs]
+    for c, out in zip((one, two), outs):
+        c.d_state.copy_(dev(c.state))
+        out.fill_(0)
+    torch.cuda.synchronize()
+    for i in range(2):
+        with torch.cuda.stream(streams[i]):
+            graphs[i].replay()
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert np.array_equal(host(outs[i])[:one.n], first[i][:one.n])
+    ap.state_pool_destroy(two.pool)
+    one.close()
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    """Rows 2^26 elements apart, and slots whose states begin past 2^31 elements."""
+    import torch
+    c = Case(830, 64, 64, 4, [37, 1], [37, 5], extra_rows=0)
+    wide = torch.empty((c.rows, 1 << 26), dtype=torch.bfloat16, device="cuda")
+    cols = {}
+    for i, name in enumerate(("x", "dt", "z", "b", "c")):
+        cols[name] = wide[:, (1 << 26) - 512 + 64 * i:(1 << 26) - 512 + 64 * (i + 1)]
+        cols[name].copy_(dev(getattr(c, name)))
+    slots, far = (1 << 19) + 8, 1 << 19
+    small_state, small_conv = dev(c.state), dev(c.conv)
+    big_state = torch.empty((slots, 64, 64), device="cuda")
+    big_conv = torch.empty((slots, 3, 64), dtype=torch.bfloat16, device="cuda")
+    assert c.num_slots <= 8
+    big_state[far:far + c.num_slots].copy_(small_state)
+    big_conv[far:far + c.num_slots].copy_(small_conv)
+    c.d_state, c.d_conv = big_state[far:far + c.num_slots], big_conv[far:far + c.num_slots]
+    pool = ap.state_pool_create(slots, 64, 64, 4, big_conv, big_state)
+    plan = ap.state_plan_create(pool, c.q_lens, c.ctx_lens, c.slots + far)
+    ws = torch.empty(max(256, ap.state_plan_workspace_bytes(plan)), dtype=torch.uint8, device="cuda")
+    for run, check in ((lambda o: ap.conv_iteration(pool, plan, cols["x"], dev(c.weight), o), lambda o: c.check_conv(o, bias=False)),
+                       (lambda o: ap.scan_iteration(pool, plan, cols["x"], cols["dt"], dev(c.a), cols["b"], cols["c"], o, z=cols["z"],
+                                                    workspace=ws), lambda o: c.check_scan(o, z=c.z))):
+        out = wide[:, (1 << 26) - 128:(1 << 26) - 64]
+        run(out)
+        torch.cuda.synchronize()
+        check(out)
+    ap.state_plan_destroy(plan)
+    ap.state_pool_destroy(pool)
+
+
+@pytest.mark.gpu
+def test_the_librarys_own_planes_begin_as_zeros_on_any_stream():
+    import torch
+    side = torch.cuda.Stream()
+    x, w = torch.ones(1, 64, dtype=torch.bfloat16, device="cuda"), torch.ones(64, 4, dtype=torch.bfloat16, device="cuda")
+    a, b = torch.zeros(64, 16, device="cuda"), torch.ones(1, 16, dtype=torch.bfloat16, device="cuda")
+    out, y = torch.empty_like(x), torch.empty_like(x)
+    torch.cuda.synchronize()
+    pool = ap.state_pool_create(20000, 64, 16, 4)
+    with torch.cuda.stream(side):
+        plan = ap.state_plan_create(pool, [1], [2], [19999])
+        ap.conv_iteration(pool, plan, x, w, out, silu=False)
+        ap.scan_iteration(pool, plan, x, x, a, b, b, y, softplus=False)
+    side.synchronize()
+    assert (out == 1).all() and (y == 16).all()                     # 0 0 0 1 convolved with ones; 16 states of 1 * 1
+    ap.state_plan_destroy(plan)
+    ap.state_pool_destroy(pool)
