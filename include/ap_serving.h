@@ -582,7 +582,7 @@ typedef struct ap_state_info {
     int64_t chunk_seqs;    /* sequences with more */
     int64_t split_seqs;    /* of these: cut along time for the scan */
     int64_t segments;      /* pieces they were cut into */
-    int64_t launches_scan; /* kernels ap_scan_iteration launches */
+    int64_t launches_scan; /* kernels ap_scan_iteration launches (single tokens go with the walks of longer ones) */
 } ap_state_info;
 int ap_state_plan_get_info(const ap_state_plan *plan, ap_state_info *info);
 

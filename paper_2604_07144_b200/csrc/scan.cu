@@ -35,7 +35,7 @@ struct Step {
     static constexpr int kHeld = N / 4;                        // states a lane holds of a channel
     static constexpr int kCh = kHeld <= 4 ? 4 : 16 / kHeld;    // channels of a quad: 16 states a lane at most
     static constexpr int kThreads = 128;
-    static constexpr int kBlockCh = kThreads / 4 * kCh;
+    static constexpr int kWarpCh = 8 * kCh, kBlockCh = kThreads / 32 * kWarpCh;
     static constexpr int kVec = kHeld < 4 ? kHeld : 4;         // states that lie together: lane q has 4 kVec i + kVec q + e
     static constexpr int kVecs = kHeld / kVec;
 };
@@ -47,9 +47,9 @@ template <int N, int H>
 struct Walk {
     static constexpr int kLanes = N / H;                       // lanes of a channel
     static constexpr int kCh = 32 / kLanes;                    // channels of a warp
-    // Warps of a block, blocks of an SM: 16 warps of 128 registers.  (Two warps a block: 376 us for 361, places come free
-    // later; 18 and 20 warps of fewer registers spill: 433 and 489 where 16 took 383.)
-    static constexpr int kWarps = 1, kBlocks = 16;
+    // A block is a warp; blocks of an SM: 16 of 128 registers.  (Two warps a block: 376 us for 361, places come free later;
+    // 18 and 20 warps of fewer registers spill: 433 and 489 where 16 took 383.)
+    static constexpr int kBlocks = 16;
     // staging: a lane takes two channels next to one another
     static constexpr int kTwos = kCh / 2, kRowsAtOnce = 32 / kTwos, kPasses = kTile / kRowsAtOnce;
     static_assert(H == 8 && kCh >= 4 && kTile % kRowsAtOnce == 0, "eight states a lane: a 16-byte piece of b");
@@ -426,39 +426,18 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
     }
 }
 
-template <int N, int H>
-__global__ void __launch_bounds__(32 * Walk<N, H>::kWarps, Walk<N, H>::kBlocks)
-scan_kernel(const StateUnit *__restrict__ units, int64_t n_warps, int blocks_c, const ScanArgs g) {
-    extern __shared__ __align__(16) uint8_t raw[];
-    const int warp = threadIdx.x >> 5;
-    const int64_t at = (int64_t)blockIdx.x * Walk<N, H>::kWarps + warp;
-    griddep_launch_dependents();
-    if (at >= n_warps) return;
-    const StateUnit unit = units[at / blocks_c];
-    const int64_t c0 = at % blocks_c * Walk<N, H>::kCh;
-    griddep_wait();
-    WalkSmem<N, H> &sm = ((WalkSmem<N, H> *)raw)[warp];
-    if (unit.flags & kUnitStateOnly) walk_unit<N, H, true>(unit, c0, g, sm);
-    else walk_unit<N, H, false>(unit, c0, g, sm);
-}
-
 // Sequences with one new token: everything in registers.  Quad Q of a warp has channels Q, Q + 8, ... (so that a load of all
 // its lanes is one run of memory); lane q works out the step and the result of the quad's channel q * kCh / 4.
 // A block takes `rows` sequences for its channels, whose a it loads once.
 template <int N>
-__global__ void __launch_bounds__(Step<N>::kThreads, 8)
-scan_step_kernel(const StateUnit *__restrict__ units, int n_units, int rows, int blocks_c, const ScanArgs g) {
+__device__ __forceinline__ void step_units(const StateUnit *__restrict__ units, int u0, int u1, int64_t c0, const ScanArgs &g) {
     using S = Step<N>;
-    const int u0 = (int)blockIdx.x / blocks_c * rows, cb = (int)blockIdx.x % blocks_c, u1 = min(u0 + rows, n_units);
     const int lane = threadIdx.x & 31, q = lane & 3;
     const int64_t D = g.channels;
-    const int64_t wc = (int64_t)cb * S::kBlockCh + (threadIdx.x >> 5) * 8 * S::kCh + (lane >> 2);    // the quad's first
+    const int64_t wc = c0 + (lane >> 2);                   // the quad's first channel, of the warp's from c0 on
     const int64_t own = wc + q * S::kCh / 4 * 8;           // this lane's channel
     const bool in = own < D;
-    const int64_t left = D - (wc - (lane >> 2));           // channels come in eights: the warp's c-th eight is there if 8 c < left
-    griddep_launch_dependents();
-    if (left <= 0) return;
-    griddep_wait();
+    const int64_t left = D - c0;                           // channels come in eights: the warp's c-th eight is there if 8 c < left
     auto load_held = [&](const float *p, float2 (&to)[S::kHeld / 2]) {        // this lane's states of a channel
 #pragma unroll
         for (int i = 0; i < S::kVecs; ++i) {
@@ -547,31 +526,70 @@ scan_step_kernel(const StateUnit *__restrict__ units, int n_units, int rows, int
     }
 }
 
+template <int N>
+__global__ void __launch_bounds__(Step<N>::kThreads, 8)
+scan_step_kernel(const StateUnit *__restrict__ units, int n_units, int rows, int blocks_c, const ScanArgs g) {
+    const int u0 = (int)blockIdx.x / blocks_c * rows, cb = (int)blockIdx.x % blocks_c;
+    const int64_t c0 = (int64_t)cb * Step<N>::kBlockCh + (threadIdx.x >> 5) * Step<N>::kWarpCh;
+    griddep_launch_dependents();
+    if (c0 >= g.channels) return;
+    griddep_wait();
+    step_units<N>(units, u0, min(u0 + rows, n_units), c0, g);
+}
+
+// Single tokens that an iteration has beside its prompts: warps of their own behind the walks', in the same launch, so that
+// their loads fill what the walks leave of HBM and their warps the places that the last walks leave (64 tokens beside 512
+// rows of a prompt, 8192 channels: 58 us; as a launch of their own behind it 63, in front of the walks 62; 61 beside the ragged
+// chunks at 64 states: 90, 105, 101).
+struct Singles {
+    const StateUnit *units;
+    int n, rows, blocks_c;      // sequences; of a warp; warps for the channels
+};
+
 template <int N, int H>
-cudaError_t launch_walk(const ap_state_pool *pool, const StateUnit *units, int n, const ScanArgs &args, cudaStream_t stream) {
-    constexpr int kWarps = Walk<N, H>::kWarps;
-    constexpr size_t kSmem = kWarps * sizeof(WalkSmem<N, H>);
-    static_assert(kSmem <= 48 << 10, "within what a kernel may have unasked");
-    const int blocks_c = (pool->desc.channels + Walk<N, H>::kCh - 1) / Walk<N, H>::kCh;
-    const int64_t warps = (int64_t)n * blocks_c;
-    return launch_overlapped(scan_kernel<N, H>, (unsigned)((warps + kWarps - 1) / kWarps), 32u * kWarps, kSmem, stream, units,
-                             warps, blocks_c, args);
+__global__ void __launch_bounds__(32, Walk<N, H>::kBlocks)
+scan_kernel(const StateUnit *__restrict__ units, int64_t n_warps, int blocks_c, const Singles singles, const ScanArgs g) {
+    extern __shared__ __align__(16) uint8_t raw[];
+    int64_t at = blockIdx.x;
+    griddep_launch_dependents();
+    if (at >= n_warps) {
+        at -= n_warps;
+        const int u0 = (int)(at / singles.blocks_c) * singles.rows;
+        griddep_wait();
+        step_units<N>(singles.units, u0, min(u0 + singles.rows, singles.n), at % singles.blocks_c * Step<N>::kWarpCh, g);
+        return;
+    }
+    const StateUnit unit = units[at / blocks_c];
+    const int64_t c0 = at % blocks_c * Walk<N, H>::kCh;
+    griddep_wait();
+    WalkSmem<N, H> &sm = *(WalkSmem<N, H> *)raw;
+    if (unit.flags & kUnitStateOnly) walk_unit<N, H, true>(unit, c0, g, sm);
+    else walk_unit<N, H, false>(unit, c0, g, sm);
 }
 
 template <int N>
 cudaError_t launch_scan_t(const ap_state_pool *pool, const ap_state_plan *plan, const ScanArgs &args, cudaStream_t stream) {
-    auto launch = [&](const StateUnit *units, int n) { return launch_walk<N, (N < kHeldStates ? N : kHeldStates)>(pool, units, n, args, stream); };
+    constexpr int H = kHeldStates;
+    constexpr size_t kSmem = sizeof(WalkSmem<N, H>);
+    static_assert(kSmem <= 48 << 10, "within what a kernel may have unasked");
+    const int walk_c = (pool->desc.channels + Walk<N, H>::kCh - 1) / Walk<N, H>::kCh;
+    // a's share of what is read falls with the sequences of a block; blocks enough for the GPU come first
+    const int step_c = (pool->desc.channels + Step<N>::kBlockCh - 1) / Step<N>::kBlockCh;
+    const int64_t spare = (int64_t)plan->n_single * step_c / ((int64_t)kStepBlocks * pool->sm_count);
+    const int rows = spare < 2 ? 1 : spare > kStepRows ? kStepRows : (int)spare;
+    const int groups = (plan->n_single + rows - 1) / rows;
+    const Singles singles{plan->d_single, plan->n_single, rows, (pool->desc.channels + Step<N>::kWarpCh - 1) / Step<N>::kWarpCh};
+    auto launch = [&](const StateUnit *units, int n, bool with) {
+        const int64_t warps = (int64_t)n * walk_c;
+        return launch_overlapped(scan_kernel<N, H>, (unsigned)(warps + (with ? (int64_t)groups * singles.blocks_c : 0)), 32u, kSmem, stream, units,
+                                 warps, walk_c, singles, args);
+    };
     cudaError_t e = cudaSuccess;
-    if (plan->n_first > 0) e = launch(plan->d_first, plan->n_first);
-    if (e == cudaSuccess && plan->n_second > 0) e = launch(plan->d_second, plan->n_second);
-    if (e == cudaSuccess && plan->n_single > 0) {
-        // a's share of what is read falls with the sequences of a block; blocks enough for the GPU come first
-        const int blocks_c = (pool->desc.channels + Step<N>::kBlockCh - 1) / Step<N>::kBlockCh;
-        const int64_t spare = (int64_t)plan->n_single * blocks_c / ((int64_t)kStepBlocks * pool->sm_count);
-        const int rows = spare < 2 ? 1 : spare > kStepRows ? kStepRows : (int)spare;
-        e = launch_overlapped(scan_step_kernel<N>, (unsigned)((plan->n_single + rows - 1) / rows * blocks_c), (unsigned)Step<N>::kThreads, 0,
-                              stream, plan->d_single, plan->n_single, rows, blocks_c, args);
-    }
+    if (plan->n_first > 0) e = launch(plan->d_first, plan->n_first, plan->n_single > 0 && plan->n_second == 0);
+    if (e == cudaSuccess && plan->n_second > 0) e = launch(plan->d_second, plan->n_second, plan->n_single > 0);
+    if (plan->n_first == 0 && plan->n_single > 0)
+        e = launch_overlapped(scan_step_kernel<N>, (unsigned)(groups * step_c), (unsigned)Step<N>::kThreads, 0, stream, plan->d_single,
+                              plan->n_single, rows, step_c, args);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

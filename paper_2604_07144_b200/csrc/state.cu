@@ -139,7 +139,7 @@ int plan_create(ap_state_plan **out, ap_state_pool *pool, const ap_state_batch *
     auto longer = [](const StateUnit &x, const StateUnit &y) { return x.rows > y.rows; };
     std::stable_sort(first.begin(), first.end(), longer);
     std::stable_sort(second.begin(), second.end(), longer);
-    const int64_t most = (int64_t)std::max({first.size(), second.size(), single.size()}) * blocks_c;
+    const int64_t most = (int64_t)std::max(first.size(), second.size()) * blocks_c + (int64_t)single.size() * (d.channels / 8);
     if (most >= (int64_t)1 << 31 || (int64_t)conv.size() * conv_blocks_c >= (int64_t)1 << 31) return AP_ERR_UNSUPPORTED;
 
     ap_state_plan *plan = new (std::nothrow) ap_state_plan();
@@ -182,7 +182,7 @@ int plan_create(ap_state_plan **out, ap_state_pool *pool, const ap_state_batch *
     plan->info.chunk_seqs = chunk_seqs;
     plan->info.split_seqs = split_seqs;
     plan->info.segments = segments;
-    plan->info.launches_scan = (first.empty() ? 0 : 1) + (second.empty() ? 0 : 1) + (single.empty() ? 0 : 1);
+    plan->info.launches_scan = first.empty() ? (single.empty() ? 0 : 1) : second.empty() ? 1 : 2;
     *out = plan;
     return AP_OK;
 }

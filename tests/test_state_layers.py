@@ -169,6 +169,10 @@ def test_plan_and_pool_refusals():
         ap.state_plan_create(pool, [1.5], [2], [0])
     plan = ap.state_plan_create(pool, [0, 1, 0], [5, 1, 0], [2, 2, 9])     # (without new tokens a slot is not looked at)
     assert ap.state_plan_get_info(plan) == dict(n_new=1, single_rows=1, chunk_seqs=0, split_seqs=0, segments=0, launches_scan=1)
+    for q, launches in (([1, 1], 1), ([1, 2], 1), ([2, 2], 1), ([1 << 16], 2), ([1 << 16, 1, 70], 2)):    # (single tokens go with the walks)
+        p = ap.state_plan_create(pool, q, q, list(range(len(q))))
+        assert ap.state_plan_get_info(p)["launches_scan"] == launches
+        ap.state_plan_destroy(p)
     empty = ap.state_plan_create(pool, [], [], [])
     assert ap.state_plan_get_info(empty)["n_new"] == 0 and ap.state_plan_workspace_bytes(empty) == 0
     for p in (plan, empty):
