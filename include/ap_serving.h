@@ -496,8 +496,8 @@ int ap_prompt_plan_destroy(ap_prompt_plan *plan);
 typedef struct ap_prompt_info {
     int64_t n_rows;      /* rows of q, k, v, out */
     int64_t pairs;       /* (query row, key) pairs, one head */
-    int64_t tiles;       /* work units on the tensor cores (prompts of more than 64 tokens) */
-    int64_t short_units; /* work units of the kernel for shorter prompts */
+    int64_t tiles;       /* work units on the tensor cores (prompts of more than 64 tokens, a few shorter ones beside them) */
+    int64_t short_units; /* work units of the kernel for short prompts */
     int64_t launches;    /* kernels ap_prompt_attention launches */
 } ap_prompt_info;
 int ap_prompt_plan_get_info(const ap_prompt_plan *plan, ap_prompt_info *info);

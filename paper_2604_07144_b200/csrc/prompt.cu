@@ -1,7 +1,7 @@
 // Causal attention of whole prompts, packed one after the other, K and V read from the projection's rows.
 //
 // Prompts of more than kShortRows tokens go to the tensor cores (tcgen05, accumulators in tensor memory), shorter ones
-// to a kernel of mma.sync tiles; a plan with both launches both.
+// to a kernel of mma.sync tiles; a plan with both launches both, but for a few short ones beside longer ones.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -37,6 +37,9 @@ using prefill::smem_desc;
 // 64 prompts of 64 tokens (32 q heads, 8 kv heads of 128): 29.2 us in the short kernel, 38.0 on the tensor cores; of 96: 58.3
 // (with room for 128 rows) and 39.9.
 constexpr int kShortRows = 64;
+// A few short prompts beside longer ones are units of theirs, up to kFewUnits / 4 an SM, and spare a launch: 7 beside 9 of up to 1000
+// tokens 37 us for 40, 7 beside one of 300 8.8 for 11.2, 11 (1.2 units an SM) 28.7 for 30.1; 15 (1.6) would be 12.3 for 11.7.
+constexpr int kFewUnits = 5;
 constexpr int kUnitSteps = 2;             // what a unit costs beside its steps, in steps
 constexpr uint64_t kDrainNs = 100000000;  // bound of the waits for copies and products under way, after a wait that ran out
 
@@ -640,15 +643,16 @@ int plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *b,
     const int G = Hq / Hkv;
     if (G > 8) return AP_ERR_UNSUPPORTED;
     const int short_blocks = std::max(1, kShortWarps / G);                    // blocks of 16 rows of a unit
-    int64_t rows = 0, pairs = 0, tiles_n = 0, shorts_n = 0;
+    int64_t rows = 0, pairs = 0, tiles_n = 0, shorts_n = 0, few = 0;
     for (int s = 0; s < b->batch; ++s) {
         const int32_t n = b->lens[s];
         if (n < 0) return AP_ERR_INVALID_ARG;
         rows += n;
         pairs += (int64_t)n * ((int64_t)n + 1) / 2;
         if (n > kShortRows) tiles_n += ((int64_t)n + kTileM - 1) / kTileM * Hkv * ((G + 1) / 2);
-        else if (n > 0) shorts_n += ((n + 15) / 16 + short_blocks - 1) / short_blocks;
+        else if (n > 0) shorts_n += ((n + 15) / 16 + short_blocks - 1) / short_blocks, few += (int64_t)Hkv * ((G + 1) / 2);
     }
+    const int32_t short_rows = tiles_n > 0 && few * 4 <= (int64_t)kFewUnits * pool->sm_count ? 0 : kShortRows;
     // (row numbers of a last tile's keys, past the end of the batch, stay within 32 bits)
     if (rows > (int64_t)1 << 30 || tiles_n > (int64_t)1 << 27 || shorts_n * Hkv >= (int64_t)1 << 31) return AP_ERR_UNSUPPORTED;
     std::vector<PromptTile> tiles[2];                    // units of one tile, of two
@@ -657,7 +661,7 @@ int plan_create(ap_prompt_plan **out, ap_kv_pool *pool, const ap_prompt_desc *b,
     int32_t start = 0;
     for (int s = 0; s < b->batch; ++s) {
         const int32_t n = b->lens[s];
-        if (n > kShortRows) {
+        if (n > short_rows) {
             for (int32_t t0 = 0; t0 < n; t0 += kTileM)
                 for (int kv = 0; kv < Hkv; ++kv)
                     for (int g = 0; g < G; g += 2) {

@@ -12,7 +12,7 @@ import layer_reference as R
 from test_state_layers import NAN, Case, bits, dev, f64, host
 
 SHAPES = [(8, 2, 64), (8, 8, 64), (6, 2, 128), (5, 1, 128), (16, 2, 128), (4, 4, 128)]
-LENS = [[1], [5, 1, 0, 16, 17], [64], [65], [63, 64, 65, 1, 128, 2], [129, 300], [0, 257, 7, 33, 511], [640]]
+LENS = [[1], [5, 1, 0, 16, 17], [64], [65], [63, 64, 65, 1, 128, 2], [129, 300], [0, 257, 7, 33, 511], [640], [*range(1, 61), 200]]
 
 
 def inputs(seed, lens, hq, hkv, d, extra=2, scale=1.0):
@@ -70,8 +70,13 @@ def test_refusals():
             ap.prompt_plan_create(pool, bad, 8)
     plan = ap.prompt_plan_create(pool, [3, 0, 200, 64, 65], 6)
     info = ap.prompt_plan_get_info(plan)
-    assert info["n_rows"] == 332 and info["pairs"] == sum(n * (n + 1) // 2 for n in (3, 200, 64, 65)) and info["launches"] == 3
-    assert info["tiles"] == 3 * 2 * 2 and info["short_units"] == 5 * 2     # (heads 0-2: two units; blocks of 16 rows; two kv heads)
+    assert info["n_rows"] == 332 and info["pairs"] == sum(n * (n + 1) // 2 for n in (3, 200, 64, 65)) and info["launches"] == 2
+    assert info["tiles"] == 5 * 2 * 2 and info["short_units"] == 0         # (heads 0-2: two units; two kv heads)
+    for lens, tiles, short, launches in (([3, 0, 64], 0, 5 * 2, 1), ([200] + [17] * 46, 48 * 4, 0, 2), ([200] + [17] * 47, 2 * 4, 94 * 2, 3)):
+        p = ap.prompt_plan_create(pool, lens, 6)                           # (blocks of 16 rows; up to 185 units of short prompts)
+        info = ap.prompt_plan_get_info(p)
+        assert (info["tiles"], info["short_units"], info["launches"]) == (tiles, short, launches), lens
+        ap.prompt_plan_destroy(p)
 
     def status(pool_=pool, strides=True, **kw):
         st = B.PromptStrides(0, 0, 0)
@@ -261,7 +266,7 @@ def test_two_streams_overlaps_and_the_profile():
     ap.profile_enable(pool)
     ap.prompt_attention(pool, plan, q, k, v, out, lse)
     times = ap.profile_collect(pool)
-    assert sum(launches for _, launches in times.values()) == ap.prompt_plan_get_info(plan)["launches"] == 3
+    assert sum(launches for _, launches in times.values()) == ap.prompt_plan_get_info(plan)["launches"] == 2
     assert sum(ms for ms, _ in times.values()) > 0
     ap.profile_enable(pool, False)
     assert ap.last_device_status(pool) == 0
