@@ -34,7 +34,7 @@ using prefill::PrefillCfg;
 using prefill::rescale_o;
 using prefill::smem_desc;
 
-// 64 prompts of 64 tokens (32 q heads, 8 kv heads of 128): 29.2 us in the short kernel, 38.0 on the tensor cores; of 96: 58.3
+// 64 prompts of 64 tokens (32 q heads, 8 kv heads of 128): 26.4 us in the short kernel, 38.0 on the tensor cores; of 96: 58.3
 // (with room for 128 rows) and 39.9.
 constexpr int kShortRows = 64;
 // A few short prompts beside longer ones are units of theirs, up to kFewUnits / 4 an SM, and spare a launch: 7 beside 9 of up to 1000
@@ -436,8 +436,12 @@ __device__ __forceinline__ void copy16_or_zero(void *to, const void *from, bool 
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
 
-template <int D>
-__global__ void __launch_bounds__(32 * kShortWarps)
+// kBlocks: blocks an SM that registers are kept for, by the units there are for an SM.  More of them hide more, and each is slower:
+// up to 2 units, 2 blocks (16 prompts of 1 to 64 tokens, 1.8 units an SM: 4.8 us, with 3 blocks 5.3, with 4 5.5); up to 4 units,
+// 3 (64 prompts at 8 / 8 heads, 3.5 units: 5.8, with 2 6.8, with 4 6.5); else 4 (64 prompts of 64 tokens: 26.4, with 3 29.2; 200 of
+// 1 to 64: 25.6, with 3 28.3).
+template <int D, int kBlocks>
+__global__ void __launch_bounds__(32 * kShortWarps, kBlocks)
 prompt_short_kernel(const ShortPrompt *__restrict__ prompts, const uint16_t *q, const uint16_t *k, const uint16_t *v, uint16_t *out,
                     float *lse_out, int Hq, int Hkv, int64_t qs, int64_t ks, int64_t vs, float scale_log2) {
     extern __shared__ __align__(16) uint8_t smem_raw[];
@@ -576,8 +580,8 @@ cudaError_t launch_prompt_t(ap_kv_pool *pool, const ap_prompt_plan *plan, const 
         cudaError_t e = cudaFuncSetAttribute(prompt_tcgen05_kernel<D, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
         if (e == cudaSuccess)
             e = cudaFuncSetAttribute(prompt_tcgen05_kernel<D, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(prompt_short_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(ShortSmem<D>));
+        for (auto kernel : {prompt_short_kernel<D, 2>, prompt_short_kernel<D, 3>, prompt_short_kernel<D, 4>})
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(ShortSmem<D>));
         if (e != cudaSuccess) return e;
         configured[dev] = true;
     }
@@ -601,9 +605,10 @@ cudaError_t launch_prompt_t(ap_kv_pool *pool, const ap_prompt_plan *plan, const 
     }
     if (e == cudaSuccess && plan->info.short_units > 0) {
         TimedScope ts(pool, AP_KERNEL_PREFILL, stream);
-        e = launch_overlapped(prompt_short_kernel<D>, (unsigned)plan->info.short_units, 32u * kShortWarps, sizeof(ShortSmem<D>), stream,
-                              plan->d_short, (const uint16_t *)q, (const uint16_t *)k, (const uint16_t *)v, (uint16_t *)out, lse, Hq, Hkv,
-                              st.q_row_stride, st.k_row_stride, st.v_row_stride, scale_log2);
+        const int64_t units = plan->info.short_units, sms = pool->sm_count;
+        e = launch_overlapped(units <= 2 * sms ? prompt_short_kernel<D, 2> : units <= 4 * sms ? prompt_short_kernel<D, 3> : prompt_short_kernel<D, 4>,
+                              (unsigned)units, 32u * kShortWarps, sizeof(ShortSmem<D>), stream, plan->d_short, (const uint16_t *)q, (const uint16_t *)k,
+                              (const uint16_t *)v, (uint16_t *)out, lse, Hq, Hkv, st.q_row_stride, st.k_row_stride, st.v_row_stride, scale_log2);
     }
     return e != cudaSuccess ? e : cudaGetLastError();
 }
