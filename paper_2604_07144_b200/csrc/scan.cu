@@ -7,7 +7,7 @@
 // (token, channel, state): at 16 states the special-function unit (16 a clock and SM) bounds it, ahead of HBM: 8 x 1024 rows
 // of 8192 channels are 1.07 G exponentials, 240 us of that unit alone, and 83 us of HBM.  Measured: 361 us (the unit 69 % busy,
 // load/store wavefronts 68 %, issue slots 59 %: 115 instructions per 32 channels and row).  A single token costs its
-// state, read and written: 128 sequences of 8192 channels 26.7 us, 5.4 TB/s.
+// state, read and written: 128 sequences of 8192 channels 24.8 us, 5.8 TB/s (at 64 states 88.8, 6.2 TB/s).
 //
 // Work split of prompts.  H states of a channel are a lane's, L = N / H lanes make a channel, and a warp walks 32 / L channels
 // alone: no barrier but its own.  Rows come in tiles of 16 by asynchronous copies, a tile ahead.  Steps and gates are worked
@@ -26,18 +26,17 @@ namespace {
 using namespace ptx;
 
 // Single tokens: a block takes a second sequence once there are kStepBlocks blocks an SM: a's share of what is read halves
-// (128 sequences: 26.7 us, with one 28.1, with four 26.9, with sixteen 30.3).
+// (128 sequences: 25.4 us, with one 26.0, with four 25.2; 64 tokens beside 512 rows 57.6, with one 60.7, with four 57.9).
 constexpr int kStepBlocks = 6, kStepRows = 2;
 
-// Single tokens: a quad of lanes takes kCh channels, each lane N / 4 states of every one of them.
+// Single tokens: kLanes lanes have a channel's states, kVec next to one another each, so that a load of a warp is one run of
+// memory, kAcross channels; a lane has kCh channels.
 template <int N>
 struct Step {
-    static constexpr int kHeld = N / 4;                        // states a lane holds of a channel
-    static constexpr int kCh = kHeld <= 4 ? 4 : 16 / kHeld;    // channels of a quad: 16 states a lane at most
+    static constexpr int kLanes = N < 16 ? 4 : N / 4, kVec = N / kLanes;
+    static constexpr int kAcross = 32 / kLanes, kCh = 4;
     static constexpr int kThreads = 128;
-    static constexpr int kWarpCh = 8 * kCh, kBlockCh = kThreads / 32 * kWarpCh;
-    static constexpr int kVec = kHeld < 4 ? kHeld : 4;         // states that lie together: lane q has 4 kVec i + kVec q + e
-    static constexpr int kVecs = kHeld / kVec;
+    static constexpr int kWarpCh = kAcross * kCh, kBlockCh = kThreads / 32 * kWarpCh;
 };
 
 // Prompts: a lane has H states of one channel.
@@ -119,24 +118,18 @@ __device__ __forceinline__ float2 gate2(float2 y, float2 z) {
 
 __device__ __forceinline__ float gate(float y, float z) { return y * (z * rcp_approx(1.f + exp2_approx(-1.4426950408889634f * z))); }
 
-// Sums a quad's partial sums: lane q ends with the sum of channel q * kCh / 4.
-template <int kCh>
-__device__ __forceinline__ float quad_sum(const float (&y)[kCh], int q) {
-    if constexpr (kCh == 4) {
-        // lanes 0, 1 keep channels 0, 1 and give away 2, 3; then each keeps one
-        const bool high = q & 2, odd = q & 1;
-        float a = high ? y[2] : y[0], b = high ? y[3] : y[1];
-        a += __shfl_xor_sync(0xffffffffu, high ? y[0] : y[2], 2);
-        b += __shfl_xor_sync(0xffffffffu, high ? y[1] : y[3], 2);
-        return (odd ? b : a) + __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
-    } else if constexpr (kCh == 2) {
-        const bool high = q & 2;
-        const float a = (high ? y[1] : y[0]) + __shfl_xor_sync(0xffffffffu, high ? y[0] : y[1], 2);
-        return a + __shfl_xor_sync(0xffffffffu, a, 1);
-    } else {
-        const float a = y[0] + __shfl_xor_sync(0xffffffffu, y[0], 2);
-        return a + __shfl_xor_sync(0xffffffffu, a, 1);
-    }
+// Sums over kLanes lanes of four channels' partial sums: lane q of them ends with the sum of channel q * 4 / kLanes.
+template <int kLanes>
+__device__ __forceinline__ float lanes_sum(const float (&y)[4], int q) {
+    // half of the lanes keep channels 0, 1 and give away 2, 3; then each half of those keeps one
+    const bool high = q & kLanes / 2, odd = q & kLanes / 4;
+    float a = high ? y[2] : y[0], b = high ? y[3] : y[1];
+    a += __shfl_xor_sync(0xffffffffu, high ? y[0] : y[2], kLanes / 2);
+    b += __shfl_xor_sync(0xffffffffu, high ? y[1] : y[3], kLanes / 2);
+    a = (odd ? b : a) + __shfl_xor_sync(0xffffffffu, odd ? a : b, kLanes / 4);
+#pragma unroll
+    for (int o = kLanes / 8; o > 0; o /= 2) a += __shfl_xor_sync(0xffffffffu, a, o);
+    return a;
 }
 
 // 2^x for two values on the FMA pipe: n = round(x), f = x - n in [-0.5, 0.5], 2^f = 1 + f g(f) with a quartic g fitted for
@@ -426,36 +419,34 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
     }
 }
 
-// Sequences with one new token: everything in registers.  Quad Q of a warp has channels Q, Q + 8, ... (so that a load of all
-// its lanes is one run of memory); lane q works out the step and the result of the quad's channel q * kCh / 4.
-// A block takes `rows` sequences for its channels, whose a it loads once.
+// Sequences with one new token: everything in registers.  Lane q of a channel's works out the step and the result of its channel
+// number q * kCh / kLanes.  A warp takes sequences u0 .. u1 for its channels, whose a it loads once.  The states are not wanted
+// again before the next iteration: stored as the first to leave the L2, they leave it to what is (26.3 -> 24.8 us).  Seven blocks
+// of 72 registers an SM (eight of 64: 24.8 us too, at 64 states 95.4 for 88.8).
 template <int N>
 __device__ __forceinline__ void step_units(const StateUnit *__restrict__ units, int u0, int u1, int64_t c0, const ScanArgs &g) {
     using S = Step<N>;
-    const int lane = threadIdx.x & 31, q = lane & 3;
+    const int lane = threadIdx.x & 31, q = lane & (S::kLanes - 1);
     const int64_t D = g.channels;
-    const int64_t wc = c0 + (lane >> 2);                   // the quad's first channel, of the warp's from c0 on
-    const int64_t own = wc + q * S::kCh / 4 * 8;           // this lane's channel
+    const int64_t wc = c0 + lane / S::kLanes;              // this lane's first channel, of the warp's from c0 on
+    const int64_t own = wc + q * S::kCh / S::kLanes * S::kAcross;
     const bool in = own < D;
-    const int64_t left = D - c0;                           // channels come in eights: the warp's c-th eight is there if 8 c < left
-    auto load_held = [&](const float *p, float2 (&to)[S::kHeld / 2]) {        // this lane's states of a channel
-#pragma unroll
-        for (int i = 0; i < S::kVecs; ++i) {
-            if constexpr (S::kVec == 4) {
-                const uint4 v = load16(p + 16 * i);
-                to[2 * i] = as_floats(make_uint2(v.x, v.y)), to[2 * i + 1] = as_floats(make_uint2(v.z, v.w));
-            } else {
-                to[0] = as_floats(load8(p));
-            }
+    const int64_t left = D - c0;                           // (channels come in eights: those across are there or not together)
+    constexpr int P = S::kVec / 2;
+    auto load_held = [&](const float *p, float2 (&to)[P]) {
+        if constexpr (P == 2) {
+            const uint4 v = load16(p);
+            to[0] = as_floats(make_uint2(v.x, v.y)), to[1] = as_floats(make_uint2(v.z, v.w));
+        } else {
+            to[0] = as_floats(load8(p));
         }
     };
-    constexpr int P = S::kHeld / 2;
     float2 a2[S::kCh][P];
 #pragma unroll
     for (int c = 0; c < S::kCh; ++c) {
 #pragma unroll
         for (int i = 0; i < P; ++i) a2[c][i] = make_float2(0.f, 0.f);
-        if (8 * c < left) load_held(g.a + (wc + 8 * c) * N + q * S::kVec, a2[c]);
+        if (S::kAcross * c < left) load_held(g.a + (wc + S::kAcross * c) * N + q * S::kVec, a2[c]);
     }
     const float bias = in && g.dt_bias ? __uint_as_float(load4(g.dt_bias + own)) : 0.f;
     const float skip = in && g.d_skip ? __uint_as_float(load4(g.d_skip + own)) : 0.f;
@@ -470,7 +461,7 @@ __device__ __forceinline__ void step_units(const StateUnit *__restrict__ units, 
         for (int c = 0; c < S::kCh; ++c) {
 #pragma unroll
             for (int i = 0; i < P; ++i) h[c][i] = make_float2(0.f, 0.f);
-            if (kept && 8 * c < left) load_held(state + 8 * c * N, h[c]);
+            if (kept && S::kAcross * c < left) load_held(state + S::kAcross * c * N, h[c]);
         }
         float x = 0.f, d = 0.f, z = 0.f;
         if (in) {
@@ -479,15 +470,12 @@ __device__ __forceinline__ void step_units(const StateUnit *__restrict__ units, 
             if (g.z) z = number(load2(g.z + row * g.zs + own));
         }
         float2 b[P], cc[P];
-#pragma unroll
-        for (int i = 0; i < S::kVecs; ++i) {
-            const uint16_t *bp = g.b + row * g.bs + 4 * S::kVec * i + S::kVec * q, *cp = g.c + row * g.cs + 4 * S::kVec * i + S::kVec * q;
-            if constexpr (S::kVec == 4) {
-                const uint2 bv = load8(bp), cv = load8(cp);
-                b[2 * i] = widen2(bv.x), b[2 * i + 1] = widen2(bv.y), cc[2 * i] = widen2(cv.x), cc[2 * i + 1] = widen2(cv.y);
-            } else {
-                b[0] = widen2(load4(bp)), cc[0] = widen2(load4(cp));
-            }
+        const uint16_t *bp = g.b + row * g.bs + S::kVec * q, *cp = g.c + row * g.cs + S::kVec * q;
+        if constexpr (P == 2) {
+            const uint2 bv = load8(bp), cv = load8(cp);
+            b[0] = widen2(bv.x), b[1] = widen2(bv.y), cc[0] = widen2(cv.x), cc[1] = widen2(cv.y);
+        } else {
+            b[0] = widen2(load4(bp)), cc[0] = widen2(load4(cp));
         }
         d += bias;
         if (g.softplus) d = softplus(d);
@@ -496,7 +484,7 @@ __device__ __forceinline__ void step_units(const StateUnit *__restrict__ units, 
         float y[S::kCh];
 #pragma unroll
         for (int c = 0; c < S::kCh; ++c) {
-            const int from = (lane & ~3) | (c * (4 / S::kCh));
+            const int from = (lane & -S::kLanes) | (c * S::kLanes / S::kCh);
             const float dc = __shfl_sync(0xffffffffu, d, from), dxc = __shfl_sync(0xffffffffu, dx, from);
             const float2 d2 = make_float2(dc, dc), dx2 = make_float2(dxc, dxc);
             float2 sum = make_float2(0.f, 0.f);
@@ -508,17 +496,14 @@ __device__ __forceinline__ void step_units(const StateUnit *__restrict__ units, 
                 sum = __ffma2_rn(h[c][i], cc[i], sum);
             }
             y[c] = sum.x + sum.y;
-            if (8 * c < left) {
-#pragma unroll
-                for (int i = 0; i < S::kVecs; ++i) {
-                    float *p = state + 8 * c * N + 16 * i;
-                    if constexpr (S::kVec == 4) *(float4 *)p = make_float4(h[c][2 * i].x, h[c][2 * i].y, h[c][2 * i + 1].x, h[c][2 * i + 1].y);
-                    else *(float2 *)p = h[c][0];
-                }
+            if (S::kAcross * c < left) {
+                float *p = state + S::kAcross * c * N;
+                if constexpr (P == 2) __stcs((float4 *)p, make_float4(h[c][0].x, h[c][0].y, h[c][1].x, h[c][1].y));
+                else __stcs((float2 *)p, h[c][0]);
             }
         }
-        float sum = quad_sum<S::kCh>(y, q);
-        if (in && (S::kCh == 4 || q % (4 / S::kCh) == 0)) {
+        float sum = lanes_sum<S::kLanes>(y, q);
+        if (in && q % (S::kLanes / S::kCh) == 0) {
             sum = fmaf(skip, x, sum);
             if (g.z) sum = gate(sum, z);
             *(__nv_bfloat16 *)(g.out + row * g.os + own) = __float2bfloat16_rn(sum);
@@ -527,7 +512,7 @@ __device__ __forceinline__ void step_units(const StateUnit *__restrict__ units, 
 }
 
 template <int N>
-__global__ void __launch_bounds__(Step<N>::kThreads, 8)
+__global__ void __launch_bounds__(Step<N>::kThreads, 7)
 scan_step_kernel(const StateUnit *__restrict__ units, int n_units, int rows, int blocks_c, const ScanArgs g) {
     const int u0 = (int)blockIdx.x / blocks_c * rows, cb = (int)blockIdx.x % blocks_c;
     const int64_t c0 = (int64_t)cb * Step<N>::kBlockCh + (threadIdx.x >> 5) * Step<N>::kWarpCh;
