@@ -243,8 +243,13 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
                 float2 own[K];
                 load_held(g.seg_state + at * N, own);
 #pragma unroll
-                for (int k = 0; k < K; ++k)
-                    h[k] = __ffma2_rn(make_float2(exp2_approx(step * a2[k].x), exp2_approx(step * a2[k].y)), h[k], own[k]);
+                for (int k = 0; k < K; ++k) {
+                    // e^(a sum d) may leave fp32's range where its product with h does not: four factors of its fourth root,
+                    // each within 2^+-126 (beyond them any state but zero is past the range), so that a state of zero stays zero
+                    auto root = [](float x) { return exp2_approx(max_nan(min_nan(0.25f * x, 126.f), -126.f)); };
+                    const float2 r = make_float2(root(step * a2[k].x), root(step * a2[k].y));
+                    h[k] = __ffma2_rn(r, __fmul2_rn(r, __fmul2_rn(r, __fmul2_rn(r, h[k]))), own[k]);
+                }
             }
         } else if ((unit.flags & kUnitFirst) && (unit.flags & kUnitKept)) {
             load_held(g.state + ((int64_t)unit.slot * D + ch) * N, h);

@@ -1,0 +1,59 @@
+"""Edges of the operators over state slots: states and decays at the ends of fp32, what a call may not depend on, refusals."""
+from unittest import mock
+
+import numpy as np
+import pytest
+
+import paper_2604_07144_b200 as ap
+from paper_2604_07144_b200 import workloads as W
+
+import layer_reference as R
+from test_state_layers import NAN, Case, dev, f64, host
+
+
+def reference(c, piece=0, z=False, softplus=False):
+    """R.scan of a case where a row's decay by itself may leave fp32 (its product with the state does not)."""
+    with mock.patch.object(R, "LARGEST", 1e300):
+        return R.scan(f64(c.x[:c.n]), f64(c.dt[:c.n]), c.a.astype(np.float64), f64(c.b[:c.n]), f64(c.c[:c.n]),
+                      np.where(c.live[:, None, None], c.state, 0), c.q_lens, c.ctx_lens, c.slots, piece=piece,
+                      z=f64(c.z[:c.n]) if z else None, softplus=softplus)
+
+
+def check(c, out, ref, slack, state, off):
+    assert np.isfinite(slack).all() and np.isfinite(off[c.touched]).all()             # (every element is compared)
+    assert max(np.abs(ref).max(), np.abs(state[c.touched]).max()) < 1e37
+    R.bf16_close(f64(host(out)[:c.n]), ref, slack, "out")
+    assert (host(out)[c.n:] == NAN).all()
+    R.fp32_close(host(c.d_state)[c.touched].astype(np.float64), state[c.touched], off[c.touched], "state")
+
+
+def bf16(v):
+    return W.f32_to_bf16_bits(np.asarray(v, np.float32))
+
+
+# ------------------------------------------------------------------ GPU --
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fresh", [True, False], ids=["from_zeros", "from_its_slot"])
+@pytest.mark.parametrize("states", [8, 16, 32, 64])
+def test_growth_over_whole_pieces_of_a_cut(states, fresh):
+    """A sequence cut along time whose layer grows by e^96 and more over one piece and decays by as much over the next: the
+    state stays in range, a piece's factor does not.  Without inputs until row 448, so from zeros it stays zero until there."""
+    n, ch = 700, 64
+    c = Case(900 + states, ch, states, 4, [n], [n if fresh else n + 5])
+    rng = np.random.default_rng(states)
+    t = np.arange(n)
+    step = np.where(t < 448, np.where(t // 64 % 2 == 0, -1.5, 1.5), -0.02)
+    c.dt[:n] = bf16(np.broadcast_to(step[:, None], (n, ch)))
+    c.x[:448] = 0
+    c.a = rng.uniform(1.0, 1.4, (ch, states)).astype(np.float32)                       # (a row: e^(1.5 a))
+    c.a[::2] *= -1                                                                      # (these begin with growth, the others with decay)
+    c.state[c.live] = (1e-2 * rng.uniform(0.5, 1, c.state[c.live].shape)).astype(np.float32)
+    c.state[c.live, ::2] *= 1e-28
+    c.state[c.live, 1::2] *= 1e28
+    c.open()
+    assert ap.state_plan_get_info(c.plan)["segments"] == n // 64
+    ref = reference(c, piece=64)
+    out = c.run_scan(softplus=False)
+    check(c, out, *ref)
+    c.close()
