@@ -618,7 +618,8 @@ int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_c
  *     y      = sum_n c[t][n] h[c][n] + d_skip[c] x[t][c]
  *     out[t][c] = y, or y z[t][c] / (1 + e^-z[t][c]) where z is given
  * with h from the sequence's slot (or zero) and back to it.  fp32 throughout; out
- * is rounded once.
+ * is rounded once.  A decay (or, with d a > 0, a growth) may leave fp32's range by
+ * itself where its product with the state does not: a state of zero stays zero.
  * x, dt, z: [n_new][channels] bf16; b, c: [n_new][state_dim] bf16; each with rows
  * *_row_stride elements apart (0: contiguous; a multiple of 8), so that they may be
  * cut out of projections' outputs.  a: [channels][state_dim] fp32, finite (beyond

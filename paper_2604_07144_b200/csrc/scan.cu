@@ -134,8 +134,8 @@ __device__ __forceinline__ float lanes_sum(const float (&y)[4], int q) {
 
 // 2^x for two values on the FMA pipe: n = round(x), f = x - n in [-0.5, 0.5], 2^f = 1 + f g(f) with a quartic g fitted for
 // relative error (4.3e-7: 2^f is off by 2.2e-7 at most, and by f 4.3e-7 for small f, where decays that last are multiplied
-// thousands of times), 2^n by adding n to the exponent field.  For |x| <= kPolyRange.
-constexpr float kPolyRange = 120.f;
+// thousands of times), 2^n by adding n to the exponent field.  For |x| <= kNear.
+constexpr float kNear = 120.f;
 __device__ __forceinline__ float2 exp2_pair(float2 x) {
     const float2 magic = make_float2(12582912.f, 12582912.f);              // 1.5 * 2^23: x + magic holds round(x) in its low bits
     const float2 t = __fadd2_rn(x, magic);
@@ -148,6 +148,23 @@ __device__ __forceinline__ float2 exp2_pair(float2 x) {
     p = __ffma2_rn(p, f, make_float2(1.f, 1.f));
     return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
                        __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+
+// 2^x, to be multiplied to `state`, for |x| > kNear: by itself it may leave fp32's range where their product does not.  So the state
+// takes its root at once, and the root is returned to be multiplied by again.  (The root is finite: a state of zero stays zero.)
+// For a pair, whatever its x: twice the error of ex2 then.
+__device__ __forceinline__ float2 exp2_far(float2 x, float2 &state) {
+    const float2 half = __fmul2_rn(x, make_float2(0.5f, 0.5f));
+    const float2 root = make_float2(exp2_approx(min_nan(half.x, 127.9f)), exp2_approx(min_nan(half.y, 127.9f)));
+    state = __fmul2_rn(state, root);
+    return root;
+}
+// The same for one of a pair that may be near.
+__device__ __forceinline__ float exp2_far(float x, float &state) {
+    const bool far = !(fabsf(x) <= kNear);
+    const float e = exp2_approx(far ? min_nan(0.5f * x, 127.9f) : x);
+    state *= far ? e : 1.f;
+    return e;
 }
 
 // One pair of states in kPolyEvery takes the FMA pipe for its exponential (8 x 1024 rows: one in eight 361 us, none 363, in four
@@ -325,10 +342,10 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
             }
         }
         // (far also where a step or an a is NaN)
-        const bool far = __any_sync(0xffffffffu, !(longest * widest <= kPolyRange));
+        const bool far = __any_sync(0xffffffffu, !(longest * widest <= kNear));
         __syncwarp();
         copy_in(t0 + kTile);                                   // (past the end: an empty group)
-        auto walk = [&](auto poly) {
+        auto walk = [&](auto near) {
 #pragma unroll 1
             for (int r0 = 0; r0 < rows; r0 += kGroup) {
                 float y[kGroup];
@@ -349,7 +366,9 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
                         float2 e = __fmul2_rn(d2, a2[k]);
-                        if (decltype(poly)::value && (r * K + k) % kPolyEvery == kPolyEvery - 1) {
+                        if (!decltype(near)::value) {
+                            e = exp2_far(e, h[k]);
+                        } else if ((r * K + k) % kPolyEvery == kPolyEvery - 1) {
                             e = exp2_pair(e);
                         } else {
                             e.x = exp2_approx(e.x);
@@ -496,7 +515,11 @@ __device__ __forceinline__ void step_units(const StateUnit *__restrict__ units, 
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 float2 e = __fmul2_rn(d2, a2[c][i]);
-                e.x = exp2_approx(e.x), e.y = exp2_approx(e.y);
+                if (!(max3_nan(0.f, fabsf(e.x), fabsf(e.y)) <= kNear)) {
+                    e = make_float2(exp2_far(e.x, h[c][i].x), exp2_far(e.y, h[c][i].y));
+                } else {
+                    e.x = exp2_approx(e.x), e.y = exp2_approx(e.y);
+                }
                 h[c][i] = __ffma2_rn(e, h[c][i], __fmul2_rn(dx2, b[i]));
                 sum = __ffma2_rn(h[c][i], cc[i], sum);
             }

@@ -57,3 +57,31 @@ def test_growth_over_whole_pieces_of_a_cut(states, fresh):
     out = c.run_scan(softplus=False)
     check(c, out, *ref)
     c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("states", [8, 16, 32, 64])
+def test_a_row_whose_decay_alone_leaves_fp32(states):
+    """Decays of a single row from e^-150 to e^150 on states that stay in range: zeros stay zeros, small states grow to large
+    ones and large ones shrink, in chunks as in single tokens."""
+    lens, ctx = [40, 1, 1, 3, 1, 17], [40, 1, 9, 3, 7, 30]
+    ch = 72
+    c = Case(920 + states, ch, states, 4, lens, ctx)
+    rng = np.random.default_rng(states)
+    row = 0
+    for s, m in enumerate(lens):
+        # growth and decay in turn, so that a state comes back to where it was; inputs, as small, with a decay only
+        step = np.where(np.arange(m) % 2 == 0, 1.25, -1.25) * (1 if s != 4 else -1)
+        c.dt[row:row + m] = bf16(np.broadcast_to(step[:, None], (m, ch)))
+        c.x[row:row + m][step > 0] = 0
+        c.x[row:row + m][step < 0] = bf16(1e-31 * f64(c.x[row:row + m][step < 0]))
+        row += m
+    c.a = rng.uniform(75, 120, (ch, states)).astype(np.float32)
+    state = rng.uniform(0.5, 1, c.state.shape) * np.where(rng.random(c.state.shape) < 0.3, 0, 1e-31)
+    state[c.slots[4]] = np.where(state[c.slots[4]] == 0, 0, state[c.slots[4]] * 1e62)   # (this one only decays)
+    c.state[c.live] = state[c.live]
+    c.open()
+    ref = reference(c)
+    out = c.run_scan(softplus=False)
+    check(c, out, *ref)
+    c.close()
