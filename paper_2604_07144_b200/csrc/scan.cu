@@ -574,8 +574,18 @@ scan_kernel(const StateUnit *__restrict__ units, int64_t n_warps, int blocks_c, 
     }
     const StateUnit unit = units[at / blocks_c];
     const int64_t c0 = at % blocks_c * Walk<N, H>::kCh;
-    griddep_wait();
     WalkSmem<N, H> &sm = *(WalkSmem<N, H> *)raw;
+    // Columns past the last channel, which no copy fills, are worked out with the others: whether a tile is far may not hang on
+    // what another kernel left there.
+    if (c0 + Walk<N, H>::kCh > g.channels) {
+        auto clear = [](auto &numbers) {
+            for (int i = threadIdx.x; i < (int)sizeof(numbers) / 16; i += 32) ((uint4 *)&numbers)[i] = make_uint4(0, 0, 0, 0);
+        };
+        clear(sm.x);
+        clear(sm.dt);
+        __syncwarp();
+    }
+    griddep_wait();
     if (unit.flags & kUnitStateOnly) walk_unit<N, H, true>(unit, c0, g, sm);
     else walk_unit<N, H, false>(unit, c0, g, sm);
 }

@@ -85,3 +85,33 @@ def test_a_row_whose_decay_alone_leaves_fp32(states):
     out = c.run_scan(softplus=False)
     check(c, out, *ref)
     c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("states,channels", [(16, 72), (16, 8), (8, 40), (8, 72), (32, 8), (64, 200)])
+def test_what_ran_before_does_not_change_a_bit(states, channels):
+    """Channels that do not fill a warp: identical calls give identical bits, whatever another call left in shared memory."""
+    import torch
+    c = Case(940 + states, channels, states, 4, [200, 1, 37], [200, 4, 45])
+    c.a /= states
+    c.open()
+    wide = 8192
+    pool = ap.state_pool_create(8, wide, states, 4)
+    plan = ap.state_plan_create(pool, [16] * 8, [16] * 8, range(8))
+    assert ap.state_plan_get_info(plan)["split_seqs"] == 0
+    rows = [torch.empty(128, wide, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    a, bc = torch.zeros(wide, states, device="cuda"), torch.ones(128, states, dtype=torch.bfloat16, device="cuda")
+    seen = []
+    for left in (0.0, float("nan"), 1e30, -0.25):
+        rows[0].fill_(left)
+        rows[1].fill_(left)
+        ap.scan_iteration(pool, plan, rows[0], rows[1], a, bc, bc, rows[2], z=rows[0], softplus=False)
+        c.d_state.copy_(dev(c.state))
+        out = c.run_scan(**c.all_scan())
+        seen.append((host(out)[:c.n], host(c.d_state)[c.touched].view(np.int32)))
+    c.check_scan(out, piece=64, **c.all_scan())
+    for got in seen[1:]:
+        assert np.array_equal(got[0], seen[0][0]) and np.array_equal(got[1], seen[0][1])
+    ap.state_plan_destroy(plan)
+    ap.state_pool_destroy(pool)
+    c.close()
