@@ -293,6 +293,8 @@ def _checked(x, nbytes: int, device: int, itemsize: Optional[int], dense: bool =
             raise ValueError(f"expected a tensor on cuda:{device}, not on {x.device}")
         if dense and not x.is_contiguous():
             raise ValueError("expected a contiguous tensor")
+        if not dense and itemsize is not None and x.element_size() != itemsize:
+            raise ValueError(f"row strides are taken in elements of {itemsize} bytes, not of {x.dtype}")
         if dense and x.nbytes < nbytes:
             raise ValueError(f"a tensor of {x.nbytes} bytes where the call takes {nbytes}")
     elif isinstance(x, np.ndarray):

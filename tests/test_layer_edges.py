@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 
 import paper_2604_07144_b200 as ap
+from paper_2604_07144_b200 import binding as B
 from paper_2604_07144_b200 import workloads as W
 
 import layer_reference as R
@@ -29,6 +30,40 @@ def check(c, out, ref, slack, state, off):
 
 def bf16(v):
     return W.f32_to_bf16_bits(np.asarray(v, np.float32))
+
+
+# ------------------------------------------------------------------ CPU --
+
+def test_strided_tensors_of_another_element_size_are_refused():
+    """The library takes row strides in elements of two bytes: a view of bytes has strides twice too long for its memory."""
+    import torch
+    pool = ap.state_pool_create(4, 64, 16, 4, device=-1)
+    plan = ap.state_plan_create(pool, [2], [2], [0])
+    kv = ap.kv_pool_create(4, 2, 64, device=-1)
+    prompts = ap.prompt_plan_create(kv, [2], 2)
+    append = ap.plan_create(kv, [2], [2], np.array([[0]], np.int32), 2)
+
+    def rows(dtype, *shape):                                   # every other part of a wider tensor's rows
+        return torch.zeros((shape[0], 2, *shape[1:]), dtype=dtype)[:, 0]
+    good = {t: rows(t, 2, 64) for t in (torch.bfloat16, torch.int16, torch.uint8)}
+    heads = {t: rows(t, 2, 2, 64) for t in good}
+    w, bc, a = torch.zeros(64, 4, dtype=torch.bfloat16), rows(torch.bfloat16, 2, 16), torch.zeros(64, 16)
+    calls = [lambda t: ap.conv_iteration(pool, plan, good[t], w, good[torch.bfloat16]),
+             lambda t: ap.conv_iteration(pool, plan, good[torch.bfloat16], w, good[t]),
+             lambda t: ap.scan_iteration(pool, plan, good[t], good[torch.bfloat16], a, bc, bc, good[torch.bfloat16].clone()),
+             lambda t: ap.scan_iteration(pool, plan, good[torch.bfloat16], good[torch.bfloat16], a, rows(t, 2, 16), bc, good[torch.bfloat16].clone()),
+             lambda t: ap.prompt_attention(kv, prompts, heads[t], heads[torch.bfloat16], heads[torch.bfloat16], torch.zeros(2, 2, 64, dtype=torch.bfloat16)),
+             lambda t: ap.kv_append_rope(kv, append, heads[t], heads[torch.bfloat16])]
+    for call in calls:
+        for t in (torch.bfloat16, torch.int16):
+            with pytest.raises(ap.ApError) as e:
+                call(t)
+            assert e.value.status == B.AP_ERR_CUDA             # (taken, but the pool is host-only)
+        with pytest.raises(ValueError):
+            call(torch.uint8)
+    for destroy, x in ((ap.state_plan_destroy, plan), (ap.prompt_plan_destroy, prompts), (ap.plan_destroy, append),
+                       (ap.state_pool_destroy, pool), (ap.kv_pool_destroy, kv)):
+        destroy(x)
 
 
 # ------------------------------------------------------------------ GPU --
