@@ -381,6 +381,8 @@ def _plane(x, nbytes: int, device: int) -> Optional[int]:
     """Address of a pool plane: at least `nbytes` on `device` (any view of memory that lies together)."""
     if hasattr(x, "nbytes") and x.nbytes < nbytes:
         raise ValueError(f"a plane of {x.nbytes} bytes where the pool takes {nbytes}")
+    if hasattr(x, "stride") and any(step == 0 and n > 1 for n, step in zip(x.shape, x.stride())):
+        raise ValueError("a plane that holds the same memory more than once (an expanded tensor?)")
     return _checked(x, 0, device, None, dense=False)
 
 

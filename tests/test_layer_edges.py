@@ -66,6 +66,18 @@ def test_strided_tensors_of_another_element_size_are_refused():
         destroy(x)
 
 
+def test_expanded_planes_are_refused():
+    """A plane that is one page many times over has fewer bytes than it says."""
+    import torch
+    one = torch.zeros(1, 2, 16, 64, dtype=torch.bfloat16)
+    whole = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    for k, v in ((one.expand(4, 2, 16, 64), whole), (whole, one.expand(4, 2, 16, 64))):
+        with pytest.raises(ValueError):
+            ap.kv_pool_create(4, 2, 64, k, v, device=-1)
+        with pytest.raises(ValueError):
+            ap.kv_pool_create_4bit(4, 2, 64, k, v, device=-1)
+
+
 # ------------------------------------------------------------------ GPU --
 
 @pytest.mark.gpu
