@@ -633,12 +633,15 @@ def _workspace(workspace, workspace_bytes: Optional[int], dev: int) -> Tuple[Opt
         room = workspace.nbytes
         if workspace_bytes is None:
             workspace_bytes = room
-        elif workspace_bytes > room:
+        elif not 0 <= workspace_bytes <= room:
             raise ValueError(f"a workspace of {room} bytes where the call is told {workspace_bytes}")
         return workspace.data_ptr() if workspace.get_device() == dev and workspace.is_contiguous() else (
             _checked(workspace, 0, dev, None)), workspace_bytes
     except AttributeError:                   # none, or an address
-        return _checked(workspace, 0, dev, None), workspace_bytes or 0
+        workspace_bytes = workspace_bytes or 0
+        if workspace_bytes < 0:              # (it would wrap)
+            raise ValueError("a workspace of less than no bytes") from None
+        return _checked(workspace, 0, dev, None), workspace_bytes
 
 
 def attention_iteration(pool: KVPool, plan: Plan, q, out, lse=None, workspace=None,

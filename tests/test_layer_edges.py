@@ -78,6 +78,26 @@ def test_expanded_planes_are_refused():
             ap.kv_pool_create_4bit(4, 2, 64, k, v, device=-1)
 
 
+def test_negative_workspaces_are_refused():
+    """A size below zero would wrap to a huge one."""
+    import torch
+    kv = ap.kv_pool_create(4, 2, 64, device=-1)
+    plan = ap.plan_create(kv, [1], [1], np.array([[0]], np.int32), 2)
+    q = torch.zeros(1, 2, 64, dtype=torch.bfloat16)
+    pool = ap.state_pool_create(4, 64, 16, 4, device=-1)
+    rows = ap.state_plan_create(pool, [2], [2], [0])
+    x, bc, a = torch.zeros(2, 64, dtype=torch.bfloat16), torch.zeros(2, 16, dtype=torch.bfloat16), torch.zeros(64, 16)
+    space = torch.zeros(256, dtype=torch.uint8)
+    for workspace in (space, 4096, None):
+        with pytest.raises(ValueError):
+            ap.attention_iteration(kv, plan, q, q.clone(), workspace=workspace, workspace_bytes=-1)
+        if workspace is not None:
+            with pytest.raises(ValueError):
+                ap.scan_iteration(pool, rows, x, x, a, bc, bc, x.clone(), workspace=workspace, workspace_bytes=-1)
+    for destroy, h in ((ap.plan_destroy, plan), (ap.state_plan_destroy, rows), (ap.state_pool_destroy, pool), (ap.kv_pool_destroy, kv)):
+        destroy(h)
+
+
 # ------------------------------------------------------------------ GPU --
 
 @pytest.mark.gpu
