@@ -703,10 +703,19 @@ def prompt_plan_get_info(plan: PromptPlan) -> dict:
     return info.as_dict()
 
 
+def _spare_rows(x, width: int, nbytes: int) -> None:
+    """A tensor larger than the call takes has to be one of more rows: some of its last dimensions make a row of `width`."""
+    if getattr(x, "nbytes", 0) > nbytes and x.ndim > 1 and width not in np.multiply.accumulate(x.shape[::-1]):
+        raise ValueError(f"expected rows of {width} elements, not {list(x.shape)}")
+
+
 def prompt_attention(pool: KVPool, plan: PromptPlan, q, k, v, out, lse=None, stream=None) -> None:
     """Causal attention of whole prompts from q, k, v [rows, heads, head_dim], which may be strided by row (slices of one
     projection); no pages, no block tables."""
     dev, n, d = pool.device, plan.rows, pool.head_dim
+    for x, heads, nbytes in ((q, plan.num_q_heads, plan.q_bytes), (k, pool.num_kv_heads, plan.kv_bytes),
+                             (v, pool.num_kv_heads, plan.kv_bytes), (out, plan.num_q_heads, plan.q_bytes)):
+        _spare_rows(x, heads * d, nbytes)
     q_at, q_stride = _strided_rows(q, n, plan.num_q_heads, d, plan.q_bytes, dev)
     k_at, k_stride = _strided_rows(k, n, pool.num_kv_heads, d, plan.kv_bytes, dev)
     v_at, v_stride = _strided_rows(v, n, pool.num_kv_heads, d, plan.kv_bytes, dev)

@@ -98,6 +98,26 @@ def test_negative_workspaces_are_refused():
         destroy(h)
 
 
+def test_larger_tensors_of_other_heads_are_refused():
+    """Rows to spare are fine; rows of another width would be read as if they were the plan's."""
+    import torch
+    kv = ap.kv_pool_create(4, 2, 64, device=-1)
+    prompts = ap.prompt_plan_create(kv, [3], 4)
+
+    def bf(*shape):
+        return torch.zeros(shape, dtype=torch.bfloat16)
+    good = dict(q=bf(3, 4, 64), k=bf(3, 2, 64), v=bf(3, 2, 64), out=bf(3, 4, 64))
+    for name, ok in dict(q=bf(5, 4, 64), k=bf(4, 128), v=bf(1000), out=bf(9, 256)).items():
+        with pytest.raises(ap.ApError) as e:
+            ap.prompt_attention(kv, prompts, **{**good, name: ok})
+        assert e.value.status == B.AP_ERR_CUDA                  # (taken, but the pool is host-only)
+    for name, bad in dict(q=bf(3, 8, 64), k=bf(3, 4, 64), v=bf(3, 3, 64), out=bf(3, 8, 64)).items():
+        with pytest.raises(ValueError):
+            ap.prompt_attention(kv, prompts, **{**good, name: bad})
+    ap.prompt_plan_destroy(prompts)
+    ap.kv_pool_destroy(kv)
+
+
 # ------------------------------------------------------------------ GPU --
 
 @pytest.mark.gpu
