@@ -594,8 +594,8 @@ size_t ap_state_plan_workspace_bytes(const ap_state_plan *plan);
  * Short causal convolution, channel by channel (w = conv_width):
  *     out[t][c] = act(bias[c] + sum_{j < w} weight[c][j] x[t - w + 1 + j][c])
  * x before a sequence's first new token comes from its slot (or is zero); the slot
- * then holds the last w - 1 inputs, bit for bit.  silu != 0: act(y) = y / (1 + e^-y).
- * Sums in fp32, rounded once.
+ * then holds the last w - 1 inputs, bit for bit.  silu != 0: act(y) = y / (1 + e^-y),
+ * and 0 for finite y below -87.3, where it is less than 1.1e-36.  Sums in fp32, rounded once.
  * x: [n_new][channels] bf16, rows x_row_stride elements apart (0: contiguous; a
  * multiple of 8); weight: [channels][w] bf16; bias: [channels] bf16 or NULL; out:
  * [n_new][channels] bf16, rows out_row_stride elements apart.  Device, 16-byte
@@ -616,7 +616,7 @@ int ap_conv_iteration(ap_state_pool *pool, const ap_state_plan *plan, const ap_c
  *     d      = dt[t][c] + dt_bias[c];  if softplus: d = ln(1 + e^d)
  *     h[c][n] <- e^(d a[c][n]) h[c][n] + d x[t][c] b[t][n]
  *     y      = sum_n c[t][n] h[c][n] + d_skip[c] x[t][c]
- *     out[t][c] = y, or y z[t][c] / (1 + e^-z[t][c]) where z is given
+ *     out[t][c] = y, or y z[t][c] / (1 + e^-z[t][c]) where z is given (0 for finite z below -87.3)
  * with h from the sequence's slot (or zero) and back to it.  fp32 throughout; out
  * is rounded once.  A decay (or, with d a > 0, a growth) may leave fp32's range by
  * itself where its product with the state does not: a state of zero stays zero.

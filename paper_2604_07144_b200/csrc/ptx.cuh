@@ -203,7 +203,7 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
-// to one step of fp32; 0 for infinity
+// to one step of fp32; 0 above 2^126 (a result below 2^-126 is flushed) and for infinity
 __device__ __forceinline__ float rcp_approx(float x) {
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -58,8 +58,8 @@ __device__ __forceinline__ float2 widen2(uint32_t v) {
     return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
 }
 
-// ln(1 + e^x) = max(x, 0) + log1p(e^-|x|); log1p(u) / u on [0, 1] by a polynomial fitted for relative error (4.7e-9,
-// 1.4e-7 with the roundings).
+// ln(1 + e^x) = max(x, 0) + log1p(e^-|x|); log1p(u) / u on [0, 1] by a polynomial fitted for relative error (3.4e-8; 1.5e-7
+// with the roundings; for x far below 0 the exponential's argument adds |x| 2^-24).
 __device__ __forceinline__ float softplus(float x) {
     const float u = exp2_approx(-1.4426950408889634f * fabsf(x));
     float p = -0.0032440212f;
@@ -133,8 +133,8 @@ __device__ __forceinline__ float lanes_sum(const float (&y)[4], int q) {
 }
 
 // 2^x for two values on the FMA pipe: n = round(x), f = x - n in [-0.5, 0.5], 2^f = 1 + f g(f) with a quartic g fitted for
-// relative error (4.3e-7: 2^f is off by 2.2e-7 at most, and by f 4.3e-7 for small f, where decays that last are multiplied
-// thousands of times), 2^n by adding n to the exponent field.  For |x| <= kNear.
+// relative error (4.7e-7, near 0 8.4e-8: 2^f is off by 2.2e-7 at most, roundings included, and by less the smaller f is, where
+// decays that last are multiplied thousands of times), 2^n by adding n to the exponent field.  For |x| <= kNear.
 constexpr float kNear = 120.f;
 __device__ __forceinline__ float2 exp2_pair(float2 x) {
     const float2 magic = make_float2(12582912.f, 12582912.f);              // 1.5 * 2^23: x + magic holds round(x) in its low bits

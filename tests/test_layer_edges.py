@@ -1,4 +1,6 @@
 """Edges of the operators over state slots: states and decays at the ends of fp32, what a call may not depend on, refusals."""
+import os
+import re
 from unittest import mock
 
 import numpy as np
@@ -10,6 +12,8 @@ from paper_2604_07144_b200 import workloads as W
 
 import layer_reference as R
 from test_state_layers import NAN, Case, dev, f64, host
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def reference(c, piece=0, z=False, softplus=False):
@@ -116,6 +120,32 @@ def test_larger_tensors_of_other_heads_are_refused():
             ap.prompt_attention(kv, prompts, **{**good, name: bad})
     ap.prompt_plan_destroy(prompts)
     ap.kv_pool_destroy(kv)
+
+
+def test_polynomials_are_as_good_as_stated():
+    """The coefficients of the scan's softplus and 2^x, as the source has them: the errors that its comments state."""
+    source = open(os.path.join(ROOT, "paper_2604_07144_b200", "csrc", "scan.cu")).read()
+
+    def part(begin, end):
+        return source[source.index(begin):source.index(end, source.index(begin))]
+
+    def poly(body, x, first):
+        p = np.zeros_like(x)
+        for c in re.findall(first, body):
+            p = p * x + float(np.float32(c))
+        return p
+
+    one, two = part("float softplus(float x)", "return"), part("float2 softplus2(float2 x)", "float max_nan(")
+    u = np.linspace(1e-9, 1, 400001)
+    want = np.log1p(u) / u
+    for body, pattern in ((one, r"(?:p = |u, )(-?\d+\.\d*)f"), (two, r"two\((-?\d+\.\d*)f\)")):
+        assert len(re.findall(pattern, body)) == 10
+        assert np.abs(poly(body, u, pattern) / want - 1).max() < 3.5e-8
+    exp2 = part("// 2^x for two values", "// 2^x, to be multiplied")
+    f = np.concatenate([np.linspace(-0.5, -1e-6, 200001), np.linspace(1e-6, 0.5, 200001)])
+    pattern = r"make_float2\((0\.\d+)f, "
+    assert len(re.findall(pattern, exp2)) == 5
+    assert np.abs(f * poly(exp2, f, pattern) / np.expm1(f * np.log(2)) - 1).max() < 4.7e-7
 
 
 # ------------------------------------------------------------------ GPU --
