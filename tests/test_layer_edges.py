@@ -232,3 +232,26 @@ def test_what_ran_before_does_not_change_a_bit(states, channels):
     ap.state_plan_destroy(plan)
     ap.state_pool_destroy(pool)
     c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("states", [8, 16, 32, 64])
+def test_raw_steps_of_either_sign_over_three_tiles(states):
+    """Growth that stays in range, so that every row of every tile is compared."""
+    c = Case(960 + states, 72, states, 4, [9, 1, 40], [9, 6, 50])
+    c.a /= 4 * states
+    c.open()
+    out = c.run_scan(softplus=False)
+    check(c, out, *reference(c))
+    c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("states,channels,lens", [(16, 64, [700]), (64, 40, [513]), (8, 128, [1025])])
+def test_cut_along_time_within_a_pieces_roundings(states, channels, lens):
+    """A sum of a piece's steps rounds as often as the piece has rows, not the sequence."""
+    c = Case(980 + states, channels, states, 4, lens, [n + 3 for n in lens]).open()
+    pieces = ap.state_plan_get_info(c.plan)["segments"]
+    assert pieces >= 5
+    c.check_scan(c.run_scan(**c.all_scan()), piece=lens[0] // pieces, **c.all_scan())
+    c.close()
