@@ -58,7 +58,9 @@ constexpr uint64_t kDrainNs = 100000000;  // bound of the waits for copies and p
 // 8192 tokens at 32 / 8 heads of 128: 437 us, 1258 TFLOP/s, at the clock that the power limit leaves (1.5 GHz).  A step of the
 // two tiles takes 2820 clocks, 2200 of them the tensor pipe's; a group's own chain (copy 280, maxima 520, exponentials 1490,
 // then waits for P V and the next scores) is as long.  A score region for each tile, P written over it: 470 us, the chain
-// then holds both products as well.
+// then holds both products as well.  Units of one tile (equal q and kv heads, the last head of an odd group) leave softmax and
+// tensor pipe to take turns: at 32 / 32 heads 619 us for the same products, at 30 / 10 468.  Heads of 64: 416 us for half the
+// products (661 TFLOP/s): the exponentials, as many, bound it.
 template <int D>
 struct PromptCfg {
     static constexpr int kHalves = D / 64;

@@ -7,7 +7,8 @@
 // (token, channel, state): at 16 states the special-function unit (16 a clock and SM) bounds it, ahead of HBM: 8 x 1024 rows
 // of 8192 channels are 1.07 G exponentials, 240 us of that unit alone, and 83 us of HBM.  Measured: 361 us (the unit 69 % busy,
 // load/store wavefronts 68 %, issue slots 59 %: 115 instructions per 32 channels and row).  A single token costs its
-// state, read and written: 128 sequences of 8192 channels 24.8 us, 5.8 TB/s (at 64 states 88.8, 6.2 TB/s).
+// state, read and written: 128 sequences of 8192 channels 24.4 us, 5.9 TB/s (at 64 states 87.9, 6.2 TB/s; at 8 15.4, 4.9 TB/s, where
+// what a channel costs beside its states counts).
 //
 // Work split of prompts.  H states of a channel are a lane's, L = N / H lanes make a channel, and a warp walks 32 / L channels
 // alone: no barrier but its own.  Rows come in tiles of 16 by asynchronous copies, a tile ahead.  Steps and gates are worked
@@ -26,7 +27,7 @@ namespace {
 using namespace ptx;
 
 // Single tokens: a block takes a second sequence once there are kStepBlocks blocks an SM: a's share of what is read halves
-// (128 sequences: 25.4 us, with one 26.0, with four 25.2; 64 tokens beside 512 rows 57.6, with one 60.7, with four 57.9).
+// (128 sequences: 24.4 us, with one 25.0, with four 24.2; 64 tokens beside 512 rows 58.5, with one 61.0, with four 59.4).
 constexpr int kStepBlocks = 6, kStepRows = 2;
 
 // Single tokens: kLanes lanes have a channel's states, kVec next to one another each, so that a load of a warp is one run of
@@ -446,7 +447,8 @@ __device__ __forceinline__ void walk_unit(const StateUnit &unit, int64_t c0, con
 // Sequences with one new token: everything in registers.  Lane q of a channel's works out the step and the result of its channel
 // number q * kCh / kLanes.  A warp takes sequences u0 .. u1 for its channels, whose a it loads once.  The states are not wanted
 // again before the next iteration: stored as the first to leave the L2, they leave it to what is (26.3 -> 24.8 us).  Seven blocks
-// of 72 registers an SM (eight of 64: 24.8 us too, at 64 states 95.4 for 88.8).
+// of 72 registers an SM (eight of 64: 24.8 us too, at 64 states 95.4 for 88.8).  Exponents past kNear are looked for pair by pair
+// (one vote a sequence and two forms of the code: 24.3 us, one token 2.20 for 2.14, 8 states 15.2 for 15.2, 64 states 88.3 for 87.8).
 template <int N>
 __device__ __forceinline__ void step_units(const StateUnit *__restrict__ units, int u0, int u1, int64_t c0, const ScanArgs &g) {
     using S = Step<N>;

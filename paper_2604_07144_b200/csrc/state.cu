@@ -15,7 +15,10 @@ namespace {
 // pieces, all but the first and the last are walked twice (once for the state behind them, once for their rows) and there
 // are two launches.  It pays below kCutBelow warps an SM (6 x 1024 rows of 4096 channels, 10.4 warps an SM: 198 us cut, 209
 // not), with pieces for kResident warps an SM, two rounds of those that are there together (8192 rows of 4096 channels: 314
-// us; 16: 327, 24: 328, 32: 326).
+// us; 16: 327, 24: 328, 32: 326).  Measured with sequences of one length: the rule counts sequences, whatever their rows, so a
+// long one beside a few short ones is not cut (8192 rows of 4096 channels alone 319 us, beside seven of 2 rows 887).  Nor do the
+// constants know what folding costs, a round a piece before: it shows where few channels make many pieces (64 channels: 8192 rows,
+// 128 pieces, 55 us; 65536 rows, 1024 pieces, 444).
 constexpr int kCutBelow = 12, kResident = 28, kLeastPiece = 64;
 
 struct Cut {
