@@ -705,7 +705,7 @@ def prompt_plan_get_info(plan: PromptPlan) -> dict:
 
 def _spare_rows(x, width: int, nbytes: int) -> None:
     """A tensor larger than the call takes has to be one of more rows: some of its last dimensions make a row of `width`."""
-    if getattr(x, "nbytes", 0) > nbytes and x.ndim > 1 and width not in np.multiply.accumulate(x.shape[::-1]):
+    if getattr(x, "nbytes", 0) > nbytes > 0 and x.ndim > 1 and width not in np.multiply.accumulate(x.shape[::-1]):
         raise ValueError(f"expected rows of {width} elements, not {list(x.shape)}")
 
 

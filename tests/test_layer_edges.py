@@ -118,6 +118,11 @@ def test_larger_tensors_of_other_heads_are_refused():
     for name, bad in dict(q=bf(3, 8, 64), k=bf(3, 4, 64), v=bf(3, 3, 64), out=bf(3, 8, 64)).items():
         with pytest.raises(ValueError):
             ap.prompt_attention(kv, prompts, **{**good, name: bad})
+    empty = ap.prompt_plan_create(kv, [0], 4)
+    with pytest.raises(ap.ApError) as e:
+        ap.prompt_attention(kv, empty, bf(3, 5), bf(3, 7), bf(2, 9), bf(3, 5))
+    assert e.value.status == B.AP_ERR_CUDA                      # (a plan without tokens takes any tensors)
+    ap.prompt_plan_destroy(empty)
     ap.prompt_plan_destroy(prompts)
     ap.kv_pool_destroy(kv)
 
